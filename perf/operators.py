@@ -1,0 +1,420 @@
+"""Measured cases of the single-kernel operators of a decoder block that attends over a sliding window, normalises with
+LayerNorm and drops elements of its residual branches.
+
+  attend, attend_grad     causal attention over the last `window` keys plus the first `sinks` keys of the sequence
+  layernorm, layernorm_grad
+  dropout                 y = resid + scale * dropout(x), the mask recomputed from a counter-based generator; without a
+                          residual it is also its own backward pass
+
+Every operator has a plain form in elementary torch operations (32-bit arithmetic, one rounding at the end), a 64-bit
+definition written separately, and the call a user of the package makes.  Tensors are laid out as the package's kernels
+take them: q, k and v heads packed in one [B*S, (heads + 2 kv_heads) * d] buffer, activations row-major.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+EPS = 1e-5
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+MAX_PAIRS, MAX_BYTES = 2.7e8, 4.1e8  # a drawn attention case has at most the largest listed one's pairs and bytes
+MAX_ELEMENTS = 33554432  # elements of a drawn row-wise case, those of the largest listed one
+
+
+# ------------------------------------------------------------------------------------------------ cases
+def listed():
+    return [
+        # the smallest configuration's batch and heads, a window of a quarter of its length: launch latency
+        dict(name="attend_tiny", op="attend", B=2, S=128, heads=4, kv_heads=4, d=64, window=32, sinks=4),
+        # a 1B decoder's training batch with a local window
+        dict(name="attend_1b", op="attend", B=4, S=2048, heads=16, kv_heads=8, d=128, window=512, sinks=4),
+        # one long document of the same decoder
+        dict(name="attend_long", op="attend", B=1, S=16384, heads=16, kv_heads=8, d=128, window=1024, sinks=4),
+        # gradients in a 124M decoder's batch, one kv head per query head, window only
+        dict(name="attend_grad_124m", op="attend_grad", B=8, S=1024, heads=12, kv_heads=12, d=64, window=256, sinks=0, rope=True),
+        # all query heads on one kv head, a length and a window that end inside every tile
+        dict(name="attend_grad_ragged", op="attend_grad", B=3, S=1531, heads=6, kv_heads=1, d=64, window=333, sinks=7, rope=False),
+        # gradients of the long document: the sink keys are seen by every position
+        dict(name="attend_grad_long", op="attend_grad", B=1, S=16384, heads=16, kv_heads=8, d=128, window=1024, sinks=4, rope=True),
+        # rows of the smallest configuration
+        dict(name="layernorm_tiny", op="layernorm", rows=256, h=256, dtype="bf16", bias=True, pad=0),
+        # a 1B decoder's activations, forward and backward
+        dict(name="layernorm_1b", op="layernorm", rows=8192, h=2048, dtype="bf16", bias=True, pad=0),
+        dict(name="layernorm_grad_1b", op="layernorm_grad", rows=8192, h=2048, dtype="bf16", bias=True, resid=True, pad=0),
+        # an odd width in 32 bits, rows cut out of a wider buffer
+        dict(name="layernorm_grad_odd", op="layernorm_grad", rows=4099, h=771, dtype="f32", bias=True, resid=False, pad=5),
+        # the smallest configuration's residual branch, and a 1B decoder's at 16384 tokens
+        dict(name="dropout_tiny", op="dropout", rows=256, h=256, dtype="bf16", p=0.1, scale=1.0, resid=True, pad=0),
+        dict(name="dropout_1b", op="dropout", rows=16384, h=2048, dtype="bf16", p=0.1, scale=0.35, resid=True, pad=0),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(["attend", "attend_grad", "layernorm", "layernorm_grad", "dropout"])
+    if op.startswith("attend"):
+        c = dict(op=op, B=rng.randint(1, 8), S=_log_int(rng, 1, 16384), heads=0, kv_heads=rng.choice([1, 2, 3, 4, 8, 12]),
+                 d=rng.choice([64, 128]), window=0, sinks=rng.choice([0, 0, 1, 4, 16, rng.randint(1, 300)]))
+        c["heads"] = c["kv_heads"] * rng.choice([1, 2, 4, 7])
+        c["window"] = _log_int(rng, 1, 2 * c["S"])
+        if op == "attend_grad":
+            c["rope"] = rng.random() < 0.5
+        while c["B"] * c["heads"] * _pairs(c["S"], c["window"], c["sinks"]) > MAX_PAIRS or work(c)["bytes"] > MAX_BYTES:
+            if c["B"] > 1:
+                c["B"] -= 1
+            else:
+                c["S"] = c["S"] * 3 // 4
+        return c
+    c = dict(op=op, rows=_log_int(rng, 1, 32768), h=_log_int(rng, 1, 8192), dtype=rng.choice(["bf16", "bf16", "f32"]), pad=rng.choice([0, 0, 8, 3]))
+    if rng.random() < 0.5:
+        c["h"] = max(8, c["h"] // 8 * 8)
+    c["rows"] = max(1, min(c["rows"], MAX_ELEMENTS // (2 if c["dtype"] == "f32" else 1) // c["h"]))
+    if op == "dropout":
+        c.update(p=rng.choice([0.0, 0.1, 0.25, 0.5]), scale=rng.choice([1.0, 0.35]), resid=rng.random() < 0.6)
+    else:
+        c["bias"] = rng.random() < 0.7
+        if op == "layernorm_grad":
+            c["resid"] = rng.random() < 0.6
+    return c
+
+
+def _pairs(S, window, sinks):
+    """(query, key) pairs one head's mask lets through."""
+    w = min(window, S)
+    near = w * (w + 1) // 2 + (S - w) * w
+    far, n = 0, S - w  # positions w .. S-1 also see sinks that their window has left behind: 1, 2, ... up to `sinks`
+    k = min(sinks, n)
+    if k > 0:
+        far = k * (k + 1) // 2 + (n - k) * k
+    return near + far
+
+
+def work(case):
+    c = case
+    if c["op"].startswith("attend"):
+        T, d = c["B"] * c["S"], c["d"]
+        qkv, o, lse = T * (c["heads"] + 2 * c["kv_heads"]) * d * 2, T * c["heads"] * d * 2, T * c["heads"] * 4
+        pairs = c["B"] * c["heads"] * _pairs(c["S"], c["window"], c["sinks"])
+        if c["op"] == "attend":  # two products of 2 d operations a pair
+            return {"bytes": qkv + o + lse, "flops": 4 * d * pairs}
+        return {"bytes": 2 * qkv + 2 * o + lse + (c["S"] * d * 4 if c["rope"] else 0), "flops": 10 * d * pairs}
+    n, e = c["rows"] * c["h"], 4 if c["dtype"] == "f32" else 2
+    gains = c["h"] * (1 + int(c.get("bias", False)))
+    if c["op"] == "layernorm":
+        return {"bytes": 2 * n * e + gains * e + 8 * c["rows"], "flops": 8 * n}
+    if c["op"] == "layernorm_grad":
+        return {"bytes": (3 + int(c["resid"])) * n * e + 8 * c["rows"] + c["h"] * e + gains * 4, "flops": 14 * n}
+    return {"bytes": (2 + int(c["resid"])) * n * e, "flops": 3 * n}
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+def _rope_tables(S, d):
+    pos = torch.arange(S, dtype=torch.float64, device="cuda")[:, None]
+    inv = 10000.0 ** (-2.0 * torch.arange(d // 2, dtype=torch.float64, device="cuda") / d)
+    return (pos * inv).cos().float(), (pos * inv).sin().float()
+
+
+def _rows(g, rows, h, dtype, pad, spread=1.0, shift=0.0):
+    """[rows, h] normal values; with pad, rows of a wider buffer."""
+    return (torch.randn(rows, h + pad, generator=g, device="cuda") * spread + shift).to(dtype)[:, :h]
+
+
+def prepare(case, seed):
+    c = dict(case)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if c["op"].startswith("attend"):
+        T, d = c["B"] * c["S"], c["d"]
+        c["qkv"] = torch.randn(T, (c["heads"] + 2 * c["kv_heads"]) * d, generator=g, device="cuda").to(torch.bfloat16)
+        c["o"] = torch.empty(T, c["heads"] * d, dtype=torch.bfloat16, device="cuda")
+        c["lse"] = torch.empty(c["B"], c["heads"], c["S"], device="cuda")
+        if c["op"] == "attend_grad":  # the forward pass has left its output and log-sum-exp
+            c["o"], c["lse"] = _plain_attend(c)
+            c["do"] = torch.randn(T, c["heads"] * d, generator=g, device="cuda").to(torch.bfloat16)
+            c["dqkv"] = torch.empty_like(c["qkv"])
+            c["cos"], c["sin"] = _rope_tables(c["S"], d) if c["rope"] else (None, None)
+        return c
+    rows, h, dt = c["rows"], c["h"], DTYPES[c["dtype"]]
+    c["x"] = _rows(g, rows, h, dt, c["pad"], 1.5, 0.25)
+    c["y"] = torch.empty(rows, h, dtype=dt, device="cuda")
+    if c["op"] == "dropout":
+        c["r"] = _rows(g, rows, h, dt, 0) if c["resid"] else None
+        c["seed"], c["site"] = int(seed) * 2654435761 + 17, 5  # one stream of masks per run, one site per branch
+        c["step"] = torch.full((1,), int(seed) % 1000, dtype=torch.int64, device="cuda")  # the training step's counter
+        return c
+    c["gain"] = (1.0 + 0.1 * torch.randn(h, generator=g, device="cuda")).to(dt)
+    c["beta"] = (0.1 * torch.randn(h, generator=g, device="cuda")).to(dt) if c["bias"] else None
+    c["mean"], c["rstd"] = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    if c["op"] == "layernorm_grad":
+        _, c["mean"], c["rstd"] = _plain_layernorm(c)
+        c["dy"] = _rows(g, rows, h, dt, 0)
+        c["r"] = _rows(g, rows, h, dt, 0) if c["resid"] else None
+        c["dgain"], c["dbeta"] = torch.empty(h, device="cuda"), torch.empty(h, device="cuda") if c["bias"] else None
+    return c
+
+
+# ------------------------------------------------------------------------------------------------ plain forms
+def _split(c, t):
+    """Packed rows -> float q [B, kv, rep, S, d], k and v [B, kv, S, d]."""
+    B, S, H, G, d = c["B"], c["S"], c["heads"], c["kv_heads"], c["d"]
+    t = t.view(B, S, H + 2 * G, d).permute(0, 2, 1, 3).float()
+    return t[:, :H].reshape(B, G, H // G, S, d), t[:, H:H + G], t[:, H + G:]
+
+
+class _Band:
+    """Queries in blocks of L rows, each block with the L + window - 1 keys its rows can see and the sink keys."""
+
+    def __init__(self, c):
+        self.S, w = c["S"], min(c["window"], c["S"])
+        self.L = min(self.S, max(64, w))
+        self.nb = -(-self.S // self.L)
+        self.sinks = min(c["sinks"], self.S)
+        dev = c["qkv"].device
+        first = torch.arange(self.nb, device=dev) * self.L
+        near = first[:, None] - (w - 1) + torch.arange(self.L + w - 1, device=dev)
+        keys = torch.cat([torch.arange(self.sinks, device=dev).expand(self.nb, -1), near], 1)  # [nb, sinks + L + w - 1]
+        rows = first[:, None] + torch.arange(self.L, device=dev)  # [nb, L]
+        i, j = rows[:, :, None], keys[:, None, :]
+        is_sink = (torch.arange(keys.shape[1], device=dev) < self.sinks)[None, None, :]
+        ok = (j >= 0) & (j <= i) & (i < self.S)
+        self.mask = ok & torch.where(is_sink, j < self.sinks, (j >= self.sinks) & (i - j < w))
+        self.keys, self.rows = keys.clamp(0, self.S - 1), rows.clamp(0, self.S - 1)
+
+    def queries(self, t):  # [B, G, rep, S, d] -> [B, G, nb, rep * L, d]
+        B, G, R, _, d = t.shape
+        return t[:, :, :, self.rows].permute(0, 1, 3, 2, 4, 5).reshape(B, G, self.nb, R * self.L, d)
+
+    def back(self, t, rep):  # [B, G, nb, rep * L, n] -> [B, G, rep, S, n]
+        B, G, _, _, n = t.shape
+        t = t.view(B, G, self.nb, rep, self.L, n).permute(0, 1, 3, 2, 4, 5)
+        return t.reshape(B, G, rep, self.nb * self.L, n)[:, :, :, :self.S]
+
+    def scores(self, q, k, scale, rep):
+        s = (q @ k.transpose(-1, -2)) * scale
+        return s.masked_fill(~self.mask.repeat(1, rep, 1), -math.inf)
+
+    def add_back(self, t):  # [B, G, nb, keys, d] -> [B, G, S, d], summed over the blocks that hold a key
+        B, G, _, _, d = t.shape
+        out = torch.zeros(B, G, self.S, d, device=t.device)
+        return out.index_add_(2, self.keys.reshape(-1), t.reshape(B, G, -1, d))
+
+
+def _plain_attend(c):
+    band, R = _Band(c), c["heads"] // c["kv_heads"]
+    q, k, v = _split(c, c["qkv"])
+    s = band.scores(band.queries(q), k[:, :, band.keys], 1.0 / math.sqrt(c["d"]), R)
+    m = s.amax(-1, keepdim=True)
+    m = torch.where(m == -math.inf, torch.zeros_like(m), m)  # rows past the end of the last block
+    p = (s - m).exp()
+    z = p.sum(-1, keepdim=True)
+    o = band.back(p @ v[:, :, band.keys] / z, R)  # [B, G, R, S, d]
+    lse = band.back(m + z.log(), R)
+    o = o.reshape(c["B"], c["heads"], c["S"], c["d"]).permute(0, 2, 1, 3).reshape(c["B"] * c["S"], -1)
+    return o.to(torch.bfloat16), lse.reshape(c["B"], c["heads"], c["S"])
+
+
+def _unrotate(t, cos, sin):
+    """Transpose of the half-split rotation; t [..., S, d], tables [S, d / 2]."""
+    a, b = t.chunk(2, -1)
+    return torch.cat([a * cos + b * sin, b * cos - a * sin], -1)
+
+
+def _plain_attend_grad(c):
+    band, B, S, H, G, d = _Band(c), c["B"], c["S"], c["heads"], c["kv_heads"], c["d"]
+    R, scale = H // G, 1.0 / math.sqrt(d)
+    q, k, v = _split(c, c["qkv"])
+    per_row = lambda t: t.view(B, S, H, d).permute(0, 2, 1, 3).reshape(B, G, R, S, d).float()  # noqa: E731
+    o, do = per_row(c["o"]), per_row(c["do"])
+    qb, dob, kb, vb = band.queries(q), band.queries(do), k[:, :, band.keys], v[:, :, band.keys]
+    lse = band.queries(c["lse"].view(B, G, R, S, 1))
+    delta = band.queries((o * do).sum(-1, keepdim=True))
+    p = (band.scores(qb, kb, scale, R) - lse).exp()
+    ds = p * (dob @ vb.transpose(-1, -2) - delta)
+    dv = band.add_back(p.transpose(-1, -2) @ dob)
+    dk = band.add_back(ds.transpose(-1, -2) @ qb) * scale
+    dq = band.back(ds @ kb, R).reshape(B, H, S, d) * scale
+    if c["rope"]:
+        dq, dk = _unrotate(dq, c["cos"], c["sin"]), _unrotate(dk, c["cos"], c["sin"])
+    return torch.cat([dq, dk, dv], 1).permute(0, 2, 1, 3).reshape(B * S, -1).to(torch.bfloat16)
+
+
+def _plain_layernorm(c):
+    x = c["x"].float()
+    mean = x.mean(-1, keepdim=True)
+    rstd = 1.0 / ((x - mean).square().mean(-1, keepdim=True) + EPS).sqrt()
+    y = (x - mean) * rstd * c["gain"].float()
+    if c["beta"] is not None:
+        y = y + c["beta"].float()
+    return y.to(c["x"].dtype), mean[:, 0], rstd[:, 0]
+
+
+def _plain_layernorm_grad(c):
+    xhat = (c["x"].float() - c["mean"][:, None]) * c["rstd"][:, None]
+    dy = c["dy"].float()
+    g = dy * c["gain"].float()
+    dx = (g - g.mean(-1, keepdim=True) - xhat * (g * xhat).mean(-1, keepdim=True)) * c["rstd"][:, None]
+    if c["r"] is not None:
+        dx = dx + c["r"].float()
+    out = [dx.to(c["x"].dtype), (dy * xhat).sum(0)]
+    return out + [dy.sum(0)] if c["bias"] else out
+
+
+_STEP, _SITE, _GROUP = 0xA24BAED4963EE407, 0xD1B54A32D192ED03, 0x8CB92BA72F3D8DD7
+
+
+def _i64(v):
+    """A 64-bit pattern as the signed number torch keeps."""
+    v &= (1 << 64) - 1
+    return v - (1 << 64) if v >> 63 else v
+
+
+def _mix(z):
+    """The splitmix64 finaliser on int64 tensors (wrapping arithmetic, logical shifts)."""
+    z = z + _i64(0x9E3779B97F4A7C15)
+    z = (z ^ ((z >> 30) & ((1 << 34) - 1))) * _i64(0xBF58476D1CE4E5B9)
+    z = (z ^ ((z >> 27) & ((1 << 37) - 1))) * _i64(0x94D049BB133111EB)
+    return z ^ ((z >> 31) & ((1 << 33) - 1))
+
+
+def _plain_dropout(c):
+    rows, h = c["rows"], c["h"]
+    site = torch.full((1,), _i64(c["seed"] ^ ((c["site"] + 1) * _SITE)), dtype=torch.int64, device="cuda")
+    key = _mix(_mix(site) ^ (c["step"] * _i64(_STEP)))
+    word = _mix(key ^ (torch.arange(-(-rows * h // 4), dtype=torch.int64, device="cuda") * _i64(_GROUP)))
+    bits = (word[:, None] >> torch.arange(0, 64, 16, device="cuda")) & 0xFFFF  # four elements a word
+    t = min(65535, int(c["p"] * 65536 + 0.5))
+    keep = bits.view(-1)[:rows * h].view(rows, h) >= t
+    y = torch.where(keep, c["x"].float() * (c["scale"] * 65536.0 / (65536 - t)), 0.0)
+    if c["r"] is not None:
+        y = y + c["r"].float()
+    return y.to(c["x"].dtype)
+
+
+# ------------------------------------------------------------------------------------------------ one pass
+def run(state):
+    c = state
+    if own:
+        return _run_own(c)
+    if c["op"] == "attend":
+        return _plain_attend(c)
+    if c["op"] == "attend_grad":
+        return _plain_attend_grad(c)
+    if c["op"] == "layernorm":
+        return _plain_layernorm(c)
+    if c["op"] == "layernorm_grad":
+        return _plain_layernorm_grad(c)
+    return _plain_dropout(c)
+
+
+def _scratch(c, nbytes):
+    """The workspace a user's program allocates once and keeps."""
+    if "scratch" not in c:
+        c["scratch"] = torch.empty(max(256, nbytes()), dtype=torch.uint8, device="cuda")
+    return c["scratch"]
+
+
+def _run_own(c):
+    from paper_2609_13645_b200 import binding as ft
+    if c["op"].startswith("attend"):
+        size = (c["B"], c["S"], c["heads"], c["kv_heads"], c["d"], c["window"], c["sinks"])
+        if c["op"] == "attend":
+            ft.k_attention_window_fwd(c["qkv"], c["o"], c["lse"], *size)
+            return c["o"], c["lse"]
+        scratch = _scratch(c, lambda: ft.attention_window_scratch_bytes(*size))
+        ft.k_attention_window_bwd(c["qkv"], c["o"], c["do"], c["lse"], c["dqkv"], scratch, *size, cos=c["cos"], sin=c["sin"])
+        return c["dqkv"]
+    if c["op"] == "layernorm":
+        ft.k_layernorm_fwd(c["x"], c["gain"], c["beta"], c["y"], c["mean"], c["rstd"], EPS)
+        return c["y"], c["mean"], c["rstd"]
+    if c["op"] == "layernorm_grad":
+        scratch = _scratch(c, lambda: ft.layernorm_scratch_bytes(c["rows"], c["h"]))
+        ft.k_layernorm_bwd(c["dy"], c["x"], c["mean"], c["rstd"], c["gain"], c["r"], c["y"], c["dgain"], c["dbeta"], scratch)
+        return [c["y"], c["dgain"], c["dbeta"]] if c["bias"] else [c["y"], c["dgain"]]
+    ft.k_dropout_add(c["x"], c["r"], c["y"], c["p"], c["seed"], c["site"], step=c["step"], scale=c["scale"])
+    return c["y"]
+
+
+# ------------------------------------------------------------------------------------------------ definitions in 64 bits
+def _exact_attend(c):
+    """Head by head over the whole score matrix, in row blocks that bound its memory."""
+    B, S, H, G, d = c["B"], c["S"], c["heads"], c["kv_heads"], c["d"]
+    grad, f64 = c["op"] == "attend_grad", dict(dtype=torch.float64, device="cuda")
+    x = c["qkv"].double().view(B, S, H + 2 * G, d)
+    o, lse, dx = torch.zeros(B, S, H, d, **f64), torch.zeros(B, H, S, **f64), torch.zeros(B, S, H + 2 * G, d, **f64)
+    j = torch.arange(S, device="cuda")[None, :]
+    for b in range(B):
+        for n in range(H):
+            kv = n * G // H
+            q, k, v = x[b, :, n], x[b, :, H + kv], x[b, :, H + G + kv]
+            for i0 in range(0, S, 4096):
+                i1 = min(S, i0 + 4096)
+                i = torch.arange(i0, i1, device="cuda")[:, None]
+                seen = (j <= i) & ((i - j < c["window"]) | (j < c["sinks"]))
+                s = torch.where(seen, q[i0:i1] @ k.T / math.sqrt(d), -math.inf)
+                p = torch.softmax(s, -1)
+                if not grad:
+                    o[b, i0:i1, n], lse[b, n, i0:i1] = p @ v, torch.logsumexp(s, -1)
+                    continue
+                do = c["do"].view(B, S, H, d)[b, i0:i1, n].double()
+                oi = c["o"].view(B, S, H, d)[b, i0:i1, n].double()
+                ds = p * (do @ v.T - (do * oi).sum(-1, keepdim=True)) / math.sqrt(d)
+                dx[b, i0:i1, n] = ds @ k
+                dx[b, :, H + kv] += ds.T @ q[i0:i1]
+                dx[b, :, H + G + kv] += p.T @ do
+    if not grad:
+        return o.view(B * S, H * d), lse
+    if c["rope"]:
+        cos, sin = c["cos"].double()[None, :, None], c["sin"].double()[None, :, None]
+        a, b2 = dx[:, :, :H + G, :d // 2].clone(), dx[:, :, :H + G, d // 2:].clone()
+        dx[:, :, :H + G, :d // 2], dx[:, :, :H + G, d // 2:] = a * cos + b2 * sin, b2 * cos - a * sin
+    return dx.view(B * S, -1)
+
+
+def _exact_layernorm(c):
+    x, gain = c["x"].double(), c["gain"].double()
+    if c["op"] == "layernorm":
+        var, mean = torch.var_mean(x, -1, correction=0)
+        rstd = (var + EPS).rsqrt()
+        y = torch.addcmul(torch.zeros_like(gain) if c["beta"] is None else c["beta"].double(), (x - mean[:, None]) * rstd[:, None], gain)
+        return y, mean, rstd
+    h, r = c["h"], c["rstd"].double()
+    n = (x - c["mean"].double()[:, None]) * r[:, None]
+    dy = c["dy"].double()
+    s1, s2 = dy @ gain, torch.einsum("th,h,th->t", dy, gain, n)
+    dx = r[:, None] * (dy * gain - (s1[:, None] + n * s2[:, None]) / h)
+    if c["r"] is not None:
+        dx += c["r"].double()
+    out = [dx, torch.einsum("th,th->h", dy, n)]
+    return out + [dy.sum(0)] if c["bias"] else out
+
+
+def _exact_dropout(c):
+    def mix(z):
+        z = z + np.uint64(0x9E3779B97F4A7C15)
+        z = (z ^ (z >> np.uint64(30))) * np.uint64(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94D049BB133111EB)
+        return z ^ (z >> np.uint64(31))
+
+    n = c["rows"] * c["h"]
+    whole = (1 << 64) - 1
+    with np.errstate(over="ignore"):
+        key = mix(np.array([(c["seed"] ^ ((c["site"] + 1) * _SITE)) & whole], dtype=np.uint64))
+        key = mix(key ^ np.array([int(c["step"][0]) * _STEP & whole], dtype=np.uint64))
+        word = mix(key ^ (np.arange((n + 3) // 4, dtype=np.uint64) * np.uint64(_GROUP)))
+    lanes = word.astype("<u8").view("<u2")[:n].reshape(c["rows"], c["h"])  # little-endian: lane 0 is the low 16 bits
+    t = min(65535, int(math.floor(c["p"] * 65536 + 0.5)))
+    kept = torch.from_numpy(lanes.astype(np.int32) >= t).cuda()
+    x = c["x"].double() * (c["scale"] / (1.0 - t / 65536.0))
+    y = torch.where(kept, x, torch.zeros_like(x))
+    return y if c["r"] is None else y + c["r"].double()
+
+
+def exact(case, seed):
+    c = prepare(case, seed)
+    if c["op"].startswith("attend"):
+        return _exact_attend(c)
+    return _exact_dropout(c) if c["op"] == "dropout" else _exact_layernorm(c)
