@@ -324,8 +324,8 @@ def _run_own(c):
         if c["op"] == "attend":
             ft.k_attention_window_fwd(c["qkv"], c["o"], c["lse"], *size)
             return c["o"], c["lse"]
-        scratch = _scratch(c, lambda: ft.attention_window_scratch_bytes(*size))
-        ft.k_attention_window_bwd(c["qkv"], c["o"], c["do"], c["lse"], c["dqkv"], scratch, *size, cos=c["cos"], sin=c["sin"])
+        scratch, lse = _scratch(c, lambda: ft.attention_window_scratch_bytes(*size)), c["lse"].contiguous()
+        ft.k_attention_window_bwd(c["qkv"], c["o"], c["do"], lse, c["dqkv"], scratch, *size, cos=c["cos"], sin=c["sin"])
         return c["dqkv"]
     if c["op"] == "layernorm":
         ft.k_layernorm_fwd(c["x"], c["gain"], c["beta"], c["y"], c["mean"], c["rstd"], EPS)
