@@ -378,6 +378,61 @@ ft_status ft_k_attention_bwd_noalloc(const void* dev_qkv, const void* dev_o, con
                                      void* dev_dqkv, const float* dev_cos, const float* dev_sin, int32_t B,
                                      int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void* stream);
 
+/* ---- Decoder-block operators beside those of the train step (single kernels like the calls above: device pointers, the
+ * caller's buffers, enqueued on `stream` without waiting, results bit-identical from run to run).  The paper has no
+ * counterpart of them.  All pointers address memory of the CURRENT device. ---- */
+
+/* Causal attention over a sliding window with sink keys: query i sees key j iff j <= i and (i - j < window or
+ * j < n_sinks).  window >= 1, n_sinks >= 0, either may exceed S (window >= S is ft_k_attention_fwd's mask).  Buffers as
+ * in ft_k_attention_fwd, 16-byte aligned; work and traffic are linear in S.  Rows past the end of a shorter sequence
+ * (right padding) are computed like any other and never reach earlier rows; every visible AND every masked value of a
+ * 128-query tile has to be finite, because a masked key's value row is multiplied by 0. */
+ft_status ft_k_attention_window_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
+                                    int32_t n_kv_heads, int32_t head_dim, int32_t window, int32_t n_sinks, void* stream);
+
+/* Its backward, with the conventions of ft_k_attention_bwd (d_q, d_k rotated back when dev_cos / dev_sin [S, d/2] are
+ * given).  dev_scratch: ft_k_attention_window_scratch_bytes(...) bytes (0: the shape is refused), 256-byte aligned,
+ * caller-owned; contents on entry do not matter and are unspecified afterwards; two calls that share it must not overlap
+ * on the GPU.  Too small a scratch returns FT_ENOMEM and launches nothing. */
+size_t ft_k_attention_window_scratch_bytes(int32_t B, int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                           int32_t window, int32_t n_sinks);
+ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* dev_o, const void* dev_do, const float* dev_lse,
+                                    void* dev_dqkv, const float* dev_cos, const float* dev_sin, void* dev_scratch,
+                                    uint64_t scratch_bytes, int32_t B, int32_t S, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t window, int32_t n_sinks, void* stream);
+
+/* LayerNorm of `rows` rows of h elements (1 <= h <= 16384), row r at dev_x + r * ldx (elements): mean and
+ * rstd = 1 / sqrt(var + eps) of each row in fp32, y = R((x - mean) rstd gain + bias).  dtype of x, gain, bias and y: 0 bf16,
+ * 1 fp32.  dev_bias may be NULL.  Any stride >= h and any alignment of the element; 16-byte aligned rows are fastest.
+ * dev_y may be dev_x. */
+ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const void* dev_gain, const void* dev_bias, void* dev_y,
+                             int64_t ldy, float* dev_mean, float* dev_rstd, int32_t rows, int32_t h, float eps,
+                             int32_t dtype, void* stream);
+
+/* Its backward from the saved statistics: with g = dy gain and xhat = (x - mean) rstd,
+ * dx = R(rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid), dgain = sum_rows dy xhat and dbias = sum_rows dy in fp32 (fixed
+ * summation order).  dev_resid (the gradient arriving along the residual connection) and dev_dbias may be NULL; dev_dx
+ * may be dev_dy or dev_resid when their strides are equal.  dev_scratch: ft_k_layernorm_scratch_bytes(rows, h) bytes (0:
+ * refused), 16-byte aligned, used as above. */
+size_t ft_k_layernorm_scratch_bytes(int32_t rows, int32_t h);
+ft_status ft_k_layernorm_bwd(const void* dev_dy, int64_t lddy, const void* dev_x, int64_t ldx, const float* dev_mean,
+                             const float* dev_rstd, const void* dev_gain, const void* dev_resid, int64_t ldr, void* dev_dx,
+                             int64_t lddx, float* dev_dgain, float* dev_dbias, void* dev_scratch, uint64_t scratch_bytes,
+                             int32_t rows, int32_t h, int32_t dtype, void* stream);
+
+/* Dropout of a residual branch: y = R(resid + scale / (1 - p') keep x), dev_resid NULL: 0.  Whether element i = r h + c is
+ * kept is a function of (seed, site, *dev_step, i) alone, so the backward pass is the same call on the gradient with
+ * dev_resid NULL, and nothing is stored: key = mix(mix(seed ^ (site + 1) C1) ^ step C2); bits = the (i mod 4)-th 16 bits
+ * (lowest first) of mix(key ^ (i / 4) C3); kept iff bits >= t, t = min(65535, round(65536 p)), p' = t / 65536.  mix is the
+ * splitmix64 finaliser, C1 = 0xD1B54A32D192ED03, C2 = 0xA24BAED4963EE407, C3 = 0x8CB92BA72F3D8DD7, all modulo 2^64.
+ * site >= 0 tells the branches of a model apart; dev_step (int64 on the device, NULL: 0) is read when the kernel runs, so
+ * that every replay of a captured step draws a new mask.  0 <= p < 1; a dropped element contributes exactly 0, whatever
+ * its value.  dtype 0 bf16, 1 fp32; strides and alignment as in LayerNorm; dev_y may be dev_x or dev_resid when their
+ * strides are equal. */
+ft_status ft_k_dropout_add(const void* dev_x, int64_t ldx, const void* dev_resid, int64_t ldr, void* dev_y, int64_t ldy,
+                           int32_t rows, int32_t h, float p, float scale, uint64_t seed, int32_t site,
+                           const int64_t* dev_step, int32_t dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

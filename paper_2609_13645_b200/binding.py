@@ -115,6 +115,18 @@ def lib():
         L.ft_k_attention_bwd_ws.restype = C.c_int
         L.ft_k_attention_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
         L.ft_k_attention_bwd_noalloc.restype = C.c_int
+        L.ft_k_attention_window_fwd.argtypes = [vp, vp, vp] + [i32] * 7 + [vp]
+        L.ft_k_attention_window_bwd.argtypes = [vp] * 8 + [C.c_uint64] + [i32] * 7 + [vp]
+        L.ft_k_attention_window_scratch_bytes.restype = C.c_size_t
+        L.ft_k_attention_window_scratch_bytes.argtypes = [i32] * 7
+        L.ft_k_layernorm_fwd.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i32, i32, C.c_float, i32, vp]
+        L.ft_k_layernorm_bwd.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, C.c_uint64, i32, i32, i32, vp]
+        L.ft_k_layernorm_scratch_bytes.restype = C.c_size_t
+        L.ft_k_layernorm_scratch_bytes.argtypes = [i32, i32]
+        L.ft_k_dropout_add.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, C.c_float, C.c_float, C.c_uint64, i32, vp, i32, vp]
+        for name in ("ft_k_attention_window_fwd", "ft_k_attention_window_bwd", "ft_k_layernorm_fwd", "ft_k_layernorm_bwd",
+                     "ft_k_dropout_add"):
+            getattr(L, name).restype = C.c_int
         for name in ("ft_init_model", "ft_train_step", "ft_train_step_host", "ft_forward_loss", "ft_forward_backward",
                      "ft_apply_update", "ft_param_info", "ft_get_param", "ft_set_param", "ft_get_step", "ft_set_step",
                      "ft_get_tap", "ft_k_gemm", "ft_k_attention_fwd", "ft_k_attention_bwd"):
@@ -408,3 +420,168 @@ def k_attention_bwd_noalloc(qkv, o, d_o, lse, dqkv, B, S, n_heads, n_kv, d, cos=
         C.c_void_p(qkv.data_ptr()), C.c_void_p(o.data_ptr()), C.c_void_p(d_o.data_ptr()), C.c_void_p(lse.data_ptr()),
         C.c_void_p(dqkv.data_ptr()), C.c_void_p(cos.data_ptr()) if cos is not None else None,
         C.c_void_p(sin.data_ptr()) if sin is not None else None, B, S, n_heads, n_kv, d, _stream_ptr())
+
+
+# ---- decoder-block operators -------------------------------------------------------------------------------
+# Unlike the calls above these check the tensors they are given (type, shape, layout, device) before anything is launched;
+# a refused call raises ForgeStepError with status FT_EINVAL.
+def _refuse(what: str):
+    raise ForgeStepError(FT_EINVAL, what)
+
+
+def _check_flat(name, t, dtype, numel, device):
+    """A contiguous tensor of exactly `numel` elements on `device`."""
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
+        _refuse(f"{name}: expected {numel} contiguous {dtype} elements on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}, "
+                f"strides {t.stride()}")
+
+
+def _check_rows(name, t, dtype, rows, h, device):
+    """A [rows, h] tensor whose rows are contiguous; returns its row stride."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != h or t.dtype != dtype or t.device != device:
+        _refuse(f"{name}: expected [{rows}, {h}] {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if h > 1 and t.stride(1) != 1:
+        _refuse(f"{name}: the elements of a row have to be contiguous, got strides {t.stride()}")
+    if rows > 1 and t.stride(0) < h:
+        _refuse(f"{name}: rows overlap, strides {t.stride()}")
+    return t.stride(0) if rows > 1 else h
+
+
+def _current_device(t):
+    """The device of the call's tensors, which has to be the current one (kernels run on its current stream)."""
+    import torch
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        _refuse(f"tensors on {t.device}, current device cuda:{torch.cuda.current_device()}" if torch.cuda.is_available()
+                else f"tensors on {t.device}: a CUDA device is needed")
+    return t.device
+
+
+def _row_dtype(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return 0
+    if t.dtype == torch.float32:
+        return 1
+    _refuse(f"{t.dtype}: bf16 and fp32 are supported")
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _window_shape(B, S, n_heads, n_kv, d, window, n_sinks):
+    if min(B, S, n_heads, n_kv, window) < 1 or n_sinks < 0 or n_heads % n_kv or d not in (64, 128):
+        _refuse(f"B {B}, S {S}, heads {n_heads} / {n_kv} of {d}, window {window}, sinks {n_sinks}")
+    return min(window, S), min(n_sinks, S)  # a mask beyond the sequence is one that covers it
+
+
+def attention_window_scratch_bytes(B, S, n_heads, n_kv, d, window, n_sinks) -> int:
+    """Bytes of device scratch k_attention_window_bwd needs."""
+    window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
+    return int(lib().ft_k_attention_window_scratch_bytes(B, S, n_heads, n_kv, d, window, n_sinks))
+
+
+def k_attention_window_fwd(qkv, o, lse, B, S, n_heads, n_kv, d, window, n_sinks=0):
+    """Causal attention in which query i sees key j iff j <= i and (i - j < window or j < n_sinks)."""
+    import torch
+    window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
+    dev = _current_device(qkv)
+    _check_flat("qkv", qkv, torch.bfloat16, B * S * (n_heads + 2 * n_kv) * d, dev)
+    _check_flat("o", o, torch.bfloat16, B * S * n_heads * d, dev)
+    _check_flat("lse", lse, torch.float32, B * S * n_heads, dev)
+    st = lib().ft_k_attention_window_fwd(qkv.data_ptr(), o.data_ptr(), lse.data_ptr(), B, S, n_heads, n_kv, d, window, n_sinks,
+                                         _stream_ptr())
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_attention_window_fwd")
+
+
+def k_attention_window_bwd(qkv, o, d_o, lse, dqkv, scratch, B, S, n_heads, n_kv, d, window, n_sinks=0, cos=None, sin=None):
+    """Gradient of k_attention_window_fwd; scratch: a uint8 tensor of attention_window_scratch_bytes(...) bytes; cos, sin: fp32
+    [S, d / 2] tables by which d_q and d_k are rotated back, or None."""
+    import torch
+    window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
+    dev = _current_device(qkv)
+    _check_flat("qkv", qkv, torch.bfloat16, B * S * (n_heads + 2 * n_kv) * d, dev)
+    _check_flat("dqkv", dqkv, torch.bfloat16, B * S * (n_heads + 2 * n_kv) * d, dev)
+    _check_flat("o", o, torch.bfloat16, B * S * n_heads * d, dev)
+    _check_flat("d_o", d_o, torch.bfloat16, B * S * n_heads * d, dev)
+    _check_flat("lse", lse, torch.float32, B * S * n_heads, dev)
+    if (cos is None) != (sin is None):
+        _refuse("cos and sin: both or neither")
+    if cos is not None:
+        _check_flat("cos", cos, torch.float32, S * d // 2, dev)
+        _check_flat("sin", sin, torch.float32, S * d // 2, dev)
+    _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev)
+    st = lib().ft_k_attention_window_bwd(qkv.data_ptr(), o.data_ptr(), d_o.data_ptr(), lse.data_ptr(), dqkv.data_ptr(), _ptr(cos),
+                                         _ptr(sin), scratch.data_ptr(), scratch.numel(), B, S, n_heads, n_kv, d, window, n_sinks,
+                                         _stream_ptr())
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_attention_window_bwd")
+
+
+def k_layernorm_fwd(x, gain, bias, y, mean, rstd, eps=1e-5):
+    """y = (x - mean) rstd gain + bias over the rows of x [rows, h] (bf16 or fp32, any row stride); bias may be None."""
+    import torch
+    dt, dev = _row_dtype(x), _current_device(x)
+    if x.dim() != 2:
+        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
+    rows, h = x.shape
+    ldx, ldy = _check_rows("x", x, x.dtype, rows, h, dev), _check_rows("y", y, x.dtype, rows, h, dev)
+    _check_flat("gain", gain, x.dtype, h, dev)
+    if bias is not None:
+        _check_flat("bias", bias, x.dtype, h, dev)
+    _check_flat("mean", mean, torch.float32, rows, dev)
+    _check_flat("rstd", rstd, torch.float32, rows, dev)
+    st = lib().ft_k_layernorm_fwd(x.data_ptr(), ldx, gain.data_ptr(), _ptr(bias), y.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
+                                  rows, h, eps, dt, _stream_ptr())
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_layernorm_fwd")
+
+
+def layernorm_scratch_bytes(rows, h) -> int:
+    """Bytes of device scratch k_layernorm_bwd needs (0: the shape is refused)."""
+    return int(lib().ft_k_layernorm_scratch_bytes(rows, h))
+
+
+def k_layernorm_bwd(dy, x, mean, rstd, gain, resid, dx, dgain, dbias, scratch):
+    """dx = R(LayerNorm's input gradient + resid), dgain and dbias in fp32; resid and dbias may be None; scratch: a uint8
+    tensor of layernorm_scratch_bytes(rows, h) bytes."""
+    import torch
+    dt, dev = _row_dtype(x), _current_device(x)
+    if x.dim() != 2:
+        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
+    rows, h = x.shape
+    ldx, lddy = _check_rows("x", x, x.dtype, rows, h, dev), _check_rows("dy", dy, x.dtype, rows, h, dev)
+    lddx = _check_rows("dx", dx, x.dtype, rows, h, dev)
+    ldr = _check_rows("resid", resid, x.dtype, rows, h, dev) if resid is not None else 0
+    _check_flat("gain", gain, x.dtype, h, dev)
+    _check_flat("mean", mean, torch.float32, rows, dev)
+    _check_flat("rstd", rstd, torch.float32, rows, dev)
+    _check_flat("dgain", dgain, torch.float32, h, dev)
+    if dbias is not None:
+        _check_flat("dbias", dbias, torch.float32, h, dev)
+    _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev)
+    st = lib().ft_k_layernorm_bwd(dy.data_ptr(), lddy, x.data_ptr(), ldx, mean.data_ptr(), rstd.data_ptr(), gain.data_ptr(), _ptr(resid),
+                                  ldr, dx.data_ptr(), lddx, dgain.data_ptr(), _ptr(dbias), scratch.data_ptr(), scratch.numel(), rows, h,
+                                  dt, _stream_ptr())
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_layernorm_bwd")
+
+
+def k_dropout_add(x, resid, y, p, seed, site, step=None, scale=1.0):
+    """y = R(resid + scale / (1 - p) keep x) over [rows, h] tensors; the mask is a function of (seed, site, step, element), so
+    the backward pass is this call on the gradient with resid None.  step: int64 tensor of one element, read when the
+    kernel runs."""
+    import torch
+    dt, dev = _row_dtype(x), _current_device(x)
+    if x.dim() != 2:
+        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
+    rows, h = x.shape
+    ldx, ldy = _check_rows("x", x, x.dtype, rows, h, dev), _check_rows("y", y, x.dtype, rows, h, dev)
+    ldr = _check_rows("resid", resid, x.dtype, rows, h, dev) if resid is not None else 0
+    if step is not None:
+        _check_flat("step", step, torch.int64, 1, dev)
+    st = lib().ft_k_dropout_add(x.data_ptr(), ldx, _ptr(resid), ldr, y.data_ptr(), ldy, rows, h, p, scale, seed & (2 ** 64 - 1), site,
+                                _ptr(step), dt, _stream_ptr())
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_dropout_add")

@@ -27,6 +27,14 @@ __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v 
 // Round an fp32 value to bf16 and back (the value a stored bf16 tensor would hold).
 __device__ __forceinline__ float round_bf16(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
 
+// The splitmix64 finaliser: the hash behind the counter-based generators (weight initialiser, dropout masks).
+__host__ __device__ __forceinline__ unsigned long long splitmix64(unsigned long long z) {
+  z += 0x9E3779B97F4A7C15ull;
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+
 // SwiGLU backward of one element: a = silu(G) U, so dU = da G s and dG = da U s (1 + G (1 - s)) with s = sigmoid(G).
 // Every operation is spelled out with its rounding so that the stand-alone kernel and the GEMM epilogue that fuses it
 // give the same bits.  The sigmoid uses the hardware exponential and reciprocal like the forward epilogue (relative

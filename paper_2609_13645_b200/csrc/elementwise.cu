@@ -748,13 +748,6 @@ qknorm_bwd_kernel(bf16* __restrict__ dqkv, const bf16* __restrict__ qkv, const f
 }
 
 // ---------------------------------------------------------------- initialisation
-__device__ __forceinline__ unsigned long long splitmix64(unsigned long long z) {
-  z += 0x9E3779B97F4A7C15ull;
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-
 // wgu_cols > 0: the tensor is the gate|up matrix [2f, wgu_cols] stored with rows interleaved 16 gate / 16 up; position i
 // of the stored tensor then holds the draw of its LOGICAL element (gate rows 0..f-1, then up rows 0..f-1)
 __global__ void init_normal_kernel(float* __restrict__ p, size_t n, unsigned long long seed, unsigned long long tensor_id,

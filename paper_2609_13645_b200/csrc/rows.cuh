@@ -1,0 +1,90 @@
+// Vector access shared by the row-wise kernels (LayerNorm, dropout): VEC consecutive elements of a bf16 or fp32 row as
+// floats.  VEC is the widest power of two, up to 16 bytes, that divides the row length, every row stride and every
+// pointer (row_vec); rows that share no more than the element's own alignment run with VEC = 1.
+#pragma once
+#include <stdint.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+
+namespace fs {
+
+template <typename T, int VEC>
+struct RowVec;
+
+template <int VEC>
+struct RowVec<bf16, VEC> {
+  typedef typename std::conditional<VEC == 8, uint4, typename std::conditional<VEC == 4, uint2, typename std::conditional<VEC == 2, uint32_t, uint16_t>::type>::type>::type Raw;
+  static __device__ __forceinline__ Raw zero() {
+    Raw r;
+    memset(&r, 0, sizeof(r));
+    return r;
+  }
+  static __device__ __forceinline__ Raw load(const bf16* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[VEC]) {
+    if constexpr (VEC == 1) {
+      f[0] = __uint_as_float((uint32_t)r << 16);
+    } else {
+      uint32_t w[VEC / 2];
+      memcpy(w, &r, sizeof(r));
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
+    }
+  }
+  static __device__ __forceinline__ void store(bf16* p, const float (&f)[VEC]) {
+    if constexpr (VEC == 1) {
+      *p = __float2bfloat16_rn(f[0]);
+    } else {
+      uint32_t w[VEC / 2];
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+      Raw r;
+      memcpy(&r, w, sizeof(r));
+      *reinterpret_cast<Raw*>(p) = r;
+    }
+  }
+};
+
+template <int VEC>
+struct RowVec<float, VEC> {
+  typedef typename std::conditional<VEC == 4, float4, typename std::conditional<VEC == 2, float2, float>::type>::type Raw;
+  static __device__ __forceinline__ Raw zero() {
+    Raw r;
+    memset(&r, 0, sizeof(r));
+    return r;
+  }
+  static __device__ __forceinline__ Raw load(const float* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[VEC]) { memcpy(f, &r, sizeof(r)); }
+  static __device__ __forceinline__ void store(float* p, const float (&f)[VEC]) {
+    Raw r;
+    memcpy(&r, f, sizeof(r));
+    *reinterpret_cast<Raw*>(p) = r;
+  }
+};
+
+// Hides from the compiler what a packed register holds, so that values unpacked before a barrier are unpacked again after
+// it instead of staying in registers in their wider form.
+template <typename Raw>
+__device__ __forceinline__ void forget(Raw& r) {
+  if constexpr (sizeof(Raw) == 2) {
+    asm volatile("" : "+h"(r));
+  } else {
+    uint32_t w[sizeof(Raw) / 4];
+    memcpy(w, &r, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Raw) / 4); ++i) asm volatile("" : "+r"(w[i]));
+    memcpy(&r, w, sizeof(r));
+  }
+}
+
+// Widest vector width for rows of h elements of `elem` bytes: h and the strides are given or-ed together, as are the
+// pointers' addresses (null pointers change nothing).
+inline int row_vec(uint64_t h_and_strides, uintptr_t pointers, int elem) {
+  int v = 16 / elem;
+  while (v > 1 && ((h_and_strides & (uint64_t)(v - 1)) != 0 || (pointers & (uintptr_t)(v * elem - 1)) != 0)) v >>= 1;
+  return v;
+}
+
+}  // namespace fs
