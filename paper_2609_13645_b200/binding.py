@@ -154,6 +154,14 @@ def _stream_ptr():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _stream_of(index: int) -> int:
+    """The current stream of device `index` as a plain address (the raw query takes 0.1 us where torch.cuda.current_stream()
+    takes 3.3, which a launch-bound operator would notice)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 def bf16_bits_to_f32(a: np.ndarray) -> np.ndarray:
     """uint16 bf16 bit patterns -> float32 values (exact)."""
     return (a.astype(np.uint32) << 16).view(np.float32)
@@ -429,31 +437,37 @@ def _refuse(what: str):
     raise ForgeStepError(FT_EINVAL, what)
 
 
-def _check_flat(name, t, dtype, numel, device):
-    """A contiguous tensor of exactly `numel` elements on `device`."""
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
-        _refuse(f"{name}: expected {numel} contiguous {dtype} elements on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}, "
+def _check_flat(name, t, dtype, numel, index):
+    """The address of a contiguous tensor of exactly `numel` elements on device `index`."""
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != index:
+        _refuse(f"{name}: expected {numel} contiguous {dtype} elements on cuda:{index}, got {tuple(t.shape)} {t.dtype} on {t.device}, "
                 f"strides {t.stride()}")
+    return t.data_ptr()
 
 
-def _check_rows(name, t, dtype, rows, h, device):
-    """A [rows, h] tensor whose rows are contiguous; returns its row stride."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != h or t.dtype != dtype or t.device != device:
-        _refuse(f"{name}: expected [{rows}, {h}] {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    if h > 1 and t.stride(1) != 1:
+def _check_rows(name, t, dtype, rows, h, index):
+    """(address, row stride) of a [rows, h] tensor whose rows are contiguous."""
+    if t.shape != (rows, h) or t.dtype != dtype or t.get_device() != index:
+        _refuse(f"{name}: expected [{rows}, {h}] {dtype} on cuda:{index}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    ld, one = t.stride()
+    if one != 1 and h > 1:
         _refuse(f"{name}: the elements of a row have to be contiguous, got strides {t.stride()}")
-    if rows > 1 and t.stride(0) < h:
+    if rows == 1:
+        ld = h
+    elif ld < h:
         _refuse(f"{name}: rows overlap, strides {t.stride()}")
-    return t.stride(0) if rows > 1 else h
+    return t.data_ptr(), ld
 
 
 def _current_device(t):
-    """The device of the call's tensors, which has to be the current one (kernels run on its current stream)."""
+    """Index of the device of the call's tensors, which has to be the current one (kernels run on its current stream)."""
     import torch
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        _refuse(f"tensors on {t.device}, current device cuda:{torch.cuda.current_device()}" if torch.cuda.is_available()
-                else f"tensors on {t.device}: a CUDA device is needed")
-    return t.device
+    index = t.get_device()
+    if index < 0:
+        _refuse(f"tensors on {t.device}: a CUDA device is needed")
+    if index != torch.cuda.current_device():
+        _refuse(f"tensors on {t.device}, current device cuda:{torch.cuda.current_device()}")
+    return index
 
 
 def _row_dtype(t):
@@ -463,10 +477,6 @@ def _row_dtype(t):
     if t.dtype == torch.float32:
         return 1
     _refuse(f"{t.dtype}: bf16 and fp32 are supported")
-
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
 
 
 def _window_shape(B, S, n_heads, n_kv, d, window, n_sinks):
@@ -486,11 +496,11 @@ def k_attention_window_fwd(qkv, o, lse, B, S, n_heads, n_kv, d, window, n_sinks=
     import torch
     window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
     dev = _current_device(qkv)
-    _check_flat("qkv", qkv, torch.bfloat16, B * S * (n_heads + 2 * n_kv) * d, dev)
-    _check_flat("o", o, torch.bfloat16, B * S * n_heads * d, dev)
-    _check_flat("lse", lse, torch.float32, B * S * n_heads, dev)
-    st = lib().ft_k_attention_window_fwd(qkv.data_ptr(), o.data_ptr(), lse.data_ptr(), B, S, n_heads, n_kv, d, window, n_sinks,
-                                         _stream_ptr())
+    T = B * S
+    st = lib().ft_k_attention_window_fwd(_check_flat("qkv", qkv, torch.bfloat16, T * (n_heads + 2 * n_kv) * d, dev),
+                                         _check_flat("o", o, torch.bfloat16, T * n_heads * d, dev),
+                                         _check_flat("lse", lse, torch.float32, T * n_heads, dev),
+                                         B, S, n_heads, n_kv, d, window, n_sinks, _stream_of(dev))
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_attention_window_fwd")
 
@@ -500,40 +510,39 @@ def k_attention_window_bwd(qkv, o, d_o, lse, dqkv, scratch, B, S, n_heads, n_kv,
     [S, d / 2] tables by which d_q and d_k are rotated back, or None."""
     import torch
     window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
-    dev = _current_device(qkv)
-    _check_flat("qkv", qkv, torch.bfloat16, B * S * (n_heads + 2 * n_kv) * d, dev)
-    _check_flat("dqkv", dqkv, torch.bfloat16, B * S * (n_heads + 2 * n_kv) * d, dev)
-    _check_flat("o", o, torch.bfloat16, B * S * n_heads * d, dev)
-    _check_flat("d_o", d_o, torch.bfloat16, B * S * n_heads * d, dev)
-    _check_flat("lse", lse, torch.float32, B * S * n_heads, dev)
+    dev, bf16, f32 = _current_device(qkv), torch.bfloat16, torch.float32
+    T = B * S
     if (cos is None) != (sin is None):
         _refuse("cos and sin: both or neither")
-    if cos is not None:
-        _check_flat("cos", cos, torch.float32, S * d // 2, dev)
-        _check_flat("sin", sin, torch.float32, S * d // 2, dev)
-    _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev)
-    st = lib().ft_k_attention_window_bwd(qkv.data_ptr(), o.data_ptr(), d_o.data_ptr(), lse.data_ptr(), dqkv.data_ptr(), _ptr(cos),
-                                         _ptr(sin), scratch.data_ptr(), scratch.numel(), B, S, n_heads, n_kv, d, window, n_sinks,
-                                         _stream_ptr())
+    st = lib().ft_k_attention_window_bwd(
+        _check_flat("qkv", qkv, bf16, T * (n_heads + 2 * n_kv) * d, dev), _check_flat("o", o, bf16, T * n_heads * d, dev),
+        _check_flat("d_o", d_o, bf16, T * n_heads * d, dev), _check_flat("lse", lse, f32, T * n_heads, dev),
+        _check_flat("dqkv", dqkv, bf16, T * (n_heads + 2 * n_kv) * d, dev),
+        _check_flat("cos", cos, f32, S * d // 2, dev) if cos is not None else None,
+        _check_flat("sin", sin, f32, S * d // 2, dev) if sin is not None else None,
+        _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev), scratch.numel(), B, S, n_heads, n_kv, d, window, n_sinks,
+        _stream_of(dev))
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_attention_window_bwd")
+
+
+def _rows_of(x):
+    if x.dim() != 2:
+        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
+    return x.shape
 
 
 def k_layernorm_fwd(x, gain, bias, y, mean, rstd, eps=1e-5):
     """y = (x - mean) rstd gain + bias over the rows of x [rows, h] (bf16 or fp32, any row stride); bias may be None."""
     import torch
-    dt, dev = _row_dtype(x), _current_device(x)
-    if x.dim() != 2:
-        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
-    rows, h = x.shape
-    ldx, ldy = _check_rows("x", x, x.dtype, rows, h, dev), _check_rows("y", y, x.dtype, rows, h, dev)
-    _check_flat("gain", gain, x.dtype, h, dev)
-    if bias is not None:
-        _check_flat("bias", bias, x.dtype, h, dev)
-    _check_flat("mean", mean, torch.float32, rows, dev)
-    _check_flat("rstd", rstd, torch.float32, rows, dev)
-    st = lib().ft_k_layernorm_fwd(x.data_ptr(), ldx, gain.data_ptr(), _ptr(bias), y.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(),
-                                  rows, h, eps, dt, _stream_ptr())
+    dt, dev, dtype = _row_dtype(x), _current_device(x), x.dtype
+    rows, h = _rows_of(x)
+    px, ldx = _check_rows("x", x, dtype, rows, h, dev)
+    py, ldy = _check_rows("y", y, dtype, rows, h, dev)
+    st = lib().ft_k_layernorm_fwd(px, ldx, _check_flat("gain", gain, dtype, h, dev),
+                                  _check_flat("bias", bias, dtype, h, dev) if bias is not None else None, py, ldy,
+                                  _check_flat("mean", mean, torch.float32, rows, dev),
+                                  _check_flat("rstd", rstd, torch.float32, rows, dev), rows, h, eps, dt, _stream_of(dev))
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_layernorm_fwd")
 
@@ -547,23 +556,17 @@ def k_layernorm_bwd(dy, x, mean, rstd, gain, resid, dx, dgain, dbias, scratch):
     """dx = R(LayerNorm's input gradient + resid), dgain and dbias in fp32; resid and dbias may be None; scratch: a uint8
     tensor of layernorm_scratch_bytes(rows, h) bytes."""
     import torch
-    dt, dev = _row_dtype(x), _current_device(x)
-    if x.dim() != 2:
-        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
-    rows, h = x.shape
-    ldx, lddy = _check_rows("x", x, x.dtype, rows, h, dev), _check_rows("dy", dy, x.dtype, rows, h, dev)
-    lddx = _check_rows("dx", dx, x.dtype, rows, h, dev)
-    ldr = _check_rows("resid", resid, x.dtype, rows, h, dev) if resid is not None else 0
-    _check_flat("gain", gain, x.dtype, h, dev)
-    _check_flat("mean", mean, torch.float32, rows, dev)
-    _check_flat("rstd", rstd, torch.float32, rows, dev)
-    _check_flat("dgain", dgain, torch.float32, h, dev)
-    if dbias is not None:
-        _check_flat("dbias", dbias, torch.float32, h, dev)
-    _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev)
-    st = lib().ft_k_layernorm_bwd(dy.data_ptr(), lddy, x.data_ptr(), ldx, mean.data_ptr(), rstd.data_ptr(), gain.data_ptr(), _ptr(resid),
-                                  ldr, dx.data_ptr(), lddx, dgain.data_ptr(), _ptr(dbias), scratch.data_ptr(), scratch.numel(), rows, h,
-                                  dt, _stream_ptr())
+    dt, dev, dtype, f32 = _row_dtype(x), _current_device(x), x.dtype, torch.float32
+    rows, h = _rows_of(x)
+    px, ldx = _check_rows("x", x, dtype, rows, h, dev)
+    pdy, lddy = _check_rows("dy", dy, dtype, rows, h, dev)
+    pdx, lddx = _check_rows("dx", dx, dtype, rows, h, dev)
+    pr, ldr = _check_rows("resid", resid, dtype, rows, h, dev) if resid is not None else (None, 0)
+    st = lib().ft_k_layernorm_bwd(pdy, lddy, px, ldx, _check_flat("mean", mean, f32, rows, dev), _check_flat("rstd", rstd, f32, rows, dev),
+                                  _check_flat("gain", gain, dtype, h, dev), pr, ldr, pdx, lddx, _check_flat("dgain", dgain, f32, h, dev),
+                                  _check_flat("dbias", dbias, f32, h, dev) if dbias is not None else None,
+                                  _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev), scratch.numel(), rows, h, dt,
+                                  _stream_of(dev))
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_layernorm_bwd")
 
@@ -573,15 +576,12 @@ def k_dropout_add(x, resid, y, p, seed, site, step=None, scale=1.0):
     the backward pass is this call on the gradient with resid None.  step: int64 tensor of one element, read when the
     kernel runs."""
     import torch
-    dt, dev = _row_dtype(x), _current_device(x)
-    if x.dim() != 2:
-        _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
-    rows, h = x.shape
-    ldx, ldy = _check_rows("x", x, x.dtype, rows, h, dev), _check_rows("y", y, x.dtype, rows, h, dev)
-    ldr = _check_rows("resid", resid, x.dtype, rows, h, dev) if resid is not None else 0
-    if step is not None:
-        _check_flat("step", step, torch.int64, 1, dev)
-    st = lib().ft_k_dropout_add(x.data_ptr(), ldx, _ptr(resid), ldr, y.data_ptr(), ldy, rows, h, p, scale, seed & (2 ** 64 - 1), site,
-                                _ptr(step), dt, _stream_ptr())
+    dt, dev, dtype = _row_dtype(x), _current_device(x), x.dtype
+    rows, h = _rows_of(x)
+    px, ldx = _check_rows("x", x, dtype, rows, h, dev)
+    py, ldy = _check_rows("y", y, dtype, rows, h, dev)
+    pr, ldr = _check_rows("resid", resid, dtype, rows, h, dev) if resid is not None else (None, 0)
+    st = lib().ft_k_dropout_add(px, ldx, pr, ldr, py, ldy, rows, h, p, scale, seed & 0xFFFFFFFFFFFFFFFF, site,
+                                _check_flat("step", step, torch.int64, 1, dev) if step is not None else None, dt, _stream_of(dev))
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_dropout_add")

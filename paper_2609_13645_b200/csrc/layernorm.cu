@@ -1,10 +1,14 @@
 // LayerNorm, forward and backward, over rows of any width and stride.  Reductions run in a fixed order (no floating-point
 // atomics), statistics and sums are fp32, each output is rounded once.
 //
-// A row belongs to a group of GW warps; a lane holds NCH chunks of VEC elements of it, chunk k of lane l of the group
-// being elements (k GW 32 + l) VEC, so every load of a warp is one contiguous run.  The whole row stays in registers
-// between the load and the store: the mean and then the centred sum of squares are taken from there (the difference of
-// sum(x^2) and mean^2 would lose the variance of rows whose mean is large), and nothing is read twice.
+// A row belongs to a group of warps; a thread holds EPL elements of it as chunks of VEC, chunk k of thread l of the group
+// being elements (k threads + l) VEC, so every load of a warp is one contiguous run.  A thread thus owns the same columns of
+// every row it meets: gains and biases stay in registers (read again for every row they would double the L1 traffic), and
+// so do its shares of the gain and bias gradients.
+//
+// Rows come through a ring of NS slots in shared memory, filled by asynchronous copies that each thread issues for its own
+// elements NS - 1 rows ahead: the loads of a row do not wait for the reductions of the one before, and cost no registers.
+// NS = 0, for rows that are only 2-byte aligned, reads global memory directly.
 #include "layernorm.cuh"
 
 #include "../../include/forgestep.h"
@@ -20,328 +24,404 @@ __device__ __forceinline__ void group_sync(int group, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
 }
 
-// ---------------------------------------------------------------- forward
-// y = (x - mean) rstd gain + bias.
-template <typename T, int VEC, int NCH>
-__global__ void __launch_bounds__(512)
-layernorm_fwd_kernel(const T* __restrict__ x, long long ldx, const T* __restrict__ gain, const T* __restrict__ bias, T* __restrict__ y,
-                     long long ldy, float* __restrict__ mean, float* __restrict__ rstd, int rows, int h, int gw, float eps) {
+// The elements of one thread in a ring of NS rows of NT tensors (NS = 0: no ring).
+template <typename T, int VEC, int NCH, int NT, int NS>
+struct RowRing {
   using V = RowVec<T, VEC>;
+  typedef typename V::Raw Raw;
+  static constexpr int SLOT = (int)sizeof(Raw), PAIRS = NCH * VEC / 2;
+  uint32_t base;  // this thread's first slot
+  int threads;
+  static constexpr size_t bytes(int threads) { return (size_t)(NS * NT * NCH * SLOT) * threads; }
+  __device__ __forceinline__ RowRing(const void* smem, int threads) : base(smem_u32(smem) + threadIdx.x * SLOT), threads(threads) {}
+  __device__ __forceinline__ uint32_t slot(int stage, int t, int k) const { return base + (uint32_t)(((stage * NT + t) * NCH + k) * threads * SLOT); }
+  __device__ __forceinline__ void fetch(int stage, int t, const T* row, bool live, int first, int stride, int h) const {
+    if constexpr (NS > 0) {
+#pragma unroll
+      for (int k = 0; k < NCH; ++k) {
+        const int c = first + k * stride;
+        const bool ok = live && c < h;
+        async_copy<SLOT>(slot(stage, t, k), ok ? row + c : row, ok);
+      }
+    }
+  }
+  // this thread's elements of tensor t of the row in `stage` (row: where it lies in global memory, read when there is no
+  // ring); 0 outside the row
+  __device__ __forceinline__ void get(int stage, int t, const T* row, int first, int stride, int h, float2 (&v)[PAIRS]) const {
+    float f[NCH * VEC];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      Raw r;
+      if constexpr (NS > 0) {
+        const uint32_t at = slot(stage, t, k);
+        uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+        if constexpr (SLOT == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+        else if constexpr (SLOT == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
+      } else {
+        const int c = first + k * stride;
+        r = c < h ? V::load(row + c) : V::zero();
+      }
+      float u[VEC];
+      V::unpack(r, u);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[k * VEC + e] = u[e];
+    }
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+  }
+  __device__ __forceinline__ static void put(T* row, int first, int stride, int h, const float2 (&v)[PAIRS]) {
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = first + k * stride;
+      if (c < h) {
+        float u[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[e] = (k * VEC + e) & 1 ? v[(k * VEC + e) / 2].y : v[(k * VEC + e) / 2].x;
+        V::store(row + c, u);
+      }
+    }
+  }
+};
+
+// A row vector (gain, bias) in registers: as fp32 pairs where a thread has few columns of it, packed as it came otherwise.
+template <typename T, int VEC, int NCH>
+struct RowConst {
+  using V = RowVec<T, VEC>;
+  static constexpr int PAIRS = NCH * VEC / 2;
+  static constexpr bool WIDE = PAIRS > 8;
+  float2 v[WIDE ? 1 : PAIRS];
+  const T* p;
+  __device__ __forceinline__ void init(const T* ptr, int first, int stride, int h) {
+    p = ptr;
+    if constexpr (!WIDE) fill(first, stride, h, v);
+  }
+  __device__ __forceinline__ void fill(int first, int stride, int h, float2 (&o)[PAIRS]) const {
+    float f[NCH * VEC];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = first + k * stride;
+      float u[VEC];
+      V::unpack(p != nullptr && c < h ? V::load(p + c) : V::zero(), u);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[k * VEC + e] = u[e];
+    }
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) o[i] = make_float2(f[2 * i], f[2 * i + 1]);
+  }
+  __device__ __forceinline__ void get(int first, int stride, int h, float2 (&o)[PAIRS]) const {
+    if constexpr (WIDE) {
+      fill(first, stride, h, o);  // stays in L1
+    } else {
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) o[i] = v[i];
+    }
+  }
+};
+
+// ---------------------------------------------------------------- forward
+// y = (x - mean) rstd gain + bias.  The row stays in registers: first the mean, then the centred sum of squares (the
+// difference of sum(x^2) / h and mean^2 would lose the variance of rows whose mean is large).
+template <typename T, int VEC, int NCH, int NS, int MAXT>
+__global__ void __launch_bounds__(MAXT)
+layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, const T* __restrict__ bias, T* y, long long ldy,
+                     float* __restrict__ mean, float* __restrict__ rstd, int rows, int h, int gw, float eps) {
+  using Ring = RowRing<T, VEC, NCH, 1, NS>;
+  constexpr int PAIRS = Ring::PAIRS;
   pdl_trigger();
   pdl_wait();
+  extern __shared__ __align__(16) uint8_t ring_mem[];
   __shared__ float s_part[2][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / gw, gwarp = warp - group * gw, groups = (blockDim.x >> 5) / gw;
   const int first = (gwarp * 32 + lane) * VEC, stride = gw * 32 * VEC;
   const float inv_h = 1.0f / (float)h;
-  // sum over the group's lanes; every thread gets the same bits.  The two sums of a row use different slots, and the
-  // second barrier of a row lies between the reads of the first sum and its next overwrite.
-  auto group_sum = [&](float v, int which) {
-    v = warp_sum(v);
+  const Ring ring(ring_mem, blockDim.x);
+  // sum over the group; every thread gets the same bits.  The two sums of a row use different slots: each slot's readers
+  // have passed the other's barrier before it is written again.
+  auto group_sum = [&](float2 p, int which) {
+    const float v = warp_sum(p.x + p.y);
     if (gw == 1) return v;
     if (lane == 0) s_part[which][warp] = v;
     group_sync(group, gw * 32);
-    float t = 0.f;
-    for (int w = 0; w < gw; ++w) t += s_part[which][group * gw + w];
+    float t = s_part[which][group * gw];
+    for (int w = 1; w < gw; ++w) t += s_part[which][group * gw + w];
     return t;
   };
-  for (long long row = (long long)blockIdx.x * groups + group; row < rows; row += (long long)gridDim.x * groups) {
-    const T* xr = x + row * ldx;
-    typename V::Raw raw[NCH];
+  const long long step = (long long)gridDim.x * groups;
+  long long row = (long long)blockIdx.x * groups + group, ahead = row;
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int c = first + k * stride;
-      raw[k] = c < h ? V::load(xr + c) : V::zero();
+  for (int s = 0; s < NS - 1; ++s, ahead += step) {
+    ring.fetch(s, 0, x + (ahead < rows ? ahead : 0) * ldx, ahead < rows, first, stride, h);
+    async_commit();
+  }
+  RowConst<T, VEC, NCH> cg, cb;
+  cg.init(gain, first, stride, h);
+  cb.init(bias, first, stride, h);
+  int stage = 0;
+  for (; row < rows; row += step, ahead += step) {
+    if constexpr (NS > 0) {
+      ring.fetch(stage == 0 ? NS - 1 : stage - 1, 0, x + (ahead < rows ? ahead : 0) * ldx, ahead < rows, first, stride, h);
+      async_commit();
+      async_wait<NS - 1>();
     }
-    float s = 0.f;
+    float2 v[PAIRS], s = both(0.f), ss = both(0.f);
+    ring.get(stage, 0, x + row * ldx, first, stride, h, v);
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      float f[VEC];
-      V::unpack(raw[k], f);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) s += f[e];
-    }
+    for (int i = 0; i < PAIRS; ++i) s = add2(s, v[i]);
     const float mu = group_sum(s, 0) * inv_h;
-    float ss = 0.f;
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      float f[VEC];
-      V::unpack(raw[k], f);
-      if (first + k * stride < h) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) ss += (f[e] - mu) * (f[e] - mu);
-      }
+    for (int i = 0; i < PAIRS; ++i) {
+      float2 m = both(-mu);  // columns outside the row stay 0
+      if (first + (2 * i / VEC) * stride >= h) m.x = 0.f;
+      if (first + ((2 * i + 1) / VEC) * stride >= h) m.y = 0.f;
+      v[i] = add2(v[i], m);
+      ss = fma2(v[i], v[i], ss);
     }
     const float rs = 1.0f / sqrtf(group_sum(ss, 1) * inv_h + eps);
     if (gwarp == 0 && lane == 0) {
       mean[row] = mu;
       rstd[row] = rs;
     }
-    T* yr = y + row * ldy;
+    float2 g[PAIRS], b[PAIRS];
+    cg.get(first, stride, h, g);
+    cb.get(first, stride, h, b);
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int c = first + k * stride;
-      if (c < h) {
-        float f[VEC], g[VEC], b[VEC];
-        V::unpack(raw[k], f);
-        V::unpack(V::load(gain + c), g);
-        if (bias != nullptr) V::unpack(V::load(bias + c), b);
+    for (int i = 0; i < PAIRS; ++i) v[i] = fma2(mul2(v[i], both(rs)), g[i], b[i]);
+    Ring::put(y + row * ldy, first, stride, h, v);
+    if (NS > 0 && ++stage == NS) stage = 0;
+  }
+}
+
+// ---------------------------------------------------------------- backward
+// dx = rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid with g = dy gain; dgain = sum over rows of dy xhat, dbias of dy.
+// g and xhat stay in registers between the two sums of a row and its update.  A block leaves one partial row of dgain and
+// dbias, which a second kernel adds in block order.
+template <typename T, int VEC, int NCH, int NS, int MAXT>
+__global__ void __launch_bounds__(MAXT, 1)
+layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, const float* __restrict__ mean,
+                     const float* __restrict__ rstd, const T* __restrict__ gain, const T* resid, long long ldr, T* dx, long long lddx,
+                     float* __restrict__ partial, int rows, int h, int gw) {
+  using Ring = RowRing<T, VEC, NCH, 3, NS>;
+  constexpr int PAIRS = Ring::PAIRS;
+  pdl_trigger();
+  pdl_wait();
+  // the ring; after the last row the groups of a block add their column sums in its place
+  extern __shared__ __align__(16) uint8_t ring_mem[];
+  __shared__ float s_part[2][16][2];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int group = warp / gw, gwarp = warp - group * gw, groups = (blockDim.x >> 5) / gw;
+  const int first = (gwarp * 32 + lane) * VEC, stride = gw * 32 * VEC;
+  const float inv_h = 1.0f / (float)h;
+  const Ring ring(ring_mem, blockDim.x);
+  const long long step = (long long)gridDim.x * groups;
+  long long row = (long long)blockIdx.x * groups + group, ahead = row;
+  auto fetch = [&](int stage) {
+    const bool live = ahead < rows;
+    const long long r = live ? ahead : 0;
+    ring.fetch(stage, 0, dy + r * lddy, live, first, stride, h);
+    ring.fetch(stage, 1, x + r * ldx, live, first, stride, h);
+    if (resid != nullptr) ring.fetch(stage, 2, resid + r * ldr, live, first, stride, h);
+    ahead += step;
+    async_commit();
+  };
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = (f[e] - mu) * rs * g[e] + (bias != nullptr ? b[e] : 0.f);
-        V::store(yr + c, f);
-      }
+  for (int s = 0; s < NS - 1; ++s) fetch(s);
+  float mu_next = row < rows ? mean[row] : 0.f, rs_next = row < rows ? rstd[row] : 0.f;
+  RowConst<T, VEC, NCH> cg;
+  cg.init(gain, first, stride, h);
+  float2 acc_g[PAIRS], acc_b[PAIRS];
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i) acc_g[i] = acc_b[i] = both(0.f);
+  int parity = 0, stage = 0;
+  for (; row < rows; row += step) {
+    const float mu = mu_next, rs = rs_next;
+    if constexpr (NS > 0) fetch(stage == 0 ? NS - 1 : stage - 1);
+    if (row + step < rows) {
+      mu_next = mean[row + step];
+      rs_next = rstd[row + step];
+    }
+    if constexpr (NS > 0) async_wait<NS - 1>();
+    float2 a[PAIRS], xh[PAIRS], g[PAIRS], p1 = both(0.f), p2 = both(0.f);
+    ring.get(stage, 0, dy + row * lddy, first, stride, h, a);
+    ring.get(stage, 1, x + row * ldx, first, stride, h, xh);
+    cg.get(first, stride, h, g);
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) {
+      xh[i] = mul2(add2(xh[i], both(-mu)), both(rs));  // outside the row a = 0 and what xh holds does not matter
+      acc_g[i] = fma2(a[i], xh[i], acc_g[i]);
+      acc_b[i] = add2(a[i], acc_b[i]);
+      a[i] = mul2(a[i], g[i]);
+      p1 = add2(p1, a[i]);
+      p2 = fma2(a[i], xh[i], p2);
+    }
+    float s1 = p1.x + p1.y, s2 = p2.x + p2.y;
+    {  // both sums in 6 shuffles: the half warps keep one each after the first
+      const bool up = (lane & 16) != 0;
+      float v = (up ? s2 : s1) + __shfl_xor_sync(0xffffffffu, up ? s1 : s2, 16);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if ((lane & 15) == 0) s_part[parity][warp][lane >> 4] = v;
+    }
+    if (gw == 1) __syncwarp(); else group_sync(group, gw * 32);
+    s1 = s_part[parity][group * gw][0];
+    s2 = s_part[parity][group * gw][1];
+    for (int w = 1; w < gw; ++w) {
+      s1 += s_part[parity][group * gw + w][0];
+      s2 += s_part[parity][group * gw + w][1];
+    }
+    parity ^= 1;  // the other slot is free: everyone passed this barrier after its last reads
+    const float2 c1 = both(-rs * (s1 * inv_h)), c2 = both(-rs * (s2 * inv_h));
+    if (resid != nullptr) {
+      float2 q[PAIRS];
+      ring.get(stage, 2, resid + row * ldr, first, stride, h, q);
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) a[i] = add2(fma2(a[i], both(rs), fma2(xh[i], c2, c1)), q[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) a[i] = fma2(a[i], both(rs), fma2(xh[i], c2, c1));
+    }
+    Ring::put(dx + row * lddx, first, stride, h, a);
+    if (NS > 0 && ++stage == NS) stage = 0;
+  }
+  // One partial row a block.  Its groups leave their sums side by side in shared memory and all threads add them, in group
+  // order.
+  float* out = partial + (long long)blockIdx.x * 2 * h;
+  float* col = reinterpret_cast<float*>(ring_mem);
+  if (groups > 1) {
+    if constexpr (NS > 0) async_wait<0>();
+    __syncthreads();
+  }
+  float* mine = groups > 1 ? col + (long long)group * 2 * h : out;
+#pragma unroll
+  for (int i = 0; i < PAIRS * 2; ++i) {
+    const int c = first + (i / VEC) * stride + i % VEC;
+    if (c < h) {
+      mine[c] = i & 1 ? acc_g[i / 2].y : acc_g[i / 2].x;
+      mine[h + c] = i & 1 ? acc_b[i / 2].y : acc_b[i / 2].x;
+    }
+  }
+  if (groups > 1) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * h; c += blockDim.x) {
+      float t = col[c];
+      for (int g = 1; g < groups; ++g) t += col[(long long)g * 2 * h + c];
+      out[c] = t;
     }
   }
 }
 
-template <typename T, int VEC, int EPL>
+// Column sums of the block partials in a fixed order: a CTA takes 32 columns, 32 strided subsets of the blocks run side by
+// side (each thread reads 4 columns at a time where they are aligned) and are then added in subset order.
+template <int VEC>
+__global__ void __launch_bounds__(32 * 32 / VEC)
+layernorm_colsum_kernel(const float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int nblk, int h) {
+  using V = RowVec<float, VEC>;
+  pdl_trigger();
+  pdl_wait();
+  __shared__ float s[32][33];
+  constexpr int TX = 32 / VEC;
+  const int cx = threadIdx.x % TX, ry = threadIdx.x / TX;
+  const int cols = dbias != nullptr ? 2 * h : h;
+  const int c = blockIdx.x * 32 + cx * VEC;
+  float a[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) a[e] = 0.f;
+  if (c < cols) {
+#pragma unroll 4
+    for (int b = ry; b < nblk; b += 32) {
+      float f[VEC];
+      V::unpack(V::load(partial + (long long)b * 2 * h + c), f);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) a[e] += f[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[ry][cx * VEC + e] = a[e];
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  const int col = blockIdx.x * 32 + threadIdx.x;
+  if (col >= cols) return;
+  float tot = 0.f;
+#pragma unroll
+  for (int w = 0; w < 32; ++w) tot += s[w][threadIdx.x];
+  if (col < h) dgain[col] = tot; else dbias[col - h] = tot;
+}
+
+int blocks_for(int rows, int groups, int most) {
+  const long long want = ((long long)rows + groups - 1) / groups;
+  return (int)(want < most ? want : most);
+}
+
+// Elements a thread holds of a row.  16 up to 8192 columns and 32 beyond, so that a group never exceeds 16 warps; 8 where a
+// warp covers the row with them, and for rows whose accesses are narrower than 16 bytes (every one of them is an
+// instruction: fewer a thread, more threads; 4099 x 771 fp32 backward 17.7 us with 8, 28.7 with 16).
+int elements_per_thread(int h, bool narrow) { return h <= 256 || (narrow && h <= 4096) ? 8 : h <= 8192 ? 16 : 32; }
+
+template <typename T, int VEC, int EPL, int NS, int MAXT>
 cudaError_t fwd_launch(const void* x, int64_t ldx, const void* gain, const void* bias, void* y, int64_t ldy, float* mean, float* rstd,
-                       int rows, int h, int gw, float eps, cudaStream_t st) {
-  constexpr int NCH = EPL / VEC > 0 ? EPL / VEC : 1;
-  const int groups = gw >= 8 ? 1 : 8 / gw;
-  const long long want = (rows + groups - 1) / groups;
-  const int blocks = (int)(want < kSms * 16 ? want : kSms * 16);
-  return launch_pdl(layernorm_fwd_kernel<T, VEC, NCH>, dim3(blocks), dim3(groups * gw * 32), 0, st, reinterpret_cast<const T*>(x),
-                    (long long)ldx, reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(bias), reinterpret_cast<T*>(y),
-                    (long long)ldy, mean, rstd, rows, h, gw, eps);
+                       int rows, int h, float eps, cudaStream_t st) {
+  using Ring = RowRing<T, VEC, EPL / VEC, 1, NS>;
+  auto kern = layernorm_fwd_kernel<T, VEC, EPL / VEC, NS, MAXT>;
+  const int gw = (h + 32 * EPL - 1) / (32 * EPL);
+  int groups = MAXT / 32 / gw;
+  if (rows <= kSms * groups) groups = 1;  // few rows: spread them over the SMs
+  const int threads = groups * gw * 32;
+  static unsigned long long smem_set = 0;
+  cudaError_t e = ensure_dynamic_smem(kern, (int)Ring::bytes(MAXT), smem_set);
+  if (e != cudaSuccess) return e;
+  // 768 threads an SM (8192 x 2048 bf16: 3 blocks of 256 15.9 us, 1 of 512 20.2, 4 of 256 18.9; as many as fit 17.0)
+  return launch_pdl(kern, dim3(blocks_for(rows, groups, kSms * (MAXT == 256 ? 3 : 1))), dim3(threads), Ring::bytes(threads), st,
+                    reinterpret_cast<const T*>(x), (long long)ldx, reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(bias),
+                    reinterpret_cast<T*>(y), (long long)ldy, mean, rstd, rows, h, gw, eps);
 }
 
 template <typename T, int VEC>
 cudaError_t fwd_width(const void* x, int64_t ldx, const void* gain, const void* bias, void* y, int64_t ldy, float* mean, float* rstd,
                       int rows, int h, float eps, cudaStream_t st) {
-  // one warp a row up to 1024 elements (2048 in bf16, whose lane then holds 64 elements in 32 registers), then a warp
-  // for every 1024 elements of the row
-  if (h <= 256) return fwd_launch<T, VEC, 8>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, 1, eps, st);
-  if constexpr (sizeof(T) == 2 && VEC == 8)
-    if (h > 1024 && h <= 2048) return fwd_launch<T, VEC, 64>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, 1, eps, st);
-  return fwd_launch<T, VEC, 32>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, (h + 1023) / 1024, eps, st);
+  constexpr int NS = VEC * sizeof(T) >= 4 ? 3 : 0;
+  const int epl = elements_per_thread(h, VEC * sizeof(T) < 16);
+#define LN_FWD_W(EPL, MAXT) fwd_launch<T, VEC, EPL, NS, MAXT>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st)
+  const bool small = h <= 256 * epl;  // a row fits a block of 256 threads
+  if (epl == 8) return small ? LN_FWD_W(8, 256) : LN_FWD_W(8, 512);
+  if (epl == 16) return small ? LN_FWD_W(16, 256) : LN_FWD_W(16, 512);
+  return LN_FWD_W(32, 512);
+#undef LN_FWD_W
 }
 
-// ---------------------------------------------------------------- backward
-// dx = rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid with g = dy gain; dgain = sum over rows of dy xhat, dbias of dy.
-// A thread owns the same columns of every row it meets, so its share of dgain and dbias stays in registers for the whole
-// launch; a block leaves one partial row of each, which a second kernel adds in block order.  R rows are in flight at a
-// time: their two sums are reduced over the group together (one barrier for R rows).  HOLD: the rows stay in registers
-// between the sums and the update; the widest rows are read a second time (from L1 or L2) instead of spilling.
-constexpr int kBwdMaxBlocks = kSms * 2;
-
-// Sums of N values over a warp, N a power of two up to 32: each step halves the values a lane still carries, so it takes
-// N - 1 + log2(32 / N) shuffles instead of 5 N.  Lane l ends with the total of value index l / (32 / N).
-template <int N>
-__device__ __forceinline__ float warp_sum_many(float (&v)[N], int lane) {
-  int half = 16;
-#pragma unroll
-  for (int n = N; n > 1; n >>= 1) {
-    const bool up = (lane & half) != 0;
-#pragma unroll
-    for (int i = 0; i < n / 2; ++i) {
-      const float send = up ? v[i] : v[i + n / 2];
-      const float keep = up ? v[i + n / 2] : v[i];
-      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, half);
-    }
-    half >>= 1;
-  }
-  float t = v[0];
-  for (; half > 0; half >>= 1) t += __shfl_xor_sync(0xffffffffu, t, half);
-  return t;
-}
-
-template <typename T, int VEC, int NCH, int R, bool HOLD>
-__global__ void __launch_bounds__(VEC * NCH == 8 ? 256 : 512, VEC * NCH == 8 ? 2 : 1)
-layernorm_bwd_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, const float* __restrict__ mean,
-                     const float* __restrict__ rstd, const T* __restrict__ gain, const T* resid, long long ldr, T* dx, long long lddx,
-                     float* __restrict__ partial, int rows, int h, int gw) {
-  using V = RowVec<T, VEC>;
-  pdl_trigger();
-  pdl_wait();
-  extern __shared__ float smem[];  // [2][warps][2 R] row sums, then (several groups) [2 h] column sums
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int group = warp / gw, gwarp = warp - group * gw, groups = warps / gw;
-  const int first = (gwarp * 32 + lane) * VEC, stride = gw * 32 * VEC;
-  const float inv_h = 1.0f / (float)h;
-  float acc_g[NCH][VEC], acc_b[NCH][VEC];
-#pragma unroll
-  for (int k = 0; k < NCH; ++k) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) acc_g[k][e] = acc_b[k][e] = 0.f;
-  }
-  int parity = 0;
-  for (long long row0 = ((long long)blockIdx.x * groups + group) * R; row0 < rows; row0 += (long long)gridDim.x * groups * R) {
-    typename V::Raw rdy[R][NCH], rx[R][NCH], rr[R][NCH];
-    float mu[R], rs[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool live = row0 + r < rows;
-#pragma unroll
-      for (int k = 0; k < NCH; ++k) {
-        const int c = first + k * stride;
-        const bool ok = live && c < h;
-        rdy[r][k] = ok ? V::load(dy + (row0 + r) * lddy + c) : V::zero();
-        rx[r][k] = ok ? V::load(x + (row0 + r) * ldx + c) : V::zero();
-        if (HOLD) rr[r][k] = ok && resid != nullptr ? V::load(resid + (row0 + r) * ldr + c) : V::zero();
-      }
-      mu[r] = live ? mean[row0 + r] : 0.f;
-      rs[r] = live ? rstd[row0 + r] : 0.f;
-    }
-    float sums[2 * R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-      for (int k = 0; k < NCH; ++k) {
-        const int c = first + k * stride;
-        float a[VEC], b[VEC], gn[VEC];
-        V::unpack(rdy[r][k], a);
-        V::unpack(rx[r][k], b);
-        V::unpack(c < h ? V::load(gain + c) : V::zero(), gn);  // gains stay in L1
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float xh = (b[e] - mu[r]) * rs[r], g = a[e] * gn[e];  // a = 0 outside the row
-          s1 += g;
-          s2 += g * xh;
-          acc_g[k][e] += a[e] * xh;
-          acc_b[k][e] += a[e];
-        }
-      }
-      sums[2 * r] = s1;
-      sums[2 * r + 1] = s2;
-    }
-    const float tot = warp_sum_many<2 * R>(sums, lane);
-    float m1[R], m2[R];
-    float* slot = smem + parity * warps * 2 * R;
-    if ((lane & (32 / (2 * R) - 1)) == 0) slot[warp * 2 * R + lane / (32 / (2 * R))] = tot;
-    if (gw == 1) __syncwarp(); else group_sync(group, gw * 32);
-#pragma unroll
-    for (int r = 0; r < R; ++r) m1[r] = m2[r] = 0.f;
-    for (int w = 0; w < gw; ++w) {
-      const float* p = slot + (group * gw + w) * 2 * R;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        m1[r] += p[2 * r];
-        m2[r] += p[2 * r + 1];
-      }
-    }
-    parity ^= 1;  // the other slot is free: everyone passed this barrier after its last reads
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (row0 + r < rows) {
-        const float a1 = m1[r] * inv_h, a2 = m2[r] * inv_h;
-#pragma unroll
-        for (int k = 0; k < NCH; ++k) {
-          const int c = first + k * stride;
-          if (c < h) {
-            if (HOLD) {
-              forget(rdy[r][k]);
-              forget(rx[r][k]);
-            } else {
-              rdy[r][k] = V::load(dy + (row0 + r) * lddy + c);
-              rx[r][k] = V::load(x + (row0 + r) * ldx + c);
-              rr[r][k] = resid != nullptr ? V::load(resid + (row0 + r) * ldr + c) : V::zero();
-            }
-            float a[VEC], b[VEC], q[VEC], o[VEC], gn[VEC];
-            V::unpack(rdy[r][k], a);
-            V::unpack(rx[r][k], b);
-            V::unpack(rr[r][k], q);
-            V::unpack(V::load(gain + c), gn);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-              const float xh = (b[e] - mu[r]) * rs[r];
-              o[e] = rs[r] * (a[e] * gn[e] - a1 - xh * a2) + q[e];
-            }
-            V::store(dx + (row0 + r) * lddx + c, o);
-          }
-        }
-      }
-    }
-  }
-  // one partial row a block: its groups are added in group order
-  float* out_g = partial + (long long)blockIdx.x * 2 * h;
-  float* out_b = out_g + h;
-  float* col = smem + 2 * warps * 2 * R;
-  for (int g = 0; g < groups; ++g) {
-    if (group == g) {
-#pragma unroll
-      for (int k = 0; k < NCH; ++k) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const int c = first + k * stride + e;
-          if (c < h) {
-            float tg = acc_g[k][e], tb = acc_b[k][e];
-            if (g > 0) { tg += col[c]; tb += col[h + c]; }
-            if (g + 1 < groups) { col[c] = tg; col[h + c] = tb; }
-            else { out_g[c] = tg; out_b[c] = tb; }
-          }
-        }
-      }
-    }
-    if (groups > 1) __syncthreads();
-  }
-}
-
-// Column sums of the block partials in block order: 32 columns x 8 strided row groups a CTA, the groups added in order.
-__global__ void __launch_bounds__(256)
-layernorm_colsum_kernel(const float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int nblk, int h) {
-  pdl_trigger();
-  pdl_wait();
-  __shared__ float s[8][33];
-  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-  const int cols = dbias != nullptr ? 2 * h : h;
-  const int c = blockIdx.x * 32 + cx;
-  float a = 0.f;
-  if (c < cols)
-    for (int b = ry; b < nblk; b += 8) a += partial[(long long)b * 2 * h + c];
-  s[ry][cx] = a;
-  __syncthreads();
-  if (ry == 0 && c < cols) {
-    float tot = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) tot += s[w][cx];
-    if (c < h) dgain[c] = tot; else dbias[c - h] = tot;
-  }
-}
-
-struct BwdShape {
-  int epl, gw, groups, blocks;
-};
-
-// 8 columns a thread up to 2048 columns; wider rows take 16 and 32 columns a thread, so that a block never exceeds 16
-// warps and a thread 128 registers.  At least 8 warps a block.  One block for every 32 / epl rows of its groups, at most two
-// an SM: the scratch size follows from rows and h alone.
-BwdShape bwd_shape(int rows, int h) {
-  BwdShape s;
-  s.epl = h <= 2048 ? 8 : h <= 8192 ? 16 : 32;
-  const int r = 32 / s.epl;
-  s.gw = (h + 32 * s.epl - 1) / (32 * s.epl);
-  s.groups = s.gw >= 8 ? 1 : 8 / s.gw;
-  const long long want = ((long long)rows + s.groups * r - 1) / (s.groups * r);
-  s.blocks = (int)(want < kBwdMaxBlocks ? want : kBwdMaxBlocks);
-  return s;
-}
-
-template <typename T, int VEC, int EPL, int R, bool HOLD>
+template <typename T, int VEC, int EPL, int NS>
 cudaError_t bwd_launch(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd, const void* gain,
                        const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias, float* scratch, int rows,
-                       int h, const BwdShape& s, cudaStream_t st) {
-  const int warps = s.gw * s.groups;
-  const size_t smem = (size_t)(2 * warps * 2 * R + (s.groups > 1 ? 2 * h : 0)) * sizeof(float);
-  cudaError_t e = launch_pdl(layernorm_bwd_kernel<T, VEC, EPL / VEC, R, HOLD>, dim3(s.blocks), dim3(warps * 32), smem, st,
-                             reinterpret_cast<const T*>(dy), (long long)lddy, reinterpret_cast<const T*>(x), (long long)ldx, mean, rstd,
-                             reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(resid), (long long)ldr,
-                             reinterpret_cast<T*>(dx), (long long)lddx, scratch, rows, h, s.gw);
+                       int h, cudaStream_t st) {
+  using Ring = RowRing<T, VEC, EPL / VEC, 3, NS>;
+  auto kern = layernorm_bwd_kernel<T, VEC, EPL / VEC, NS, 512>;
+  const int gw = (h + 32 * EPL - 1) / (32 * EPL), groups = 16 / gw, threads = groups * gw * 32;
+  const int blocks = blocks_for(rows, groups, kSms);
+  const size_t col = groups > 1 ? (size_t)groups * 2 * h * sizeof(float) : 0;  // at most 2 * 512 * EPL floats
+  constexpr size_t most = Ring::bytes(512) > 4096 * EPL ? Ring::bytes(512) : 4096 * EPL;
+  static unsigned long long smem_set = 0;
+  cudaError_t e = ensure_dynamic_smem(kern, (int)most, smem_set);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(kern, dim3(blocks), dim3(threads), Ring::bytes(threads) > col ? Ring::bytes(threads) : col, st,
+                 reinterpret_cast<const T*>(dy), (long long)lddy, reinterpret_cast<const T*>(x), (long long)ldx, mean, rstd,
+                 reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(resid), (long long)ldr, reinterpret_cast<T*>(dx),
+                 (long long)lddx, scratch, rows, h, gw);
   if (e != cudaSuccess) return e;
   const int cols = dbias != nullptr ? 2 * h : h;
-  return launch_pdl(layernorm_colsum_kernel, dim3((cols + 31) / 32), dim3(256), 0, st, scratch, dgain, dbias, s.blocks, h);
+  if (h % 4 == 0) return launch_pdl(layernorm_colsum_kernel<4>, dim3((cols + 31) / 32), dim3(256), 0, st, scratch, dgain, dbias, blocks, h);
+  return launch_pdl(layernorm_colsum_kernel<1>, dim3((cols + 31) / 32), dim3(1024), 0, st, scratch, dgain, dbias, blocks, h);
 }
 
 template <typename T, int VEC>
 cudaError_t bwd_width(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd, const void* gain,
                       const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias, float* scratch, int rows,
                       int h, cudaStream_t st) {
-  const BwdShape s = bwd_shape(rows, h);
-  // rows in flight at 8 columns a thread, by the registers a row takes (a packed 16-byte chunk: 4, single elements: 8)
-  constexpr int R8 = sizeof(T) == 2 && VEC >= 4 ? 4 : 2;
-#define LN_BWD_W(EPL, R, HOLD) bwd_launch<T, VEC, EPL, R, HOLD>(dy, lddy, x, ldx, mean, rstd, gain, resid, ldr, dx, lddx, dgain, dbias, scratch, rows, h, s, st)
-  return s.epl == 8 ? LN_BWD_W(8, R8, true) : s.epl == 16 ? LN_BWD_W(16, R8 / 2, true) : LN_BWD_W(32, 1, false);
+  // two rows in the ring: one under way hides the memory (a third changes nothing); none where 512 threads' slots would
+  // not fit an SM's shared memory (fp32 rows of more than 8192 columns) or the accesses are too narrow to be copied
+  constexpr bool RING = VEC * sizeof(T) >= 4;
+#define LN_BWD_W(EPL, NS) bwd_launch<T, VEC, EPL, RING ? NS : 0>(dy, lddy, x, ldx, mean, rstd, gain, resid, ldr, dx, lddx, dgain, dbias, scratch, rows, h, st)
+  const int epl = elements_per_thread(h, VEC * sizeof(T) < 16);
+  return epl == 8 ? LN_BWD_W(8, 2) : epl == 16 ? LN_BWD_W(16, 2) : LN_BWD_W(32, (sizeof(T) == 2 ? 2 : 0));
 #undef LN_BWD_W
 }
 
@@ -365,7 +445,7 @@ cudaError_t layernorm_fwd(const void* x, int64_t ldx, const void* gain, const vo
 
 size_t layernorm_scratch_bytes(int rows, int h) {
   if (rows <= 0 || h <= 0 || h > kLayerNormMaxWidth) return 0;
-  return (size_t)bwd_shape(rows, h).blocks * 2 * (size_t)h * sizeof(float);
+  return (size_t)(rows < kSms ? rows : kSms) * 2 * (size_t)h * sizeof(float);  // one partial row of both gradients a block
 }
 
 cudaError_t layernorm_bwd(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd,

@@ -64,20 +64,47 @@ struct RowVec<float, VEC> {
   }
 };
 
-// Hides from the compiler what a packed register holds, so that values unpacked before a barrier are unpacked again after
-// it instead of staying in registers in their wider form.
-template <typename Raw>
-__device__ __forceinline__ void forget(Raw& r) {
-  if constexpr (sizeof(Raw) == 2) {
-    asm volatile("" : "+h"(r));
-  } else {
-    uint32_t w[sizeof(Raw) / 4];
-    memcpy(w, &r, sizeof(r));
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(Raw) / 4); ++i) asm volatile("" : "+r"(w[i]));
-    memcpy(&r, w, sizeof(r));
-  }
+// Asynchronous copies from global memory into slots of shared memory that only the issuing thread reads: a thread keeps the
+// next rows' elements on their way without holding registers for them, and needs no barrier.  4, 8 or 16 bytes each;
+// valid = false fills the slot with zeros and reads nothing.
+template <int BYTES>
+__device__ __forceinline__ void async_copy(uint32_t dst, const void* src, bool valid) {
+  const int n = valid ? BYTES : 0;
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
 }
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Pairs of fp32 numbers in one instruction each (two independent IEEE operations): the row-wise kernels are bound by
+// instruction issue before they are bound by memory.
+__device__ __forceinline__ unsigned long long pair_bits(float2 v) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+  return r;
+}
+__device__ __forceinline__ float2 bits_pair(unsigned long long r) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+  return v;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+  return bits_pair(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+  return bits_pair(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+  return bits_pair(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // Widest vector width for rows of h elements of `elem` bytes: h and the strides are given or-ed together, as are the
 // pointers' addresses (null pointers change nothing).
