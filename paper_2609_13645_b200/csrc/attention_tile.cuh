@@ -45,4 +45,50 @@ __device__ __forceinline__ void store_bf16_row(bf16* dst, const float (&v)[W]) {
   }
 }
 
+// Backward of the rotation: its transpose, on pairs (i, i + d/2) of one row; cs, sn: the row's tables from column i on.
+template <int W>
+__device__ __forceinline__ void unrotate(float (&lo)[W], float (&hi)[W], const float* cs, const float* sn) {
+#pragma unroll
+  for (int i = 0; i < W; i += 4) {
+    const float4 c4 = *reinterpret_cast<const float4*>(cs + i);
+    const float4 s4 = *reinterpret_cast<const float4*>(sn + i);
+    const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float y1 = lo[i + u], y2 = hi[i + u];
+      lo[i + u] = y1 * cc[u] + y2 * ss[u];
+      hi[i + u] = y2 * cc[u] - y1 * ss[u];
+    }
+  }
+}
+
+// MMA issue from code that the whole warp runs: the operands stay warp-uniform and one elected lane issues.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t e;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+  return e;
+}
+__device__ __forceinline__ void umma_bf16_if(uint32_t elected, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                             uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(elected)
+      : "memory");
+}
+__device__ __forceinline__ void umma_bf16_ts_if(uint32_t elected, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(elected)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_if(uint32_t elected, uint32_t bar) {
+  asm volatile(
+      "{\n .reg .pred e;\n setp.ne.b32 e, %1, 0;\n"
+      " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(elected)
+      : "memory");
+}
+
 }  // namespace fs

@@ -319,120 +319,121 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
 }
 
 // ============================================================================ backward
-// MODE_DQ : resident X = (Q, dO) of 128 queries, streamed Y = (K, V) blocks of 64 keys  -> dQ  = dS K
-// MODE_DKV: resident X = (K, V) of 128 keys, streamed Y = (Q, dO) blocks of 64 queries of every query head of the group
-//                                                                                       -> dV = P^T dO, dK = dS^T Q
-// Per streamed block S = X1 Y1^T and dP = X2 Y2^T go to one of two TMEM buffers; the compute warps (one X row per thread)
-// turn them into P = exp2(S c - LSE) and dS = P (dP - delta), packed to bf16 over the columns they came from, and the
-// accumulating products read those as their A operand and the streamed tiles again as mn-major B operands.  warp 0 = TMA
-// producer, warps 1 and 10 = MMA issuers (one thread cannot issue products this small fast enough), warps 2..9 compute.
-enum { MODE_DQ = 0, MODE_DKV = 1 };
-enum { BB_XFULL = 0, BB_YFULL = 1, BB_YEMPTY = 5, BB_SDPFULL = 9, BB_TFULL = 11, BB_ACCDONE = 13, BB_COUNT = 14 };
-constexpr int BWD_THREADS = 352;
+// dK, dV: one CTA per (128 keys, kv head, batch row) or part of its queries; K and V stay in shared memory, 128-query blocks
+// of Q and dO of every query head of the group are streamed.  Per block (all products 128 x 128 x D on the tensor cores)
+//   S^T = K Q^T, dP^T = V dO^T        accumulators in TMEM
+//   P^T = exp2(S^T c - LSE), dS^T = P^T (dP^T - delta)    compute warps, bf16 back over the columns they came from
+//   dV += P^T dO, dK += dS^T Q        A operand from TMEM, the streamed tiles again as mn-major B operands
+// TMEM is full (four 128-column accumulators at D = 128), so S and dP have one buffer each; what keeps the tensor pipe busy is
+// that the two chains alternate: side 0 (dV_j, S_{j+1}) runs while the compute warps turn dP_j into dS_j, side 1 (dK_j,
+// dP_{j+1}) while they turn S_{j+1} into P_{j+1}.  Blocks of 128 queries and not 64: an MMA of N = 64 takes as long as one
+// of N = 128, because it is bound by the reads of its operands from shared memory.
+// dS^T also goes to a scratch array, from which dQ = dS K is one banded contraction (below): five products per pair of
+// blocks in all instead of the seven of a backward pass that computes S and dP twice.
+enum { K_XFULL = 0, K_QFULL = 1, K_QEMPTY = 4, K_OFULL = 7, K_OEMPTY = 10, K_STFULL = 13, K_STEMPTY = 15, K_SFULL = 17, K_DPFULL = 18,
+       K_PFULL = 19, K_DSFULL = 20, K_ACCDONE = 21, K_COUNT = 22 };
+constexpr int BWD_THREADS = 352;  // producer, MMA issuer (side 0), 8 compute warps, MMA issuer (side 1)
 
 template <int D>
-struct BwdCfg {
+struct DkvCfg {
   static constexpr int KC = D / 64;
-  static constexpr int X_BYTES = 128 * D * 2;
-  static constexpr int Y_BYTES = 64 * D * 2;
-  static constexpr int NST = 4;
-  static constexpr int OFF_X1 = 0, OFF_X2 = X_BYTES, OFF_Y = 2 * X_BYTES;
-  static constexpr int OFF_STAT = OFF_Y + NST * 2 * Y_BYTES;
+  static constexpr int TILE = 128 * D * 2;  // bytes of a 128-row tile
+  static constexpr int NQ = 3, NO = D == 64 ? 3 : 2;  // Q is needed by the first and the last product of a block
+  static constexpr int OFF_K = 0, OFF_V = TILE, OFF_Q = 2 * TILE, OFF_O = OFF_Q + NQ * TILE;
+  static constexpr int OFF_STAT = OFF_O + NO * TILE;  // [2][lse * log2e, delta][128]
   static constexpr int OFF_BAR = OFF_STAT + 2048;
   static constexpr int SMEM_BYTES = OFF_BAR + 256;
-  static constexpr int TMEM_COLS = 512;  // buffer b: S at b*128, dP at b*128+64; accumulators from column 256
-  static constexpr int ACC0 = 256, ACC1 = 256 + D;
+  static constexpr int TMEM_COLS = 512;
+  static constexpr int COL_S = 0, COL_DP = 128, COL_DV = 256, COL_DK = 256 + D;
 };
+static_assert(DkvCfg<128>::SMEM_BYTES <= 232448, "shared memory of one SM");
 
-// How the key blocks' streamed lists are cut (host and device agree on it through this).
-struct Split {
+// The backward pass as the host plans it and the kernels read it.  A key block's streamed list (128-query blocks of every
+// query head of the group) is cut into parts; dS^T is kept for a number of (batch row, kv head) groups at a time.
+struct Plan {
+  int S, n_heads, n_kv, window, sinks;
+  int nxb;                // 128-row blocks of the sequence
+  int nb;                 // query blocks a key block meets through the window
+  int n_sink;             // key blocks that hold sink keys
   int chunk;              // streamed blocks a part has, at most
-  int n_sink;             // 128-key blocks that hold sink keys
   int parts_sink, parts;  // parts of a sink block and of any other, at most
-  // queries [x0, end) see a key of block x; streamed 64-query blocks, over all query heads of the group
-  static __host__ __device__ int queries_end(int x, int S, int window, int sinks) {
-    const int x0 = x * 128;
-    return x0 < sinks || S - x0 < 127 + window ? S : x0 + 127 + window;
+  int group0, groups;     // groups of this launch: [group0, group0 + groups)
+  int all_groups;
+  // blocks [x, queries_end(x)) of the queries see a key of block x
+  __host__ __device__ int blocks_seen(int x) const {
+    if (x < n_sink) return nxb - x;
+    return nxb - x < nb ? nxb - x : nb;
   }
-  static __host__ __device__ int per_head(int x, int S, int window, int sinks) {
-    return (queries_end(x, S, window, sinks) + 63) / 64 - x * 2;
+  __host__ __device__ int parts_of(int x) const {
+    return (int)(((long long)blocks_seen(x) * (n_heads / n_kv) + chunk - 1) / chunk);
   }
-  __host__ __device__ int parts_of(int x, int S, int window, int sinks, int n_rep) const {
-    return (int)(((long long)per_head(x, S, window, sinks) * n_rep + chunk - 1) / chunk);
+  // first slot of a key block's partial sums
+  __host__ __device__ int rank_of(int x) const {
+    return x < n_sink ? x * parts_sink : n_sink * parts_sink + (x - n_sink) * parts;
   }
+  __host__ __device__ int ranks() const { return n_sink * parts_sink + (nxb - n_sink) * parts; }
 };
 
-template <int D, int MODE>
+template <int D>
 __global__ void __launch_bounds__(BWD_THREADS, 1)
-attn_window_bwd_kernel(const __grid_constant__ CUtensorMap tm_qkv128, const __grid_constant__ CUtensorMap tm_qkv64,
-                       const __grid_constant__ CUtensorMap tm_do128, const __grid_constant__ CUtensorMap tm_do64,
+attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                        const float* __restrict__ lse, const float* __restrict__ delta, bf16* __restrict__ dqkv,
-                       float* __restrict__ partial, const float* __restrict__ rope_cos, const float* __restrict__ rope_sin, int S,
-                       int n_heads, int n_kv, int n_batch, int n_xblocks, int window, int sinks, const Split split, float scale,
-                       float scale_log2, int* err) {
-  using C = BwdCfg<D>;
+                       float* __restrict__ partial, bf16* __restrict__ ds_band, bf16* __restrict__ ds_sink,
+                       const float* __restrict__ rope_cos, const float* __restrict__ rope_sin, const __grid_constant__ Plan pl,
+                       float scale, float scale_log2, int* err) {
+  using C = DkvCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
   const uint32_t bar0 = sbase + C::OFF_BAR;
   auto bar = [&](int i) { return bar0 + 8u * i; };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BB_COUNT);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + K_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float* s_stat = reinterpret_cast<float*>(smem + C::OFF_STAT);  // [stage][0: lse*log2e, 1: delta][64]
+  float* s_stat = reinterpret_cast<float*>(smem + C::OFF_STAT);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if ((sbase & 1023u) != 0u) {
     if (threadIdx.x == 0) atomicExch(err, (int)ERR_BAD_ALIGNMENT);
     return;
   }
-  const int n_rep = n_heads / n_kv;
+  const int S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv, n_rep = n_heads / n_kv;
   const int hq = n_heads * D, hkv = n_kv * D;
   const long long ld = hq + 2 * hkv;
-  const int heads_here = MODE == MODE_DQ ? n_heads : n_kv;
-  const int groups = heads_here * n_batch;
-  const int rank = (int)blockIdx.x / groups, grp = (int)blockIdx.x % groups;
-  const int b = grp / heads_here;
-  int x0, kvh, n_q = 0, qb0 = 0, per_head = 1, first_it = 0, iters;
-  bool direct = true;  // this CTA holds the whole sum of its rows
-  KeyRuns runs(0, 1, 1, 0);
-  if constexpr (MODE == MODE_DQ) {
-    x0 = (n_xblocks - 1 - rank) * 128;  // the first query blocks, with fewer keys, end the launch
-    n_q = grp % heads_here;
-    kvh = n_q / n_rep;
-    runs = KeyRuns(x0, S, window, sinks);
-    iters = runs.count;
-  } else {
-    const int n_sink_ctas = split.n_sink * split.parts_sink;
-    const int x = rank < n_sink_ctas ? rank / split.parts_sink : split.n_sink + (rank - n_sink_ctas) / split.parts;
-    const int part = rank < n_sink_ctas ? rank % split.parts_sink : (rank - n_sink_ctas) % split.parts;
-    x0 = x * 128;
-    kvh = grp % heads_here;
-    qb0 = x * 2;
-    per_head = Split::per_head(x, S, window, sinks);
-    const int total = per_head * n_rep, np = split.parts_of(x, S, window, sinks, n_rep);
-    if (part >= np) return;
-    first_it = (int)((long long)total * part / np);
-    iters = (int)((long long)total * (part + 1) / np) - first_it;
-    direct = np == 1;
-  }
+  // sink blocks, with the longest lists, first
+  const int rank = (int)blockIdx.x / pl.groups, local = (int)blockIdx.x % pl.groups, grp = pl.group0 + local;
+  const int kvh = grp % n_kv, b = grp / n_kv;
+  const int n_sink_ranks = pl.n_sink * pl.parts_sink;
+  const int x = rank < n_sink_ranks ? rank / pl.parts_sink : pl.n_sink + (rank - n_sink_ranks) / pl.parts;
+  const int part = rank < n_sink_ranks ? rank % pl.parts_sink : (rank - n_sink_ranks) % pl.parts;
+  const int x0 = x * 128;
+  const int per_head = pl.blocks_seen(x), total = per_head * n_rep, np = pl.parts_of(x);
+  if (part >= np) return;
+  const int first_it = (int)((long long)total * part / np);
+  const int iters = (int)((long long)total * (part + 1) / np) - first_it;
 
   if (threadIdx.x == 0) {
-    mbar_init(bar(BB_XFULL), 1);
-    for (int i = 0; i < C::NST; ++i) {
-      mbar_init(bar(BB_YFULL + i), MODE == MODE_DKV ? 2 : 1);
-      mbar_init(bar(BB_YEMPTY + i), 2);   // one commit from each MMA-issuing warp
+    mbar_init(bar(K_XFULL), 1);
+    for (int i = 0; i < C::NQ; ++i) {
+      mbar_init(bar(K_QFULL + i), 1);
+      mbar_init(bar(K_QEMPTY + i), 2);  // S (side 0) and dK (side 1) read Q
+    }
+    for (int i = 0; i < C::NO; ++i) {
+      mbar_init(bar(K_OFULL + i), 1);
+      mbar_init(bar(K_OEMPTY + i), 2);  // dV (side 0) and dP (side 1) read dO
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(BB_SDPFULL + i), 2);
-      mbar_init(bar(BB_TFULL + i), 8);
+      mbar_init(bar(K_STFULL + i), 1);
+      mbar_init(bar(K_STEMPTY + i), 8);
     }
-    mbar_init(bar(BB_ACCDONE), 2);
+    mbar_init(bar(K_SFULL), 1);
+    mbar_init(bar(K_DPFULL), 1);
+    mbar_init(bar(K_PFULL), 8);
+    mbar_init(bar(K_DSFULL), 8);
+    mbar_init(bar(K_ACCDONE), 2);
     *abort_flag = 0;
     mbar_fence_init();
-    tma_prefetch_desc(&tm_qkv128);
-    tma_prefetch_desc(&tm_qkv64);
-    tma_prefetch_desc(&tm_do128);
-    tma_prefetch_desc(&tm_do64);
+    tma_prefetch_desc(&tm_qkv);
+    tma_prefetch_desc(&tm_do);
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
@@ -448,268 +449,244 @@ attn_window_bwd_kernel(const __grid_constant__ CUtensorMap tm_qkv128, const __gr
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
     if (lane == 0) {
-      mbar_expect_tx(bar(BB_XFULL), 2 * C::X_BYTES);
+      mbar_expect_tx(bar(K_XFULL), 2 * C::TILE);
 #pragma unroll
       for (int kc = 0; kc < C::KC; ++kc) {
-        if constexpr (MODE == MODE_DQ) {
-          tma_load_3d(sbase + C::OFF_X1 + kc * 16384, &tm_qkv128, bar(BB_XFULL), n_q * D + kc * 64, x0, b);
-          tma_load_3d(sbase + C::OFF_X2 + kc * 16384, &tm_do128, bar(BB_XFULL), n_q * D + kc * 64, x0, b);
-        } else {
-          tma_load_3d(sbase + C::OFF_X1 + kc * 16384, &tm_qkv128, bar(BB_XFULL), hq + kvh * D + kc * 64, x0, b);
-          tma_load_3d(sbase + C::OFF_X2 + kc * 16384, &tm_qkv128, bar(BB_XFULL), hq + hkv + kvh * D + kc * 64, x0, b);
-        }
+        tma_load_3d(sbase + C::OFF_K + kc * 16384, &tm_qkv, bar(K_XFULL), hq + kvh * D + kc * 64, x0, b);
+        tma_load_3d(sbase + C::OFF_V + kc * 16384, &tm_qkv, bar(K_XFULL), hq + hkv + kvh * D + kc * 64, x0, b);
       }
     }
     for (int it = 0; it < iters; ++it) {
-      const int st = it % C::NST;
-      bool ok = mbar_wait(bar(BB_YEMPTY + st), (((uint32_t)(it / C::NST)) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x71);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      const uint32_t ydst = sbase + C::OFF_Y + st * 2 * C::Y_BYTES;
-      if constexpr (MODE == MODE_DQ) {
-        if (lane == 0) {
-          const int y0 = runs.block(it) * 64;
-          mbar_expect_tx(bar(BB_YFULL + st), 2 * C::Y_BYTES);
+      const int n = kvh * n_rep + (first_it + it) / per_head, q0 = (x + (first_it + it) % per_head) * 128;
+      const int sq = it % C::NQ, so = it % C::NO, ss = it & 1;
+      bool ok = mbar_wait(bar(K_QEMPTY + sq), ((uint32_t)(it / C::NQ) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x71);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (lane == 0) {
+        mbar_expect_tx(bar(K_QFULL + sq), C::TILE);
 #pragma unroll
-          for (int kc = 0; kc < C::KC; ++kc) {
-            tma_load_3d(ydst + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), hq + kvh * D + kc * 64, y0, b);
-            tma_load_3d(ydst + C::Y_BYTES + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), hq + hkv + kvh * D + kc * 64, y0, b);
-          }
-        }
-      } else {
-        const int rep = (first_it + it) / per_head, qb = qb0 + (first_it + it) % per_head;
-        const int n = kvh * n_rep + rep;
-        if (lane == 0) {
-          mbar_expect_tx(bar(BB_YFULL + st), 2 * C::Y_BYTES);
-#pragma unroll
-          for (int kc = 0; kc < C::KC; ++kc) {
-            tma_load_3d(ydst + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), n * D + kc * 64, qb * 64, b);
-            tma_load_3d(ydst + C::Y_BYTES + kc * 8192, &tm_do64, bar(BB_YFULL + st), n * D + kc * 64, qb * 64, b);
-          }
-        }
-        const long long stat = ((long long)b * n_heads + n) * S;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int qq = qb * 64 + lane * 2 + e;
-          s_stat[st * 128 + lane * 2 + e] = qq < S ? lse[stat + qq] * kLog2e : 0.f;
-          s_stat[st * 128 + 64 + lane * 2 + e] = qq < S ? delta[stat + qq] : 0.f;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(BB_YFULL + st));
+        for (int kc = 0; kc < C::KC; ++kc)
+          tma_load_3d(sbase + C::OFF_Q + sq * C::TILE + kc * 16384, &tm_qkv, bar(K_QFULL + sq), n * D + kc * 64, q0, b);
       }
+      ok = mbar_wait(bar(K_OEMPTY + so), ((uint32_t)(it / C::NO) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x72);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (lane == 0) {
+        mbar_expect_tx(bar(K_OFULL + so), C::TILE);
+#pragma unroll
+        for (int kc = 0; kc < C::KC; ++kc)
+          tma_load_3d(sbase + C::OFF_O + so * C::TILE + kc * 16384, &tm_do, bar(K_OFULL + so), n * D + kc * 64, q0, b);
+      }
+      ok = mbar_wait(bar(K_STEMPTY + ss), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x73);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      const long long stat = ((long long)b * n_heads + n) * S;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int qq = q0 + lane + 32 * e;
+        s_stat[ss * 256 + lane + 32 * e] = qq < S ? lse[stat + qq] * kLog2e : 0.f;
+        s_stat[ss * 256 + 128 + lane + 32 * e] = qq < S ? delta[stat + qq] : 0.f;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(K_STFULL + ss));
     }
   } else if (warp == 1 || warp == 10) {
     // ------------------------------------------------------------------ MMA issuers
-    // side 0 owns S (and dV, which reads P^T from the S columns), side 1 owns dP (and dK / dQ, which read dS from the dP
-    // columns): each chain stays in issue order
-    if (lane == 0) {
-      const int side = warp == 1 ? 0 : 1;
-      const uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
-      const uint32_t idesc_sdp = idesc_base | ((uint32_t)(64 >> 3) << 17);            // N = 64, both K-major
-      const uint32_t idesc_acc = idesc_base | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // N = D, B mn-major
-      const uint64_t dx = umma_desc_sw128(sbase + (side == 0 ? C::OFF_X1 : C::OFF_X2), 0, 1024);
-      auto issue_sdp = [&](int it) {
-        const int st = it % C::NST;
-        const uint32_t y = sbase + C::OFF_Y + st * 2 * C::Y_BYTES + side * C::Y_BYTES;
-        const uint64_t dy = umma_desc_sw128(y, 0, 1024);
-        const uint32_t d_t = tmem_base + (uint32_t)((it & 1) * 128 + side * 64);
+    // side 0: S, then dV over the P it became; side 1: dP, then dK over dS.  A score buffer is overwritten by the product
+    // that this same thread issued behind its last reader: in order.
+    const uint32_t elected = elect_one();
+    const bool side0 = warp == 1;
+    const uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
+    const uint32_t idesc_s = idesc_base | ((uint32_t)(128 >> 3) << 17);               // N = 128, both K-major
+    const uint32_t idesc_acc = idesc_base | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // N = D, B mn-major
+    const uint64_t dx = umma_desc_sw128(sbase + (side0 ? C::OFF_K : C::OFF_V), 0, 1024);
+    const uint32_t t_score = tmem_base + (uint32_t)(side0 ? C::COL_S : C::COL_DP);
+    const uint32_t t_acc = tmem_base + (uint32_t)(side0 ? C::COL_DV : C::COL_DK);
+    // the score product of block it: reads Q (side 0) or dO (side 1); false when a wait ran out
+    auto scores = [&](int it) -> bool {
+      const int st = side0 ? it % C::NQ : it % C::NO;
+      const uint32_t ph = (uint32_t)(side0 ? it / C::NQ : it / C::NO) & 1u;
+      bool ok = mbar_wait(bar((side0 ? K_QFULL : K_OFULL) + st), ph, abort_flag, err, kWaitLimitCycles, 0x74);
+      if (!__all_sync(0xffffffffu, ok)) return false;
+      tc_fence_after();
+      const uint64_t dy = umma_desc_sw128(sbase + (side0 ? C::OFF_Q : C::OFF_O) + st * C::TILE, 0, 1024);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint64_t xo = (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
-          const uint64_t yo = (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4);
-          umma_bf16(d_t, dx + xo, dy + yo, idesc_sdp, k > 0 ? 1u : 0u);
-        }
-        umma_commit(bar(BB_SDPFULL + (it & 1)));
-      };
-      bool ok = mbar_wait(bar(BB_XFULL), 0, abort_flag, err, kWaitLimitCycles, 0x72) &&
-                mbar_wait(bar(BB_YFULL), 0, abort_flag, err, kWaitLimitCycles, 0x73);
-      if (ok) {
-        tc_fence_after();
-        issue_sdp(0);
+      for (int k = 0; k < D / 16; ++k) {
+        const uint64_t o = (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
+        umma_bf16_if(elected, t_score, dx + o, dy + o, idesc_s, k > 0 ? 1u : 0u);
       }
-      for (int it = 0; it < iters && ok; ++it) {
-        if (it + 1 < iters) {
-          const int y1s = (it + 1) % C::NST;
-          if (!mbar_wait(bar(BB_YFULL + y1s), ((uint32_t)((it + 1) / C::NST)) & 1u, abort_flag, err, kWaitLimitCycles, 0x74)) { ok = false; break; }
-          // the TMEM columns this writes were last read by this same thread's accumulating MMAs of block it-1: in order
-          tc_fence_after();
-          issue_sdp(it + 1);
-        }
-        const int bf = it & 1;
-        if (!mbar_wait(bar(BB_TFULL + bf), ((uint32_t)it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x75)) { ok = false; break; }
-        tc_fence_after();
-        const int yst = it % C::NST;
-        const uint32_t y1 = sbase + C::OFF_Y + yst * 2 * C::Y_BYTES, y2 = y1 + C::Y_BYTES;
-        // A operands (bf16) sit in TMEM where S / dP were: 16 streamed rows (K = 16) = 8 columns; the two compute warps of
-        // a lane quarter each wrote their 32 at the start of their own 32 fp32 columns
-        const uint32_t ta = tmem_base + (uint32_t)(bf * 128 + side * 64);
-        const uint32_t first = it > 0 ? 1u : 0u;
-        if (MODE == MODE_DKV || side == 1) {
-          const uint64_t by = umma_desc_sw128((MODE == MODE_DKV && side == 0) ? y2 : y1, 8192, 1024);
-          const uint32_t dacc = tmem_base + (uint32_t)((MODE == MODE_DKV && side == 1) ? C::ACC1 : C::ACC0);
+      umma_commit_if(elected, bar(side0 ? K_SFULL : K_DPFULL));
+      // this reader is done with its tile once the product is: the other reader of it is the other side
+      umma_commit_if(elected, bar((side0 ? K_QEMPTY : K_OEMPTY) + st));
+      return true;
+    };
+    bool ok = mbar_wait(bar(K_XFULL), 0, abort_flag, err, kWaitLimitCycles, 0x75);
+    ok = __all_sync(0xffffffffu, ok) && scores(0);
+    for (int it = 0; it < iters && ok; ++it) {
+      ok = mbar_wait(bar(side0 ? K_PFULL : K_DSFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x76);
+      // the B operand (dO for dV, Q for dK) was waited for by the other side only
+      const int st = side0 ? it % C::NO : it % C::NQ;
+      const uint32_t ph = (uint32_t)(side0 ? it / C::NO : it / C::NQ) & 1u;
+      ok = ok && mbar_wait(bar((side0 ? K_OFULL : K_QFULL) + st), ph, abort_flag, err, kWaitLimitCycles, 0x77);
+      if (!(ok = __all_sync(0xffffffffu, ok))) break;
+      tc_fence_after();
+      const uint64_t by = umma_desc_sw128(sbase + (side0 ? C::OFF_O : C::OFF_Q) + st * C::TILE, 16384, 1024);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t acol = (uint32_t)((k >> 1) * 32 + (k & 1) * 8);
-            umma_bf16_ts(dacc, ta + acol, by + (uint64_t)((k * 2048) >> 4), idesc_acc, k > 0 ? 1u : first);
-          }
-        }
-        umma_commit(bar(BB_YEMPTY + yst));
+      for (int k = 0; k < 8; ++k) {
+        // bf16 A operand: 16 queries = 8 columns; each half of the queries sits at the start of its 64 fp32 columns
+        const uint32_t acol = (uint32_t)((k >> 2) * 64 + (k & 3) * 8);
+        umma_bf16_ts_if(elected, t_acc, t_score + acol, by + (uint64_t)((k * 2048) >> 4), idesc_acc, (it > 0 || k > 0) ? 1u : 0u);
       }
-      if (ok) umma_commit(bar(BB_ACCDONE));
+      umma_commit_if(elected, bar((side0 ? K_OEMPTY : K_QEMPTY) + st));
+      if (it + 1 < iters) ok = scores(it + 1);
     }
+    if (ok) umma_commit_if(elected, bar(K_ACCDONE));
   } else {
-    // ------------------------------------------------------------------ compute warps
+    // ------------------------------------------------------------------ compute warps: one key per thread, 64 queries each
     const int q = warp & 3, ch = (warp - 2) >> 2;
-    const int rloc = q * 32 + lane;
-    const int row = x0 + rloc;  // query (MODE_DQ) or key (MODE_DKV) position
-    const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
+    const int rloc = q * 32 + lane, row = x0 + rloc;
     const int rmin = x0 + q * 32, rmax = rmin + 31;
-    float lse2_row = 0.f, delta_row = 0.f;
-    if constexpr (MODE == MODE_DQ) {
-      if (row < S) {
-        const long long stat = ((long long)b * n_heads + n_q) * S;
-        lse2_row = lse[stat + row] * kLog2e;
-        delta_row = delta[stat + row];
-      }
-    }
-    // MODE_DKV: the queries that see key `row` are [row, row_end)
-    const int row_end = row < sinks || S - row < window ? S : row + window;
+    const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
+    const uint32_t t_s = tlane + (uint32_t)(C::COL_S + ch * 64), t_dp = tlane + (uint32_t)(C::COL_DP + ch * 64);
+    // the queries that see key `row` are [row, row_end)
+    const int row_end = row < pl.sinks || S - row < pl.window ? S : row + pl.window;
     bool ok = true;
     for (int it = 0; it < iters; ++it) {
-      const int bf = it & 1;
-      ok = mbar_wait(bar(BB_SDPFULL + bf), ((uint32_t)it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x76);
+      const int ss = it & 1;
+      const int rel = (first_it + it) % per_head;
+      const int cmin = (x + rel) * 128 + ch * 64;
+      const float* st_lse = s_stat + ss * 256 + ch * 64;
+      const float* st_dl = st_lse + 128;
+      ok = mbar_wait(bar(K_STFULL + ss), (uint32_t)(it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x78) &&
+           mbar_wait(bar(K_SFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x79);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      uint32_t rs[32], rp[32];
-      tmem_ld32(tlane + (uint32_t)(bf * 128 + ch * 32), rs);
-      tmem_ld32(tlane + (uint32_t)(bf * 128 + 64 + ch * 32), rp);
-      tmem_ld_wait();
-
-      // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
-      if constexpr (MODE == MODE_DQ) {
-        const int cmin = runs.block(it) * 64 + ch * 32;
-        const bool full = cmin + 31 <= rmin && (rmax - cmin < window || cmin + 32 <= sinks);
-        const float nl = -lse2_row;
-        const int hi = row - cmin, lo = row - window + 1 - cmin, sk = sinks - cmin;
+      float p[64];
+      {
+        uint32_t r0[32], r1[32];
+        tmem_ld32(t_s, r0);
+        tmem_ld32(t_s + 32, r1);
+        tmem_ld_wait();
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-          float p = fast_exp2(fmaf(__uint_as_float(rs[i]), scale_log2, nl));
-          if (!full && (i > hi || (i < lo && i >= sk))) p = 0.f;
-          rs[i] = __float_as_uint(p);
-          rp[i] = __float_as_uint(p * (__uint_as_float(rp[i]) - delta_row));
-        }
-      } else {
-        const int yst = it % C::NST;
-        const float* st_lse = s_stat + yst * 128 + ch * 32;
-        const float* st_dl = st_lse + 64;
-        const int cmin = (qb0 + (first_it + it) % per_head) * 64 + ch * 32;
-        ok = mbar_wait(bar(BB_YFULL + yst), ((uint32_t)(it / C::NST)) & 1u, abort_flag, err, kWaitLimitCycles, 0x77);  // acquire the staged statistics
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const bool full = cmin >= rmax && cmin + 32 <= S && (rmax < sinks || cmin + 31 - rmin < window);
-        if (full) {
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 l4 = *reinterpret_cast<const float4*>(st_lse + i);
-            const float4 d4 = *reinterpret_cast<const float4*>(st_dl + i);
-            const float ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float p = fast_exp2(fmaf(__uint_as_float(rs[i + u]), scale_log2, -ll[u]));
-              rs[i + u] = __float_as_uint(p);
-              rp[i + u] = __float_as_uint(p * (__uint_as_float(rp[i + u]) - dd[u]));
-            }
-          }
-        } else {
-          const int lo = row - cmin, hi = row_end - cmin;
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 l4 = *reinterpret_cast<const float4*>(st_lse + i);
-            const float4 d4 = *reinterpret_cast<const float4*>(st_dl + i);
-            const float ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              float p = fast_exp2(fmaf(__uint_as_float(rs[i + u]), scale_log2, -ll[u]));
-              if (i + u < lo || i + u >= hi) p = 0.f;
-              rs[i + u] = __float_as_uint(p);
-              rp[i + u] = __float_as_uint(p * (__uint_as_float(rp[i + u]) - dd[u]));
-            }
-          }
+          p[i] = __uint_as_float(r0[i]);
+          p[32 + i] = __uint_as_float(r1[i]);
         }
       }
-      // bf16 pairs back into TMEM, over this warp's own (already loaded) fp32 columns
-      uint32_t wp[16], wd[16];
 #pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        wp[c] = pack_bf16(__uint_as_float(rs[2 * c]), __uint_as_float(rs[2 * c + 1]));
-        wd[c] = pack_bf16(__uint_as_float(rp[2 * c]), __uint_as_float(rp[2 * c + 1]));
+      for (int i = 0; i < 64; i += 4) {
+        const float4 l4 = *reinterpret_cast<const float4*>(st_lse + i);
+        p[i] = fast_exp2(fmaf(p[i], scale_log2, -l4.x));
+        p[i + 1] = fast_exp2(fmaf(p[i + 1], scale_log2, -l4.y));
+        p[i + 2] = fast_exp2(fmaf(p[i + 2], scale_log2, -l4.z));
+        p[i + 3] = fast_exp2(fmaf(p[i + 3], scale_log2, -l4.w));
       }
-      if constexpr (MODE == MODE_DKV) tmem_st16(tlane + (uint32_t)(bf * 128 + ch * 32), wp);
-      tmem_st16(tlane + (uint32_t)(bf * 128 + 64 + ch * 32), wd);
+      // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
+      const bool full = cmin >= rmax && cmin + 64 <= S && (rmax < pl.sinks || cmin + 63 - rmin < pl.window);
+      if (!full) {
+        const int lo = row - cmin, hi = row_end - cmin;
+#pragma unroll
+        for (int i = 0; i < 64; ++i)
+          if (i < lo || i >= hi) p[i] = 0.f;
+      }
+      uint32_t w[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) w[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
+      tmem_st32(t_s, w);  // over this warp's own (already loaded) columns
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(BB_TFULL + bf));
+      if (lane == 0) mbar_arrive(bar(K_PFULL));
+
+      ok = mbar_wait(bar(K_DPFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x7a);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      {
+        uint32_t r0[32], r1[32];
+        tmem_ld32(t_dp, r0);
+        tmem_ld32(t_dp + 32, r1);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const float4 d0 = *reinterpret_cast<const float4*>(st_dl + i), d1 = *reinterpret_cast<const float4*>(st_dl + 32 + i);
+          const float e0[4] = {d0.x, d0.y, d0.z, d0.w}, e1[4] = {d1.x, d1.y, d1.z, d1.w};
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            p[i + u] *= __uint_as_float(r0[i + u]) - e0[u];
+            p[32 + i + u] *= __uint_as_float(r1[i + u]) - e1[u];
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 32; ++c) w[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
+      tmem_st32(t_dp, w);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar(K_DSFULL));
+        mbar_arrive(bar(K_STEMPTY + ss));
+      }
+      // off the chain's critical path: the same rounded dS^T to the scratch of the dQ contraction, as 32-query chunks
+      // [chunk][key][32]: a thread stores one contiguous 64-byte row per chunk, its warp 2 KiB
+      if (ds_band != nullptr) {
+        const long long z = (long long)local * n_rep + (first_it + it) / per_head;
+        if (rel < pl.nb) {
+          bf16* dst = ds_band + ((((z * pl.nxb + x) * pl.nb + rel) * 4 + ch * 2) * 128 + rloc) * 32;
+          store8_b32(dst, w);
+          store8_b32(dst + 16, w + 8);
+          store8_b32(dst + 4096, w + 16);
+          store8_b32(dst + 4096 + 16, w + 24);
+        } else if (row < pl.sinks) {  // beyond the window only sink keys are seen
+          bf16* dst = ds_sink + ((((z * pl.nxb + x + rel) * 4 + ch * 2) * pl.sinks + row) * 32);
+          store8_b32(dst, w);
+          store8_b32(dst + 16, w + 8);
+          dst += (long long)pl.sinks * 32;
+          store8_b32(dst, w + 16);
+          store8_b32(dst + 16, w + 24);
+        }
+      }
     }
     if (ok) {
-      ok = mbar_wait(bar(BB_ACCDONE), 0, abort_flag, err, kWaitLimitCycles, 0x78);
+      ok = mbar_wait(bar(K_ACCDONE), 0, abort_flag, err, kWaitLimitCycles, 0x7b);
       ok = __all_sync(0xffffffffu, ok);
     }
     if (ok) {
       tc_fence_after();
       constexpr int W = D / 4, H = D / 2;
       const int i0 = ch * W;
-      const uint32_t racc = tlane + (uint32_t)(MODE == MODE_DQ ? C::ACC0 : C::ACC1);
-      if (direct) {
-        // rotated output (dQ or dK): this warp owns columns [i0, i0+W) and their partners D/2 further
+      const uint32_t t_dk = tlane + (uint32_t)C::COL_DK, t_dv = tlane + (uint32_t)C::COL_DV;
+      if (np == 1) {
+        // this CTA holds the whole sum: scale, rotate back (columns [i0, i0 + W) and their partners D / 2 further), round
         float lo[W], hi[W];
-        tmem_load_cols<W>(racc + (uint32_t)i0, lo);
-        tmem_load_cols<W>(racc + (uint32_t)(H + i0), hi);
+        tmem_load_cols<W>(t_dk + (uint32_t)i0, lo);
+        tmem_load_cols<W>(t_dk + (uint32_t)(H + i0), hi);
 #pragma unroll
         for (int i = 0; i < W; ++i) { lo[i] *= scale; hi[i] *= scale; }
         if (rope_cos != nullptr) {
           const int pos = min(row, S - 1);
-          const float* cs = rope_cos + (long long)pos * H + i0;
-          const float* sn = rope_sin + (long long)pos * H + i0;
-#pragma unroll
-          for (int i = 0; i < W; i += 4) {
-            const float4 c4 = *reinterpret_cast<const float4*>(cs + i);
-            const float4 s4 = *reinterpret_cast<const float4*>(sn + i);
-            const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float y1 = lo[i + u], y2 = hi[i + u];
-              lo[i + u] = y1 * cc[u] + y2 * ss[u];
-              hi[i + u] = y2 * cc[u] - y1 * ss[u];
-            }
-          }
+          unrotate<W>(lo, hi, rope_cos + (long long)pos * H + i0, rope_sin + (long long)pos * H + i0);
         }
-        const int colbase = MODE == MODE_DQ ? n_q * D : hq + kvh * D;
+        bf16* dst = dqkv + ((long long)b * S + row) * ld + hq + kvh * D;
         if (row < S) {
-          bf16* dst = dqkv + ((long long)b * S + row) * ld + colbase;
           store_bf16_row<W>(dst + i0, lo);
           store_bf16_row<W>(dst + H + i0, hi);
         }
-        if constexpr (MODE == MODE_DKV) {
-          bf16* dstv = dqkv + ((long long)b * S + row) * ld + hq + hkv + kvh * D;
-#pragma unroll 1
-          for (int c = ch * H; c < (ch + 1) * H; c += 32) {
-            float v[32];
-            tmem_load_cols<32>(tlane + (uint32_t)(C::ACC0 + c), v);
-            if (row < S) store_bf16_row<32>(dstv + c, v);
-          }
-        }
-      } else if constexpr (MODE == MODE_DKV) {
-        // partial sums [part][dK columns, dV columns][128 keys]: a warp writes 32 consecutive keys of a column
-        float* dst = partial + (long long)blockIdx.x * (2 * D * 128) + rloc;
 #pragma unroll 1
         for (int c = ch * H; c < (ch + 1) * H; c += 32) {
           float v[32];
-          tmem_load_cols<32>(racc + (uint32_t)c, v);
+          tmem_load_cols<32>(t_dv + (uint32_t)c, v);
+          if (row < S) store_bf16_row<32>(dst + hkv + c, v);
+        }
+      } else {
+        // partial sums [part][dK columns, dV columns][128 keys]: a warp writes 32 consecutive keys of a column
+        float* dst = partial + ((long long)rank * pl.all_groups + grp) * (2 * D * 128) + rloc;
+#pragma unroll 1
+        for (int c = ch * H; c < (ch + 1) * H; c += 32) {
+          float v[32];
+          tmem_load_cols<32>(t_dk + (uint32_t)c, v);
 #pragma unroll
           for (int i = 0; i < 32; ++i) dst[(c + i) * 128] = v[i];
-          tmem_load_cols<32>(tlane + (uint32_t)(C::ACC0 + c), v);
+          tmem_load_cols<32>(t_dv + (uint32_t)c, v);
 #pragma unroll
           for (int i = 0; i < 32; ++i) dst[(D + c + i) * 128] = v[i];
         }
@@ -731,29 +708,462 @@ attn_window_bwd_kernel(const __grid_constant__ CUtensorMap tm_qkv128, const __gr
   }
 }
 
+// ---------------------------------------------------------------- dQ from the stored dS^T
+// dQ[i] = scale * sum over visible keys j of dS[i, j] K[j], rotated back: per 128-query tile one product over the keys of its
+// band and the sink keys behind it.  Persistent: warp 0 TMA producer, warp 1 MMA issuer, warps 2..5 epilogue, accumulators
+// double-buffered in TMEM, two CTAs an SM.  Both operands are mn-major (the contraction index is the row of dS^T and of K).
+// The kernel is bound by the bytes of dS^T.
+enum { DQ_THREADS = 192 };
+
+template <int D>
+struct DqCfg {
+  static constexpr int A_BYTES = 64 * 128 * 2;  // one box of dS^T: 4 chunks of [64 keys][32 queries], 64-byte swizzle
+  static constexpr int B_BYTES = 64 * D * 2;
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int STAGES = D == 64 ? 4 : 3;
+  static constexpr int OFF_BAR = STAGES * STAGE_BYTES;
+  static constexpr int SMEM_BYTES = OFF_BAR + 128;
+  static constexpr int TMEM_COLS = 2 * D;
+};
+
+template <int D>
+__global__ void __launch_bounds__(DQ_THREADS, 2)
+attn_window_dq_kernel(const __grid_constant__ CUtensorMap tm_band, const __grid_constant__ CUtensorMap tm_sink,
+                      const __grid_constant__ CUtensorMap tm_qkv, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
+                      const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale, int* err) {
+  using C = DqCfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
+  const uint32_t bar0 = sbase + C::OFF_BAR;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * C::STAGES + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * C::STAGES + 2 + a); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((sbase & 1023u) != 0u) {
+    if (threadIdx.x == 0) atomicExch(err, (int)ERR_BAD_ALIGNMENT);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(tfull_bar(a), 1);
+      mbar_init(tempty_bar(a), 4);
+    }
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tm_band);
+    tma_prefetch_desc(&tm_sink);
+    tma_prefetch_desc(&tm_qkv);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_trigger();
+  pdl_wait();
+
+  const int S = pl.S, n_rep = pl.n_heads / pl.n_kv;
+  const int hq = pl.n_heads * D;
+  const long long ld = (long long)(pl.n_heads + 2 * pl.n_kv) * D;
+  const int nz = pl.groups * n_rep, ntiles = pl.nxb * nz;
+  // tile t: query block qt of head z of this launch; 64-key steps: sink keys behind the band, then the band
+  struct Tile {
+    int qt, z, kvh, n, b, x_first, n_sink64, steps;
+  };
+  auto tile_of = [&](int t) {
+    Tile r;
+    r.qt = pl.nxb - 1 - t / nz;
+    r.z = t % nz;
+    const int grp = pl.group0 + r.z / n_rep;
+    r.kvh = grp % pl.n_kv;
+    r.b = grp / pl.n_kv;
+    r.n = r.kvh * n_rep + r.z % n_rep;
+    r.x_first = max(0, r.qt - pl.nb + 1);
+    r.n_sink64 = (min(pl.sinks, r.x_first * 128) + 63) / 64;
+    r.steps = r.n_sink64 + (r.qt - r.x_first + 1) * 2;
+    return r;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+        const Tile r = tile_of(t);
+        for (int i = 0; i < r.steps; ++i) {
+          if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, err, kWaitLimitCycles, 0x81)) { ok = false; break; }
+          const uint32_t fb = full_bar(stage);
+          mbar_expect_tx(fb, C::STAGE_BYTES);
+          const uint32_t a_dst = sbase + stage * C::STAGE_BYTES, b_dst = a_dst + C::A_BYTES;
+          int key0;
+          if (i < r.n_sink64) {
+            key0 = i * 64;
+            tma_load_4d(a_dst, &tm_sink, fb, 0, key0, r.qt * 4, r.z);  // keys past the last sink read as 0
+          } else {
+            const int j = i - r.n_sink64, x = r.x_first + (j >> 1);
+            key0 = x * 128 + (j & 1) * 64;
+            tma_load_4d(a_dst, &tm_band, fb, 0, (j & 1) * 64, (r.qt - x) * 4, r.z * pl.nxb + x);
+          }
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(b_dst + c * 8192, &tm_qkv, fb, hq + r.kvh * D + 64 * c, key0, r.b);
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(D >> 3) << 17) |
+                             ((uint32_t)(128 >> 4) << 24);  // both operands mn-major, N = D, M = 128
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+        const Tile r = tile_of(t);
+        if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, err, kWaitLimitCycles, 0x82)) break;
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * D);
+        for (int i = 0; i < r.steps; ++i) {
+          if (!mbar_wait(full_bar(stage), phase, abort_flag, err, kWaitLimitCycles, 0x83)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t a_addr = sbase + stage * C::STAGE_BYTES, b_addr = a_addr + C::A_BYTES;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_bf16(d_tmem, umma_desc_sw64(a_addr + k * 1024, 4096, 512), umma_desc_sw128(b_addr + k * 2048, 8192, 1024), idesc,
+                      (i | k) != 0 ? 1u : 0u);
+          umma_commit(empty_bar(stage));
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        umma_commit(tfull_bar(acc));
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+    }
+  } else {
+    const int q = warp & 3;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    constexpr int H = D / 2;
+    for (int t = blockIdx.x; t < ntiles; t += gridDim.x) {
+      const Tile r = tile_of(t);
+      bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, err, kWaitLimitCycles, 0x84);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after();
+      const int row = r.qt * 128 + q * 32 + lane, pos = min(row, S - 1);
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * D);
+      bf16* dst = dqkv + ((long long)r.b * S + row) * ld + r.n * D;
+#pragma unroll 1
+      for (int i0 = 0; i0 < H; i0 += 32) {
+        float lo[32], hi[32];
+        tmem_load_cols<32>(taddr + (uint32_t)i0, lo);
+        tmem_load_cols<32>(taddr + (uint32_t)(H + i0), hi);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) { lo[i] *= scale; hi[i] *= scale; }
+        if (rope_cos != nullptr) unrotate<32>(lo, hi, rope_cos + (long long)pos * H + i0, rope_sin + (long long)pos * H + i0);
+        if (row < S) {
+          store_bf16_row<32>(dst + i0, lo);
+          store_bf16_row<32>(dst + H + i0, hi);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(tempty_bar(acc));
+      acc ^= 1;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag != 0) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, C::TMEM_COLS);
+  }
+}
+
+// ---------------------------------------------------------------- dQ without stored dS^T
+// For sequences and windows whose dS^T would not fit the scratch even for one group: 128 queries (Q, dO) resident, 64-key
+// blocks (K, V) streamed, S and dP computed again into one of two TMEM buffers, dQ += dS K.
+enum { BB_XFULL = 0, BB_YFULL = 1, BB_YEMPTY = 5, BB_SDPFULL = 9, BB_TFULL = 11, BB_ACCDONE = 13, BB_COUNT = 14 };
+
+template <int D>
+struct DqrCfg {
+  static constexpr int KC = D / 64;
+  static constexpr int X_BYTES = 128 * D * 2;
+  static constexpr int Y_BYTES = 64 * D * 2;
+  static constexpr int NST = 4;
+  static constexpr int OFF_X1 = 0, OFF_X2 = X_BYTES, OFF_Y = 2 * X_BYTES;
+  static constexpr int OFF_BAR = OFF_Y + NST * 2 * Y_BYTES;
+  static constexpr int SMEM_BYTES = OFF_BAR + 256;
+  static constexpr int TMEM_COLS = 512;  // buffer b: S at b*128, dP at b*128+64; accumulator from column 256
+  static constexpr int ACC0 = 256;
+};
+
+template <int D>
+__global__ void __launch_bounds__(BWD_THREADS, 1)
+attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, const __grid_constant__ CUtensorMap tm_qkv64,
+                                const __grid_constant__ CUtensorMap tm_do128, const float* __restrict__ lse,
+                                const float* __restrict__ delta, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
+                                const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale,
+                                float scale_log2, int* err) {
+  using C = DqrCfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
+  const uint32_t bar0 = sbase + C::OFF_BAR;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + BB_COUNT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((sbase & 1023u) != 0u) {
+    if (threadIdx.x == 0) atomicExch(err, (int)ERR_BAD_ALIGNMENT);
+    return;
+  }
+  const int S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv;
+  const int hq = n_heads * D, hkv = n_kv * D;
+  const long long ld = hq + 2 * hkv;
+  const int all = pl.all_groups / n_kv * n_heads;
+  const int rank = (int)blockIdx.x / all, grp = (int)blockIdx.x % all;
+  const int x0 = (pl.nxb - 1 - rank) * 128;  // the first query blocks, with fewer keys, end the launch
+  const int n_q = grp % n_heads, b = grp / n_heads, kvh = n_q / (n_heads / n_kv);
+  const KeyRuns runs(x0, S, pl.window, pl.sinks);
+  const int iters = runs.count;
+
+  if (threadIdx.x == 0) {
+    mbar_init(bar(BB_XFULL), 1);
+    for (int i = 0; i < C::NST; ++i) {
+      mbar_init(bar(BB_YFULL + i), 1);
+      mbar_init(bar(BB_YEMPTY + i), 2);   // one commit from each MMA-issuing warp
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(BB_SDPFULL + i), 2);
+      mbar_init(bar(BB_TFULL + i), 8);
+    }
+    mbar_init(bar(BB_ACCDONE), 2);
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tm_qkv128);
+    tma_prefetch_desc(&tm_qkv64);
+    tma_prefetch_desc(&tm_do128);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_trigger();
+  pdl_wait();  // set-up done; from here on the kernel touches what its predecessor wrote
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ producer
+    if (lane == 0) {
+      mbar_expect_tx(bar(BB_XFULL), 2 * C::X_BYTES);
+#pragma unroll
+      for (int kc = 0; kc < C::KC; ++kc) {
+        tma_load_3d(sbase + C::OFF_X1 + kc * 16384, &tm_qkv128, bar(BB_XFULL), n_q * D + kc * 64, x0, b);
+        tma_load_3d(sbase + C::OFF_X2 + kc * 16384, &tm_do128, bar(BB_XFULL), n_q * D + kc * 64, x0, b);
+      }
+      for (int it = 0; it < iters; ++it) {
+        const int st = it % C::NST, y0 = runs.block(it) * 64;
+        if (!mbar_wait(bar(BB_YEMPTY + st), (((uint32_t)(it / C::NST)) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x91)) break;
+        const uint32_t ydst = sbase + C::OFF_Y + st * 2 * C::Y_BYTES;
+        mbar_expect_tx(bar(BB_YFULL + st), 2 * C::Y_BYTES);
+#pragma unroll
+        for (int kc = 0; kc < C::KC; ++kc) {
+          tma_load_3d(ydst + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), hq + kvh * D + kc * 64, y0, b);
+          tma_load_3d(ydst + C::Y_BYTES + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), hq + hkv + kvh * D + kc * 64, y0, b);
+        }
+      }
+    }
+  } else if (warp == 1 || warp == 10) {
+    // ------------------------------------------------------------------ MMA issuers
+    // two threads, because one cannot issue products this small fast enough: side 0 owns S, side 1 owns dP and dQ += dS K
+    if (lane == 0) {
+      const int side = warp == 1 ? 0 : 1;
+      const uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
+      const uint32_t idesc_sdp = idesc_base | ((uint32_t)(64 >> 3) << 17);            // N = 64, both K-major
+      const uint32_t idesc_acc = idesc_base | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // N = D, B mn-major
+      const uint64_t dx = umma_desc_sw128(sbase + (side == 0 ? C::OFF_X1 : C::OFF_X2), 0, 1024);
+      auto issue_sdp = [&](int it) {
+        const int st = it % C::NST;
+        const uint32_t y = sbase + C::OFF_Y + st * 2 * C::Y_BYTES + side * C::Y_BYTES;
+        const uint64_t dy = umma_desc_sw128(y, 0, 1024);
+        const uint32_t d_t = tmem_base + (uint32_t)((it & 1) * 128 + side * 64);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t xo = (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
+          const uint64_t yo = (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4);
+          umma_bf16(d_t, dx + xo, dy + yo, idesc_sdp, k > 0 ? 1u : 0u);
+        }
+        umma_commit(bar(BB_SDPFULL + (it & 1)));
+      };
+      bool ok = mbar_wait(bar(BB_XFULL), 0, abort_flag, err, kWaitLimitCycles, 0x92) &&
+                mbar_wait(bar(BB_YFULL), 0, abort_flag, err, kWaitLimitCycles, 0x93);
+      if (ok) {
+        tc_fence_after();
+        issue_sdp(0);
+      }
+      for (int it = 0; it < iters && ok; ++it) {
+        if (it + 1 < iters) {
+          const int y1s = (it + 1) % C::NST;
+          if (!mbar_wait(bar(BB_YFULL + y1s), ((uint32_t)((it + 1) / C::NST)) & 1u, abort_flag, err, kWaitLimitCycles, 0x94)) { ok = false; break; }
+          // the TMEM columns this writes were last read by this same thread's accumulating MMAs of block it-1: in order
+          tc_fence_after();
+          issue_sdp(it + 1);
+        }
+        const int bf = it & 1;
+        if (!mbar_wait(bar(BB_TFULL + bf), ((uint32_t)it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x95)) { ok = false; break; }
+        tc_fence_after();
+        const int yst = it % C::NST;
+        const uint32_t y1 = sbase + C::OFF_Y + yst * 2 * C::Y_BYTES;
+        // A operands (bf16) sit in TMEM where S / dP were: 16 streamed rows (K = 16) = 8 columns; the two compute warps of
+        // a lane quarter each wrote their 32 at the start of their own 32 fp32 columns
+        const uint32_t ta = tmem_base + (uint32_t)(bf * 128 + side * 64);
+        const uint32_t first = it > 0 ? 1u : 0u;
+        if (side == 1) {
+          const uint64_t by = umma_desc_sw128(y1, 8192, 1024);
+          const uint32_t dacc = tmem_base + (uint32_t)C::ACC0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t acol = (uint32_t)((k >> 1) * 32 + (k & 1) * 8);
+            umma_bf16_ts(dacc, ta + acol, by + (uint64_t)((k * 2048) >> 4), idesc_acc, k > 0 ? 1u : first);
+          }
+        }
+        umma_commit(bar(BB_YEMPTY + yst));
+      }
+      if (ok) umma_commit(bar(BB_ACCDONE));
+    }
+  } else {
+    // ------------------------------------------------------------------ compute warps
+    const int q = warp & 3, ch = (warp - 2) >> 2;
+    const int rloc = q * 32 + lane;
+    const int row = x0 + rloc;
+    const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
+    const int rmin = x0 + q * 32, rmax = rmin + 31;
+    float lse2_row = 0.f, delta_row = 0.f;
+    if (row < S) {
+      const long long stat = ((long long)b * n_heads + n_q) * S;
+      lse2_row = lse[stat + row] * kLog2e;
+      delta_row = delta[stat + row];
+    }
+    bool ok = true;
+    for (int it = 0; it < iters; ++it) {
+      const int bf = it & 1;
+      ok = mbar_wait(bar(BB_SDPFULL + bf), ((uint32_t)it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x96);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t rs[32], rp[32];
+      tmem_ld32(tlane + (uint32_t)(bf * 128 + ch * 32), rs);
+      tmem_ld32(tlane + (uint32_t)(bf * 128 + 64 + ch * 32), rp);
+      tmem_ld_wait();
+
+      // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
+      const int cmin = runs.block(it) * 64 + ch * 32;
+      const bool full = cmin + 31 <= rmin && (rmax - cmin < pl.window || cmin + 32 <= pl.sinks);
+      const int hi = row - cmin, lo = row - pl.window + 1 - cmin, sk = pl.sinks - cmin;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        float p = fast_exp2(fmaf(__uint_as_float(rs[i]), scale_log2, -lse2_row));
+        if (!full && (i > hi || (i < lo && i >= sk))) p = 0.f;
+        rp[i] = __float_as_uint(p * (__uint_as_float(rp[i]) - delta_row));
+      }
+      // bf16 pairs back into TMEM, over this warp's own (already loaded) fp32 columns
+      uint32_t wd[16];
+#pragma unroll
+      for (int c = 0; c < 16; ++c) wd[c] = pack_bf16(__uint_as_float(rp[2 * c]), __uint_as_float(rp[2 * c + 1]));
+      tmem_st16(tlane + (uint32_t)(bf * 128 + 64 + ch * 32), wd);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(BB_TFULL + bf));
+    }
+    if (ok) {
+      ok = mbar_wait(bar(BB_ACCDONE), 0, abort_flag, err, kWaitLimitCycles, 0x98);
+      ok = __all_sync(0xffffffffu, ok);
+    }
+    if (ok) {
+      tc_fence_after();
+      constexpr int W = D / 4, H = D / 2;
+      const int i0 = ch * W;
+      // this warp owns columns [i0, i0+W) and their partners D/2 further
+      float lo[W], hi[W];
+      tmem_load_cols<W>(tlane + (uint32_t)(C::ACC0 + i0), lo);
+      tmem_load_cols<W>(tlane + (uint32_t)(C::ACC0 + H + i0), hi);
+#pragma unroll
+      for (int i = 0; i < W; ++i) { lo[i] *= scale; hi[i] *= scale; }
+      if (rope_cos != nullptr) {
+        const int pos = min(row, S - 1);
+        unrotate<W>(lo, hi, rope_cos + (long long)pos * H + i0, rope_sin + (long long)pos * H + i0);
+      }
+      if (row < S) {
+        bf16* dst = dqkv + ((long long)b * S + row) * ld + n_q * D;
+        store_bf16_row<W>(dst + i0, lo);
+        store_bf16_row<W>(dst + H + i0, hi);
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag != 0) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, C::TMEM_COLS);
+  }
+}
+
+
 // Adds the partial sums of a key block's parts in part order, scales and rotates dK, rounds once.  One thread per key; block
 // (cut key block, 8 columns of dK with their partners D / 2 further, or 8 of dV).
 template <int D>
 __global__ void __launch_bounds__(128)
 attn_window_join_kernel(const float* __restrict__ partial, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
-                        const float* __restrict__ rope_sin, int S, int n_heads, int n_kv, int groups, int window, int sinks,
-                        const Split split, float scale) {
+                        const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale) {
   pdl_trigger();
   pdl_wait();
+  const int groups = pl.all_groups, S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv;
   const int x = (int)blockIdx.x / groups, grp = (int)blockIdx.x % groups;
-  const int np = split.parts_of(x, S, window, sinks, n_heads / n_kv);
+  const int np = pl.parts_of(x);
   if (np == 1) return;
-  const int rank0 = x < split.n_sink ? x * split.parts_sink : split.n_sink * split.parts_sink + (x - split.n_sink) * split.parts;
   const int row = x * 128 + threadIdx.x;
   const int kvh = grp % n_kv, b = grp / n_kv;
   const long long part_stride = (long long)groups * (2 * D * 128);
-  const float* src = partial + ((long long)rank0 * groups + grp) * (2 * D * 128) + threadIdx.x;
+  const float* src = partial + ((long long)pl.rank_of(x) * groups + grp) * (2 * D * 128) + threadIdx.x;
   constexpr int H = D / 2;
   const bool is_k = (int)blockIdx.y < H / 8;
   const int c0 = is_k ? (int)blockIdx.y * 8 : ((int)blockIdx.y - H / 8) * 8;
   float lo[8], hi[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) lo[i] = hi[i] = 0.f;
+#pragma unroll 4
   for (int p = 0; p < np; ++p) {
     const float* s = src + p * part_stride;
 #pragma unroll
@@ -778,82 +1188,113 @@ attn_window_join_kernel(const float* __restrict__ partial, bf16* __restrict__ dq
   store_bf16_row<8>(dst, lo);
 }
 
-// Parts of a key block's list.  Where the launch has several times more streamed blocks than SMs, a part is as long as a
-// window block's whole list (or an eighth of an SM's share, if that is longer), so that only sink blocks are cut.  Smaller
-// launches are cut into one part per SM, of at least 8 blocks: the set-up and the partial sums of a part cost about as
-// much as 4.
-Split make_split(int B, int S, int nh, int nkv, int window, int sinks) {
-  const long long n_rep = nh / nkv, groups = (long long)nkv * B;
-  const int nxb = (S + 127) / 128;
-  Split s;
-  s.n_sink = (int)(((long long)sinks + 127) / 128);
-  const long long sink_len = s.n_sink > 0 ? n_rep * Split::per_head(0, S, window, sinks) : 0;
-  const long long window_len = s.n_sink < nxb ? n_rep * Split::per_head(s.n_sink, S, window, 0) : 0;
-  long long total = window_len * (nxb - s.n_sink) * groups;
-  for (int x = 0; x < s.n_sink; ++x) total += n_rep * Split::per_head(x, S, window, sinks) * groups;
+
+// Parts: where the launch has several times more streamed blocks than SMs, a part is as long as a window block's whole list
+// (or an eighth of an SM's share, if that is longer), so that only sink blocks are cut.  Smaller launches are cut into one
+// part per SM, of at least 4 blocks: the set-up and the partial sums of a part cost about as much as 2.
+// Groups: dS^T is kept for as many (batch row, kv head) groups at a time as kDsBytes holds.
+constexpr size_t kDsBytes = (size_t)1 << 30;
+
+struct Scratch {
+  size_t delta, partial, band, sink, total;  // byte offsets and size
+  bool stored;                               // dS^T is stored (else dQ recomputes it)
+};
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l, int d) {
+  Plan p;
+  p.S = S; p.n_heads = nh; p.n_kv = nkv; p.window = window; p.sinks = sinks;
+  p.nxb = (S + 127) / 128;
+  p.nb = (127 + window + 127) / 128 < p.nxb ? (127 + window + 127) / 128 : p.nxb;
+  p.n_sink = (sinks + 127) / 128;
+  p.group0 = 0;
+  p.all_groups = p.groups = nkv * B;
+  const long long n_rep = nh / nkv;
+  const long long sink_len = p.n_sink > 0 ? n_rep * p.nxb : 0;
+  const long long window_len = p.n_sink < p.nxb ? n_rep * p.blocks_seen(p.n_sink) : 0;
+  long long total = window_len * (p.nxb - p.n_sink);
+  for (int x = 0; x < p.n_sink; ++x) total += n_rep * p.blocks_seen(x);
+  total *= p.all_groups;
   const long long per_sm = (total + kSms - 1) / kSms;
   const long long longest = window_len > 0 ? window_len : sink_len;
   long long chunk = per_sm < longest ? per_sm : longest;
-  if (chunk < 8) chunk = 8;
+  if (chunk < 4) chunk = 4;
   if (per_sm >= longest && chunk < (per_sm + 7) / 8) chunk = (per_sm + 7) / 8;
-  if (chunk > INT_MAX) chunk = INT_MAX;
-  s.chunk = (int)chunk;
-  s.parts = window_len > chunk ? (int)((window_len + chunk - 1) / chunk) : 1;
-  s.parts_sink = sink_len > chunk ? (int)((sink_len + chunk - 1) / chunk) : 1;
-  return s;
-}
+  p.chunk = (int)(chunk < INT_MAX ? chunk : INT_MAX);
+  p.parts = window_len > chunk ? (int)((window_len + chunk - 1) / chunk) : 1;
+  p.parts_sink = sink_len > chunk ? (int)((sink_len + chunk - 1) / chunk) : 1;
 
-struct Scratch {
-  size_t delta, partial, total;  // byte offsets and size
-};
-
-Scratch scratch_layout(int B, int S, int nh, int nkv, int d, const Split& s) {
-  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  const int nxb = (S + 127) / 128;
-  size_t slots = 0;
-  if (s.parts > 1) slots = (size_t)s.n_sink * s.parts_sink + (size_t)(nxb - s.n_sink) * s.parts;
-  else if (s.parts_sink > 1) slots = (size_t)s.n_sink * s.parts_sink;
-  Scratch l;
-  l.delta = 0;
-  l.partial = up((size_t)B * nh * S * sizeof(float));
-  l.total = l.partial + slots * B * nkv * (2 * d * 128) * sizeof(float);
-  return l;
+  const size_t slots = p.parts > 1 ? (size_t)p.ranks() : p.parts_sink > 1 ? (size_t)p.n_sink * p.parts_sink : 0;
+  l->delta = 0;
+  l->partial = round256((size_t)B * nh * S * sizeof(float));
+  l->band = l->partial + slots * p.all_groups * (2 * d * 128) * sizeof(float);
+  const size_t band = (size_t)n_rep * p.nxb * p.nb * 32768;  // of one group
+  const size_t sink = p.nxb > p.nb ? (size_t)n_rep * p.nxb * 4 * sinks * 64 : 0;
+  l->stored = band + sink <= 2 * kDsBytes;
+  l->sink = l->total = l->band;
+  if (l->stored) {
+    size_t fit = kDsBytes / (band + sink);
+    if (fit < 1) fit = 1;
+    const int rounds = (int)((p.all_groups + fit - 1) / fit);
+    p.groups = (p.all_groups + rounds - 1) / rounds;
+    l->sink = l->band + round256(p.groups * band);
+    l->total = l->sink + round256(p.groups * sink);
+  }
+  return p;
 }
 
 template <int D>
 cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs, const float* sn,
                   uint8_t* scratch, int B, int S, int nh, int nkv, int window, int sinks, int* err, cudaStream_t st) {
-  using C = BwdCfg<D>;
-  static unsigned long long smem_set_q = 0, smem_set_k = 0;
-  cudaError_t e = ensure_dynamic_smem(attn_window_bwd_kernel<D, MODE_DQ>, C::SMEM_BYTES, smem_set_q);
+  Scratch l;
+  Plan pl = make_plan(B, S, nh, nkv, window, sinks, &l, D);
+  static unsigned long long set_kv = 0, set_q = 0, set_r = 0;
+  cudaError_t e = ensure_dynamic_smem(attn_window_dkv_kernel<D>, DkvCfg<D>::SMEM_BYTES, set_kv);
+  if (e == cudaSuccess && l.stored) e = ensure_dynamic_smem(attn_window_dq_kernel<D>, DqCfg<D>::SMEM_BYTES, set_q);
+  if (e == cudaSuccess && !l.stored) e = ensure_dynamic_smem(attn_window_dq_recompute_kernel<D>, DqrCfg<D>::SMEM_BYTES, set_r);
   if (e != cudaSuccess) return e;
-  e = ensure_dynamic_smem(attn_window_bwd_kernel<D, MODE_DKV>, C::SMEM_BYTES, smem_set_k);
-  if (e != cudaSuccess) return e;
-  const Split split = make_split(B, S, nh, nkv, window, sinks);
-  const Scratch l = scratch_layout(B, S, nh, nkv, D, split);
   float* delta = reinterpret_cast<float*>(scratch + l.delta);
   float* partial = reinterpret_cast<float*>(scratch + l.partial);
-  const int hq = nh * D, nqkv = (nh + 2 * nkv) * D;
-  CUtensorMap tq128, tq64, td128, td64;
+  bf16* band = l.stored ? reinterpret_cast<bf16*>(scratch + l.band) : nullptr;
+  bf16* sink = l.stored ? reinterpret_cast<bf16*>(scratch + l.sink) : nullptr;
+  const int hq = nh * D, nqkv = (nh + 2 * nkv) * D, n_rep = nh / nkv;
+  const bool has_sink = sinks > 0 && pl.nxb > pl.nb;
+  CUtensorMap tq128, tq64, td128, tband, tsink;
   if (!make_tmap_3d(&tq128, qkv, nqkv, S, B, nqkv, 128) || !make_tmap_3d(&tq64, qkv, nqkv, S, B, nqkv, 64) ||
-      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128) || !make_tmap_3d(&td64, d_o, hq, S, B, hq, 64))
+      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128))
     return cudaErrorInvalidValue;
+  if (l.stored) {
+    if (!make_tmap_ds(&tband, band, 128, (uint64_t)pl.nb * 4, (uint64_t)pl.groups * n_rep * pl.nxb)) return cudaErrorInvalidValue;
+    if (!has_sink) tsink = tband;  // not read
+    else if (!make_tmap_ds(&tsink, sink, sinks, (uint64_t)pl.nxb * 4, (uint64_t)pl.groups * n_rep)) return cudaErrorInvalidValue;
+  }
   const float scale = (float)(1.0 / sqrt((double)D));
   const float scale_log2 = (float)((1.0 / sqrt((double)D)) * 1.4426950408889634);
+  int dev = 0, sms = kSms;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   e = attention_delta(o, d_o, delta, B, S, nh, D, st);
+  const int per_round = pl.groups;
+  for (int g0 = 0; g0 < pl.all_groups && e == cudaSuccess; g0 += per_round) {
+    pl.group0 = g0;
+    pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
+    e = launch_pdl(attn_window_dkv_kernel<D>, dim3((unsigned)pl.ranks() * pl.groups), dim3(BWD_THREADS), DkvCfg<D>::SMEM_BYTES, st,
+                   tq128, td128, lse, delta, dqkv, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
+    if (e != cudaSuccess || !l.stored) continue;
+    const int tiles = pl.nxb * pl.groups * n_rep;
+    e = launch_pdl(attn_window_dq_kernel<D>, dim3(tiles < 2 * sms ? tiles : 2 * sms), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st, tband,
+                   tsink, tq64, dqkv, cs, sn, pl, scale, err);
+  }
   if (e != cudaSuccess) return e;
-  const int nxb = (S + 127) / 128;
-  const unsigned ranks = (unsigned)(split.n_sink * split.parts_sink + (nxb - split.n_sink) * split.parts);
-  e = launch_pdl(attn_window_bwd_kernel<D, MODE_DKV>, dim3(ranks * nkv * B), dim3(BWD_THREADS), C::SMEM_BYTES, st, tq128, tq64, td128,
-                 td64, lse, delta, dqkv, partial, cs, sn, S, nh, nkv, B, nxb, window, sinks, split, scale, scale_log2, err);
-  if (e != cudaSuccess) return e;
-  e = launch_pdl(attn_window_bwd_kernel<D, MODE_DQ>, dim3((unsigned)(nxb * nh * B)), dim3(BWD_THREADS), C::SMEM_BYTES, st, tq128, tq64,
-                 td128, td64, lse, delta, dqkv, partial, cs, sn, S, nh, nkv, B, nxb, window, sinks, split, scale, scale_log2, err);
-  if (e != cudaSuccess) return e;
-  const int cut = split.parts > 1 ? nxb : split.parts_sink > 1 ? split.n_sink : 0;
+  if (!l.stored) {
+    e = launch_pdl(attn_window_dq_recompute_kernel<D>, dim3((unsigned)(pl.nxb * nh * B)), dim3(BWD_THREADS), DqrCfg<D>::SMEM_BYTES, st,
+                   tq128, tq64, td128, lse, delta, dqkv, cs, sn, pl, scale, scale_log2, err);
+    if (e != cudaSuccess) return e;
+  }
+  const int cut = pl.parts > 1 ? pl.nxb : pl.parts_sink > 1 ? pl.n_sink : 0;
   if (cut == 0) return cudaSuccess;
-  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)(cut * nkv * B), 3 * D / 16), dim3(128), 0, st, partial, dqkv, cs, sn, S,
-                    nh, nkv, nkv * B, window, sinks, split, scale);
+  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)cut * pl.all_groups, 3 * D / 16), dim3(128), 0, st, partial, dqkv, cs, sn,
+                    pl, scale);
 }
 
 // Shapes the kernels take: 32-bit grids and tensor-map extents, element counts of one row within 31 bits.
@@ -884,7 +1325,9 @@ cudaError_t attention_window_fwd(const bf16* qkv, bf16* o, float* lse, int B, in
 size_t attention_window_scratch_bytes(int B, int S, int nh, int nkv, int d, int window, int sinks) {
   if (!shape_ok(B, S, nh, nkv, d, window, sinks)) return 0;
   clamp_mask(S, window, sinks);
-  return scratch_layout(B, S, nh, nkv, d, make_split(B, S, nh, nkv, window, sinks)).total;
+  Scratch l;
+  make_plan(B, S, nh, nkv, window, sinks, &l, d);
+  return l.total;
 }
 
 cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs,

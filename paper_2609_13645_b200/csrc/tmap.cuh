@@ -77,6 +77,19 @@ inline bool make_tmap_3d(CUtensorMap* tm, const bf16* base, uint64_t cols, uint6
 // 64-byte rows (what the lanes of a warp of the dK/dV kernel store).  A box is 64 keys of 4 chunks (128 queries) and
 // lands in shared memory as 4 blocks of [64 keys][32 queries], 64-byte rows with the 64-byte swizzle: the MN-major
 // operand layout of that swizzle mode.  Strides ascend with the dimension.
+// make_tmap_ds: the same tiles for any number of keys, chunks and outer slices, [outer][chunks][keys][32].
+inline bool make_tmap_ds(CUtensorMap* tm, const bf16* base, uint64_t keys, uint64_t chunks, uint64_t outer) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[4] = {32, keys, chunks, outer};
+  cuuint64_t strides[3] = {32 * sizeof(bf16), keys * 32 * sizeof(bf16), chunks * keys * 32 * sizeof(bf16)};
+  cuuint32_t box[4] = {32, 64, 4, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<bf16*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 inline bool make_tmap_ds_chunked(CUtensorMap* tm, const bf16* base, uint64_t S, uint64_t nz) {
   EncodeTiledFn enc = get_encode_fn();
   if (!enc || S % 128 != 0) return false;
