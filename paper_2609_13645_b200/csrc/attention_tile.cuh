@@ -62,6 +62,15 @@ __device__ __forceinline__ void unrotate(float (&lo)[W], float (&hi)[W], const f
   }
 }
 
+// Untiled bulk copies (both addresses and the size multiples of 16 bytes).
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+
 // MMA issue from code that the whole warp runs: the operands stay warp-uniform and one elected lane issues.
 __device__ __forceinline__ uint32_t elect_one() {
   uint32_t e;

@@ -325,22 +325,23 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
 //   P^T = exp2(S^T c - LSE), dS^T = P^T (dP^T - delta)    compute warps, bf16 back over the columns they came from
 //   dV += P^T dO, dK += dS^T Q        A operand from TMEM, the streamed tiles again as mn-major B operands
 // TMEM is full (four 128-column accumulators at D = 128), so S and dP have one buffer each; what keeps the tensor pipe busy is
-// that the two chains alternate: side 0 (dV_j, S_{j+1}) runs while the compute warps turn dP_j into dS_j, side 1 (dK_j,
-// dP_{j+1}) while they turn S_{j+1} into P_{j+1}.  Blocks of 128 queries and not 64: an MMA of N = 64 takes as long as one
+// that two chains alternate: dV_j and S_{j+1} run while the compute warps turn dP_j into dS_j, dK_j and dP_{j+1} while they
+// turn S_{j+1} into P_{j+1}.  Blocks of 128 queries and not 64: an MMA of N = 64 takes as long as one
 // of N = 128, because it is bound by the reads of its operands from shared memory.
 // dS^T also goes to a scratch array, from which dQ = dS K is one banded contraction (below): five products per pair of
 // blocks in all instead of the seven of a backward pass that computes S and dP twice.
 enum { K_XFULL = 0, K_QFULL = 1, K_QEMPTY = 4, K_OFULL = 7, K_OEMPTY = 10, K_STFULL = 13, K_STEMPTY = 15, K_SFULL = 17, K_DPFULL = 18,
        K_PFULL = 19, K_DSFULL = 20, K_ACCDONE = 21, K_COUNT = 22 };
-constexpr int BWD_THREADS = 352;  // producer, MMA issuer (side 0), 8 compute warps, MMA issuer (side 1)
+constexpr int DKV_THREADS = 320;  // producer, MMA issuer, 8 compute warps
 
 template <int D>
 struct DkvCfg {
   static constexpr int KC = D / 64;
   static constexpr int TILE = 128 * D * 2;  // bytes of a 128-row tile
-  static constexpr int NQ = 3, NO = D == 64 ? 3 : 2;  // Q is needed by the first and the last product of a block
+  static constexpr int NQ = D == 64 ? 3 : 2, NO = D == 64 ? 3 : 2;
   static constexpr int OFF_K = 0, OFF_V = TILE, OFF_Q = 2 * TILE, OFF_O = OFF_Q + NQ * TILE;
-  static constexpr int OFF_STAT = OFF_O + NO * TILE;  // [2][lse * log2e, delta][128]
+  static constexpr int OFF_DS = OFF_O + NO * TILE;  // 4 KB a compute warp: its share of dS^T on the way to memory
+  static constexpr int OFF_STAT = OFF_DS + 8 * 4096;  // [2][lse * log2e, delta][128]
   static constexpr int OFF_BAR = OFF_STAT + 2048;
   static constexpr int SMEM_BYTES = OFF_BAR + 256;
   static constexpr int TMEM_COLS = 512;
@@ -375,7 +376,7 @@ struct Plan {
 };
 
 template <int D>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
+__global__ void __launch_bounds__(DKV_THREADS, 1)
 attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
                        const float* __restrict__ lse, const float* __restrict__ delta, bf16* __restrict__ dqkv,
                        float* __restrict__ partial, bf16* __restrict__ ds_band, bf16* __restrict__ ds_sink,
@@ -415,11 +416,11 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     mbar_init(bar(K_XFULL), 1);
     for (int i = 0; i < C::NQ; ++i) {
       mbar_init(bar(K_QFULL + i), 1);
-      mbar_init(bar(K_QEMPTY + i), 2);  // S (side 0) and dK (side 1) read Q
+      mbar_init(bar(K_QEMPTY + i), 1);
     }
     for (int i = 0; i < C::NO; ++i) {
       mbar_init(bar(K_OFULL + i), 1);
-      mbar_init(bar(K_OEMPTY + i), 2);  // dV (side 0) and dP (side 1) read dO
+      mbar_init(bar(K_OEMPTY + i), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(K_STFULL + i), 1);
@@ -429,7 +430,7 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     mbar_init(bar(K_DPFULL), 1);
     mbar_init(bar(K_PFULL), 8);
     mbar_init(bar(K_DSFULL), 8);
-    mbar_init(bar(K_ACCDONE), 2);
+    mbar_init(bar(K_ACCDONE), 1);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tm_qkv);
@@ -487,55 +488,68 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(K_STFULL + ss));
     }
-  } else if (warp == 1 || warp == 10) {
-    // ------------------------------------------------------------------ MMA issuers
-    // side 0: S, then dV over the P it became; side 1: dP, then dK over dS.  A score buffer is overwritten by the product
-    // that this same thread issued behind its last reader: in order.
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    // One queue in the order dV_j, S_{j+1}, dK_j, dP_{j+1}.  A score buffer is overwritten by the product issued behind its
+    // last reader.  (Two issuers, one a chain, let the four products of a block run interleaved: S_{j+1} then ends with
+    // the last of them and the compute warps wait for all four; 3800 cycles a block.)
     const uint32_t elected = elect_one();
-    const bool side0 = warp == 1;
     const uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
     const uint32_t idesc_s = idesc_base | ((uint32_t)(128 >> 3) << 17);               // N = 128, both K-major
     const uint32_t idesc_acc = idesc_base | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // N = D, B mn-major
-    const uint64_t dx = umma_desc_sw128(sbase + (side0 ? C::OFF_K : C::OFF_V), 0, 1024);
-    const uint32_t t_score = tmem_base + (uint32_t)(side0 ? C::COL_S : C::COL_DP);
-    const uint32_t t_acc = tmem_base + (uint32_t)(side0 ? C::COL_DV : C::COL_DK);
-    // the score product of block it: reads Q (side 0) or dO (side 1); false when a wait ran out
-    auto scores = [&](int it) -> bool {
-      const int st = side0 ? it % C::NQ : it % C::NO;
-      const uint32_t ph = (uint32_t)(side0 ? it / C::NQ : it / C::NO) & 1u;
-      bool ok = mbar_wait(bar((side0 ? K_QFULL : K_OFULL) + st), ph, abort_flag, err, kWaitLimitCycles, 0x74);
-      if (!__all_sync(0xffffffffu, ok)) return false;
-      tc_fence_after();
-      const uint64_t dy = umma_desc_sw128(sbase + (side0 ? C::OFF_Q : C::OFF_O) + st * C::TILE, 0, 1024);
+    auto wait_all = [&](int i, uint32_t parity, int site) {
+      const bool ok = mbar_wait(bar(i), parity, abort_flag, err, kWaitLimitCycles, site);
+      return __all_sync(0xffffffffu, ok) != 0;
+    };
+    // K or V (resident, at x_off) times the streamed tile y
+    auto scores = [&](uint32_t x_off, uint32_t y_off, uint32_t col) {
+      const uint64_t dx = umma_desc_sw128(sbase + x_off, 0, 1024), dy = umma_desc_sw128(sbase + y_off, 0, 1024);
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         const uint64_t o = (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
-        umma_bf16_if(elected, t_score, dx + o, dy + o, idesc_s, k > 0 ? 1u : 0u);
+        umma_bf16_if(elected, tmem_base + col, dx + o, dy + o, idesc_s, k > 0 ? 1u : 0u);
       }
-      umma_commit_if(elected, bar(side0 ? K_SFULL : K_DPFULL));
-      // this reader is done with its tile once the product is: the other reader of it is the other side
-      umma_commit_if(elected, bar((side0 ? K_QEMPTY : K_OEMPTY) + st));
-      return true;
     };
-    bool ok = mbar_wait(bar(K_XFULL), 0, abort_flag, err, kWaitLimitCycles, 0x75);
-    ok = __all_sync(0xffffffffu, ok) && scores(0);
-    for (int it = 0; it < iters && ok; ++it) {
-      ok = mbar_wait(bar(side0 ? K_PFULL : K_DSFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x76);
-      // the B operand (dO for dV, Q for dK) was waited for by the other side only
-      const int st = side0 ? it % C::NO : it % C::NQ;
-      const uint32_t ph = (uint32_t)(side0 ? it / C::NO : it / C::NQ) & 1u;
-      ok = ok && mbar_wait(bar((side0 ? K_OFULL : K_QFULL) + st), ph, abort_flag, err, kWaitLimitCycles, 0x77);
-      if (!(ok = __all_sync(0xffffffffu, ok))) break;
-      tc_fence_after();
-      const uint64_t by = umma_desc_sw128(sbase + (side0 ? C::OFF_O : C::OFF_Q) + st * C::TILE, 16384, 1024);
+    // the bf16 tile at score column `col` (TMEM) times the streamed tile y; each half of the 128 queries sits at the start
+    // of its 64 fp32 columns, 16 queries = 8 columns
+    auto accumulate = [&](uint32_t col, uint32_t y_off, uint32_t acc_col, bool first) {
+      const uint64_t by = umma_desc_sw128(sbase + y_off, 16384, 1024);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        // bf16 A operand: 16 queries = 8 columns; each half of the queries sits at the start of its 64 fp32 columns
-        const uint32_t acol = (uint32_t)((k >> 2) * 64 + (k & 3) * 8);
-        umma_bf16_ts_if(elected, t_acc, t_score + acol, by + (uint64_t)((k * 2048) >> 4), idesc_acc, (it > 0 || k > 0) ? 1u : 0u);
+      for (int k = 0; k < 8; ++k)
+        umma_bf16_ts_if(elected, tmem_base + acc_col, tmem_base + col + (uint32_t)((k >> 2) * 64 + (k & 3) * 8),
+                        by + (uint64_t)((k * 2048) >> 4), idesc_acc, (first && k == 0) ? 0u : 1u);
+    };
+    bool ok = wait_all(K_XFULL, 0, 0x74) && wait_all(K_QFULL, 0, 0x75) && wait_all(K_OFULL, 0, 0x76);
+    if (ok) {
+      tc_fence_after();
+      scores(C::OFF_K, C::OFF_Q, C::COL_S);
+      umma_commit_if(elected, bar(K_SFULL));
+      scores(C::OFF_V, C::OFF_O, C::COL_DP);
+      umma_commit_if(elected, bar(K_DPFULL));
+    }
+    for (int it = 0; it < iters && ok; ++it) {
+      const int sq = it % C::NQ, so = it % C::NO, nq = (it + 1) % C::NQ, no = (it + 1) % C::NO;
+      const bool more = it + 1 < iters;
+      if (!(ok = wait_all(K_PFULL, (uint32_t)it & 1u, 0x77))) break;
+      tc_fence_after();
+      accumulate(C::COL_S, C::OFF_O + so * C::TILE, C::COL_DV, it == 0);
+      umma_commit_if(elected, bar(K_OEMPTY + so));  // dP_j and dV_j have read dO_j
+      if (more) {
+        if (!(ok = wait_all(K_QFULL + nq, (uint32_t)((it + 1) / C::NQ) & 1u, 0x78))) break;
+        tc_fence_after();
+        scores(C::OFF_K, C::OFF_Q + nq * C::TILE, C::COL_S);
+        umma_commit_if(elected, bar(K_SFULL));
       }
-      umma_commit_if(elected, bar((side0 ? K_OEMPTY : K_QEMPTY) + st));
-      if (it + 1 < iters) ok = scores(it + 1);
+      if (!(ok = wait_all(K_DSFULL, (uint32_t)it & 1u, 0x79))) break;
+      tc_fence_after();
+      accumulate(C::COL_DP, C::OFF_Q + sq * C::TILE, C::COL_DK, it == 0);
+      umma_commit_if(elected, bar(K_QEMPTY + sq));  // S_j and dK_j have read Q_j
+      if (more) {
+        if (!(ok = wait_all(K_OFULL + no, (uint32_t)((it + 1) / C::NO) & 1u, 0x7a))) break;
+        tc_fence_after();
+        scores(C::OFF_V, C::OFF_O + no * C::TILE, C::COL_DP);
+        umma_commit_if(elected, bar(K_DPFULL));
+      }
     }
     if (ok) umma_commit_if(elected, bar(K_ACCDONE));
   } else {
@@ -545,6 +559,7 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     const int rmin = x0 + q * 32, rmax = rmin + 31;
     const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
     const uint32_t t_s = tlane + (uint32_t)(C::COL_S + ch * 64), t_dp = tlane + (uint32_t)(C::COL_DP + ch * 64);
+    const uint32_t stage = sbase + (uint32_t)(C::OFF_DS + (warp - 2) * 4096);
     // the queries that see key `row` are [row, row_end)
     const int row_end = row < pl.sinks || S - row < pl.window ? S : row + pl.window;
     bool ok = true;
@@ -554,8 +569,8 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       const int cmin = (x + rel) * 128 + ch * 64;
       const float* st_lse = s_stat + ss * 256 + ch * 64;
       const float* st_dl = st_lse + 128;
-      ok = mbar_wait(bar(K_STFULL + ss), (uint32_t)(it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x78) &&
-           mbar_wait(bar(K_SFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x79);
+      ok = mbar_wait(bar(K_STFULL + ss), (uint32_t)(it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x7b) &&
+           mbar_wait(bar(K_SFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x7c);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -596,7 +611,7 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(K_PFULL));
 
-      ok = mbar_wait(bar(K_DPFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x7a);
+      ok = mbar_wait(bar(K_DPFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x7d);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -626,17 +641,30 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
         mbar_arrive(bar(K_DSFULL));
         mbar_arrive(bar(K_STEMPTY + ss));
       }
-      // off the chain's critical path: the same rounded dS^T to the scratch of the dQ contraction, as 32-query chunks
-      // [chunk][key][32]: a thread stores one contiguous 64-byte row per chunk, its warp 2 KiB
+      // Off the chain's critical path: the same rounded dS^T to the scratch of the dQ contraction, whose operand tiles of
+      // 64 keys x 128 queries lie there as the very bytes its shared memory will hold: [key half][32-query chunk][64 keys]
+      // rows of 64 bytes under the 64-byte swizzle.  A warp's 32 keys of a chunk are 2 KB in one piece and leave as a bulk
+      // copy.  (Stored by the threads themselves they held up the next block by 1900 cycles.)
       if (ds_band != nullptr) {
         const long long z = (long long)local * n_rep + (first_it + it) / per_head;
         if (rel < pl.nb) {
-          bf16* dst = ds_band + ((((z * pl.nxb + x) * pl.nb + rel) * 4 + ch * 2) * 128 + rloc) * 32;
-          store8_b32(dst, w);
-          store8_b32(dst + 16, w + 8);
-          store8_b32(dst + 4096, w + 16);
-          store8_b32(dst + 4096 + 16, w + 24);
-        } else if (row < pl.sinks) {  // beyond the window only sink keys are seen
+          if (lane == 0) bulk_wait_group_read0();
+          __syncwarp();
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {  // 16-byte piece c & 3 of chunk c >> 2
+            const uint32_t at = stage + (uint32_t)((c >> 2) * 2048 + lane * 64 + (((c & 3) ^ ((lane >> 1) & 3)) * 16));
+            st_shared_v4(at, make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            uint8_t* dst = reinterpret_cast<uint8_t*>(ds_band) +
+                           (((z * pl.nxb + x) * pl.nb + rel) * 8 + (q >> 1) * 4 + ch * 2) * 4096 + (q & 1) * 2048;
+            bulk_store(dst, stage, 2048);
+            bulk_store(dst + 4096, stage + 2048, 2048);
+            bulk_commit_group();
+          }
+        } else if (row < pl.sinks) {  // beyond the window only sink keys are seen: rows of [chunk][sink key][32 queries]
           bf16* dst = ds_sink + ((((z * pl.nxb + x + rel) * 4 + ch * 2) * pl.sinks + row) * 32);
           store8_b32(dst, w);
           store8_b32(dst + 16, w + 8);
@@ -646,8 +674,10 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
         }
       }
     }
+    if (lane == 0) bulk_wait_group0();
+    __syncwarp();
     if (ok) {
-      ok = mbar_wait(bar(K_ACCDONE), 0, abort_flag, err, kWaitLimitCycles, 0x7b);
+      ok = mbar_wait(bar(K_ACCDONE), 0, abort_flag, err, kWaitLimitCycles, 0x7e);
       ok = __all_sync(0xffffffffu, ok);
     }
     if (ok) {
@@ -728,7 +758,7 @@ struct DqCfg {
 
 template <int D>
 __global__ void __launch_bounds__(DQ_THREADS, 2)
-attn_window_dq_kernel(const __grid_constant__ CUtensorMap tm_band, const __grid_constant__ CUtensorMap tm_sink,
+attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ CUtensorMap tm_sink,
                       const __grid_constant__ CUtensorMap tm_qkv, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
                       const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale, int* err) {
   using C = DqCfg<D>;
@@ -758,7 +788,6 @@ attn_window_dq_kernel(const __grid_constant__ CUtensorMap tm_band, const __grid_
     }
     *abort_flag = 0;
     mbar_fence_init();
-    tma_prefetch_desc(&tm_band);
     tma_prefetch_desc(&tm_sink);
     tma_prefetch_desc(&tm_qkv);
   }
@@ -814,7 +843,7 @@ attn_window_dq_kernel(const __grid_constant__ CUtensorMap tm_band, const __grid_
           } else {
             const int j = i - r.n_sink64, x = r.x_first + (j >> 1);
             key0 = x * 128 + (j & 1) * 64;
-            tma_load_4d(a_dst, &tm_band, fb, 0, (j & 1) * 64, (r.qt - x) * 4, r.z * pl.nxb + x);
+            bulk_load(a_dst, ds_band + ((((long long)r.z * pl.nxb + x) * pl.nb + r.qt - x) * 2 + (j & 1)) * 8192, C::A_BYTES, fb);
           }
 #pragma unroll
           for (int c = 0; c < D / 64; ++c) tma_load_3d(b_dst + c * 8192, &tm_qkv, fb, hq + r.kvh * D + 64 * c, key0, r.b);
@@ -903,6 +932,7 @@ attn_window_dq_kernel(const __grid_constant__ CUtensorMap tm_band, const __grid_
 // For sequences and windows whose dS^T would not fit the scratch even for one group: 128 queries (Q, dO) resident, 64-key
 // blocks (K, V) streamed, S and dP computed again into one of two TMEM buffers, dQ += dS K.
 enum { BB_XFULL = 0, BB_YFULL = 1, BB_YEMPTY = 5, BB_SDPFULL = 9, BB_TFULL = 11, BB_ACCDONE = 13, BB_COUNT = 14 };
+constexpr int DQR_THREADS = 352;  // producer, 2 MMA issuers, 8 compute warps
 
 template <int D>
 struct DqrCfg {
@@ -918,7 +948,7 @@ struct DqrCfg {
 };
 
 template <int D>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
+__global__ void __launch_bounds__(DQR_THREADS, 1)
 attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, const __grid_constant__ CUtensorMap tm_qkv64,
                                 const __grid_constant__ CUtensorMap tm_do128, const float* __restrict__ lse,
                                 const float* __restrict__ delta, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
@@ -1260,13 +1290,12 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   bf16* sink = l.stored ? reinterpret_cast<bf16*>(scratch + l.sink) : nullptr;
   const int hq = nh * D, nqkv = (nh + 2 * nkv) * D, n_rep = nh / nkv;
   const bool has_sink = sinks > 0 && pl.nxb > pl.nb;
-  CUtensorMap tq128, tq64, td128, tband, tsink;
+  CUtensorMap tq128, tq64, td128, tsink;
   if (!make_tmap_3d(&tq128, qkv, nqkv, S, B, nqkv, 128) || !make_tmap_3d(&tq64, qkv, nqkv, S, B, nqkv, 64) ||
       !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128))
     return cudaErrorInvalidValue;
   if (l.stored) {
-    if (!make_tmap_ds(&tband, band, 128, (uint64_t)pl.nb * 4, (uint64_t)pl.groups * n_rep * pl.nxb)) return cudaErrorInvalidValue;
-    if (!has_sink) tsink = tband;  // not read
+    if (!has_sink) tsink = tq64;  // not read
     else if (!make_tmap_ds(&tsink, sink, sinks, (uint64_t)pl.nxb * 4, (uint64_t)pl.groups * n_rep)) return cudaErrorInvalidValue;
   }
   const float scale = (float)(1.0 / sqrt((double)D));
@@ -1278,16 +1307,16 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   for (int g0 = 0; g0 < pl.all_groups && e == cudaSuccess; g0 += per_round) {
     pl.group0 = g0;
     pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
-    e = launch_pdl(attn_window_dkv_kernel<D>, dim3((unsigned)pl.ranks() * pl.groups), dim3(BWD_THREADS), DkvCfg<D>::SMEM_BYTES, st,
+    e = launch_pdl(attn_window_dkv_kernel<D>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D>::SMEM_BYTES, st,
                    tq128, td128, lse, delta, dqkv, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess || !l.stored) continue;
     const int tiles = pl.nxb * pl.groups * n_rep;
-    e = launch_pdl(attn_window_dq_kernel<D>, dim3(tiles < 2 * sms ? tiles : 2 * sms), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st, tband,
-                   tsink, tq64, dqkv, cs, sn, pl, scale, err);
+    e = launch_pdl(attn_window_dq_kernel<D>, dim3(tiles < 2 * sms ? tiles : 2 * sms), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
+                   (const bf16*)band, tsink, tq64, dqkv, cs, sn, pl, scale, err);
   }
   if (e != cudaSuccess) return e;
   if (!l.stored) {
-    e = launch_pdl(attn_window_dq_recompute_kernel<D>, dim3((unsigned)(pl.nxb * nh * B)), dim3(BWD_THREADS), DqrCfg<D>::SMEM_BYTES, st,
+    e = launch_pdl(attn_window_dq_recompute_kernel<D>, dim3((unsigned)(pl.nxb * nh * B)), dim3(DQR_THREADS), DqrCfg<D>::SMEM_BYTES, st,
                    tq128, tq64, td128, lse, delta, dqkv, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess) return e;
   }
