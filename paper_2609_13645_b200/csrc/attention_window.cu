@@ -61,8 +61,8 @@ struct FwdCfg {
 
 template <int D>
 __global__ void __launch_bounds__(FWD_THREADS, 2)
-attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKV, bf16* __restrict__ o,
-                       float* __restrict__ lse, int S, int n_heads, int n_kv, int n_batch, int n_qblocks, int window, int sinks,
+attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKV,
+                       const __grid_constant__ CUtensorMap tmO, float* __restrict__ lse, int S, int n_heads, int n_kv, int n_batch, int n_qblocks, int window, int sinks,
                        float scale_log2, int* err) {
   using C = FwdCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -89,6 +89,14 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   const KeyRuns runs(q0, S, window, sinks);
   const int nb = runs.count;
 
+  auto load_k = [&](int j) {
+    const int st = j % C::NK;
+    mbar_expect_tx(bar(B_KFULL + st), C::KV_BYTES);
+#pragma unroll
+    for (int kc = 0; kc < C::KC; ++kc)
+      tma_load_3d(sbase + C::OFF_K + st * C::KV_BYTES + kc * (C::BK * 128), &tmKV, bar(B_KFULL + st), hq + kvh * D + kc * 64,
+                  runs.block(j) * C::BK, b);
+  };
   if (threadIdx.x == 0) {
     mbar_init(bar(B_QFULL), 1);
     for (int i = 0; i < C::NK; ++i) {
@@ -107,8 +115,13 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     mbar_init(bar(B_OFINAL), 1);
     *abort_flag = 0;
     mbar_fence_init();
-    tma_prefetch_desc(&tmQ);
-    tma_prefetch_desc(&tmKV);
+    // the first loads do not wait for the rest of the set-up
+    pdl_wait();
+    mbar_expect_tx(bar(B_QFULL), C::Q_BYTES);
+#pragma unroll
+    for (int kc = 0; kc < C::KC; ++kc)
+      tma_load_3d(sbase + kc * (C::BQ * 128), &tmQ, bar(B_QFULL), n * D + kc * 64, q0, b);
+    for (int j = 0; j < nb && j < C::NK; ++j) load_k(j);
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
@@ -123,18 +136,9 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
 
   if (warp == 0) {
     if (lane == 0) {
-      mbar_expect_tx(bar(B_QFULL), C::Q_BYTES);
-#pragma unroll
-      for (int kc = 0; kc < C::KC; ++kc)
-        tma_load_3d(sbase + kc * (C::BQ * 128), &tmQ, bar(B_QFULL), n * D + kc * 64, q0, b);
-      for (int j = 0; j < nb; ++j) {
-        const int st = j % C::NK;
-        if (!mbar_wait(bar(B_KEMPTY + st), ((uint32_t)(j / C::NK) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x61)) break;
-        mbar_expect_tx(bar(B_KFULL + st), C::KV_BYTES);
-#pragma unroll
-        for (int kc = 0; kc < C::KC; ++kc)
-          tma_load_3d(sbase + C::OFF_K + st * C::KV_BYTES + kc * (C::BK * 128), &tmKV, bar(B_KFULL + st),
-                      hq + kvh * D + kc * 64, runs.block(j) * C::BK, b);
+      for (int j = C::NK; j < nb; ++j) {
+        if (!mbar_wait(bar(B_KEMPTY + j % C::NK), ((uint32_t)(j / C::NK) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x61)) break;
+        load_k(j);
       }
     }
   } else if (warp == 6) {
@@ -270,19 +274,11 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     }
     if (ok) {
       tc_fence_after();
-      const float inv = 1.0f / lsum;
-      bf16* orow = o + ((long long)b * S + row) * hq + n * D;
-#pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        float t[32];
-        tmem_load_cols<32>(tlane + (uint32_t)(C::O_COL + c), t);
-        if (row < S) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) t[i] *= inv;
-          store_bf16_row<32>(orow + c, t);
-        }
-      }
+      const uint32_t out = sbase + (uint32_t)(q * 32 * D * 2);  // Q has been read
+      stage_rows<D>(out, lane, tlane + (uint32_t)C::O_COL, 1.0f / lsum);
+      send_rows<D>(&tmO, out, lane, n * D, q0 + q * 32, b, S);
       if (row < S) lse[((long long)b * n_heads + n) * S + row] = (mref + log2f(lsum)) * kLn2;
+      if (lane == 0) bulk_wait_group0();
     }
   }
 
@@ -309,12 +305,13 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
   cudaError_t e = ensure_dynamic_smem(attn_window_fwd_kernel<D>, C::SMEM_BYTES, smem_set);
   if (e != cudaSuccess) return e;
   const int nqkv = (nh + 2 * nkv) * D;
-  CUtensorMap tmQ, tmKV;
-  if (!make_tmap_3d(&tmQ, qkv, nqkv, S, B, nqkv, C::BQ) || !make_tmap_3d(&tmKV, qkv, nqkv, S, B, nqkv, C::BK))
+  CUtensorMap tmQ, tmKV, tmO;
+  if (!make_tmap_3d(&tmQ, qkv, nqkv, S, B, nqkv, C::BQ) || !make_tmap_3d(&tmKV, qkv, nqkv, S, B, nqkv, C::BK) ||
+      !make_tmap_3d(&tmO, o, nh * D, S, B, nh * D, 32))
     return cudaErrorInvalidValue;
   const float scale_log2 = (float)((1.0 / sqrt((double)D)) * 1.4426950408889634);
   const int nqb = (S + C::BQ - 1) / C::BQ;
-  return launch_pdl(attn_window_fwd_kernel<D>, dim3((unsigned)(nqb * nh * B)), dim3(FWD_THREADS), C::SMEM_BYTES, st, tmQ, tmKV, o, lse,
+  return launch_pdl(attn_window_fwd_kernel<D>, dim3((unsigned)(nqb * nh * B)), dim3(FWD_THREADS), C::SMEM_BYTES, st, tmQ, tmKV, tmO, lse,
                     S, nh, nkv, B, nqb, window, sinks, scale_log2, err);
 }
 
@@ -378,7 +375,7 @@ struct Plan {
 template <int D>
 __global__ void __launch_bounds__(DKV_THREADS, 1)
 attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
-                       const float* __restrict__ lse, const float* __restrict__ delta, bf16* __restrict__ dqkv,
+                       const __grid_constant__ CUtensorMap tm_out, const float* __restrict__ lse, const float* __restrict__ delta,
                        float* __restrict__ partial, bf16* __restrict__ ds_band, bf16* __restrict__ ds_sink,
                        const float* __restrict__ rope_cos, const float* __restrict__ rope_sin, const __grid_constant__ Plan pl,
                        float scale, float scale_log2, int* err) {
@@ -399,7 +396,6 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   }
   const int S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv, n_rep = n_heads / n_kv;
   const int hq = n_heads * D, hkv = n_kv * D;
-  const long long ld = hq + 2 * hkv;
   // sink blocks, with the longest lists, first
   const int rank = (int)blockIdx.x / pl.groups, local = (int)blockIdx.x % pl.groups, grp = pl.group0 + local;
   const int kvh = grp % n_kv, b = grp / n_kv;
@@ -412,6 +408,22 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   const int first_it = (int)((long long)total * part / np);
   const int iters = (int)((long long)total * (part + 1) / np) - first_it;
 
+  auto head_of = [&](int it) { return kvh * n_rep + (first_it + it) / per_head; };
+  auto query_of = [&](int it) { return (x + (first_it + it) % per_head) * 128; };
+  auto load_q = [&](int it) {
+    const int st = it % C::NQ;
+    mbar_expect_tx(bar(K_QFULL + st), C::TILE);
+#pragma unroll
+    for (int kc = 0; kc < C::KC; ++kc)
+      tma_load_3d(sbase + C::OFF_Q + st * C::TILE + kc * 16384, &tm_qkv, bar(K_QFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
+  };
+  auto load_do = [&](int it) {
+    const int st = it % C::NO;
+    mbar_expect_tx(bar(K_OFULL + st), C::TILE);
+#pragma unroll
+    for (int kc = 0; kc < C::KC; ++kc)
+      tma_load_3d(sbase + C::OFF_O + st * C::TILE + kc * 16384, &tm_do, bar(K_OFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
+  };
   if (threadIdx.x == 0) {
     mbar_init(bar(K_XFULL), 1);
     for (int i = 0; i < C::NQ; ++i) {
@@ -433,8 +445,17 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     mbar_init(bar(K_ACCDONE), 1);
     *abort_flag = 0;
     mbar_fence_init();
-    tma_prefetch_desc(&tm_qkv);
-    tma_prefetch_desc(&tm_do);
+    // the first loads do not wait for the rest of the set-up
+    pdl_wait();
+    mbar_expect_tx(bar(K_XFULL), 2 * C::TILE);
+#pragma unroll
+    for (int kc = 0; kc < C::KC; ++kc)
+      tma_load_3d(sbase + C::OFF_K + kc * 16384, &tm_qkv, bar(K_XFULL), hq + kvh * D + kc * 64, x0, b);
+    load_q(0);
+#pragma unroll
+    for (int kc = 0; kc < C::KC; ++kc)
+      tma_load_3d(sbase + C::OFF_V + kc * 16384, &tm_qkv, bar(K_XFULL), hq + hkv + kvh * D + kc * 64, x0, b);
+    load_do(0);
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
@@ -449,32 +470,16 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
-    if (lane == 0) {
-      mbar_expect_tx(bar(K_XFULL), 2 * C::TILE);
-#pragma unroll
-      for (int kc = 0; kc < C::KC; ++kc) {
-        tma_load_3d(sbase + C::OFF_K + kc * 16384, &tm_qkv, bar(K_XFULL), hq + kvh * D + kc * 64, x0, b);
-        tma_load_3d(sbase + C::OFF_V + kc * 16384, &tm_qkv, bar(K_XFULL), hq + hkv + kvh * D + kc * 64, x0, b);
-      }
-    }
     for (int it = 0; it < iters; ++it) {
-      const int n = kvh * n_rep + (first_it + it) / per_head, q0 = (x + (first_it + it) % per_head) * 128;
-      const int sq = it % C::NQ, so = it % C::NO, ss = it & 1;
-      bool ok = mbar_wait(bar(K_QEMPTY + sq), ((uint32_t)(it / C::NQ) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x71);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      if (lane == 0) {
-        mbar_expect_tx(bar(K_QFULL + sq), C::TILE);
-#pragma unroll
-        for (int kc = 0; kc < C::KC; ++kc)
-          tma_load_3d(sbase + C::OFF_Q + sq * C::TILE + kc * 16384, &tm_qkv, bar(K_QFULL + sq), n * D + kc * 64, q0, b);
-      }
-      ok = mbar_wait(bar(K_OEMPTY + so), ((uint32_t)(it / C::NO) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x72);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      if (lane == 0) {
-        mbar_expect_tx(bar(K_OFULL + so), C::TILE);
-#pragma unroll
-        for (int kc = 0; kc < C::KC; ++kc)
-          tma_load_3d(sbase + C::OFF_O + so * C::TILE + kc * 16384, &tm_do, bar(K_OFULL + so), n * D + kc * 64, q0, b);
+      const int n = head_of(it), q0 = query_of(it), ss = it & 1;
+      bool ok = true;
+      if (it > 0) {  // block 0 is on its way
+        ok = mbar_wait(bar(K_QEMPTY + it % C::NQ), ((uint32_t)(it / C::NQ) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x71);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        if (lane == 0) load_q(it);
+        ok = mbar_wait(bar(K_OEMPTY + it % C::NO), ((uint32_t)(it / C::NO) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x72);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        if (lane == 0) load_do(it);
       }
       ok = mbar_wait(bar(K_STEMPTY + ss), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x73);
       if (!__all_sync(0xffffffffu, ok)) break;
@@ -682,31 +687,19 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     }
     if (ok) {
       tc_fence_after();
-      constexpr int W = D / 4, H = D / 2;
-      const int i0 = ch * W;
+      constexpr int H = D / 2;
       const uint32_t t_dk = tlane + (uint32_t)C::COL_DK, t_dv = tlane + (uint32_t)C::COL_DV;
       if (np == 1) {
-        // this CTA holds the whole sum: scale, rotate back (columns [i0, i0 + W) and their partners D / 2 further), round
-        float lo[W], hi[W];
-        tmem_load_cols<W>(t_dk + (uint32_t)i0, lo);
-        tmem_load_cols<W>(t_dk + (uint32_t)(H + i0), hi);
-#pragma unroll
-        for (int i = 0; i < W; ++i) { lo[i] *= scale; hi[i] *= scale; }
-        if (rope_cos != nullptr) {
-          const int pos = min(row, S - 1);
-          unrotate<W>(lo, hi, rope_cos + (long long)pos * H + i0, rope_sin + (long long)pos * H + i0);
+        // this CTA holds the whole sum: one warp of a lane quarter takes dK (scaled, rotated back), the other dV
+        const uint32_t out = sbase + (uint32_t)((warp - 2) * 32 * D * 2);  // K and V have been read
+        if (ch == 0) {
+          if (rope_cos != nullptr) stage_rows_unrotated<D>(out, stage, lane, t_dk, scale, rope_cos, rope_sin, rmin, S);
+          else stage_rows<D>(out, lane, t_dk, scale);
+        } else {
+          stage_rows<D>(out, lane, t_dv, 1.0f);
         }
-        bf16* dst = dqkv + ((long long)b * S + row) * ld + hq + kvh * D;
-        if (row < S) {
-          store_bf16_row<W>(dst + i0, lo);
-          store_bf16_row<W>(dst + H + i0, hi);
-        }
-#pragma unroll 1
-        for (int c = ch * H; c < (ch + 1) * H; c += 32) {
-          float v[32];
-          tmem_load_cols<32>(t_dv + (uint32_t)c, v);
-          if (row < S) store_bf16_row<32>(dst + hkv + c, v);
-        }
+        send_rows<D>(&tm_out, out, lane, hq + ch * hkv + kvh * D, rmin, b, S);
+        if (lane == 0) bulk_wait_group0();
       } else {
         // partial sums [part][dK columns, dV columns][128 keys]: a warp writes 32 consecutive keys of a column
         float* dst = partial + ((long long)rank * pl.all_groups + grp) * (2 * D * 128) + rloc;
@@ -750,8 +743,10 @@ struct DqCfg {
   static constexpr int A_BYTES = 64 * 128 * 2;  // one box of dS^T: 4 chunks of [64 keys][32 queries], 64-byte swizzle
   static constexpr int B_BYTES = 64 * D * 2;
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int STAGES = D == 64 ? 4 : 3;
-  static constexpr int OFF_BAR = STAGES * STAGE_BYTES;
+  static constexpr int STAGES = D == 64 ? 3 : 2;
+  static constexpr int OFF_OUT = STAGES * STAGE_BYTES;    // an epilogue warp's rows
+  static constexpr int OFF_TABLE = OFF_OUT + 128 * D * 2;  // and its piece of the rotation tables
+  static constexpr int OFF_BAR = OFF_TABLE + 4 * 4096;
   static constexpr int SMEM_BYTES = OFF_BAR + 128;
   static constexpr int TMEM_COLS = 2 * D;
 };
@@ -759,7 +754,7 @@ struct DqCfg {
 template <int D>
 __global__ void __launch_bounds__(DQ_THREADS, 2)
 attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ CUtensorMap tm_sink,
-                      const __grid_constant__ CUtensorMap tm_qkv, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
+                      const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_out, const float* __restrict__ rope_cos,
                       const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale, int* err) {
   using C = DqCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -804,7 +799,6 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
 
   const int S = pl.S, n_rep = pl.n_heads / pl.n_kv;
   const int hq = pl.n_heads * D;
-  const long long ld = (long long)(pl.n_heads + 2 * pl.n_kv) * D;
   const int nz = pl.groups * n_rep, ntiles = pl.nxb * nz;
   // tile t: query block qt of head z of this launch; 64-key steps: sink keys behind the band, then the band
   struct Tile {
@@ -884,34 +878,26 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
     const int q = warp & 3;
     int acc = 0;
     uint32_t acc_phase = 0;
-    constexpr int H = D / 2;
+    const uint32_t out = sbase + (uint32_t)(C::OFF_OUT + q * 32 * D * 2), table = sbase + (uint32_t)(C::OFF_TABLE + q * 4096);
     for (int t = blockIdx.x; t < ntiles; t += gridDim.x) {
       const Tile r = tile_of(t);
       bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, err, kWaitLimitCycles, 0x84);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
-      const int row = r.qt * 128 + q * 32 + lane, pos = min(row, S - 1);
+      const int row0 = r.qt * 128 + q * 32;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * D);
-      bf16* dst = dqkv + ((long long)r.b * S + row) * ld + r.n * D;
-#pragma unroll 1
-      for (int i0 = 0; i0 < H; i0 += 32) {
-        float lo[32], hi[32];
-        tmem_load_cols<32>(taddr + (uint32_t)i0, lo);
-        tmem_load_cols<32>(taddr + (uint32_t)(H + i0), hi);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) { lo[i] *= scale; hi[i] *= scale; }
-        if (rope_cos != nullptr) unrotate<32>(lo, hi, rope_cos + (long long)pos * H + i0, rope_sin + (long long)pos * H + i0);
-        if (row < S) {
-          store_bf16_row<32>(dst + i0, lo);
-          store_bf16_row<32>(dst + H + i0, hi);
-        }
-      }
+      if (lane == 0) bulk_wait_group_read0();  // the last tile's rows have left the staging buffer
+      __syncwarp();
+      if (rope_cos != nullptr) stage_rows_unrotated<D>(out, table, lane, taddr, scale, rope_cos, rope_sin, row0, S);
+      else stage_rows<D>(out, lane, taddr, scale);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
+      send_rows<D>(&tm_out, out, lane, r.n * D, row0, r.b, S);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
     }
+    if (lane == 0) bulk_wait_group0();
   }
 
   tc_fence_before();
@@ -1290,9 +1276,9 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   bf16* sink = l.stored ? reinterpret_cast<bf16*>(scratch + l.sink) : nullptr;
   const int hq = nh * D, nqkv = (nh + 2 * nkv) * D, n_rep = nh / nkv;
   const bool has_sink = sinks > 0 && pl.nxb > pl.nb;
-  CUtensorMap tq128, tq64, td128, tsink;
+  CUtensorMap tq128, tq64, td128, tsink, tout;
   if (!make_tmap_3d(&tq128, qkv, nqkv, S, B, nqkv, 128) || !make_tmap_3d(&tq64, qkv, nqkv, S, B, nqkv, 64) ||
-      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128))
+      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128) || !make_tmap_3d(&tout, dqkv, nqkv, S, B, nqkv, 32))
     return cudaErrorInvalidValue;
   if (l.stored) {
     if (!has_sink) tsink = tq64;  // not read
@@ -1308,11 +1294,11 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
     pl.group0 = g0;
     pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
     e = launch_pdl(attn_window_dkv_kernel<D>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D>::SMEM_BYTES, st,
-                   tq128, td128, lse, delta, dqkv, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
+                   tq128, td128, tout, lse, delta, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess || !l.stored) continue;
     const int tiles = pl.nxb * pl.groups * n_rep;
     e = launch_pdl(attn_window_dq_kernel<D>, dim3(tiles < 2 * sms ? tiles : 2 * sms), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
-                   (const bf16*)band, tsink, tq64, dqkv, cs, sn, pl, scale, err);
+                   (const bf16*)band, tsink, tq64, tout, cs, sn, pl, scale, err);
   }
   if (e != cudaSuccess) return e;
   if (!l.stored) {
