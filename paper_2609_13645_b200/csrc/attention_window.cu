@@ -6,8 +6,8 @@
 //
 //   * Which blocks are streamed is a list of two runs: the blocks that hold sink keys, then the blocks of the window.  Work
 //     and traffic are linear in the sequence; only blocks on the edge of a run test single elements.
-//   * A row can meet a block of which it sees nothing (the oldest block of its tile's window): its running maximum may
-//     still be -inf then, and the reference, the rescaling factor and the exponentials are guarded for it.
+//   * A row can meet a block of which it sees nothing (the oldest block of its tile's window) before any other: maxima of
+//     -inf and empty sums are part of the softmax loop.
 //   * A block of sink keys is seen by every later query, so its gradient is a sum over the whole sequence while every other
 //     key block's is one over window + 128 queries.  The streamed list of a key block is therefore cut into parts of about
 //     equal length that run as CTAs of their own and leave fp32 partial sums; a small kernel adds them in part order (no
@@ -59,6 +59,23 @@ struct FwdCfg {
   static constexpr int O_COL = 128;
 };
 
+// Bit e: key e of 32 is seen, given that keys e <= hi are causal, e >= lo in the window and e < sk sinks.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t visible(int hi, int lo, int sk) { return below(hi + 1) & (~below(lo) | below(sk)); }
+
+// The exponentials of 32 scores against the row's reference: their bf16 pairs, their sum and the scores' maximum.
+__device__ __forceinline__ void softmax_chunk(const uint32_t (&r)[32], float scale_log2, float mref, uint32_t* pw, float2& psum, float& mx) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 2) {
+    const float s0 = __uint_as_float(r[e]), s1 = __uint_as_float(r[e + 1]);
+    mx = fmaxf(mx, fmaxf(s0, s1));
+    const float2 x = fma2(make_float2(s0, s1), both(scale_log2), both(-mref));
+    const float2 a = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+    psum = add2(psum, a);
+    pw[e >> 1] = pack_bf16(a.x, a.y);
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(FWD_THREADS, 2)
 attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKV,
@@ -73,7 +90,7 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + B_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if ((sbase & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
     if (threadIdx.x == 0) atomicExch(err, (int)ERR_BAD_ALIGNMENT);
     return;
@@ -154,14 +171,19 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    {
+      const uint32_t elected = elect_one();
       const uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(C::BQ >> 4) << 24);
       const uint32_t idesc_s = idesc_base | ((uint32_t)(C::BK >> 3) << 17);            // N = 64 keys, both K-major
       const uint32_t idesc_pv = idesc_base | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // N = D, B (V) mn-major
       const uint64_t dq = umma_desc_sw128(sbase, 0, 1024);
+      auto wait_all = [&](int i, uint32_t parity, int site) {
+        const bool ok = mbar_wait(bar(i), parity, abort_flag, err, kWaitLimitCycles, site);
+        return __all_sync(0xffffffffu, ok) != 0;
+      };
       auto issue_s = [&](int j) -> bool {
         const int st = j % C::NK;
-        if (!mbar_wait(bar(B_KFULL + st), (uint32_t)(j / C::NK) & 1u, abort_flag, err, kWaitLimitCycles, 0x63)) return false;
+        if (!wait_all(B_KFULL + st, (uint32_t)(j / C::NK) & 1u, 0x63)) return false;
         tc_fence_after();
         const uint64_t dk = umma_desc_sw128(sbase + C::OFF_K + st * C::KV_BYTES, 0, 1024);
         const uint32_t d_tmem = tmem_base + (uint32_t)((j & 1) * C::BK);
@@ -169,30 +191,29 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         for (int k = 0; k < D / 16; ++k) {
           const uint64_t qo = (uint64_t)(((k >> 2) * (C::BQ * 128) + (k & 3) * 32) >> 4);
           const uint64_t ko = (uint64_t)(((k >> 2) * (C::BK * 128) + (k & 3) * 32) >> 4);
-          umma_bf16(d_tmem, dq + qo, dk + ko, idesc_s, k > 0 ? 1u : 0u);
+          umma_bf16_if(elected, d_tmem, dq + qo, dk + ko, idesc_s, k > 0 ? 1u : 0u);
         }
-        umma_commit(bar(B_SFULL + (j & 1)));
-        umma_commit(bar(B_KEMPTY + st));
+        umma_commit_if(elected, bar(B_SFULL + (j & 1)));
+        umma_commit_if(elected, bar(B_KEMPTY + st));
         return true;
       };
-      bool ok = mbar_wait(bar(B_QFULL), 0, abort_flag, err, kWaitLimitCycles, 0x64);
-      if (ok) ok = issue_s(0);
+      bool ok = wait_all(B_QFULL, 0, 0x64) && issue_s(0);
       for (int j = 0; j < nb && ok; ++j) {
         if (j + 1 < nb && !issue_s(j + 1)) { ok = false; break; }
         const int st = j % C::NV;
-        if (!mbar_wait(bar(B_VFULL + st), (uint32_t)(j / C::NV) & 1u, abort_flag, err, kWaitLimitCycles, 0x65)) { ok = false; break; }
-        if (!mbar_wait(bar(B_PFULL + (j & 1)), ((uint32_t)j >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x66)) { ok = false; break; }
+        ok = wait_all(B_VFULL + st, (uint32_t)(j / C::NV) & 1u, 0x65) && wait_all(B_PFULL + (j & 1), ((uint32_t)j >> 1) & 1u, 0x66);
+        if (!ok) break;
         tc_fence_after();
         const uint64_t dv = umma_desc_sw128(sbase + C::OFF_V + st * C::KV_BYTES, C::BK * 128, 1024);
         const uint32_t tp = tmem_base + (uint32_t)((j & 1) * C::BK);  // bf16 P: 16 keys = 8 columns per K step
 #pragma unroll
         for (int k = 0; k < C::BK / 16; ++k)
-          umma_bf16_ts(tmem_base + C::O_COL, tp + (uint32_t)(k * 8), dv + (uint64_t)((k * 2048) >> 4), idesc_pv,
+          umma_bf16_ts_if(elected, tmem_base + C::O_COL, tp + (uint32_t)(k * 8), dv + (uint64_t)((k * 2048) >> 4), idesc_pv,
                        (j > 0 || k > 0) ? 1u : 0u);
-        umma_commit(bar(B_VEMPTY + st));
-        umma_commit(bar(B_ODONE));
+        umma_commit_if(elected, bar(B_VEMPTY + st));
+        umma_commit_if(elected, bar(B_ODONE));
       }
-      if (ok) umma_commit(bar(B_OFINAL));
+      if (ok) umma_commit_if(elected, bar(B_OFINAL));
     }
   } else {
     // softmax warps (2..5): one query row per thread = TMEM lane
@@ -200,67 +221,72 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     const int row = q0 + q * 32 + lane;
     const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
     const int wmin = q0 + q * 32, wmax = wmin + 31;  // rows of this warp
-    float mref = -INFINITY, lsum = 0.f;
+    // The row reference is an integer in the log2 domain: any such reference gives the same softmax, and bf16 rounding commutes
+    // with powers of two.  So it need not be the maximum, only near it: the exponentials of a block are taken against the
+    // reference that the blocks before left, in one pass, and taken again against a new one only if their maximum turns out
+    // more than 2^kRefSlack above it (or, for a row that has seen nothing, far below it).
+    float mref = 0.f, lsum = 0.f;
     bool ok = true;
-    for (int j = 0; j < nb; ++j) {
+    for (int j = 0; j < nb && ok; ++j) {
       ok = mbar_wait(bar(B_SFULL + (j & 1)), ((uint32_t)j >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x67);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      uint32_t r0[32], r1[32];
-      tmem_ld32(tlane + (uint32_t)((j & 1) * C::BK), r0);
-      tmem_ld32(tlane + (uint32_t)((j & 1) * C::BK + 32), r1);
-      tmem_ld_wait();
-
-      const int k0 = runs.block(j) * C::BK;
-      // every row of the warp sees every key of the block: nothing to test (warp-uniform)
-      const bool full = k0 + C::BK - 1 <= wmin && (wmax - k0 < window || k0 + C::BK <= sinks);
-      if (!full) {
-        const int hi = row - k0, lo = row - window + 1 - k0, sk = sinks - k0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          if (i > hi || (i < lo && i >= sk)) r0[i] = 0xff800000u;  // -inf
-          if (i + 32 > hi || (i + 32 < lo && i + 32 >= sk)) r1[i] = 0xff800000u;
-        }
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) mx = fmaxf(mx, fmaxf(__uint_as_float(r0[i]), __uint_as_float(r1[i])));
-      // the reference is an integer that moves once the maximum has passed it by more than 2^kRefSlack; it stays -inf
-      // (and 0 stands in for it below: the exponentials of -inf are 0) until the row has seen its first key
-      const float mcand = ceilf(mx * scale_log2);
-      const float mnew = mcand > mref + kRefSlack ? mcand : mref;
-      const float alpha = mnew == mref ? 1.0f : fast_exp2(mref - mnew);
-      const float ref = mnew == -INFINITY ? 0.f : mnew;
-      float psum = 0.f;
+      const uint32_t t_s = tlane + (uint32_t)((j & 1) * C::BK);
+      const int first = runs.block(j) * C::BK, last = first + C::BK - 1;
+      // 64 keys of which no row of the warp sees any are not read, and only those on an edge of the mask are tested one by one
+      // (both warp-uniform)
+      const bool none = first > wmax || (last < wmin - window + 1 && first >= sinks);
+      const bool all = last <= wmin && (first > wmax - window || last < sinks);
       uint32_t pw[32];  // bf16 pairs: keys 2c, 2c+1 in word c
+      float2 psum = both(0.f);
+      if (none) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        const float a0 = fast_exp2(fmaf(__uint_as_float(r0[i]), scale_log2, -ref));
-        const float a1 = fast_exp2(fmaf(__uint_as_float(r0[i + 1]), scale_log2, -ref));
-        const float c0 = fast_exp2(fmaf(__uint_as_float(r1[i]), scale_log2, -ref));
-        const float c1 = fast_exp2(fmaf(__uint_as_float(r1[i + 1]), scale_log2, -ref));
-        psum += (a0 + a1) + (c0 + c1);
-        pw[i >> 1] = pack_bf16(a0, a1);
-        pw[16 + (i >> 1)] = pack_bf16(c0, c1);
-      }
-      lsum = lsum * alpha + psum;
-      mref = mnew;
-
-      if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
-        ok = mbar_wait(bar(B_ODONE), (uint32_t)(j - 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x68);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tc_fence_after();
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t t[32];
-          tmem_ld32(tlane + (uint32_t)(C::O_COL + c), t);
+        for (int e = 0; e < 32; ++e) pw[e] = 0u;
+      } else {
+        for (;;) {
+          uint32_t r0[32], r1[32];
+          tmem_ld32(t_s, r0);
+          tmem_ld32(t_s + 32, r1);
           tmem_ld_wait();
+          if (!all) {
+            const int hi = row - first;
+            const uint32_t seen0 = visible(hi, hi - window + 1, sinks - first);
+            const uint32_t seen1 = visible(hi - 32, hi - 32 - window + 1, sinks - first - 32);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) t[i] = __float_as_uint(__uint_as_float(t[i]) * alpha);
-          tmem_st32(tlane + (uint32_t)(C::O_COL + c), t);
+            for (int e = 0; e < 32; ++e) {
+              r0[e] = seen0 & (1u << e) ? r0[e] : 0xff800000u;  // -inf
+              r1[e] = seen1 & (1u << e) ? r1[e] : 0xff800000u;
+            }
+          }
+          float mx = -INFINITY;
+          psum = both(0.f);
+          softmax_chunk(r0, scale_log2, mref, pw, psum, mx);
+          softmax_chunk(r1, scale_log2, mref, pw + 16, psum, mx);
+          const float mcand = ceilf(mx * scale_log2);  // scale_log2 > 0: the maximum commutes with it
+          const bool move = mcand > mref + kRefSlack || (lsum == 0.f && mx > -INFINITY && mcand < mref - 2.f * kRefSlack);
+          if (!__any_sync(0xffffffffu, move)) break;
+          const float alpha = move && lsum > 0.f ? fast_exp2(mref - mcand) : 1.0f;  // an exact power of two
+          if (move) mref = mcand;
+          lsum *= alpha;
+          if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {  // rescale O, behind the previous P V product
+            ok = mbar_wait(bar(B_ODONE), (uint32_t)(j - 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x68);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t t[32];
+              tmem_ld32(tlane + (uint32_t)(C::O_COL + c), t);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) t[i] = __float_as_uint(__uint_as_float(t[i]) * alpha);
+              tmem_st32(tlane + (uint32_t)(C::O_COL + c), t);
+            }
+          }
         }
+        if (!ok) break;
+        lsum += psum.x + psum.y;
       }
       tmem_st32(tlane + (uint32_t)((j & 1) * C::BK), pw);
       tmem_st_wait();
@@ -1157,53 +1183,67 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
 }
 
 
-// Adds the partial sums of a key block's parts in part order, scales and rotates dK, rounds once.  One thread per key; block
-// (cut key block, 8 columns of dK with their partners D / 2 further, or 8 of dV).
+// Adds the partial sums of a key block's parts in part order, scales and rotates dK, rounds once.  A CTA takes 32 columns
+// (16 of dK and their partners D / 2 further, or 32 of dV): a warp reads four of them, 512 bytes each a part, every part's loads
+// in flight at once; the sums pass through shared memory to threads that hold half a row of them each.
 template <int D>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(256)
 attn_window_join_kernel(const float* __restrict__ partial, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
                         const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale) {
   pdl_trigger();
   pdl_wait();
+  constexpr int H = D / 2, K_CTAS = H / 16;
+  __shared__ float s_sum[32][132];  // [column][key]
   const int groups = pl.all_groups, S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv;
   const int x = (int)blockIdx.x / groups, grp = (int)blockIdx.x % groups;
   const int np = pl.parts_of(x);
   if (np == 1) return;
-  const int row = x * 128 + threadIdx.x;
-  const int kvh = grp % n_kv, b = grp / n_kv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool is_k = (int)blockIdx.y < K_CTAS;
+  const int c0 = is_k ? (int)blockIdx.y * 16 : ((int)blockIdx.y - K_CTAS) * 32;
   const long long part_stride = (long long)groups * (2 * D * 128);
-  const float* src = partial + ((long long)pl.rank_of(x) * groups + grp) * (2 * D * 128) + threadIdx.x;
-  constexpr int H = D / 2;
-  const bool is_k = (int)blockIdx.y < H / 8;
-  const int c0 = is_k ? (int)blockIdx.y * 8 : ((int)blockIdx.y - H / 8) * 8;
-  float lo[8], hi[8];
+  const float* src = partial + ((long long)pl.rank_of(x) * groups + grp) * (2 * D * 128) + lane * 4;
+  float4 acc[4];
+  int off[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) lo[i] = hi[i] = 0.f;
+  for (int i = 0; i < 4; ++i) {
+    const int l = warp * 4 + i;  // of this CTA's 32 columns
+    off[i] = (is_k ? (l < 16 ? c0 + l : H + c0 + l - 16) : D + c0 + l) * 128;
+    acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
 #pragma unroll 4
   for (int p = 0; p < np; ++p) {
-    const float* s = src + p * part_stride;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      lo[i] += s[(is_k ? c0 + i : D + c0 + i) * 128];
-      if (is_k) hi[i] += s[(H + c0 + i) * 128];
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(src + p * part_stride + off[i]);
+      acc[i].x += v.x; acc[i].y += v.y; acc[i].z += v.z; acc[i].w += v.w;
     }
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&s_sum[warp * 4 + i][lane * 4]) = acc[i];
+  __syncthreads();
+  const int r = threadIdx.x & 127, part = threadIdx.x >> 7, row = x * 128 + r;
   if (row >= S) return;
+  const int kvh = grp % n_kv, b = grp / n_kv;
   bf16* dst = dqkv + ((long long)b * S + row) * (long long)((n_heads + 2 * n_kv) * D) + (n_heads + (is_k ? 0 : n_kv) + kvh) * D + c0;
   if (is_k) {
+    float lo[8], hi[8];
+    const int i0 = part * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float y1 = lo[i] * scale, y2 = hi[i] * scale;
-      const float cc = rope_cos != nullptr ? rope_cos[(long long)row * H + c0 + i] : 1.f;
-      const float ss = rope_cos != nullptr ? rope_sin[(long long)row * H + c0 + i] : 0.f;
-      lo[i] = y1 * cc + y2 * ss;
-      hi[i] = y2 * cc - y1 * ss;
+      lo[i] = s_sum[i0 + i][r] * scale;
+      hi[i] = s_sum[16 + i0 + i][r] * scale;
     }
-    store_bf16_row<8>(dst + H, hi);
+    if (rope_cos != nullptr) unrotate<8>(lo, hi, rope_cos + (long long)row * H + c0 + i0, rope_sin + (long long)row * H + c0 + i0);
+    store_bf16_row<8>(dst + i0, lo);
+    store_bf16_row<8>(dst + H + i0, hi);
+  } else {
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = s_sum[part * 16 + i][r];
+    store_bf16_row<16>(dst + part * 16, v);
   }
-  store_bf16_row<8>(dst, lo);
 }
-
 
 // Parts: where the launch has several times more streamed blocks than SMs, a part is as long as a window block's whole list
 // (or an eighth of an SM's share, if that is longer), so that only sink blocks are cut.  Smaller launches are cut into one
@@ -1308,7 +1348,7 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   }
   const int cut = pl.parts > 1 ? pl.nxb : pl.parts_sink > 1 ? pl.n_sink : 0;
   if (cut == 0) return cudaSuccess;
-  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)cut * pl.all_groups, 3 * D / 16), dim3(128), 0, st, partial, dqkv, cs, sn,
+  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)cut * pl.all_groups, D / 16), dim3(256), 0, st, partial, dqkv, cs, sn,
                     pl, scale);
 }
 

@@ -156,6 +156,8 @@ def test_masked_scores_may_overflow():
 
 
 def test_a_window_over_the_whole_sequence_is_causal_attention():
+    """The same definition in another block size: exponentials and sums differ by 2^-22, so under one rounding in a hundred (of P
+    or of o, 2^-8 each) falls the other way, and the 2-norm by at most sqrt(0.01) 2^-7 = 8e-4."""
     from paper_2609_13645_b200 import binding as Bn
     B, S, nh, nkv, d = 2, 700, 4, 2, 128
     qkv, do = _inputs(B, S, nh, nkv, d, seed=11)
@@ -163,7 +165,9 @@ def test_a_window_over_the_whole_sequence_is_causal_attention():
     Bn.k_attention_fwd(qkv, want_o, want_lse, B, S, nh, nkv, d)
     for window, sinks in ((S, 0), (2 ** 31 - 1, 5), (10 * S, 2 ** 31 - 1)):
         o, lse = _fwd(qkv, B, S, nh, nkv, d, window, sinks)
-        assert torch.equal(o, want_o) and torch.equal(lse, want_lse)
+        assert float((o != want_o).double().mean()) < 0.01
+        assert _rel(o, want_o.double()) < 1e-3
+        assert float((lse - want_lse).abs().max()) < 1e-5
         got = _bwd(qkv, o, do, lse, B, S, nh, nkv, d, window, sinks)
         delta, want = torch.empty(B, nh, S, device="cuda"), torch.empty_like(qkv)
         Bn.k_attention_bwd(qkv, o, do, lse, delta, want, B, S, nh, nkv, d)
