@@ -225,7 +225,10 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     // with powers of two.  So it need not be the maximum, only near it: the exponentials of a block are taken against the
     // reference that the blocks before left, in one pass, and taken again against a new one only if their maximum turns out
     // more than 2^kRefSlack above it (or, for a row that has seen nothing, far below it).
-    float mref = 0.f, lsum = 0.f;
+    // lsum is the sum of the exponentials; o is divided by nsum, in which blocks on an edge of the mask count with their
+    // rounded P: the weights of a row that sees few keys then add up to 1, and a row that sees one key returns its value.
+    // (Over many keys the roundings average out, and the unrounded sum serves.)
+    float mref = 0.f, lsum = 0.f, nsum = 0.f;
     bool ok = true;
     for (int j = 0; j < nb && ok; ++j) {
       ok = mbar_wait(bar(B_SFULL + (j & 1)), ((uint32_t)j >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x67);
@@ -269,6 +272,7 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
           const float alpha = move && lsum > 0.f ? fast_exp2(mref - mcand) : 1.0f;  // an exact power of two
           if (move) mref = mcand;
           lsum *= alpha;
+          nsum *= alpha;
           if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {  // rescale O, behind the previous P V product
             ok = mbar_wait(bar(B_ODONE), (uint32_t)(j - 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x68);
             ok = __all_sync(0xffffffffu, ok);
@@ -287,6 +291,12 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
         }
         if (!ok) break;
         lsum += psum.x + psum.y;
+        if (!all) {
+          psum = both(0.f);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) psum = add2(psum, make_float2(bf16_lo(pw[e]), bf16_hi(pw[e])));
+        }
+        nsum += psum.x + psum.y;
       }
       tmem_st32(tlane + (uint32_t)((j & 1) * C::BK), pw);
       tmem_st_wait();
@@ -301,7 +311,7 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     if (ok) {
       tc_fence_after();
       const uint32_t out = sbase + (uint32_t)(q * 32 * D * 2);  // Q has been read
-      stage_rows<D>(out, lane, tlane + (uint32_t)C::O_COL, 1.0f / lsum);
+      stage_rows<D>(out, lane, tlane + (uint32_t)C::O_COL, 1.0f / nsum);
       send_rows<D>(&tmO, out, lane, n * D, q0 + q * 32, b, S);
       if (row < S) lse[((long long)b * n_heads + n) * S + row] = (mref + log2f(lsum)) * kLn2;
       if (lane == 0) bulk_wait_group0();
@@ -343,34 +353,38 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
 
 // ============================================================================ backward
 // dK, dV: one CTA per (128 keys, kv head, batch row) or part of its queries; K and V stay in shared memory, 128-query blocks
-// of Q and dO of every query head of the group are streamed.  Per block (all products 128 x 128 x D on the tensor cores)
+// of Q and dO of every query head of the group are streamed.  Per block (D = 128; all products 128 x 128 x D on the tensor cores)
 //   S^T = K Q^T, dP^T = V dO^T        accumulators in TMEM
 //   P^T = exp2(S^T c - LSE), dS^T = P^T (dP^T - delta)    compute warps, bf16 back over the columns they came from
 //   dV += P^T dO, dK += dS^T Q        A operand from TMEM, the streamed tiles again as mn-major B operands
 // TMEM is full (four 128-column accumulators at D = 128), so S and dP have one buffer each; what keeps the tensor pipe busy is
 // that two chains alternate: dV_j and S_{j+1} run while the compute warps turn dP_j into dS_j, dK_j and dP_{j+1} while they
 // turn S_{j+1} into P_{j+1}.  Blocks of 128 queries and not 64: an MMA of N = 64 takes as long as one
-// of N = 128, because it is bound by the reads of its operands from shared memory.
+// of N = 128, because it is bound by the reads of its operands from shared memory.  (D = 64: blocks of 64 queries, half of
+// everything, and two CTAs an SM: there the products are small against what a CTA's start and end cost, and the other CTA
+// fills both.)
 // dS^T also goes to a scratch array, from which dQ = dS K is one banded contraction (below): five products per pair of
 // blocks in all instead of the seven of a backward pass that computes S and dP twice.
 enum { K_XFULL = 0, K_QFULL = 1, K_QEMPTY = 4, K_OFULL = 7, K_OEMPTY = 10, K_STFULL = 13, K_STEMPTY = 15, K_SFULL = 17, K_DPFULL = 18,
        K_PFULL = 19, K_DSFULL = 20, K_ACCDONE = 21, K_COUNT = 22 };
 constexpr int DKV_THREADS = 320;  // producer, MMA issuer, 8 compute warps
 
-template <int D>
+template <int D, int BLOCK>
 struct DkvCfg {
   static constexpr int KC = D / 64;
-  static constexpr int TILE = 128 * D * 2;  // bytes of a 128-row tile
-  static constexpr int NQ = D == 64 ? 3 : 2, NO = D == 64 ? 3 : 2;
-  static constexpr int OFF_K = 0, OFF_V = TILE, OFF_Q = 2 * TILE, OFF_O = OFF_Q + NQ * TILE;
-  static constexpr int OFF_DS = OFF_O + NO * TILE;  // 4 KB a compute warp: its share of dS^T on the way to memory
-  static constexpr int OFF_STAT = OFF_DS + 8 * 4096;  // [2][lse * log2e, delta][128]
-  static constexpr int OFF_BAR = OFF_STAT + 2048;
+  static constexpr int BQ = BLOCK, SUB = 128 / BQ, W = BQ / 2;  // queries a block; blocks in 128 queries; queries a thread
+  static constexpr int TILE = 128 * D * 2, Y_TILE = BQ * D * 2;  // bytes of a resident, of a streamed tile
+  static constexpr int NQ = D == 64 ? 3 : 2, NO = BQ == 128 && D == 64 ? 3 : 2;
+  static constexpr int OFF_K = 0, OFF_V = TILE, OFF_Q = 2 * TILE, OFF_O = OFF_Q + NQ * Y_TILE;
+  static constexpr int OFF_DS = OFF_O + NO * Y_TILE;  // 4 KB a compute warp: its share of dS^T on the way to memory
+  static constexpr int OFF_STAT = OFF_DS + 8 * 4096;  // [2][lse * log2e, delta][BQ]
+  static constexpr int OFF_BAR = OFF_STAT + 16 * BQ;
   static constexpr int SMEM_BYTES = OFF_BAR + 256;
-  static constexpr int TMEM_COLS = 512;
-  static constexpr int COL_S = 0, COL_DP = 128, COL_DV = 256, COL_DK = 256 + D;
+  static constexpr int CTAS = BQ == 64 ? 2 : 1;  // an SM
+  static constexpr int TMEM_COLS = BQ == 64 ? 256 : 512;
+  static constexpr int COL_S = 0, COL_DP = BQ, COL_DV = 2 * BQ, COL_DK = 2 * BQ + D;
 };
-static_assert(DkvCfg<128>::SMEM_BYTES <= 232448, "shared memory of one SM");
+static_assert(DkvCfg<128, 128>::SMEM_BYTES <= 232448 && DkvCfg<64, 64>::SMEM_BYTES <= 115712, "shared memory of one SM, of half of one");
 
 // The backward pass as the host plans it and the kernels read it.  A key block's streamed list (128-query blocks of every
 // query head of the group) is cut into parts; dS^T is kept for a number of (batch row, kv head) groups at a time.
@@ -398,14 +412,27 @@ struct Plan {
   __host__ __device__ int ranks() const { return n_sink * parts_sink + (nxb - n_sink) * parts; }
 };
 
-template <int D>
-__global__ void __launch_bounds__(DKV_THREADS, 1)
-attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_do,
+// A thread's row of 32 or 64 scores out of TMEM, and their bf16 pairs back into it.
+template <int W>
+__device__ __forceinline__ void load_scores(uint32_t t, float (&v)[W]) {
+  uint32_t r[W / 32][32];
+#pragma unroll
+  for (int c = 0; c < W / 32; ++c) tmem_ld32(t + 32 * c, r[c]);
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = __uint_as_float(r[i / 32][i % 32]);
+}
+__device__ __forceinline__ void store_pairs(uint32_t t, const uint32_t (&w)[32]) { tmem_st32(t, w); }
+__device__ __forceinline__ void store_pairs(uint32_t t, const uint32_t (&w)[16]) { tmem_st16(t, w); }
+
+template <int D, int BLOCK>
+__global__ void __launch_bounds__(DKV_THREADS, DkvCfg<D, BLOCK>::CTAS)
+attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
                        const __grid_constant__ CUtensorMap tm_out, const float* __restrict__ lse, const float* __restrict__ delta,
                        float* __restrict__ partial, bf16* __restrict__ ds_band, bf16* __restrict__ ds_sink,
                        const float* __restrict__ rope_cos, const float* __restrict__ rope_sin, const __grid_constant__ Plan pl,
                        float scale, float scale_log2, int* err) {
-  using C = DkvCfg<D>;
+  using C = DkvCfg<D, BLOCK>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
@@ -431,24 +458,27 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   const int x0 = x * 128;
   const int per_head = pl.blocks_seen(x), total = per_head * n_rep, np = pl.parts_of(x);
   if (part >= np) return;
-  const int first_it = (int)((long long)total * part / np);
-  const int iters = (int)((long long)total * (part + 1) / np) - first_it;
+  const int first128 = (int)((long long)total * part / np);
+  const int iters = ((int)((long long)total * (part + 1) / np) - first128) * C::SUB;
 
-  auto head_of = [&](int it) { return kvh * n_rep + (first_it + it) / per_head; };
-  auto query_of = [&](int it) { return (x + (first_it + it) % per_head) * 128; };
+  // block `it` of this CTA: query head of the group, 128-query block counted from x, first query
+  auto rep_of = [&](int it) { return (first128 + it / C::SUB) / per_head; };
+  auto rel_of = [&](int it) { return (first128 + it / C::SUB) % per_head; };
+  auto head_of = [&](int it) { return kvh * n_rep + rep_of(it); };
+  auto query_of = [&](int it) { return (x + rel_of(it)) * 128 + it % C::SUB * C::BQ; };
   auto load_q = [&](int it) {
     const int st = it % C::NQ;
-    mbar_expect_tx(bar(K_QFULL + st), C::TILE);
+    mbar_expect_tx(bar(K_QFULL + st), C::Y_TILE);
 #pragma unroll
     for (int kc = 0; kc < C::KC; ++kc)
-      tma_load_3d(sbase + C::OFF_Q + st * C::TILE + kc * 16384, &tm_qkv, bar(K_QFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
+      tma_load_3d(sbase + C::OFF_Q + st * C::Y_TILE + kc * (C::BQ * 128), &tm_q, bar(K_QFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
   };
   auto load_do = [&](int it) {
     const int st = it % C::NO;
-    mbar_expect_tx(bar(K_OFULL + st), C::TILE);
+    mbar_expect_tx(bar(K_OFULL + st), C::Y_TILE);
 #pragma unroll
     for (int kc = 0; kc < C::KC; ++kc)
-      tma_load_3d(sbase + C::OFF_O + st * C::TILE + kc * 16384, &tm_do, bar(K_OFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
+      tma_load_3d(sbase + C::OFF_O + st * C::Y_TILE + kc * (C::BQ * 128), &tm_do, bar(K_OFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
   };
   if (threadIdx.x == 0) {
     mbar_init(bar(K_XFULL), 1);
@@ -511,10 +541,10 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       if (!__all_sync(0xffffffffu, ok)) break;
       const long long stat = ((long long)b * n_heads + n) * S;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < C::BQ / 32; ++e) {
         const int qq = q0 + lane + 32 * e;
-        s_stat[ss * 256 + lane + 32 * e] = qq < S ? lse[stat + qq] * kLog2e : 0.f;
-        s_stat[ss * 256 + 128 + lane + 32 * e] = qq < S ? delta[stat + qq] : 0.f;
+        s_stat[ss * 2 * C::BQ + lane + 32 * e] = qq < S ? lse[stat + qq] * kLog2e : 0.f;
+        s_stat[ss * 2 * C::BQ + C::BQ + lane + 32 * e] = qq < S ? delta[stat + qq] : 0.f;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(K_STFULL + ss));
@@ -526,7 +556,7 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     // the last of them and the compute warps wait for all four; 3800 cycles a block.)
     const uint32_t elected = elect_one();
     const uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
-    const uint32_t idesc_s = idesc_base | ((uint32_t)(128 >> 3) << 17);               // N = 128, both K-major
+    const uint32_t idesc_s = idesc_base | ((uint32_t)(C::BQ >> 3) << 17);             // N = BQ, both K-major
     const uint32_t idesc_acc = idesc_base | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // N = D, B mn-major
     auto wait_all = [&](int i, uint32_t parity, int site) {
       const bool ok = mbar_wait(bar(i), parity, abort_flag, err, kWaitLimitCycles, site);
@@ -537,17 +567,19 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       const uint64_t dx = umma_desc_sw128(sbase + x_off, 0, 1024), dy = umma_desc_sw128(sbase + y_off, 0, 1024);
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
-        const uint64_t o = (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
-        umma_bf16_if(elected, tmem_base + col, dx + o, dy + o, idesc_s, k > 0 ? 1u : 0u);
+        const uint64_t ox = (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
+        const uint64_t oy = (uint64_t)(((k >> 2) * (C::BQ * 128) + (k & 3) * 32) >> 4);
+        umma_bf16_if(elected, tmem_base + col, dx + ox, dy + oy, idesc_s, k > 0 ? 1u : 0u);
       }
     };
-    // the bf16 tile at score column `col` (TMEM) times the streamed tile y; each half of the 128 queries sits at the start
-    // of its 64 fp32 columns, 16 queries = 8 columns
+    // the bf16 tile at score column `col` (TMEM) times the streamed tile y; each half of the queries sits at the start of its
+    // fp32 columns, 16 queries = 8 columns
     auto accumulate = [&](uint32_t col, uint32_t y_off, uint32_t acc_col, bool first) {
-      const uint64_t by = umma_desc_sw128(sbase + y_off, 16384, 1024);
+      const uint64_t by = umma_desc_sw128(sbase + y_off, C::BQ * 128, 1024);
+      constexpr int HALF = C::W / 16;  // steps of 16 queries in a half
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        umma_bf16_ts_if(elected, tmem_base + acc_col, tmem_base + col + (uint32_t)((k >> 2) * 64 + (k & 3) * 8),
+      for (int k = 0; k < 2 * HALF; ++k)
+        umma_bf16_ts_if(elected, tmem_base + acc_col, tmem_base + col + (uint32_t)(k / HALF * C::W + k % HALF * 8),
                         by + (uint64_t)((k * 2048) >> 4), idesc_acc, (first && k == 0) ? 0u : 1u);
     };
     bool ok = wait_all(K_XFULL, 0, 0x74) && wait_all(K_QFULL, 0, 0x75) && wait_all(K_OFULL, 0, 0x76);
@@ -563,62 +595,52 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       const bool more = it + 1 < iters;
       if (!(ok = wait_all(K_PFULL, (uint32_t)it & 1u, 0x77))) break;
       tc_fence_after();
-      accumulate(C::COL_S, C::OFF_O + so * C::TILE, C::COL_DV, it == 0);
+      accumulate(C::COL_S, C::OFF_O + so * C::Y_TILE, C::COL_DV, it == 0);
       umma_commit_if(elected, bar(K_OEMPTY + so));  // dP_j and dV_j have read dO_j
       if (more) {
         if (!(ok = wait_all(K_QFULL + nq, (uint32_t)((it + 1) / C::NQ) & 1u, 0x78))) break;
         tc_fence_after();
-        scores(C::OFF_K, C::OFF_Q + nq * C::TILE, C::COL_S);
+        scores(C::OFF_K, C::OFF_Q + nq * C::Y_TILE, C::COL_S);
         umma_commit_if(elected, bar(K_SFULL));
       }
       if (!(ok = wait_all(K_DSFULL, (uint32_t)it & 1u, 0x79))) break;
       tc_fence_after();
-      accumulate(C::COL_DP, C::OFF_Q + sq * C::TILE, C::COL_DK, it == 0);
+      accumulate(C::COL_DP, C::OFF_Q + sq * C::Y_TILE, C::COL_DK, it == 0);
       umma_commit_if(elected, bar(K_QEMPTY + sq));  // S_j and dK_j have read Q_j
       if (more) {
         if (!(ok = wait_all(K_OFULL + no, (uint32_t)((it + 1) / C::NO) & 1u, 0x7a))) break;
         tc_fence_after();
-        scores(C::OFF_V, C::OFF_O + no * C::TILE, C::COL_DP);
+        scores(C::OFF_V, C::OFF_O + no * C::Y_TILE, C::COL_DP);
         umma_commit_if(elected, bar(K_DPFULL));
       }
     }
     if (ok) umma_commit_if(elected, bar(K_ACCDONE));
   } else {
-    // ------------------------------------------------------------------ compute warps: one key per thread, 64 queries each
+    // ------------------------------------------------------------------ compute warps: one key a thread, half of the queries each
     const int q = warp & 3, ch = (warp - 2) >> 2;
     const int rloc = q * 32 + lane, row = x0 + rloc;
     const int rmin = x0 + q * 32, rmax = rmin + 31;
     const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
-    const uint32_t t_s = tlane + (uint32_t)(C::COL_S + ch * 64), t_dp = tlane + (uint32_t)(C::COL_DP + ch * 64);
+    const uint32_t t_s = tlane + (uint32_t)(C::COL_S + ch * C::W), t_dp = tlane + (uint32_t)(C::COL_DP + ch * C::W);
     const uint32_t stage = sbase + (uint32_t)(C::OFF_DS + (warp - 2) * 4096);
     // the queries that see key `row` are [row, row_end)
     const int row_end = row < pl.sinks || S - row < pl.window ? S : row + pl.window;
     bool ok = true;
     for (int it = 0; it < iters; ++it) {
       const int ss = it & 1;
-      const int rel = (first_it + it) % per_head;
-      const int cmin = (x + rel) * 128 + ch * 64;
-      const float* st_lse = s_stat + ss * 256 + ch * 64;
-      const float* st_dl = st_lse + 128;
+      const int rel = rel_of(it);
+      const int cmin = query_of(it) + ch * C::W;
+      const float* st_lse = s_stat + ss * 2 * C::BQ + ch * C::W;
+      const float* st_dl = st_lse + C::BQ;
       ok = mbar_wait(bar(K_STFULL + ss), (uint32_t)(it >> 1) & 1u, abort_flag, err, kWaitLimitCycles, 0x7b) &&
            mbar_wait(bar(K_SFULL), (uint32_t)it & 1u, abort_flag, err, kWaitLimitCycles, 0x7c);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      float p[64];
-      {
-        uint32_t r0[32], r1[32];
-        tmem_ld32(t_s, r0);
-        tmem_ld32(t_s + 32, r1);
-        tmem_ld_wait();
+      float p[C::W];
+      load_scores(t_s, p);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          p[i] = __uint_as_float(r0[i]);
-          p[32 + i] = __uint_as_float(r1[i]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 64; i += 4) {
+      for (int i = 0; i < C::W; i += 4) {
         const float4 l4 = *reinterpret_cast<const float4*>(st_lse + i);
         p[i] = fast_exp2(fmaf(p[i], scale_log2, -l4.x));
         p[i + 1] = fast_exp2(fmaf(p[i + 1], scale_log2, -l4.y));
@@ -626,17 +648,17 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
         p[i + 3] = fast_exp2(fmaf(p[i + 3], scale_log2, -l4.w));
       }
       // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
-      const bool full = cmin >= rmax && cmin + 64 <= S && (rmax < pl.sinks || cmin + 63 - rmin < pl.window);
+      const bool full = cmin >= rmax && cmin + C::W <= S && (rmax < pl.sinks || cmin + C::W - 1 - rmin < pl.window);
       if (!full) {
         const int lo = row - cmin, hi = row_end - cmin;
 #pragma unroll
-        for (int i = 0; i < 64; ++i)
+        for (int i = 0; i < C::W; ++i)
           if (i < lo || i >= hi) p[i] = 0.f;
       }
-      uint32_t w[32];
+      uint32_t w[C::W / 2];
 #pragma unroll
-      for (int c = 0; c < 32; ++c) w[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
-      tmem_st32(t_s, w);  // over this warp's own (already loaded) columns
+      for (int c = 0; c < C::W / 2; ++c) w[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
+      store_pairs(t_s, w);  // over this warp's own (already loaded) columns
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -647,24 +669,20 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       if (!ok) break;
       tc_fence_after();
       {
-        uint32_t r0[32], r1[32];
-        tmem_ld32(t_dp, r0);
-        tmem_ld32(t_dp + 32, r1);
-        tmem_ld_wait();
+        float d[C::W];
+        load_scores(t_dp, d);
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          const float4 d0 = *reinterpret_cast<const float4*>(st_dl + i), d1 = *reinterpret_cast<const float4*>(st_dl + 32 + i);
-          const float e0[4] = {d0.x, d0.y, d0.z, d0.w}, e1[4] = {d1.x, d1.y, d1.z, d1.w};
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            p[i + u] *= __uint_as_float(r0[i + u]) - e0[u];
-            p[32 + i + u] *= __uint_as_float(r1[i + u]) - e1[u];
-          }
+        for (int i = 0; i < C::W; i += 4) {
+          const float4 e4 = *reinterpret_cast<const float4*>(st_dl + i);
+          p[i] *= d[i] - e4.x;
+          p[i + 1] *= d[i + 1] - e4.y;
+          p[i + 2] *= d[i + 2] - e4.z;
+          p[i + 3] *= d[i + 3] - e4.w;
         }
       }
 #pragma unroll
-      for (int c = 0; c < 32; ++c) w[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
-      tmem_st32(t_dp, w);
+      for (int c = 0; c < C::W / 2; ++c) w[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
+      store_pairs(t_dp, w);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -677,12 +695,13 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       // rows of 64 bytes under the 64-byte swizzle.  A warp's 32 keys of a chunk are 2 KB in one piece and leave as a bulk
       // copy.  (Stored by the threads themselves they held up the next block by 1900 cycles.)
       if (ds_band != nullptr) {
-        const long long z = (long long)local * n_rep + (first_it + it) / per_head;
+        const long long z = (long long)local * n_rep + rep_of(it);
+        const int chunk = (cmin & 127) >> 5;  // of the 128 queries' four
         if (rel < pl.nb) {
           if (lane == 0) bulk_wait_group_read0();
           __syncwarp();
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {  // 16-byte piece c & 3 of chunk c >> 2
+          for (int c = 0; c < C::W / 8; ++c) {  // 16-byte piece c & 3 of chunk c >> 2
             const uint32_t at = stage + (uint32_t)((c >> 2) * 2048 + lane * 64 + (((c & 3) ^ ((lane >> 1) & 3)) * 16));
             st_shared_v4(at, make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
           }
@@ -690,18 +709,18 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
           __syncwarp();
           if (lane == 0) {
             uint8_t* dst = reinterpret_cast<uint8_t*>(ds_band) +
-                           (((z * pl.nxb + x) * pl.nb + rel) * 8 + (q >> 1) * 4 + ch * 2) * 4096 + (q & 1) * 2048;
-            bulk_store(dst, stage, 2048);
-            bulk_store(dst + 4096, stage + 2048, 2048);
+                           (((z * pl.nxb + x) * pl.nb + rel) * 8 + (q >> 1) * 4 + chunk) * 4096 + (q & 1) * 2048;
+#pragma unroll
+            for (int c = 0; c < C::W / 32; ++c) bulk_store(dst + c * 4096, stage + c * 2048, 2048);
             bulk_commit_group();
           }
         } else if (row < pl.sinks) {  // beyond the window only sink keys are seen: rows of [chunk][sink key][32 queries]
-          bf16* dst = ds_sink + ((((z * pl.nxb + x + rel) * 4 + ch * 2) * pl.sinks + row) * 32);
-          store8_b32(dst, w);
-          store8_b32(dst + 16, w + 8);
-          dst += (long long)pl.sinks * 32;
-          store8_b32(dst, w + 16);
-          store8_b32(dst + 16, w + 24);
+          bf16* dst = ds_sink + ((((z * pl.nxb + x + rel) * 4 + chunk) * pl.sinks + row) * 32);
+#pragma unroll
+          for (int c = 0; c < C::W / 32; ++c, dst += (long long)pl.sinks * 32) {
+            store8_b32(dst, w + 16 * c);
+            store8_b32(dst + 16, w + 16 * c + 8);
+          }
         }
       }
     }
@@ -1246,8 +1265,8 @@ attn_window_join_kernel(const float* __restrict__ partial, bf16* __restrict__ dq
 }
 
 // Parts: where the launch has several times more streamed blocks than SMs, a part is as long as a window block's whole list
-// (or an eighth of an SM's share, if that is longer), so that only sink blocks are cut.  Smaller launches are cut into one
-// part per SM, of at least 4 blocks: the set-up and the partial sums of a part cost about as much as 2.
+// (or an eighth of a slot's share, if that is longer), so that only sink blocks are cut.  Smaller launches are cut into one
+// part per slot (of a CTA on an SM), of at least 4 blocks: the set-up and the partial sums of a part cost about as much as 2.
 // Groups: dS^T is kept for as many (batch row, kv head) groups at a time as kDsBytes holds.
 constexpr size_t kDsBytes = (size_t)1 << 30;
 
@@ -1258,11 +1277,24 @@ struct Scratch {
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l, int d) {
+// Query blocks that a key block meets through the window, at most.
+int window_blocks(int S, int window) {
+  const int nxb = (S + 127) / 128, nb = (127 + window + 127) / 128;
+  return nb < nxb ? nb : nxb;
+}
+
+// Queries that a streamed block of the dK/dV kernel has.  Heads of 64: half blocks and two CTAs an SM, except in launches of
+// no more than six whole blocks an SM, whose CTAs run alone and want to be quick (B 8, S 1024, 12 heads: 57 against 69 us at
+// window 128, 67 against 79 at 256, 91 against 103 at 1024; B 3, S 1531, 6 heads on one: 41 against 37).
+int block_of(int B, int S, int nh, int d, int window) {
+  return d == 64 && (long long)B * nh * ((S + 127) / 128) * window_blocks(S, window) > 6 * kSms ? 64 : 128;
+}
+
+Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l, int d, int block) {
   Plan p;
   p.S = S; p.n_heads = nh; p.n_kv = nkv; p.window = window; p.sinks = sinks;
   p.nxb = (S + 127) / 128;
-  p.nb = (127 + window + 127) / 128 < p.nxb ? (127 + window + 127) / 128 : p.nxb;
+  p.nb = window_blocks(S, window);
   p.n_sink = (sinks + 127) / 128;
   p.group0 = 0;
   p.all_groups = p.groups = nkv * B;
@@ -1272,19 +1304,20 @@ Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l,
   long long total = window_len * (p.nxb - p.n_sink);
   for (int x = 0; x < p.n_sink; ++x) total += n_rep * p.blocks_seen(x);
   total *= p.all_groups;
-  const long long per_sm = (total + kSms - 1) / kSms;
+  const long long slots = kSms * (block == 64 ? 2 : 1);  // CTAs that run at a time
+  const long long per_slot = (total + slots - 1) / slots;
   const long long longest = window_len > 0 ? window_len : sink_len;
-  long long chunk = per_sm < longest ? per_sm : longest;
+  long long chunk = per_slot < longest ? per_slot : longest;
   if (chunk < 4) chunk = 4;
-  if (per_sm >= longest && chunk < (per_sm + 7) / 8) chunk = (per_sm + 7) / 8;
+  if (per_slot >= longest && chunk < (per_slot + 7) / 8) chunk = (per_slot + 7) / 8;
   p.chunk = (int)(chunk < INT_MAX ? chunk : INT_MAX);
   p.parts = window_len > chunk ? (int)((window_len + chunk - 1) / chunk) : 1;
   p.parts_sink = sink_len > chunk ? (int)((sink_len + chunk - 1) / chunk) : 1;
 
-  const size_t slots = p.parts > 1 ? (size_t)p.ranks() : p.parts_sink > 1 ? (size_t)p.n_sink * p.parts_sink : 0;
+  const size_t part_slots = p.parts > 1 ? (size_t)p.ranks() : p.parts_sink > 1 ? (size_t)p.n_sink * p.parts_sink : 0;
   l->delta = 0;
   l->partial = round256((size_t)B * nh * S * sizeof(float));
-  l->band = l->partial + slots * p.all_groups * (2 * d * 128) * sizeof(float);
+  l->band = l->partial + part_slots * p.all_groups * (2 * d * 128) * sizeof(float);
   const size_t band = (size_t)n_rep * p.nxb * p.nb * 32768;  // of one group
   const size_t sink = p.nxb > p.nb ? (size_t)n_rep * p.nxb * 4 * sinks * 64 : 0;
   l->stored = band + sink <= 2 * kDsBytes;
@@ -1300,13 +1333,13 @@ Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l,
   return p;
 }
 
-template <int D>
+template <int D, int BLOCK>
 cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs, const float* sn,
                   uint8_t* scratch, int B, int S, int nh, int nkv, int window, int sinks, int* err, cudaStream_t st) {
   Scratch l;
-  Plan pl = make_plan(B, S, nh, nkv, window, sinks, &l, D);
+  Plan pl = make_plan(B, S, nh, nkv, window, sinks, &l, D, BLOCK);
   static unsigned long long set_kv = 0, set_q = 0, set_r = 0;
-  cudaError_t e = ensure_dynamic_smem(attn_window_dkv_kernel<D>, DkvCfg<D>::SMEM_BYTES, set_kv);
+  cudaError_t e = ensure_dynamic_smem(attn_window_dkv_kernel<D, BLOCK>, DkvCfg<D, BLOCK>::SMEM_BYTES, set_kv);
   if (e == cudaSuccess && l.stored) e = ensure_dynamic_smem(attn_window_dq_kernel<D>, DqCfg<D>::SMEM_BYTES, set_q);
   if (e == cudaSuccess && !l.stored) e = ensure_dynamic_smem(attn_window_dq_recompute_kernel<D>, DqrCfg<D>::SMEM_BYTES, set_r);
   if (e != cudaSuccess) return e;
@@ -1316,9 +1349,10 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   bf16* sink = l.stored ? reinterpret_cast<bf16*>(scratch + l.sink) : nullptr;
   const int hq = nh * D, nqkv = (nh + 2 * nkv) * D, n_rep = nh / nkv;
   const bool has_sink = sinks > 0 && pl.nxb > pl.nb;
-  CUtensorMap tq128, tq64, td128, tsink, tout;
+  CUtensorMap tq128, tq64, td128, tsink, tout, tdo;
   if (!make_tmap_3d(&tq128, qkv, nqkv, S, B, nqkv, 128) || !make_tmap_3d(&tq64, qkv, nqkv, S, B, nqkv, 64) ||
-      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128) || !make_tmap_3d(&tout, dqkv, nqkv, S, B, nqkv, 32))
+      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128) || !make_tmap_3d(&tout, dqkv, nqkv, S, B, nqkv, 32) ||
+      !make_tmap_3d(&tdo, d_o, hq, S, B, hq, DkvCfg<D, BLOCK>::BQ))
     return cudaErrorInvalidValue;
   if (l.stored) {
     if (!has_sink) tsink = tq64;  // not read
@@ -1333,8 +1367,8 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   for (int g0 = 0; g0 < pl.all_groups && e == cudaSuccess; g0 += per_round) {
     pl.group0 = g0;
     pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
-    e = launch_pdl(attn_window_dkv_kernel<D>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D>::SMEM_BYTES, st,
-                   tq128, td128, tout, lse, delta, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
+    e = launch_pdl(attn_window_dkv_kernel<D, BLOCK>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D, BLOCK>::SMEM_BYTES, st,
+                   tq128, DkvCfg<D, BLOCK>::BQ == 128 ? tq128 : tq64, tdo, tout, lse, delta, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess || !l.stored) continue;
     const int tiles = pl.nxb * pl.groups * n_rep;
     e = launch_pdl(attn_window_dq_kernel<D>, dim3(tiles < 2 * sms ? tiles : 2 * sms), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
@@ -1381,7 +1415,7 @@ size_t attention_window_scratch_bytes(int B, int S, int nh, int nkv, int d, int 
   if (!shape_ok(B, S, nh, nkv, d, window, sinks)) return 0;
   clamp_mask(S, window, sinks);
   Scratch l;
-  make_plan(B, S, nh, nkv, window, sinks, &l, d);
+  make_plan(B, S, nh, nkv, window, sinks, &l, d, block_of(B, S, nh, d, window));
   return l.total;
 }
 
@@ -1391,8 +1425,9 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
   if (!shape_ok(B, S, nh, nkv, d, window, sinks) || !err || (cs == nullptr) != (sn == nullptr)) return cudaErrorInvalidValue;
   clamp_mask(S, window, sinks);
   uint8_t* s = reinterpret_cast<uint8_t*>(scratch);
-  if (d == 64) return bwd_t<64>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
-  return bwd_t<128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
+  if (block_of(B, S, nh, d, window) == 64) return bwd_t<64, 64>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
+  if (d == 64) return bwd_t<64, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
+  return bwd_t<128, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
 }
 
 }  // namespace fs

@@ -128,6 +128,18 @@ def test_backward_matches_the_definition(B, S, nh, nkv, d, window, sinks, rope):
     assert torch.isfinite(got.float()).all()
 
 
+def test_a_row_that_sees_one_key_returns_its_value():
+    """window 1: the only weight is 1 whatever the score, so the rounding of P must cancel."""
+    B, S, nh, nkv, d = 2, 200, 4, 2, 64
+    qkv, do = _inputs(B, S, nh, nkv, d, seed=8, qscale=3.0)
+    o, lse = _fwd(qkv, B, S, nh, nkv, d, 1, 0)
+    v = qkv.view(B * S, nh + 2 * nkv, d)[:, nh + nkv:].repeat_interleave(nh // nkv, 1).reshape(B * S, nh * d)
+    assert torch.equal(o, v)
+    got = _bwd(qkv, o, do, lse, B, S, nh, nkv, d, 1, 0)
+    ref = do.double().view(B * S, nkv, nh // nkv, d).sum(2).reshape(B * S, nkv * d)
+    assert _rel(got[:, (nh + nkv) * d:], ref) < 3e-3
+
+
 @pytest.mark.parametrize("qscale", [6.0, 40.0])
 def test_large_scores_and_references_that_jump_between_blocks(qscale):
     """Rows whose maximum moves by hundreds between blocks, and whose oldest block shows them nothing at all."""
@@ -156,8 +168,8 @@ def test_masked_scores_may_overflow():
 
 
 def test_a_window_over_the_whole_sequence_is_causal_attention():
-    """The same definition in another block size: exponentials and sums differ by 2^-22, so under one rounding in a hundred (of P
-    or of o, 2^-8 each) falls the other way, and the 2-norm by at most sqrt(0.01) 2^-7 = 8e-4."""
+    """The same definition; the two kernels differ in whether P enters the normalising sum rounded (2.4e-3 from the definition
+    each, as above, and the same way for most elements)."""
     from paper_2609_13645_b200 import binding as Bn
     B, S, nh, nkv, d = 2, 700, 4, 2, 128
     qkv, do = _inputs(B, S, nh, nkv, d, seed=11)
@@ -165,8 +177,7 @@ def test_a_window_over_the_whole_sequence_is_causal_attention():
     Bn.k_attention_fwd(qkv, want_o, want_lse, B, S, nh, nkv, d)
     for window, sinks in ((S, 0), (2 ** 31 - 1, 5), (10 * S, 2 ** 31 - 1)):
         o, lse = _fwd(qkv, B, S, nh, nkv, d, window, sinks)
-        assert float((o != want_o).double().mean()) < 0.01
-        assert _rel(o, want_o.double()) < 1e-3
+        assert _rel(o, want_o.double()) < 3e-3
         assert float((lse - want_lse).abs().max()) < 1e-5
         got = _bwd(qkv, o, do, lse, B, S, nh, nkv, d, window, sinks)
         delta, want = torch.empty(B, nh, S, device="cuda"), torch.empty_like(qkv)
