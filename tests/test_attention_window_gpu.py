@@ -266,3 +266,65 @@ def test_captured_and_replayed_on_another_stream():
     L = Bn.lib()
     L.ft_k_status.argtypes = [c_void_p]
     assert L.ft_k_status(c_void_p(torch.cuda.current_stream().cuda_stream)) == Bn.FT_OK
+
+
+def _check_backward_by_heads(B, S, nh, nkv, d, window, sinks, seed, heads_at_once, rope=True):
+    """The backward pass against the definition, a few query heads at a time (the 64-bit score matrices of all do not fit)."""
+    qkv, do = _inputs(B, S, nh, nkv, d, seed=seed)
+    o, lse = _fwd(qkv, B, S, nh, nkv, d, window, sinks)
+    cos, sin = _rope(S, d) if rope else (None, None)
+    got = _bwd(qkv, o, do, lse, B, S, nh, nkv, d, window, sinks, cos, sin)
+    t = qkv.view(B, S, nh + 2 * nkv, d)
+    n_rep, w = nh // nkv, min(heads_at_once, nh // nkv)
+    ref = torch.zeros(B, S, nh + 2 * nkv, d, dtype=torch.float64, device="cuda")
+    for b in range(B):
+        for h0 in range(0, nh, w):
+            kv = h0 // n_rep
+            sub = torch.cat([t[b, :, h0:h0 + w], t[b, :, nh + kv:nh + kv + 1], t[b, :, nh + nkv + kv:nh + nkv + kv + 1]], 1)
+            cut = lambda x: x.view(B, S, nh, d)[b, :, h0:h0 + w].reshape(S, w * d)  # noqa: E731
+            r = _reference_bwd(sub.reshape(S, -1), cut(o), cut(do), 1, S, w, 1, d, window, sinks, cos, sin).view(S, w + 2, d)
+            ref[b, :, h0:h0 + w] = r[:, :w]
+            ref[b, :, nh + kv] += r[:, w]  # rotating back is linear: the sum of the heads' parts
+            ref[b, :, nh + nkv + kv] += r[:, w + 1]
+    got = got.view(B, S, nh + 2 * nkv, d)
+    for part in (slice(0, nh), slice(nh, nh + nkv), slice(nh + nkv, nh + 2 * nkv)):
+        if window == 1 and sinks == 0 and part.start < nh + nkv:
+            continue  # d_q and d_k are 0 up to the rounding of delta
+        assert _rel(got[:, :, part], ref[:, :, part]) < 3e-3
+
+
+# heads of 64 in launches of many blocks, where the streamed blocks are half as long: odd lengths, sinks over several blocks,
+# blocks split between CTAs, one block, a window of one key, the whole sequence
+@pytest.mark.parametrize("B,S,nh,nkv,window,sinks", [
+    (2, 1531, 20, 4, 300, 0), (1, 1500, 32, 1, 190, 133), (4, 449, 64, 64, 1, 0), (2, 700, 40, 8, 700, 0), (40, 70, 24, 24, 20, 2),
+    (2, 1300, 36, 36, 129, 65), (1, 2049, 64, 2, 64, 300)])
+def test_backward_of_many_heads_of_64(B, S, nh, nkv, window, sinks):
+    _check_backward_by_heads(B, S, nh, nkv, 64, window, sinks, seed=S, heads_at_once=64)
+
+
+# dS^T of one kv head's queries is over a third of what is kept at a time (two rounds, of two heads and one), and over all of
+# it (the queries' gradients recompute the scores), with and without sink blocks outside the window
+@pytest.mark.parametrize("S,nh,nkv,d,window,sinks", [
+    (4200, 36, 3, 64, 4150, 3), (4200, 36, 3, 128, 4150, 0), (8400, 64, 1, 64, 2000, 130), (8400, 64, 1, 128, 2000, 1)])
+def test_backward_of_scores_beyond_the_scratch(S, nh, nkv, d, window, sinks):
+    _check_backward_by_heads(1, S, nh, nkv, d, window, sinks, seed=7, heads_at_once=4)
+
+
+def test_two_calls_at_once_with_scratch_of_their_own():
+    shapes = [(1, 1531, 6, 1, 64, 333, 7), (2, 700, 4, 2, 128, 190, 3)]
+    ins = [_inputs(*s[:5], seed=i) for i, s in enumerate(shapes)]
+    alone = []
+    for (qkv, do), s in zip(ins, shapes):
+        o, lse = _fwd(qkv, *s)
+        alone.append((o, _bwd(qkv, o, do, lse, *s)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in shapes]
+    for _ in range(5):
+        got = []
+        for st, (qkv, do), s in zip(streams, ins, shapes):
+            with torch.cuda.stream(st):
+                o, lse = _fwd(qkv, *s)
+                got.append((o, _bwd(qkv, o, do, lse, *s)))
+        torch.cuda.synchronize()
+        for (o, g), (o1, g1) in zip(got, alone):
+            assert torch.equal(o, o1) and torch.equal(g, g1)
