@@ -157,9 +157,19 @@ def _stream_ptr():
 def _stream_of(index: int) -> int:
     """The current stream of device `index` as a plain address (the raw query takes 0.1 us where torch.cuda.current_stream()
     takes 3.3, which a launch-bound operator would notice)."""
-    import torch
+    torch = _torch or _import_torch()
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
+_torch = None
+
+
+def _import_torch():
+    global _torch
+    import torch
+    _torch = torch
+    return torch
 
 
 def bf16_bits_to_f32(a: np.ndarray) -> np.ndarray:
@@ -439,7 +449,7 @@ def _refuse(what: str):
 
 def _check_flat(name, t, dtype, numel, index):
     """The address of a contiguous tensor of exactly `numel` elements on device `index`."""
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != index:
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != index:
         _refuse(f"{name}: expected {numel} contiguous {dtype} elements on cuda:{index}, got {tuple(t.shape)} {t.dtype} on {t.device}, "
                 f"strides {t.stride()}")
     return t.data_ptr()
@@ -447,7 +457,7 @@ def _check_flat(name, t, dtype, numel, index):
 
 def _check_rows(name, t, dtype, rows, h, index):
     """(address, row stride) of a [rows, h] tensor whose rows are contiguous."""
-    if t.shape != (rows, h) or t.dtype != dtype or t.get_device() != index:
+    if t.dtype is not dtype or t.shape != (rows, h) or t.get_device() != index:
         _refuse(f"{name}: expected [{rows}, {h}] {dtype} on cuda:{index}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     ld, one = t.stride()
     if one != 1 and h > 1:
@@ -461,17 +471,17 @@ def _check_rows(name, t, dtype, rows, h, index):
 
 def _current_device(t):
     """Index of the device of the call's tensors, which has to be the current one (kernels run on its current stream)."""
-    import torch
     index = t.get_device()
     if index < 0:
         _refuse(f"tensors on {t.device}: a CUDA device is needed")
-    if index != torch.cuda.current_device():
-        _refuse(f"tensors on {t.device}, current device cuda:{torch.cuda.current_device()}")
+    current = (_torch or _import_torch()).cuda.current_device()
+    if index != current:
+        _refuse(f"tensors on {t.device}, current device cuda:{current}")
     return index
 
 
 def _row_dtype(t):
-    import torch
+    torch = _torch or _import_torch()
     if t.dtype == torch.bfloat16:
         return 0
     if t.dtype == torch.float32:
@@ -493,7 +503,7 @@ def attention_window_scratch_bytes(B, S, n_heads, n_kv, d, window, n_sinks) -> i
 
 def k_attention_window_fwd(qkv, o, lse, B, S, n_heads, n_kv, d, window, n_sinks=0):
     """Causal attention in which query i sees key j iff j <= i and (i - j < window or j < n_sinks)."""
-    import torch
+    torch = _torch or _import_torch()
     window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
     dev = _current_device(qkv)
     T = B * S
@@ -508,7 +518,7 @@ def k_attention_window_fwd(qkv, o, lse, B, S, n_heads, n_kv, d, window, n_sinks=
 def k_attention_window_bwd(qkv, o, d_o, lse, dqkv, scratch, B, S, n_heads, n_kv, d, window, n_sinks=0, cos=None, sin=None):
     """Gradient of k_attention_window_fwd; scratch: a uint8 tensor of attention_window_scratch_bytes(...) bytes; cos, sin: fp32
     [S, d / 2] tables by which d_q and d_k are rotated back, or None."""
-    import torch
+    torch = _torch or _import_torch()
     window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
     dev, bf16, f32 = _current_device(qkv), torch.bfloat16, torch.float32
     T = B * S
@@ -534,7 +544,7 @@ def _rows_of(x):
 
 def k_layernorm_fwd(x, gain, bias, y, mean, rstd, eps=1e-5):
     """y = (x - mean) rstd gain + bias over the rows of x [rows, h] (bf16 or fp32, any row stride); bias may be None."""
-    import torch
+    torch = _torch or _import_torch()
     dt, dev, dtype = _row_dtype(x), _current_device(x), x.dtype
     rows, h = _rows_of(x)
     px, ldx = _check_rows("x", x, dtype, rows, h, dev)
@@ -555,7 +565,7 @@ def layernorm_scratch_bytes(rows, h) -> int:
 def k_layernorm_bwd(dy, x, mean, rstd, gain, resid, dx, dgain, dbias, scratch):
     """dx = R(LayerNorm's input gradient + resid), dgain and dbias in fp32; resid and dbias may be None; scratch: a uint8
     tensor of layernorm_scratch_bytes(rows, h) bytes."""
-    import torch
+    torch = _torch or _import_torch()
     dt, dev, dtype, f32 = _row_dtype(x), _current_device(x), x.dtype, torch.float32
     rows, h = _rows_of(x)
     px, ldx = _check_rows("x", x, dtype, rows, h, dev)
@@ -575,7 +585,7 @@ def k_dropout_add(x, resid, y, p, seed, site, step=None, scale=1.0):
     """y = R(resid + scale / (1 - p) keep x) over [rows, h] tensors; the mask is a function of (seed, site, step, element), so
     the backward pass is this call on the gradient with resid None.  step: int64 tensor of one element, read when the
     kernel runs."""
-    import torch
+    torch = _torch or _import_torch()
     dt, dev, dtype = _row_dtype(x), _current_device(x), x.dtype
     rows, h = _rows_of(x)
     px, ldx = _check_rows("x", x, dtype, rows, h, dev)

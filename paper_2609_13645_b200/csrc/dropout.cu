@@ -11,9 +11,6 @@
 // expectation is exact.  A word costs about 25 integer instructions for 16-24 bytes of traffic: the kernel stays bound
 // by memory.
 #include <math.h>
-#include <string.h>
-
-#include <type_traits>
 
 #include "../../include/forgestep.h"
 #include "layernorm.cuh"
@@ -24,51 +21,63 @@ namespace {
 
 constexpr unsigned long long kSite = 0xD1B54A32D192ED03ull, kStep = 0xA24BAED4963EE407ull, kGroup = 0x8CB92BA72F3D8DD7ull;
 
-// f[e] <- scale * f[e] where element first + e is kept, else 0.  A chunk of 4 or 8 starts on a multiple of 4.
-template <int VEC>
-__device__ __forceinline__ void drop(float (&f)[VEC], unsigned long long first, unsigned long long key, uint32_t t, float scale) {
-  unsigned long long word = 0;
+// f[e] <- scale * f[e] where element first + e is kept, else 0.  ALIGNED: first is a multiple of 4.  Elements in front of the
+// first one (first < 0) are nobody's.
+template <int VEC, bool ALIGNED>
+__device__ __forceinline__ void drop(float (&f)[VEC], long long first, unsigned long long key, uint32_t t, float scale) {
+  const long long group = first >> 2;
+  unsigned long long next = splitmix64(key ^ ((unsigned long long)group * kGroup));
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    const unsigned long long i = first + e;
-    if (VEC < 4 ? (e == 0 || (i & 3) == 0) : (e & 3) == 0) word = splitmix64(key ^ ((i >> 2) * kGroup));
-    const uint32_t lane = VEC < 4 ? (uint32_t)(i & 3) : (uint32_t)(e & 3);
-    const uint32_t bits = (uint32_t)(word >> (16 * lane)) & 0xffffu;
-    f[e] = bits >= t ? f[e] * scale : 0.f;
+  for (int e = 0; e < VEC; e += 4) {
+    unsigned long long word = next;
+    if (!ALIGNED || e + 4 < VEC) next = splitmix64(key ^ ((unsigned long long)(group + e / 4 + 1) * kGroup));
+    if constexpr (!ALIGNED) {
+      const int s = 16 * (int)(first & 3);
+      if (s != 0) word = word >> s | next << (64 - s);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t bits = (uint32_t)(word >> (16 * k)) & 0xffffu;
+      f[e + k] = bits >= t ? f[e + k] * scale : 0.f;
+    }
   }
 }
 
-// U chunks of VEC elements in flight a thread.  FLAT: rows follow one another without gaps, so the chunk index is the
-// element index; the last `n % VEC` elements are handled one by one.
-template <typename T, int VEC, bool FLAT, int U>
+// VEC elements from p on, of which those at [from, to) are in the tensor [begin, end) and are read; the others may hold anything.
+template <typename T, int VEC>
+__device__ __forceinline__ void load_chunk(const T* p, int from, int to, const T* begin, const T* end, float (&f)[VEC]) {
+  const int d = behind_boundary(p);
+  const T* a = p - d;
+  if (a >= begin && a + 2 * VEC <= end) {
+    uint4 r = load_piece(a);
+    if (d != 0) r = realign(r, load_piece(a + VEC), d, sizeof(T));
+    unpack_piece(r, f);
+  } else {  // at the tensor's ends
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = e >= from && e < to ? to_float(p[e]) : 0.f;
+  }
+}
+
+// Rows without gaps between them, whole 16-byte pieces from the start: the chunk index is the element index; the last n % VEC
+// elements are handled one by one.  U chunks in flight a thread.
+template <typename T, int U>
 __global__ void __launch_bounds__(256)
-dropout_add_kernel(const T* x, long long ldx, const T* resid, long long ldr, T* y, long long ldy, long long n, unsigned h,
-                   unsigned long long base, const long long* __restrict__ step, uint32_t t, float scale) {
+dropout_add_flat_kernel(const T* x, const T* resid, T* y, long long n, unsigned long long base, const long long* __restrict__ step,
+                        uint32_t t, float scale) {
+  constexpr int VEC = 16 / (int)sizeof(T);
   using V = RowVec<T, VEC>;
   pdl_trigger();
   pdl_wait();
   const unsigned long long key = splitmix64(base ^ ((unsigned long long)(step != nullptr ? *step : 0) * kStep));
   const long long chunks = n / VEC;
-  const unsigned per_row = h / VEC;
   const long long stride = (long long)gridDim.x * blockDim.x;
   for (long long c0 = (long long)blockIdx.x * blockDim.x + threadIdx.x; c0 < chunks; c0 += stride * U) {
     typename V::Raw a[U], b[U];
-    long long row[U];
-    unsigned col[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long long c = c0 + u * stride;
-      if constexpr (FLAT) {
-        row[u] = 0;
-        col[u] = 0;
-        a[u] = c < chunks ? V::load(x + c * VEC) : V::zero();
-        b[u] = c < chunks && resid != nullptr ? V::load(resid + c * VEC) : V::zero();
-      } else {
-        row[u] = c <= 0xffffffffll ? (long long)((unsigned)c / per_row) : c / per_row;
-        col[u] = (unsigned)(c - row[u] * per_row) * VEC;
-        a[u] = c < chunks ? V::load(x + row[u] * ldx + col[u]) : V::zero();
-        b[u] = c < chunks && resid != nullptr ? V::load(resid + row[u] * ldr + col[u]) : V::zero();
-      }
+      a[u] = c < chunks ? V::load(x + c * VEC) : V::zero();
+      b[u] = c < chunks && resid != nullptr ? V::load(resid + c * VEC) : V::zero();
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -77,36 +86,89 @@ dropout_add_kernel(const T* x, long long ldx, const T* resid, long long ldr, T* 
         float f[VEC], q[VEC];
         V::unpack(a[u], f);
         V::unpack(b[u], q);
-        drop<VEC>(f, (unsigned long long)c * VEC, key, t, scale);
+        drop<VEC, true>(f, c * VEC, key, t, scale);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) f[e] += q[e];
-        V::store(FLAT ? y + c * VEC : y + row[u] * ldy + col[u], f);
+        V::store(y + c * VEC, f);
       }
     }
   }
-  if (FLAT && VEC > 1) {
-    const long long i = chunks * VEC + threadIdx.x;
-    if (blockIdx.x == 0 && i < n) {
-      float f[1], q[1] = {0.f};
-      RowVec<T, 1>::unpack(RowVec<T, 1>::load(x + i), f);
-      if (resid != nullptr) RowVec<T, 1>::unpack(RowVec<T, 1>::load(resid + i), q);
-      drop<1>(f, (unsigned long long)i, key, t, scale);
-      f[0] += q[0];
-      RowVec<T, 1>::store(y + i, f);
+  const long long rest = chunks * VEC;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && rest < n) {
+    float f[VEC], q[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      f[e] = rest + e < n ? to_float(x[rest + e]) : 0.f;
+      q[e] = rest + e < n && resid != nullptr ? to_float(resid[rest + e]) : 0.f;
+    }
+    drop<VEC, true>(f, rest, key, t, scale);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (rest + e < n) store_one(y + rest + e, f[e] + q[e]);
+  }
+}
+
+// Any rows: the chunks of a row are cut at the 16-byte boundaries of its output (the first and the last are partial); a chunk of an
+// input that lies otherwise is put together from the two aligned pieces that hold it, the second of which its neighbour
+// reads too.
+template <typename T>
+__global__ void __launch_bounds__(256)
+dropout_add_rows_kernel(const T* x, long long ldx, const T* resid, long long ldr, T* y, long long ldy, unsigned rows, unsigned h,
+                        unsigned per_row, unsigned long long base, const long long* __restrict__ step, uint32_t t, float scale) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  using V = RowVec<T, VEC>;
+  pdl_trigger();
+  pdl_wait();
+  const unsigned long long key = splitmix64(base ^ ((unsigned long long)(step != nullptr ? *step : 0) * kStep));
+  const T *x_end = x + (long long)(rows - 1) * ldx + h, *r_end = resid != nullptr ? resid + (long long)(rows - 1) * ldr + h : nullptr;
+  const long long chunks = (long long)rows * per_row, stride = (long long)gridDim.x * blockDim.x;
+  for (long long c = (long long)blockIdx.x * blockDim.x + threadIdx.x; c < chunks; c += stride) {
+    const long long row = c <= 0xffffffffll ? (long long)((unsigned)c / per_row) : c / per_row;
+    T* out = y + row * ldy;
+    const long long col = (c - row * per_row) * VEC - behind_boundary(out);  // of the chunk's first element
+    if (col >= (long long)h) continue;
+    const int from = col < 0 ? (int)-col : 0, to = (long long)h - col < VEC ? (int)((long long)h - col) : VEC;
+    float f[VEC], q[VEC];
+    load_chunk<T, VEC>(x + row * ldx + col, from, to, x, x_end, f);
+    if (resid != nullptr) {
+      load_chunk<T, VEC>(resid + row * ldr + col, from, to, resid, r_end, q);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) q[e] = 0.f;
+    }
+    drop<VEC, false>(f, row * h + col, key, t, scale);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] += q[e];
+    if (from == 0 && to == VEC) {
+      V::store(out + col, f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (e >= from && e < to) store_one(out + col + e, f[e]);
     }
   }
 }
 
-template <typename T, int VEC, bool FLAT>
+int blocks_for(long long chunks, int per_thread) {
+  const long long want = (chunks + 256 * per_thread - 1) / (256 * per_thread);
+  return (int)(want < 1 ? 1 : want < 148 * 16 ? want : 148 * 16);
+}
+
+template <typename T>
 cudaError_t launch(const void* x, int64_t ldx, const void* resid, int64_t ldr, void* y, int64_t ldy, int rows, int h,
                    unsigned long long base, const long long* step, uint32_t t, float scale, cudaStream_t st) {
-  constexpr int U = 2;
-  const long long n = (long long)rows * h, chunks = n / VEC;
-  const long long want = (chunks + 256 * U - 1) / (256 * U);
-  const int blocks = (int)(want < 1 ? 1 : want < 148 * 16 ? want : 148 * 16);
-  return launch_pdl(dropout_add_kernel<T, VEC, FLAT, U>, dim3(blocks), dim3(256), 0, st, reinterpret_cast<const T*>(x), (long long)ldx,
-                    reinterpret_cast<const T*>(resid), (long long)ldr, reinterpret_cast<T*>(y), (long long)ldy, n, (unsigned)h, base,
-                    step, t, scale);
+  constexpr int VEC = 16 / (int)sizeof(T), U = 2;
+  const T *xp = reinterpret_cast<const T*>(x), *rp = reinterpret_cast<const T*>(resid);
+  T* yp = reinterpret_cast<T*>(y);
+  if (ldx == h && ldy == h && (resid == nullptr || ldr == h) && ((uintptr_t)x | (uintptr_t)resid | (uintptr_t)y) % 16 == 0) {
+    const long long n = (long long)rows * h;
+    return launch_pdl(dropout_add_flat_kernel<T, U>, dim3(blocks_for(n / VEC, U)), dim3(256), 0, st, xp, rp, yp, n, base, step, t, scale);
+  }
+  // a row has one chunk more where it may start behind a boundary
+  const bool whole = ((uint64_t)ldy * sizeof(T) & 15u) == 0 && ((uintptr_t)y & 15u) == 0;
+  const unsigned per_row = (unsigned)(((long long)h + (whole ? 0 : VEC - 1) + VEC - 1) / VEC);
+  return launch_pdl(dropout_add_rows_kernel<T>, dim3(blocks_for((long long)rows * per_row, 1)), dim3(256), 0, st, xp, (long long)ldx, rp,
+                    (long long)ldr, yp, (long long)ldy, (unsigned)rows, (unsigned)h, per_row, base, step, t, scale);
 }
 
 }  // namespace
@@ -116,16 +178,8 @@ cudaError_t dropout_add(const void* x, int64_t ldx, const void* resid, int64_t l
   const uint32_t t = (uint32_t)fmin(65535.0, floor((double)p * 65536.0 + 0.5));
   const float factor = (float)((double)scale * 65536.0 / (65536.0 - (double)t));
   const unsigned long long base = splitmix64(seed ^ ((unsigned long long)(long long)(site + 1ll) * kSite));
-  const int elem = dtype == 0 ? 2 : 4;
-  const bool flat = ldx == h && ldy == h && (resid == nullptr || ldr == h);
-  const uintptr_t ptrs = (uintptr_t)x | (uintptr_t)resid | (uintptr_t)y;
-  const int v = flat ? row_vec(0, ptrs, elem) : row_vec((uint64_t)h | (uint64_t)ldx | (uint64_t)ldy | (resid ? (uint64_t)ldr : 0), ptrs, elem);
-#define DROP(T, V, F) launch<T, V, F>(x, ldx, resid, ldr, y, ldy, rows, h, base, step, t, factor, st)
-#define DROP_T(T, F) (v == 8 ? DROP(T, (sizeof(T) == 2 ? 8 : 4), F) : v == 4 ? DROP(T, 4, F) : v == 2 ? DROP(T, 2, F) : DROP(T, 1, F))
-  if (dtype == 0) return flat ? DROP_T(bf16, true) : DROP_T(bf16, false);
-  return flat ? DROP_T(float, true) : DROP_T(float, false);
-#undef DROP_T
-#undef DROP
+  if (dtype == 0) return launch<bf16>(x, ldx, resid, ldr, y, ldy, rows, h, base, step, t, factor, st);
+  return launch<float>(x, ldx, resid, ldr, y, ldy, rows, h, base, step, t, factor, st);
 }
 
 }  // namespace fs

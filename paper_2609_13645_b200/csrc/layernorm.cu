@@ -6,9 +6,8 @@
 // every row it meets: gains and biases stay in registers (read again for every row they would double the L1 traffic), and
 // so do its shares of the gain and bias gradients.
 //
-// Rows come through a ring of NS slots in shared memory, filled by asynchronous copies that each thread issues for its own
-// elements NS - 1 rows ahead: the loads of a row do not wait for the reductions of the one before, and cost no registers.
-// NS = 0, for rows that are only 2-byte aligned, reads global memory directly.
+// Rows come through a ring of NS slots in shared memory, filled by asynchronous copies that each thread issues NS - 1 rows
+// ahead: the loads of a row do not wait for the reductions of the one before, and cost no registers.
 #include "layernorm.cuh"
 
 #include "../../include/forgestep.h"
@@ -19,23 +18,32 @@ namespace {
 
 constexpr int kSms = 148;
 
-// barrier of one group of warps (bar 0 is __syncthreads)
-__device__ __forceinline__ void group_sync(int group, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
+// barrier of a group of `warps` warps (bar 0 is __syncthreads; a block has at most 8 groups of more than one warp)
+__device__ __forceinline__ void group_sync(int group, int warps) {
+  if (warps == 1) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
 }
 
-// The elements of one thread in a ring of NS rows of NT tensors (NS = 0: no ring).
-template <typename T, int VEC, int NCH, int NT, int NS>
+// The elements of one thread in a ring of NS rows of NT tensors (NS = 0: no ring).  A thread copies its own chunks and needs
+// no barrier.
+template <typename T, int VEC, int EPL, int NT, int NS>
 struct RowRing {
+  static constexpr bool kShared = false;  // slots between the threads of a group
+  static constexpr int NCH = EPL / VEC, PAIRS = EPL / 2;
   using V = RowVec<T, VEC>;
   typedef typename V::Raw Raw;
-  static constexpr int SLOT = (int)sizeof(Raw), PAIRS = NCH * VEC / 2;
+  static constexpr int SLOT = (int)sizeof(Raw);
   uint32_t base;  // this thread's first slot
-  int threads;
+  int threads, first, stride, h;
   static constexpr size_t bytes(int threads) { return (size_t)(NS * NT * NCH * SLOT) * threads; }
-  __device__ __forceinline__ RowRing(const void* smem, int threads) : base(smem_u32(smem) + threadIdx.x * SLOT), threads(threads) {}
+  // l: this thread's number among the gthreads of its group
+  __device__ __forceinline__ RowRing(const void* smem, int gthreads, int l, int h, const T*)
+      : base(smem_u32(smem) + threadIdx.x * SLOT), threads(blockDim.x), first(l * VEC), stride(gthreads * VEC), h(h) {}
   __device__ __forceinline__ uint32_t slot(int stage, int t, int k) const { return base + (uint32_t)(((stage * NT + t) * NCH + k) * threads * SLOT); }
-  __device__ __forceinline__ void fetch(int stage, int t, const T* row, bool live, int first, int stride, int h) const {
+  // column of this thread's element i, and whether the row has it
+  __device__ __forceinline__ int column(int i) const { return first + i / VEC * stride + i % VEC; }
+  __device__ __forceinline__ bool inside(int i) const { return first + i / VEC * stride < h; }
+  __device__ __forceinline__ void fetch(int stage, int t, const T* row, bool live, bool) const {
     if constexpr (NS > 0) {
 #pragma unroll
       for (int k = 0; k < NCH; ++k) {
@@ -47,8 +55,8 @@ struct RowRing {
   }
   // this thread's elements of tensor t of the row in `stage` (row: where it lies in global memory, read when there is no
   // ring); 0 outside the row
-  __device__ __forceinline__ void get(int stage, int t, const T* row, int first, int stride, int h, float2 (&v)[PAIRS]) const {
-    float f[NCH * VEC];
+  __device__ __forceinline__ void get(int stage, int t, const T* row, float2 (&v)[PAIRS]) const {
+    float f[EPL];
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       Raw r;
@@ -70,7 +78,21 @@ struct RowRing {
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) v[i] = make_float2(f[2 * i], f[2 * i + 1]);
   }
-  __device__ __forceinline__ static void put(T* row, int first, int stride, int h, const float2 (&v)[PAIRS]) {
+  // the same of a vector that every row uses (null: 0)
+  __device__ __forceinline__ void constant(const T* p, float2 (&v)[PAIRS]) const {
+    float f[EPL];
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = first + k * stride;
+      float u[VEC];
+      V::unpack(p != nullptr && c < h ? V::load(p + c) : V::zero(), u);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[k * VEC + e] = u[e];
+    }
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+  }
+  __device__ __forceinline__ void put(T* row, const float2 (&v)[PAIRS]) const {
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = first + k * stride;
@@ -84,34 +106,121 @@ struct RowRing {
   }
 };
 
-// A row vector (gain, bias) in registers: as fp32 pairs where a thread has few columns of it, packed as it came otherwise.
-template <typename T, int VEC, int NCH>
+// The same for bf16 rows that start at any element.  Chunks of 8 are cut at the 16-byte boundaries of the OUTPUT rows (the
+// first and the last of a row are partial), so that all others are stored whole; a group takes only rows that start equally far
+// behind a boundary, which keeps its threads' columns.  The ring holds the aligned pieces of the input rows, and a thread
+// puts a chunk together from its own piece and its neighbour's: the group passes a barrier between the pieces' arrival and
+// get, and another one before the slot is filled again.
+template <int EPL, int NT, int NS>
+struct EdgeRing {
+  static constexpr bool kShared = true;
+  static constexpr int VEC = 8, NCH = EPL / VEC, PAIRS = EPL / 2;
+  uint32_t base;  // this thread's first slot
+  int threads, first, stride, h;
+  bool last;      // thread of its group
+  static constexpr size_t bytes(int threads) { return (size_t)(NS * NT * NCH * 16) * threads; }
+  // out: an output row of the group
+  __device__ __forceinline__ EdgeRing(const void* smem, int gthreads, int l, int h, const bf16* out)
+      : base(smem_u32(smem) + threadIdx.x * 16), threads(blockDim.x), first(l * VEC - behind_boundary(out)), stride(gthreads * VEC), h(h),
+        last(l == gthreads - 1) {}
+  __device__ __forceinline__ uint32_t slot(int stage, int t, int k) const { return base + (uint32_t)(((stage * NT + t) * NCH + k) * threads * 16); }
+  __device__ __forceinline__ int column(int i) const { return first + i / VEC * stride + i % VEC; }
+  __device__ __forceinline__ bool inside(int i) const { return (unsigned)column(i) < (unsigned)h; }
+  __device__ __forceinline__ bool partial(int k) const { return first + k * stride < 0 || first + k * stride + VEC > h; }
+  // inner: the 15 bytes on either side of the row are inside the tensor too
+  __device__ __forceinline__ void fetch(int stage, int t, const bf16* row, bool live, bool inner) const {
+    const int d = behind_boundary(row + first);  // the same in all threads and chunks
+    const bf16* at = row + first - d;
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      // a piece that holds nothing of the row is left out
+      if (!live || (unsigned)(first - d + VEC - 1 + k * stride) >= (unsigned)(h + VEC - 1)) continue;
+      if (inner) {
+        async_copy<16>(slot(stage, t, k), at + k * stride, true);
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < VEC; ++e) {
+          const bf16* p = at + k * stride + e;
+          if (p >= row && p < row + h)
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(slot(stage, t, k) + e * 2), "h"(*reinterpret_cast<const unsigned short*>(p)) : "memory");
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ uint4 load(uint32_t at) {
+    uint4 r;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
+    return r;
+  }
+  __device__ __forceinline__ void spread(int k, const uint4& r, float2 (&v)[PAIRS]) const {
+    float u[VEC];
+    unpack_piece(r, u);
+    if (partial(k)) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (!inside(k * VEC + e)) u[e] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) v[k * VEC / 2 + i] = make_float2(u[2 * i], u[2 * i + 1]);
+  }
+  __device__ __forceinline__ void get(int stage, int t, const bf16* row, float2 (&v)[PAIRS]) const {
+    const int d = behind_boundary(row + first);
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      uint4 r = load(slot(stage, t, k));
+      if (d != 0) {  // behind the group's last piece lies nothing of the row
+        const uint32_t next = !last ? slot(stage, t, k) + 16 : slot(stage, t, k + 1 < NCH ? k + 1 : k) - (uint32_t)(stride / VEC - 1) * 16;
+        r = realign(r, load(next), d, 2);
+      }
+      spread(k, r, v);
+    }
+  }
+  __device__ __forceinline__ void constant(const bf16* p, float2 (&v)[PAIRS]) const {
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i)
+      v[i] = make_float2(p != nullptr && inside(2 * i) ? to_float(p[column(2 * i)]) : 0.f,
+                         p != nullptr && inside(2 * i + 1) ? to_float(p[column(2 * i + 1)]) : 0.f);
+  }
+  __device__ __forceinline__ void put(bf16* row, const float2 (&v)[PAIRS]) const {
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      bf16* out = row + first + k * stride;
+      if (!partial(k)) {
+        const float2* p = v + k * VEC / 2;
+        *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(p[0].x, p[0].y), pack_bf16(p[1].x, p[1].y), pack_bf16(p[2].x, p[2].y), pack_bf16(p[3].x, p[3].y));
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (inside(k * VEC + e)) store_one(out + e, e & 1 ? v[(k * VEC + e) / 2].y : v[(k * VEC + e) / 2].x);
+      }
+    }
+  }
+};
+
+// VEC = 0: EdgeRing.
+template <typename T, int VEC, int EPL, int NT, int NS>
+struct RingOf {
+  typedef RowRing<T, VEC, EPL, NT, NS> type;
+};
+template <int EPL, int NT, int NS>
+struct RingOf<bf16, 0, EPL, NT, NS> {
+  typedef EdgeRing<EPL, NT, NS> type;
+};
+
+// A row vector (gain, bias) in registers, where a thread has few columns of it; read again for every row otherwise.
+template <typename Ring, typename T>
 struct RowConst {
-  using V = RowVec<T, VEC>;
-  static constexpr int PAIRS = NCH * VEC / 2;
+  static constexpr int PAIRS = Ring::PAIRS;
   static constexpr bool WIDE = PAIRS > 8;
   float2 v[WIDE ? 1 : PAIRS];
   const T* p;
-  __device__ __forceinline__ void init(const T* ptr, int first, int stride, int h) {
+  __device__ __forceinline__ void init(const T* ptr, const Ring& ring) {
     p = ptr;
-    if constexpr (!WIDE) fill(first, stride, h, v);
+    if constexpr (!WIDE) ring.constant(p, v);
   }
-  __device__ __forceinline__ void fill(int first, int stride, int h, float2 (&o)[PAIRS]) const {
-    float f[NCH * VEC];
-#pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-      const int c = first + k * stride;
-      float u[VEC];
-      V::unpack(p != nullptr && c < h ? V::load(p + c) : V::zero(), u);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) f[k * VEC + e] = u[e];
-    }
-#pragma unroll
-    for (int i = 0; i < PAIRS; ++i) o[i] = make_float2(f[2 * i], f[2 * i + 1]);
-  }
-  __device__ __forceinline__ void get(int first, int stride, int h, float2 (&o)[PAIRS]) const {
+  __device__ __forceinline__ void get(const Ring& ring, float2 (&o)[PAIRS]) const {
     if constexpr (WIDE) {
-      fill(first, stride, h, o);  // stays in L1
+      ring.constant(p, o);  // stays in L1
     } else {
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) o[i] = v[i];
@@ -119,62 +228,65 @@ struct RowConst {
   }
 };
 
+// The 15 bytes on either side of this row are inside the tensor too: it has rows of 16 bytes before and behind.
+__device__ __forceinline__ bool inner_row(long long row, int rows, int h) { return row > 0 && row + 1 < rows && h >= 8; }
+
 // ---------------------------------------------------------------- forward
 // y = (x - mean) rstd gain + bias.  The row stays in registers: first the mean, then the centred sum of squares (the
 // difference of sum(x^2) / h and mean^2 would lose the variance of rows whose mean is large).
-template <typename T, int VEC, int NCH, int NS, int MAXT>
-__global__ void __launch_bounds__(MAXT)
+template <typename T, int VEC, int EPL, int NS, int MAXT>
+__global__ void __launch_bounds__(VEC == 0 && EPL <= 16 ? 1024 : MAXT == 256 ? 768 : MAXT)  // of all blocks of an SM (fwd_launch)
 layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, const T* __restrict__ bias, T* y, long long ldy,
                      float* __restrict__ mean, float* __restrict__ rstd, int rows, int h, int gw, float eps) {
-  using Ring = RowRing<T, VEC, NCH, 1, NS>;
+  using Ring = typename RingOf<T, VEC, EPL, 1, NS>::type;
   constexpr int PAIRS = Ring::PAIRS;
   pdl_trigger();
   pdl_wait();
   extern __shared__ __align__(16) uint8_t ring_mem[];
-  __shared__ float s_part[2][16];
+  __shared__ float s_part[2][MAXT / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / gw, gwarp = warp - group * gw, groups = (blockDim.x >> 5) / gw;
-  const int first = (gwarp * 32 + lane) * VEC, stride = gw * 32 * VEC;
   const float inv_h = 1.0f / (float)h;
-  const Ring ring(ring_mem, blockDim.x);
+  const long long step = (long long)gridDim.x * groups;
+  long long row = (long long)blockIdx.x * groups + group, ahead = row;
+  const Ring ring(ring_mem, gw * 32, gwarp * 32 + lane, h, y + row * ldy);
+  auto fetch = [&](int stage) {
+    const bool live = ahead < rows;
+    ring.fetch(stage, 0, x + (live ? ahead : 0) * ldx, live, inner_row(ahead, rows, h));
+    ahead += step;
+    async_commit();
+  };
   // sum over the group; every thread gets the same bits.  The two sums of a row use different slots: each slot's readers
   // have passed the other's barrier before it is written again.
   auto group_sum = [&](float2 p, int which) {
     const float v = warp_sum(p.x + p.y);
     if (gw == 1) return v;
     if (lane == 0) s_part[which][warp] = v;
-    group_sync(group, gw * 32);
+    group_sync(group, gw);
     float t = s_part[which][group * gw];
     for (int w = 1; w < gw; ++w) t += s_part[which][group * gw + w];
     return t;
   };
-  const long long step = (long long)gridDim.x * groups;
-  long long row = (long long)blockIdx.x * groups + group, ahead = row;
 #pragma unroll
-  for (int s = 0; s < NS - 1; ++s, ahead += step) {
-    ring.fetch(s, 0, x + (ahead < rows ? ahead : 0) * ldx, ahead < rows, first, stride, h);
-    async_commit();
-  }
-  RowConst<T, VEC, NCH> cg, cb;
-  cg.init(gain, first, stride, h);
-  cb.init(bias, first, stride, h);
+  for (int s = 0; s < NS - 1; ++s) fetch(s);
+  RowConst<Ring, T> cg, cb;
+  cg.init(gain, ring);
+  cb.init(bias, ring);
   int stage = 0;
-  for (; row < rows; row += step, ahead += step) {
-    if constexpr (NS > 0) {
-      ring.fetch(stage == 0 ? NS - 1 : stage - 1, 0, x + (ahead < rows ? ahead : 0) * ldx, ahead < rows, first, stride, h);
-      async_commit();
-      async_wait<NS - 1>();
-    }
+  for (; row < rows; row += step) {
+    fetch(stage == 0 ? NS - 1 : stage - 1);
+    async_wait<NS - 1>();
+    if (Ring::kShared) group_sync(group, gw);
     float2 v[PAIRS], s = both(0.f), ss = both(0.f);
-    ring.get(stage, 0, x + row * ldx, first, stride, h, v);
+    ring.get(stage, 0, x + row * ldx, v);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) s = add2(s, v[i]);
     const float mu = group_sum(s, 0) * inv_h;
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) {
       float2 m = both(-mu);  // columns outside the row stay 0
-      if (first + (2 * i / VEC) * stride >= h) m.x = 0.f;
-      if (first + ((2 * i + 1) / VEC) * stride >= h) m.y = 0.f;
+      if (!ring.inside(2 * i)) m.x = 0.f;
+      if (!ring.inside(2 * i + 1)) m.y = 0.f;
       v[i] = add2(v[i], m);
       ss = fma2(v[i], v[i], ss);
     }
@@ -184,12 +296,12 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
       rstd[row] = rs;
     }
     float2 g[PAIRS], b[PAIRS];
-    cg.get(first, stride, h, g);
-    cb.get(first, stride, h, b);
+    cg.get(ring, g);
+    cb.get(ring, b);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) v[i] = fma2(mul2(v[i], both(rs)), g[i], b[i]);
-    Ring::put(y + row * ldy, first, stride, h, v);
-    if (NS > 0 && ++stage == NS) stage = 0;
+    ring.put(y + row * ldy, v);
+    if (++stage == NS) stage = 0;
   }
 }
 
@@ -197,39 +309,39 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
 // dx = rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid with g = dy gain; dgain = sum over rows of dy xhat, dbias of dy.
 // g and xhat stay in registers between the two sums of a row and its update.  A block leaves one partial row of dgain and
 // dbias, which a second kernel adds in block order.
-template <typename T, int VEC, int NCH, int NS, int MAXT>
+template <typename T, int VEC, int EPL, int NS, int MAXT>
 __global__ void __launch_bounds__(MAXT, 1)
 layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, const float* __restrict__ mean,
                      const float* __restrict__ rstd, const T* __restrict__ gain, const T* resid, long long ldr, T* dx, long long lddx,
-                     float* __restrict__ partial, int rows, int h, int gw) {
-  using Ring = RowRing<T, VEC, NCH, 3, NS>;
+                     float* __restrict__ partial, int rows, int h, int hp, int gw) {
+  using Ring = typename RingOf<T, VEC, EPL, 3, NS>::type;
   constexpr int PAIRS = Ring::PAIRS;
   pdl_trigger();
   pdl_wait();
   // the ring; after the last row the groups of a block add their column sums in its place
   extern __shared__ __align__(16) uint8_t ring_mem[];
-  __shared__ float s_part[2][16][2];
+  __shared__ float s_part[2][MAXT / 32][2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / gw, gwarp = warp - group * gw, groups = (blockDim.x >> 5) / gw;
-  const int first = (gwarp * 32 + lane) * VEC, stride = gw * 32 * VEC;
   const float inv_h = 1.0f / (float)h;
-  const Ring ring(ring_mem, blockDim.x);
   const long long step = (long long)gridDim.x * groups;
   long long row = (long long)blockIdx.x * groups + group, ahead = row;
+  const Ring ring(ring_mem, gw * 32, gwarp * 32 + lane, h, dx + row * lddx);
   auto fetch = [&](int stage) {
     const bool live = ahead < rows;
     const long long r = live ? ahead : 0;
-    ring.fetch(stage, 0, dy + r * lddy, live, first, stride, h);
-    ring.fetch(stage, 1, x + r * ldx, live, first, stride, h);
-    if (resid != nullptr) ring.fetch(stage, 2, resid + r * ldr, live, first, stride, h);
+    const bool inner = inner_row(ahead, rows, h);
+    ring.fetch(stage, 0, dy + r * lddy, live, inner);
+    ring.fetch(stage, 1, x + r * ldx, live, inner);
+    if (resid != nullptr) ring.fetch(stage, 2, resid + r * ldr, live, inner);
     ahead += step;
     async_commit();
   };
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) fetch(s);
   float mu_next = row < rows ? mean[row] : 0.f, rs_next = row < rows ? rstd[row] : 0.f;
-  RowConst<T, VEC, NCH> cg;
-  cg.init(gain, first, stride, h);
+  RowConst<Ring, T> cg;
+  cg.init(gain, ring);
   float2 acc_g[PAIRS], acc_b[PAIRS];
 #pragma unroll
   for (int i = 0; i < PAIRS; ++i) acc_g[i] = acc_b[i] = both(0.f);
@@ -241,11 +353,16 @@ layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, con
       mu_next = mean[row + step];
       rs_next = rstd[row + step];
     }
-    if constexpr (NS > 0) async_wait<NS - 1>();
-    float2 a[PAIRS], xh[PAIRS], g[PAIRS], p1 = both(0.f), p2 = both(0.f);
-    ring.get(stage, 0, dy + row * lddy, first, stride, h, a);
-    ring.get(stage, 1, x + row * ldx, first, stride, h, xh);
-    cg.get(first, stride, h, g);
+    if constexpr (NS > 0) {
+      async_wait<NS - 1>();
+      if (Ring::kShared) group_sync(group, gw);
+    }
+    float2 a[PAIRS], xh[PAIRS], g[PAIRS], q[PAIRS], p1 = both(0.f), p2 = both(0.f);
+    ring.get(stage, 0, dy + row * lddy, a);
+    ring.get(stage, 1, x + row * ldx, xh);
+    // shared slots are read ahead of the barrier below, after which they may be filled again
+    if (Ring::kShared && resid != nullptr) ring.get(stage, 2, resid + row * ldr, q);
+    cg.get(ring, g);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) {
       xh[i] = mul2(add2(xh[i], both(-mu)), both(rs));  // outside the row a = 0 and what xh holds does not matter
@@ -263,7 +380,7 @@ layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, con
       for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       if ((lane & 15) == 0) s_part[parity][warp][lane >> 4] = v;
     }
-    if (gw == 1) __syncwarp(); else group_sync(group, gw * 32);
+    group_sync(group, gw);
     s1 = s_part[parity][group * gw][0];
     s2 = s_part[parity][group * gw][1];
     for (int w = 1; w < gw; ++w) {
@@ -273,79 +390,71 @@ layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, con
     parity ^= 1;  // the other slot is free: everyone passed this barrier after its last reads
     const float2 c1 = both(-rs * (s1 * inv_h)), c2 = both(-rs * (s2 * inv_h));
     if (resid != nullptr) {
-      float2 q[PAIRS];
-      ring.get(stage, 2, resid + row * ldr, first, stride, h, q);
+      if (!Ring::kShared) ring.get(stage, 2, resid + row * ldr, q);
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) a[i] = add2(fma2(a[i], both(rs), fma2(xh[i], c2, c1)), q[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) a[i] = fma2(a[i], both(rs), fma2(xh[i], c2, c1));
     }
-    Ring::put(dx + row * lddx, first, stride, h, a);
+    ring.put(dx + row * lddx, a);
     if (NS > 0 && ++stage == NS) stage = 0;
   }
   // One partial row a block.  Its groups leave their sums side by side in shared memory and all threads add them, in group
   // order.
-  float* out = partial + (long long)blockIdx.x * 2 * h;
+  float* out = partial + (long long)blockIdx.x * 2 * hp;
   float* col = reinterpret_cast<float*>(ring_mem);
   if (groups > 1) {
     if constexpr (NS > 0) async_wait<0>();
     __syncthreads();
   }
-  float* mine = groups > 1 ? col + (long long)group * 2 * h : out;
+  float* mine = groups > 1 ? col + (long long)group * 2 * hp : out;
 #pragma unroll
   for (int i = 0; i < PAIRS * 2; ++i) {
-    const int c = first + (i / VEC) * stride + i % VEC;
-    if (c < h) {
-      mine[c] = i & 1 ? acc_g[i / 2].y : acc_g[i / 2].x;
-      mine[h + c] = i & 1 ? acc_b[i / 2].y : acc_b[i / 2].x;
+    if (ring.inside(i)) {
+      mine[ring.column(i)] = i & 1 ? acc_g[i / 2].y : acc_g[i / 2].x;
+      mine[hp + ring.column(i)] = i & 1 ? acc_b[i / 2].y : acc_b[i / 2].x;
     }
   }
   if (groups > 1) {
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * h; c += blockDim.x) {
+    for (int c = threadIdx.x; c < 2 * hp; c += blockDim.x) {
+      if (c >= h && c < hp) continue;
+      if (c >= hp + h) break;
       float t = col[c];
-      for (int g = 1; g < groups; ++g) t += col[(long long)g * 2 * h + c];
+      for (int g = 1; g < groups; ++g) t += col[(long long)g * 2 * hp + c];
       out[c] = t;
     }
   }
 }
 
-// Column sums of the block partials in a fixed order: a CTA takes 32 columns, 32 strided subsets of the blocks run side by
-// side (each thread reads 4 columns at a time where they are aligned) and are then added in subset order.
-template <int VEC>
-__global__ void __launch_bounds__(32 * 32 / VEC)
-layernorm_colsum_kernel(const float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int nblk, int h) {
-  using V = RowVec<float, VEC>;
+// Column sums of the block partials (rows of hp columns each of dgain and dbias, hp: h rounded up to 4) in a fixed order: a CTA
+// takes 32 columns, 32 strided subsets of the blocks run side by side and are then added in subset order.
+__global__ void __launch_bounds__(256)
+layernorm_colsum_kernel(const float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int nblk, int h, int hp) {
   pdl_trigger();
   pdl_wait();
   __shared__ float s[32][33];
-  constexpr int TX = 32 / VEC;
-  const int cx = threadIdx.x % TX, ry = threadIdx.x / TX;
-  const int cols = dbias != nullptr ? 2 * h : h;
-  const int c = blockIdx.x * 32 + cx * VEC;
-  float a[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) a[e] = 0.f;
+  const int cx = threadIdx.x % 8, ry = threadIdx.x / 8;
+  const int cols = dbias != nullptr ? 2 * hp : hp;
+  const int c = blockIdx.x * 32 + cx * 4;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < cols) {
 #pragma unroll 4
     for (int b = ry; b < nblk; b += 32) {
-      float f[VEC];
-      V::unpack(V::load(partial + (long long)b * 2 * h + c), f);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) a[e] += f[e];
+      const float4 v = *reinterpret_cast<const float4*>(partial + (long long)b * 2 * hp + c);
+      a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
     }
   }
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) s[ry][cx * VEC + e] = a[e];
+  s[ry][cx * 4] = a.x; s[ry][cx * 4 + 1] = a.y; s[ry][cx * 4 + 2] = a.z; s[ry][cx * 4 + 3] = a.w;
   __syncthreads();
   if (threadIdx.x >= 32) return;
-  const int col = blockIdx.x * 32 + threadIdx.x;
-  if (col >= cols) return;
+  const int col = blockIdx.x * 32 + threadIdx.x, rest = col - hp;
+  if (col >= cols || (col >= h && rest < 0) || rest >= h) return;
   float tot = 0.f;
 #pragma unroll
   for (int w = 0; w < 32; ++w) tot += s[w][threadIdx.x];
-  if (col < h) dgain[col] = tot; else dbias[col - h] = tot;
+  if (col < h) dgain[col] = tot; else dbias[rest] = tot;
 }
 
 int blocks_for(int rows, int groups, int most) {
@@ -353,63 +462,78 @@ int blocks_for(int rows, int groups, int most) {
   return (int)(want < most ? want : most);
 }
 
-// Elements a thread holds of a row.  16 up to 8192 columns and 32 beyond, so that a group never exceeds 16 warps; 8 where a
-// warp covers the row with them, and for rows whose accesses are narrower than 16 bytes (every one of them is an
-// instruction: fewer a thread, more threads; 4099 x 771 fp32 backward 17.7 us with 8, 28.7 with 16).
-int elements_per_thread(int h, bool narrow) { return h <= 256 || (narrow && h <= 4096) ? 8 : h <= 8192 ? 16 : 32; }
+// Blocks of a launch whose groups take every (blocks * groups)-th row, so that these start equally far behind a boundary.
+int blocks_of_period(int blocks, int groups, int rows, int64_t ld) {
+  int period = 1;
+  while (ld * period % 8 != 0) period *= 2;
+  while ((long long)blocks * groups < rows && blocks * groups % period != 0) --blocks;
+  return blocks;
+}
 
-template <typename T, int VEC, int EPL, int NS, int MAXT>
+// Columns that a group has chunks for; EdgeRing: the partial chunk's in front and one chunk's behind the row too.
+int cover_of(int h, int vec) { return vec == 0 ? h + 15 : h; }
+
+// Elements a thread holds of a row.  16 up to 8192 columns and 32 beyond, so that a group never exceeds 16 warps (17 of
+// EdgeRing); 8 where a warp covers the row with them, and for rows whose accesses are narrower than 16 bytes (every one of
+// them is an instruction: fewer a thread, more threads; 4099 x 771 fp32 backward 17.7 us with 8, 28.7 with 16).
+int elements_per_thread(int cover, bool narrow) { return cover <= 256 || (narrow && cover <= 4096) ? 8 : cover <= 8192 ? 16 : 32; }
+
+template <typename T, int VEC, int EPL, int MAXT>
 cudaError_t fwd_launch(const void* x, int64_t ldx, const void* gain, const void* bias, void* y, int64_t ldy, float* mean, float* rstd,
                        int rows, int h, float eps, cudaStream_t st) {
-  using Ring = RowRing<T, VEC, EPL / VEC, 1, NS>;
-  auto kern = layernorm_fwd_kernel<T, VEC, EPL / VEC, NS, MAXT>;
-  const int gw = (h + 32 * EPL - 1) / (32 * EPL);
+  constexpr int NS = 3;
+  using Ring = typename RingOf<T, VEC, EPL, 1, NS>::type;
+  auto kern = layernorm_fwd_kernel<T, VEC, EPL, NS, MAXT>;
+  const int gw = (cover_of(h, VEC) + 32 * EPL - 1) / (32 * EPL);
   int groups = MAXT / 32 / gw;
   if (rows <= kSms * groups) groups = 1;  // few rows: spread them over the SMs
   const int threads = groups * gw * 32;
   static unsigned long long smem_set = 0;
   cudaError_t e = ensure_dynamic_smem(kern, (int)Ring::bytes(MAXT), smem_set);
   if (e != cudaSuccess) return e;
-  // 768 threads an SM (8192 x 2048 bf16: 3 blocks of 256 15.9 us, 1 of 512 20.2, 4 of 256 18.9; as many as fit 17.0)
-  return launch_pdl(kern, dim3(blocks_for(rows, groups, kSms * (MAXT == 256 ? 3 : 1))), dim3(threads), Ring::bytes(threads), st,
-                    reinterpret_cast<const T*>(x), (long long)ldx, reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(bias),
-                    reinterpret_cast<T*>(y), (long long)ldy, mean, rstd, rows, h, gw, eps);
+  // 768 threads an SM (8192 x 2048 bf16: 3 blocks of 256 15.9 us, 1 of 512 20.2, 4 of 256 18.9; as many as fit 17.0).  EdgeRing,
+  // which computes more for its bytes: 1024 (8192 x 2047: 30 us, 40 with 480)
+  int blocks = blocks_for(rows, groups, kSms * (VEC == 0 && EPL <= 16 ? 1024 / MAXT : MAXT == 256 ? 3 : 1));
+  if (VEC == 0) blocks = blocks_of_period(blocks, groups, rows, ldy);
+  return launch_pdl(kern, dim3(blocks), dim3(threads), Ring::bytes(threads), st, reinterpret_cast<const T*>(x), (long long)ldx,
+                    reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(bias), reinterpret_cast<T*>(y), (long long)ldy, mean,
+                    rstd, rows, h, gw, eps);
 }
 
 template <typename T, int VEC>
 cudaError_t fwd_width(const void* x, int64_t ldx, const void* gain, const void* bias, void* y, int64_t ldy, float* mean, float* rstd,
                       int rows, int h, float eps, cudaStream_t st) {
-  constexpr int NS = VEC * sizeof(T) >= 4 ? 3 : 0;
-  const int epl = elements_per_thread(h, VEC * sizeof(T) < 16);
-#define LN_FWD_W(EPL, MAXT) fwd_launch<T, VEC, EPL, NS, MAXT>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st)
-  const bool small = h <= 256 * epl;  // a row fits a block of 256 threads
+  const int cover = cover_of(h, VEC), epl = elements_per_thread(cover, VEC != 0 && VEC * sizeof(T) < 16);
+#define LN_FWD_W(EPL, MAXT) fwd_launch<T, VEC, EPL, MAXT>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st)
+  const bool small = cover <= 256 * epl;  // a row fits a block of 256 threads
   if (epl == 8) return small ? LN_FWD_W(8, 256) : LN_FWD_W(8, 512);
-  if (epl == 16) return small ? LN_FWD_W(16, 256) : LN_FWD_W(16, 512);
-  return LN_FWD_W(32, 512);
+  if (epl == 16) return small ? LN_FWD_W(16, (VEC == 0 ? 512 : 256)) : LN_FWD_W(16, 512);
+  return LN_FWD_W(32, (VEC == 0 ? 544 : 512));
 #undef LN_FWD_W
 }
 
-template <typename T, int VEC, int EPL, int NS>
+template <typename T, int VEC, int EPL, int NS, int MAXT>
 cudaError_t bwd_launch(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd, const void* gain,
                        const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias, float* scratch, int rows,
                        int h, cudaStream_t st) {
-  using Ring = RowRing<T, VEC, EPL / VEC, 3, NS>;
-  auto kern = layernorm_bwd_kernel<T, VEC, EPL / VEC, NS, 512>;
-  const int gw = (h + 32 * EPL - 1) / (32 * EPL), groups = 16 / gw, threads = groups * gw * 32;
-  const int blocks = blocks_for(rows, groups, kSms);
-  const size_t col = groups > 1 ? (size_t)groups * 2 * h * sizeof(float) : 0;  // at most 2 * 512 * EPL floats
-  constexpr size_t most = Ring::bytes(512) > 4096 * EPL ? Ring::bytes(512) : 4096 * EPL;
+  using Ring = typename RingOf<T, VEC, EPL, 3, NS>::type;
+  auto kern = layernorm_bwd_kernel<T, VEC, EPL, NS, MAXT>;
+  const int gw = (cover_of(h, VEC) + 32 * EPL - 1) / (32 * EPL), groups = MAXT / 32 / gw, threads = groups * gw * 32;
+  const int hp = (h + 3) / 4 * 4;
+  int blocks = blocks_for(rows, groups, kSms);
+  if (VEC == 0) blocks = blocks_of_period(blocks, groups, rows, lddx);
+  const size_t col = groups > 1 ? (size_t)groups * 2 * hp * sizeof(float) : 0;  // at most 2 * MAXT * EPL floats
+  constexpr size_t most = Ring::bytes(MAXT) > 8 * MAXT * EPL ? Ring::bytes(MAXT) : 8 * MAXT * EPL;
   static unsigned long long smem_set = 0;
   cudaError_t e = ensure_dynamic_smem(kern, (int)most, smem_set);
   if (e != cudaSuccess) return e;
   e = launch_pdl(kern, dim3(blocks), dim3(threads), Ring::bytes(threads) > col ? Ring::bytes(threads) : col, st,
                  reinterpret_cast<const T*>(dy), (long long)lddy, reinterpret_cast<const T*>(x), (long long)ldx, mean, rstd,
                  reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(resid), (long long)ldr, reinterpret_cast<T*>(dx),
-                 (long long)lddx, scratch, rows, h, gw);
+                 (long long)lddx, scratch, rows, h, hp, gw);
   if (e != cudaSuccess) return e;
-  const int cols = dbias != nullptr ? 2 * h : h;
-  if (h % 4 == 0) return launch_pdl(layernorm_colsum_kernel<4>, dim3((cols + 31) / 32), dim3(256), 0, st, scratch, dgain, dbias, blocks, h);
-  return launch_pdl(layernorm_colsum_kernel<1>, dim3((cols + 31) / 32), dim3(1024), 0, st, scratch, dgain, dbias, blocks, h);
+  const int cols = dbias != nullptr ? 2 * hp : hp;
+  return launch_pdl(layernorm_colsum_kernel, dim3((cols + 31) / 32), dim3(256), 0, st, scratch, dgain, dbias, blocks, h, hp);
 }
 
 template <typename T, int VEC>
@@ -417,11 +541,10 @@ cudaError_t bwd_width(const void* dy, int64_t lddy, const void* x, int64_t ldx, 
                       const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias, float* scratch, int rows,
                       int h, cudaStream_t st) {
   // two rows in the ring: one under way hides the memory (a third changes nothing); none where 512 threads' slots would
-  // not fit an SM's shared memory (fp32 rows of more than 8192 columns) or the accesses are too narrow to be copied
-  constexpr bool RING = VEC * sizeof(T) >= 4;
-#define LN_BWD_W(EPL, NS) bwd_launch<T, VEC, EPL, RING ? NS : 0>(dy, lddy, x, ldx, mean, rstd, gain, resid, ldr, dx, lddx, dgain, dbias, scratch, rows, h, st)
-  const int epl = elements_per_thread(h, VEC * sizeof(T) < 16);
-  return epl == 8 ? LN_BWD_W(8, 2) : epl == 16 ? LN_BWD_W(16, 2) : LN_BWD_W(32, (sizeof(T) == 2 ? 2 : 0));
+  // not fit an SM's shared memory (fp32 rows of more than 8192 columns)
+#define LN_BWD_W(EPL, NS, MAXT) bwd_launch<T, VEC, EPL, NS, MAXT>(dy, lddy, x, ldx, mean, rstd, gain, resid, ldr, dx, lddx, dgain, dbias, scratch, rows, h, st)
+  const int epl = elements_per_thread(cover_of(h, VEC), VEC != 0 && VEC * sizeof(T) < 16);
+  return epl == 8 ? LN_BWD_W(8, 2, 512) : epl == 16 ? LN_BWD_W(16, 2, 512) : LN_BWD_W(32, (sizeof(T) == 2 ? 2 : 0), (VEC == 0 ? 544 : 512));
 #undef LN_BWD_W
 }
 
@@ -429,33 +552,26 @@ cudaError_t bwd_width(const void* dy, int64_t lddy, const void* x, int64_t ldx, 
 
 cudaError_t layernorm_fwd(const void* x, int64_t ldx, const void* gain, const void* bias, void* y, int64_t ldy, float* mean,
                           float* rstd, int rows, int h, float eps, int dtype, cudaStream_t st) {
-  const int elem = dtype == 0 ? 2 : 4;
   const uintptr_t ptrs = (uintptr_t)x | (uintptr_t)gain | (uintptr_t)bias | (uintptr_t)y;
-  const int v = row_vec((uint64_t)h | (uint64_t)ldx | (uint64_t)ldy, ptrs, elem);
-  if (dtype == 0) {
-    if (v == 8) return fwd_width<bf16, 8>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
-    if (v == 4) return fwd_width<bf16, 4>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
-    if (v == 2) return fwd_width<bf16, 2>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
-    return fwd_width<bf16, 1>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
-  }
-  if (v == 4) return fwd_width<float, 4>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
-  if (v == 2) return fwd_width<float, 2>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
-  return fwd_width<float, 1>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st);
+  const int v = row_vec((uint64_t)h | (uint64_t)ldx | (uint64_t)ldy, ptrs, dtype == 0 ? 2 : 4);
+#define LN_FWD(T, V) fwd_width<T, V>(x, ldx, gain, bias, y, ldy, mean, rstd, rows, h, eps, st)
+  if (dtype == 0) return v == 8 ? LN_FWD(bf16, 8) : v == 4 ? LN_FWD(bf16, 4) : v == 2 ? LN_FWD(bf16, 2) : LN_FWD(bf16, 0);
+  return v == 4 ? LN_FWD(float, 4) : v == 2 ? LN_FWD(float, 2) : LN_FWD(float, 1);
+#undef LN_FWD
 }
 
 size_t layernorm_scratch_bytes(int rows, int h) {
   if (rows <= 0 || h <= 0 || h > kLayerNormMaxWidth) return 0;
-  return (size_t)(rows < kSms ? rows : kSms) * 2 * (size_t)h * sizeof(float);  // one partial row of both gradients a block
+  return (size_t)(rows < kSms ? rows : kSms) * 2 * (size_t)((h + 3) / 4 * 4) * sizeof(float);  // one partial row of both gradients a block
 }
 
 cudaError_t layernorm_bwd(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd,
                           const void* gain, const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias,
                           float* scratch, int rows, int h, int dtype, cudaStream_t st) {
-  const int elem = dtype == 0 ? 2 : 4;
   const uintptr_t ptrs = (uintptr_t)dy | (uintptr_t)x | (uintptr_t)gain | (uintptr_t)resid | (uintptr_t)dx;
-  const int v = row_vec((uint64_t)h | (uint64_t)lddy | (uint64_t)ldx | (resid ? (uint64_t)ldr : 0) | (uint64_t)lddx, ptrs, elem);
+  const int v = row_vec((uint64_t)h | (uint64_t)lddy | (uint64_t)ldx | (resid ? (uint64_t)ldr : 0) | (uint64_t)lddx, ptrs, dtype == 0 ? 2 : 4);
 #define LN_BWD(T, V) bwd_width<T, V>(dy, lddy, x, ldx, mean, rstd, gain, resid, ldr, dx, lddx, dgain, dbias, scratch, rows, h, st)
-  if (dtype == 0) return v == 8 ? LN_BWD(bf16, 8) : v == 4 ? LN_BWD(bf16, 4) : v == 2 ? LN_BWD(bf16, 2) : LN_BWD(bf16, 1);
+  if (dtype == 0) return v == 8 ? LN_BWD(bf16, 8) : v == 4 ? LN_BWD(bf16, 4) : v == 2 ? LN_BWD(bf16, 2) : LN_BWD(bf16, 0);
   return v == 4 ? LN_BWD(float, 4) : v == 2 ? LN_BWD(float, 2) : LN_BWD(float, 1);
 #undef LN_BWD
 }

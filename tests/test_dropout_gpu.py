@@ -126,3 +126,27 @@ def test_replays_read_the_step_on_the_device():
         step.fill_(s)
         graph.replay()
         assert torch.equal(y != 0, keep_mask(rows, h, 0.25, 77, 4, s)[0])
+
+
+@pytest.mark.parametrize("rows,h", [(1, 3), (5, 7), (3, 16), (40, 241), (700, 2047), (1500, 33)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_every_tensor_at_an_alignment_of_its_own(rows, h, dtype):
+    from paper_2609_13645_b200 import binding as Bn
+    g = torch.Generator(device="cuda").manual_seed(rows + h)
+
+    def at(ld, offset):  # rows that begin `offset` elements into an allocation which ends with the last of them
+        buf = torch.randn(offset + (rows - 1) * ld + h, generator=g, device="cuda").to(dtype)
+        return torch.as_strided(buf, (rows, h), (ld, 1), offset)
+    x, r, y = at(h + 3, 1), at(h + 8, 6), at(h + 1, 3)
+    Bn.k_dropout_add(x, r, y, 0.25, 11, 1, scale=0.5)
+    keep, t = keep_mask(rows, h, 0.25, 11, 1, 0)
+    want = r.double() + x.double() * keep * (0.5 * 65536.0 / (65536.0 - t))
+    eps = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22
+    assert ((y.double() - want).abs() <= eps * want.abs() + 2.0 ** -22 * (r.double().abs() + x.double().abs())).all()
+    x2 = x.clone()  # packed
+    r2 = r.clone()
+    out = torch.empty_like(x2)
+    Bn.k_dropout_add(x2, r2, out, 0.25, 11, 1, scale=0.5)
+    assert torch.equal(out, y)
+    Bn.k_dropout_add(x, r, r, 0.25, 11, 1, scale=0.5)  # in place
+    assert torch.equal(r, y)

@@ -194,3 +194,48 @@ def test_gradients_agree_with_differences():
         up[at], down[at] = args[at] + eps * v, args[at] - eps * v
         diff = float((f(*up) - f(*down)) / (2 * eps))
         assert abs(diff - float((grad.double() * v).sum())) < 1e-4 * float(grad.double().norm()) * float(v.norm()) ** 0.5
+
+
+def _at(t, ld, offset):
+    """A copy of t whose rows are ld apart and begin `offset` elements into an allocation that ends with the last of them."""
+    rows, h = t.shape
+    buf = torch.empty(offset + (rows - 1) * ld + h, dtype=t.dtype, device=t.device)
+    view = torch.as_strided(buf, (rows, h), (ld, 1), offset)
+    view.copy_(t)
+    return view
+
+
+# every tensor starts elsewhere against the 16-byte boundaries, and moves on differently from row to row
+@pytest.mark.parametrize("rows,h", [(1, 3), (3, 1), (5, 7), (2, 9), (40, 241), (40, 243), (1500, 33), (2600, 300), (700, 2047), (9, 4095), (4, 8179), (3, 8191),
+                                    (3, 16371), (3, 16384)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_tensor_at_an_alignment_of_its_own(rows, h, dtype):
+    from paper_2609_13645_b200 import binding as Bn
+    g = torch.Generator(device="cuda").manual_seed(rows + h)
+    x, dy, r = (_at(_rand(g, rows, h, dtype), h + e, o) for e, o in ((3, 1), (0, 6), (10, 3)))
+    y, dx = (_at(torch.full((rows, h), 7.0, dtype=dtype, device="cuda"), h + e, o) for e, o in ((1, 5), (5, 2)))
+    gain = torch.randn(h + 1, generator=g, device="cuda").to(dtype)[1:]
+    bias = torch.randn(h + 3, generator=g, device="cuda").to(dtype)[3:]
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    Bn.k_layernorm_fwd(x, gain, bias, y, mean, rstd)
+    y_ref, mean_ref, rstd_ref = _reference(x, gain, bias, 1e-5)
+    tol = 1e-5 if dtype == F32 else 2.5e-3 if rows * h >= 100 else 2.0 ** -8
+    assert float((mean.double() - mean_ref).abs().max()) < 1e-5 * float(x.float().abs().max()) and _rel(rstd, rstd_ref) < 1e-5
+    assert _rel(y, y_ref) < tol
+    dgain, dbias = torch.empty(h, device="cuda"), torch.empty(h, device="cuda")
+    scratch = torch.full((Bn.layernorm_scratch_bytes(rows, h) // 4,), float("nan"), device="cuda").view(torch.uint8)
+    Bn.k_layernorm_bwd(dy, x, mean, rstd, gain, r, dx, dgain, dbias, scratch)
+    dx_ref, dg_ref, db_ref = _reference_bwd(dy, x, mean, rstd, gain, r)
+    # the terms of dx, rstd g, rstd mean(g) and rstd xhat mean(g xhat), are rounded where they are as large as rstd |g|, and may
+    # cancel (of one column nothing is left, with rstd = 1 / sqrt(eps) = 316): 4 roundings of 2^-24 of that beside the relative error
+    slack = 4 * 2.0 ** -24 * float((rstd.double()[:, None] * dy.double() * gain.double()).norm())
+    assert float((dx.double() - dx_ref).norm()) < tol * float(dx_ref.norm()) + slack
+    terms = (dy.double() * ((x.double() - mean.double()[:, None]) * rstd.double()[:, None])).norm()
+    assert float((dgain.double() - dg_ref).norm()) <= 1e-5 * float(dg_ref.norm()) + 1e-6 * float(terms)
+    assert float((dbias.double() - db_ref).norm()) <= 1e-5 * float(db_ref.norm()) + 1e-6 * float(dy.double().norm())
+    # in place, over the rows the kernel reads
+    z = _at(x, h + 3, 1)
+    Bn.k_layernorm_fwd(z, gain, bias, z, mean, rstd)
+    assert torch.equal(z, y) or _rel(z, y_ref) < tol
+    Bn.k_layernorm_bwd(dy, x, mean, rstd, gain, r, r, dgain, dbias, scratch)
+    assert float((r.double() - dx_ref).norm()) < tol * float(dx_ref.norm()) + slack
