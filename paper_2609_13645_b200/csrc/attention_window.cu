@@ -776,6 +776,91 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   }
 }
 
+// ---------------------------------------------------------------- partial sums of dK and dV
+// Adds the partial sums of a key block's parts in part order, scales and rotates dK, rounds once.  A unit of this work is 32
+// columns of a key block (16 of dK and their partners D / 2 further, or 32 of dV): a warp reads whole columns, 512 bytes each a
+// part, every part's loads in flight at once; the sums pass through shared memory to threads that hold half a row of them
+// each.  The units are taken by CTAs of the dQ kernel that have no tile (left), which need none of them: as a launch of its own
+// behind it this cost 8 us.
+struct Join {
+  const float* partial;
+  bf16* dqkv;
+  const float *rope_cos, *rope_sin;
+  float scale;
+  int cut;  // key blocks with partial sums
+  __host__ __device__ int units(const Plan& pl, int d) const { return cut * pl.all_groups * (d / 16); }
+};
+constexpr int JOIN_SMEM = 32 * 132 * 4;
+
+// all THREADS of a CTA; s_sum: [column][key]
+template <int D, int THREADS>
+__device__ __forceinline__ void join_unit(const Join& jn, const Plan& pl, int unit, float (*s_sum)[132]) {
+  constexpr int H = D / 2, K_UNITS = H / 16, WARPS = THREADS / 32, OWN = (32 + WARPS - 1) / WARPS;
+  const int groups = pl.all_groups, S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv;
+  const int piece = unit % (D / 16), x = unit / (D / 16) / groups, grp = unit / (D / 16) % groups;
+  const int np = pl.parts_of(x);
+  if (np == 1) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool is_k = piece < K_UNITS;
+  const int c0 = is_k ? piece * 16 : (piece - K_UNITS) * 32;
+  const long long part_stride = (long long)groups * (2 * D * 128);
+  const float* src = jn.partial + ((long long)pl.rank_of(x) * groups + grp) * (2 * D * 128) + lane * 4;
+  float4 acc[OWN];
+  int off[OWN];
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    const int l = min(warp + i * WARPS, 31);  // of the unit's 32 columns
+    off[i] = (is_k ? (l < 16 ? c0 + l : H + c0 + l - 16) : D + c0 + l) * 128;
+    acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll 4
+  for (int p = 0; p < np; ++p) {
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(src + p * part_stride + off[i]);
+      acc[i].x += v.x; acc[i].y += v.y; acc[i].z += v.z; acc[i].w += v.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < OWN; ++i)
+    if (warp + i * WARPS < 32) *reinterpret_cast<float4*>(&s_sum[warp + i * WARPS][lane * 4]) = acc[i];
+  __syncthreads();
+  const int kvh = grp % n_kv, b = grp / n_kv;
+  for (int v = threadIdx.x; v < 256; v += THREADS) {
+    const int r = v & 127, part = v >> 7, row = x * 128 + r;
+    if (row >= S) continue;
+    bf16* dst = jn.dqkv + ((long long)b * S + row) * (long long)((n_heads + 2 * n_kv) * D) + (n_heads + (is_k ? 0 : n_kv) + kvh) * D + c0;
+    if (is_k) {
+      float lo[8], hi[8];
+      const int i0 = part * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        lo[i] = s_sum[i0 + i][r] * jn.scale;
+        hi[i] = s_sum[16 + i0 + i][r] * jn.scale;
+      }
+      if (jn.rope_cos != nullptr) unrotate<8>(lo, hi, jn.rope_cos + (long long)row * H + c0 + i0, jn.rope_sin + (long long)row * H + c0 + i0);
+      store_bf16_row<8>(dst + i0, lo);
+      store_bf16_row<8>(dst + H + i0, hi);
+    } else {
+      float f[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = s_sum[part * 16 + i][r];
+      store_bf16_row<16>(dst + part * 16, f);
+    }
+  }
+  __syncthreads();  // s_sum is free again
+}
+
+// The same behind the dQ kernel that recomputes the scores.
+template <int D>
+__global__ void __launch_bounds__(256)
+attn_window_join_kernel(const __grid_constant__ Join jn, const __grid_constant__ Plan pl) {
+  pdl_trigger();
+  pdl_wait();
+  __shared__ float s_sum[32][132];
+  join_unit<D, 256>(jn, pl, (int)blockIdx.x, s_sum);
+}
+
 // ---------------------------------------------------------------- dQ from the stored dS^T
 // dQ[i] = scale * sum over visible keys j of dS[i, j] K[j], rotated back: per 128-query tile one product over the keys of its
 // band and the sink keys behind it.  Persistent: warp 0 TMA producer, warp 1 MMA issuer, warps 2..5 epilogue, accumulators
@@ -800,7 +885,8 @@ template <int D>
 __global__ void __launch_bounds__(DQ_THREADS, 2)
 attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ CUtensorMap tm_sink,
                       const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_out, const float* __restrict__ rope_cos,
-                      const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale, int* err) {
+                      const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, const __grid_constant__ Join jn, float scale,
+                      int* err) {
   using C = DqCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
@@ -957,6 +1043,11 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
     tc_fence_after();
     tmem_dealloc(tmem_base, C::TMEM_COLS);
   }
+  // the tiles' loads and stores have left shared memory (waited for above); the CTAs with the fewest tiles begin with the units
+  static_assert(JOIN_SMEM <= C::OFF_OUT, "the stages hold a unit's columns");
+  const int units = jn.units(pl, D);
+  for (int u = (int)(gridDim.x - 1 - blockIdx.x); u < units; u += (int)gridDim.x)
+    join_unit<D, DQ_THREADS>(jn, pl, u, reinterpret_cast<float (*)[132]>(smem));
 }
 
 // ---------------------------------------------------------------- dQ without stored dS^T
@@ -1202,68 +1293,6 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
 }
 
 
-// Adds the partial sums of a key block's parts in part order, scales and rotates dK, rounds once.  A CTA takes 32 columns
-// (16 of dK and their partners D / 2 further, or 32 of dV): a warp reads four of them, 512 bytes each a part, every part's loads
-// in flight at once; the sums pass through shared memory to threads that hold half a row of them each.
-template <int D>
-__global__ void __launch_bounds__(256)
-attn_window_join_kernel(const float* __restrict__ partial, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
-                        const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, float scale) {
-  pdl_trigger();
-  pdl_wait();
-  constexpr int H = D / 2, K_CTAS = H / 16;
-  __shared__ float s_sum[32][132];  // [column][key]
-  const int groups = pl.all_groups, S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv;
-  const int x = (int)blockIdx.x / groups, grp = (int)blockIdx.x % groups;
-  const int np = pl.parts_of(x);
-  if (np == 1) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool is_k = (int)blockIdx.y < K_CTAS;
-  const int c0 = is_k ? (int)blockIdx.y * 16 : ((int)blockIdx.y - K_CTAS) * 32;
-  const long long part_stride = (long long)groups * (2 * D * 128);
-  const float* src = partial + ((long long)pl.rank_of(x) * groups + grp) * (2 * D * 128) + lane * 4;
-  float4 acc[4];
-  int off[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int l = warp * 4 + i;  // of this CTA's 32 columns
-    off[i] = (is_k ? (l < 16 ? c0 + l : H + c0 + l - 16) : D + c0 + l) * 128;
-    acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-#pragma unroll 4
-  for (int p = 0; p < np; ++p) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 v = *reinterpret_cast<const float4*>(src + p * part_stride + off[i]);
-      acc[i].x += v.x; acc[i].y += v.y; acc[i].z += v.z; acc[i].w += v.w;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(&s_sum[warp * 4 + i][lane * 4]) = acc[i];
-  __syncthreads();
-  const int r = threadIdx.x & 127, part = threadIdx.x >> 7, row = x * 128 + r;
-  if (row >= S) return;
-  const int kvh = grp % n_kv, b = grp / n_kv;
-  bf16* dst = dqkv + ((long long)b * S + row) * (long long)((n_heads + 2 * n_kv) * D) + (n_heads + (is_k ? 0 : n_kv) + kvh) * D + c0;
-  if (is_k) {
-    float lo[8], hi[8];
-    const int i0 = part * 8;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      lo[i] = s_sum[i0 + i][r] * scale;
-      hi[i] = s_sum[16 + i0 + i][r] * scale;
-    }
-    if (rope_cos != nullptr) unrotate<8>(lo, hi, rope_cos + (long long)row * H + c0 + i0, rope_sin + (long long)row * H + c0 + i0);
-    store_bf16_row<8>(dst + i0, lo);
-    store_bf16_row<8>(dst + H + i0, hi);
-  } else {
-    float v[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = s_sum[part * 16 + i][r];
-    store_bf16_row<16>(dst + part * 16, v);
-  }
-}
-
 // Parts: where the launch has several times more streamed blocks than SMs, a part is as long as a window block's whole list
 // (or an eighth of a slot's share, if that is longer), so that only sink blocks are cut.  Smaller launches are cut into one
 // part per slot (of a CTA on an SM), of at least 4 blocks: the set-up and the partial sums of a part cost about as much as 2.
@@ -1364,15 +1393,18 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   e = attention_delta(o, d_o, delta, B, S, nh, D, st);
   const int per_round = pl.groups;
+  Join jn{partial, dqkv, cs, sn, scale, pl.parts > 1 ? pl.nxb : pl.parts_sink > 1 ? pl.n_sink : 0};
+  const Join none{partial, dqkv, cs, sn, scale, 0};
   for (int g0 = 0; g0 < pl.all_groups && e == cudaSuccess; g0 += per_round) {
     pl.group0 = g0;
     pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
     e = launch_pdl(attn_window_dkv_kernel<D, BLOCK>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D, BLOCK>::SMEM_BYTES, st,
                    tq128, DkvCfg<D, BLOCK>::BQ == 128 ? tq128 : tq64, tdo, tout, lse, delta, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess || !l.stored) continue;
-    const int tiles = pl.nxb * pl.groups * n_rep;
-    e = launch_pdl(attn_window_dq_kernel<D>, dim3(tiles < 2 * sms ? tiles : 2 * sms), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
-                   (const bf16*)band, tsink, tq64, tout, cs, sn, pl, scale, err);
+    const bool last = g0 + per_round >= pl.all_groups;
+    const long long ctas = (long long)pl.nxb * pl.groups * n_rep + (last ? jn.units(pl, D) : 0);
+    e = launch_pdl(attn_window_dq_kernel<D>, dim3((unsigned)(ctas < 2 * sms ? ctas : 2 * sms)), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
+                   (const bf16*)band, tsink, tq64, tout, cs, sn, pl, last ? jn : none, scale, err);
   }
   if (e != cudaSuccess) return e;
   if (!l.stored) {
@@ -1380,10 +1412,8 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
                    tq128, tq64, td128, lse, delta, dqkv, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess) return e;
   }
-  const int cut = pl.parts > 1 ? pl.nxb : pl.parts_sink > 1 ? pl.n_sink : 0;
-  if (cut == 0) return cudaSuccess;
-  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)cut * pl.all_groups, D / 16), dim3(256), 0, st, partial, dqkv, cs, sn,
-                    pl, scale);
+  if (l.stored || jn.cut == 0) return cudaSuccess;
+  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)jn.units(pl, D)), dim3(256), 0, st, jn, pl);
 }
 
 // Shapes the kernels take: 32-bit grids and tensor-map extents, element counts of one row within 31 bits.
