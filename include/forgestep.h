@@ -132,6 +132,15 @@ ft_status ft_set_overlap(ft_model* m, int32_t enable);
  * recomputing dQ kernel.  On by default; 0 selects the recomputing kernel always.  Changing it drops a captured graph. */
 ft_status ft_set_attention_stored_ds(ft_model* m, int32_t enable);
 
+/* Sliding-window attention in every layer of the step (MTP head included): query i sees key j iff j <= i and (i - j < window
+ * or j < n_sinks); see ft_k_attention_window_fwd.  The paper has no counterpart.  window 0 (the default): causal over the whole
+ * sequence, with results that do not depend on this setting ever having been used.  dev_scratch: device memory of
+ * ft_attention_window_bytes(m, window, n_sinks) bytes (0: refused), 256-byte aligned, the caller's, alive and not used by
+ * anything else while the setting lasts; less returns FT_ENOMEM, and so does a step whose batch needs more.  Results are
+ * bit-identical from run to run and with recomputation, graph and second stream.  Changing it drops a captured graph. */
+size_t ft_attention_window_bytes(const ft_model* m, int32_t window, int32_t n_sinks);
+ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, void* dev_scratch, uint64_t scratch_bytes);
+
 /* Streaming cross-entropy (the appendix' "chunked / streaming cross-entropy" that folds the LM-head GEMM, the loss and
  * the logit gradient into one chunked loop without ever holding logits): the logits GEMM of a row chunk reduces every
  * 256-column tile of a row to (max, sum of exponentials) in its epilogue, a small kernel combines the pairs into the
@@ -331,7 +340,8 @@ ft_status ft_k_gemm_ws(const void* dev_A, int32_t a_mn, int64_t lda, const void*
 
 /* The single-kernel attention calls below keep their device status word inside the library (ft_k_gemm takes the
  * caller's dev_err instead).  ft_k_status waits for `stream`, then returns FT_ETIMEOUT if a bounded device-side wait ran
- * out in any ft_k_attention_* call on the current device since the last ft_k_status (and clears the word), else FT_OK.
+ * out in any ft_k_attention_* call (ft_k_attention_window_* among them) on the current device since the last ft_k_status (and
+ * clears the word), else FT_OK.
  * (Keeping host synchronisation out of the hot loop, Section "Sources of the Speedup", is why the calls themselves do not check.) */
 ft_status ft_k_status(void* stream);
 

@@ -98,6 +98,10 @@ def lib():
         L.ft_set_streaming_ce.restype = C.c_int
         L.ft_set_attention_stored_ds.argtypes = [vp, i32]
         L.ft_set_attention_stored_ds.restype = C.c_int
+        L.ft_attention_window_bytes.argtypes = [vp, i32, i32]
+        L.ft_attention_window_bytes.restype = C.c_size_t
+        L.ft_set_attention_window.argtypes = [vp, i32, i32, vp, C.c_uint64]
+        L.ft_set_attention_window.restype = C.c_int
         L.ft_set_fused_swiglu_bwd.argtypes = [vp, i32]
         L.ft_set_fused_swiglu_bwd.restype = C.c_int
         L.ft_set_graph.argtypes = [vp, i32]
@@ -333,6 +337,20 @@ class Model:
     def set_attention_stored_ds(self, enable: bool):
         """Attention backward that stores dS^T once and computes dQ as one batched contraction (default on)."""
         self._check(lib().ft_set_attention_stored_ds(self._h, 1 if enable else 0))
+
+    def set_attention_window(self, window: int, n_sinks: int = 0):
+        """Sliding-window attention with sink keys in every layer (query i sees key j iff j <= i and (i - j < window or
+        j < n_sinks)); window 0: causal over the whole sequence (the default).  Holds the scratch of its backward pass."""
+        import torch
+        scratch = None
+        if window > 0 and n_sinks >= 0:
+            window, n_sinks = min(window, self.cfg.max_seq), min(n_sinks, self.cfg.max_seq)
+            nbytes = int(lib().ft_attention_window_bytes(self._h, window, n_sinks))
+            scratch = torch.empty(nbytes, dtype=torch.uint8, device=self.workspace.device)
+        self._check(lib().ft_set_attention_window(self._h, window, n_sinks, C.c_void_p(scratch.data_ptr()) if scratch is not None else None,
+                                                  scratch.numel() if scratch is not None else 0))
+        torch.cuda.synchronize(self.workspace.device)  # steps in flight still use the old scratch
+        self._attn_window_scratch = scratch
 
     def set_fused_swiglu_bwd(self, enable: bool):
         """SwiGLU backward in the epilogue of the down projection's data-gradient GEMM (default on; bit-identical)."""

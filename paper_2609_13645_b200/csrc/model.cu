@@ -12,6 +12,7 @@
 #include "../../include/forgestep.h"
 #include "forgestep_debug.h"
 #include "attention.cuh"
+#include "attention_window.cuh"
 #include "elementwise.cuh"
 #include "gemm.cuh"
 
@@ -139,6 +140,9 @@ struct ft_model {
   bf16* attn_ds = nullptr;    // dS^T scratch of the attention backward (one layer's worth), or null
   size_t attn_ds_bytes = 0;
   bool attn_ds_on = true;
+  int attn_window = 0, attn_sinks = 0;  // sliding-window attention of every layer (0: causal over the whole sequence)
+  void* attn_window_ws = nullptr;       // the caller's scratch for its backward pass
+  size_t attn_window_ws_bytes = 0;
 
   // AdamW inside the weight-gradient GEMM epilogues (clipping off): the train step then never stores those gradients
   bool fused_update = true;   // policy switch (ft_set_fused_update)
@@ -423,6 +427,16 @@ cudaEvent_t prof_event(ft_model* m) {
   cudaEventCreate(&e);
   return e;
 }
+// Model FLOPs of one layer's attention core, forward: 4 d a visible (query, key) pair and head (causal: S^2 / 2 pairs).
+double attention_flops(const ft_model* m, int B, int S) {
+  double pairs = 0.5 * (double)S * S;
+  if (m->attn_window > 0 && m->attn_window < S) {
+    const double w = m->attn_window, n = S - w, k = m->attn_sinks < n ? m->attn_sinks : n;  // n queries have left keys behind
+    pairs = 0.5 * w * (w + 1) + n * w + 0.5 * k * (k + 1) + (n - k) * k;
+  }
+  return 4.0 * B * m->cfg.n_heads * pairs * m->d;
+}
+
 inline void prof_begin(ft_model* m) {
   if (!m->prof) return;
   m->prof_cur = prof_event(m);
@@ -517,9 +531,12 @@ ft_status layer_forward(ft_model* m, int l, LayerActs& a, int B, int S) {
     FT_GEMM(g);
   }
   prof_begin(m);
-  FT_CUDA(attention_fwd(a.qkv, a.o, a.lse, B, S, m->cfg.n_heads, m->cfg.n_kv_heads, m->d, &m->sc->err, st));
+  if (m->attn_window > 0)
+    FT_CUDA(attention_window_fwd(a.qkv, a.o, a.lse, B, S, m->cfg.n_heads, m->cfg.n_kv_heads, m->d, m->attn_window, m->attn_sinks, &m->sc->err, st));
+  else
+    FT_CUDA(attention_fwd(a.qkv, a.o, a.lse, B, S, m->cfg.n_heads, m->cfg.n_kv_heads, m->d, &m->sc->err, st));
   m->launches += 1;
-  prof_end(m, FT_PROF_ATTN_FWD, 2.0 * B * m->cfg.n_heads * (double)S * S * m->d, 1);
+  prof_end(m, FT_PROF_ATTN_FWD, attention_flops(m, B, S), 1);
   {
     GemmArgs g = gemm_base(m);
     g.A = a.o; g.lda = hq; g.B = m->wb(m->idx_layer(l, 2)); g.ldb = hq; g.C = a.x_mid; g.ldc = h; g.resid = m->x[l];
@@ -662,11 +679,15 @@ ft_status layer_backward(ft_model* m, int l, LayerActs& a, int B, int S) {
   if (s) return s;
   if ((s = wait_wgrad(m, 3))) return s;  // the previous layer's qkv weight gradient still reads d_qkv
   prof_begin(m);
-  FT_CUDA(attention_bwd_ws(a.qkv, a.o, m->d_o, a.lse, m->delta, m->d_qkv, m->rope_cos, m->rope_sin,
-                           m->attn_ds_on ? m->attn_ds : nullptr, m->attn_ds_bytes, B, S, m->cfg.n_heads, m->cfg.n_kv_heads,
-                           m->d, &m->sc->err, st));
-  m->launches += 3;
-  prof_end(m, FT_PROF_ATTN_BWD, 4.0 * B * m->cfg.n_heads * (double)S * S * m->d, 3);
+  if (m->attn_window > 0)
+    FT_CUDA(attention_window_bwd(a.qkv, a.o, m->d_o, a.lse, m->d_qkv, m->rope_cos, m->rope_sin, m->attn_window_ws, B, S, m->cfg.n_heads,
+                                 m->cfg.n_kv_heads, m->d, m->attn_window, m->attn_sinks, &m->sc->err, st));
+  else
+    FT_CUDA(attention_bwd_ws(a.qkv, a.o, m->d_o, a.lse, m->delta, m->d_qkv, m->rope_cos, m->rope_sin,
+                             m->attn_ds_on ? m->attn_ds : nullptr, m->attn_ds_bytes, B, S, m->cfg.n_heads, m->cfg.n_kv_heads,
+                             m->d, &m->sc->err, st));
+  m->launches += 3;  // delta, dK / dV, dQ
+  prof_end(m, FT_PROF_ATTN_BWD, 2.0 * attention_flops(m, B, S), 3);
   if (m->cfg.qk_norm) {
     // d_q, d_k so far are gradients of the normalised heads: through the per-head norm, in place, and the two gain gradients
     FT_LAUNCH(FT_PROF_NORM, 6.0 * T * (hq + m->hkv),
@@ -829,6 +850,9 @@ ft_status run_forward_backward(ft_model* m, const int32_t* tok, const int32_t* l
                                bool fuse = false) {
   if (!m || !tok || !lab) return fail(m, FT_EINVAL, "null argument");
   if (B < 1 || S < 1 || B > m->cfg.max_batch || S > m->cfg.max_seq) return fail(m, FT_EINVAL, "B or S out of range");
+  if (with_bwd && m->attn_window > 0 &&
+      attention_window_scratch_bytes(B, S, m->cfg.n_heads, m->cfg.n_kv_heads, m->d, m->attn_window, m->attn_sinks) > m->attn_window_ws_bytes)
+    return fail(m, FT_ENOMEM, "the scratch of ft_set_attention_window is too small for this batch");
   const int T = B * S, h = m->h, V = m->V, L = m->L;
   cudaStream_t st = m->stream;
   m->lastB = B; m->lastS = S; m->have_bwd = false;
@@ -1254,6 +1278,35 @@ ft_status ft_set_overlap(ft_model* m, int32_t enable) {
 ft_status ft_set_attention_stored_ds(ft_model* m, int32_t enable) {
   if (!m) return FT_EINVAL;
   m->attn_ds_on = enable != 0;
+  if (m->graph_exec) { cudaGraphExecDestroy(m->graph_exec); m->graph_exec = nullptr; }  // captured with the old setting
+  return FT_OK;
+}
+
+size_t ft_attention_window_bytes(const ft_model* m, int32_t window, int32_t n_sinks) {
+  if (!m || window < 1 || n_sinks < 0) return 0;
+  const ft_config& c = m->cfg;
+  size_t most = 0;
+  // both ends of every 128-token block: what is kept grows with the blocks, how the work is split with what there is of it
+  for (int B = 1; B <= c.max_batch; ++B)
+    for (int S0 = 1; S0 <= c.max_seq; S0 += 128)
+      for (int S : {S0, S0 + 127 < c.max_seq ? S0 + 127 : c.max_seq}) {
+        const size_t n = attention_window_scratch_bytes(B, S, c.n_heads, c.n_kv_heads, m->d, window, n_sinks);
+        if (n > most) most = n;
+      }
+  return most;
+}
+
+ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, void* dev_scratch, uint64_t scratch_bytes) {
+  if (!m) return FT_EINVAL;
+  if (window < 0 || n_sinks < 0) return fail(m, FT_EINVAL, "window and n_sinks must not be negative");
+  if (window > 0) {
+    if (!dev_scratch || (reinterpret_cast<uintptr_t>(dev_scratch) & 255u) != 0) return fail(m, FT_EINVAL, "scratch: null or not 256-byte aligned");
+    if (scratch_bytes < ft_attention_window_bytes(m, window, n_sinks)) return fail(m, FT_ENOMEM, "scratch smaller than ft_attention_window_bytes");
+  }
+  m->attn_window = window;
+  m->attn_sinks = n_sinks;
+  m->attn_window_ws = window > 0 ? dev_scratch : nullptr;
+  m->attn_window_ws_bytes = window > 0 ? (size_t)scratch_bytes : 0;
   if (m->graph_exec) { cudaGraphExecDestroy(m->graph_exec); m->graph_exec = nullptr; }  // captured with the old setting
   return FT_OK;
 }
