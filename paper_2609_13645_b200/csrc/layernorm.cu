@@ -233,7 +233,8 @@ __device__ __forceinline__ bool inner_row(long long row, int rows, int h) { retu
 
 // ---------------------------------------------------------------- forward
 // y = (x - mean) rstd gain + bias.  The row stays in registers: first the mean, then the centred sum of squares (the
-// difference of sum(x^2) / h and mean^2 would lose the variance of rows whose mean is large).
+// difference of sum(x^2) / h and mean^2 would lose the variance of rows whose mean is large).  Bound by memory: 8192 x 2048
+// bf16 15.1 us (a copy of the same bytes 11.6), fp32 22.3 (6.0 TB/s); 8192 x 2047 bf16 31 us, by instructions.
 template <typename T, int VEC, int EPL, int NS, int MAXT>
 __global__ void __launch_bounds__(VEC == 0 && EPL <= 16 ? 1024 : MAXT == 256 ? 768 : MAXT)  // of all blocks of an SM (fwd_launch)
 layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, const T* __restrict__ bias, T* y, long long ldy,
@@ -308,7 +309,8 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
 // ---------------------------------------------------------------- backward
 // dx = rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid with g = dy gain; dgain = sum over rows of dy xhat, dbias of dy.
 // g and xhat stay in registers between the two sums of a row and its update.  A block leaves one partial row of dgain and
-// dbias, which a second kernel adds in block order.
+// dbias, which a second kernel adds in block order.  Bound by memory beside 8 us of start, drain and column sums: 8192 x
+// 2048 bf16 with resid 28.4 us for 134 MB; 8192 x 2047 bf16 64 us, by instructions.
 template <typename T, int VEC, int EPL, int NS, int MAXT>
 __global__ void __launch_bounds__(MAXT, 1)
 layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, const float* __restrict__ mean,
