@@ -136,7 +136,7 @@ ft_status ft_set_attention_stored_ds(ft_model* m, int32_t enable);
  * or j < n_sinks); see ft_k_attention_window_fwd.  The paper has no counterpart.  window 0 (the default): causal over the whole
  * sequence, with results that do not depend on this setting ever having been used.  dev_scratch: device memory of
  * ft_attention_window_bytes(m, window, n_sinks) bytes (0: refused), 256-byte aligned, the caller's, alive and not used by
- * anything else while the setting lasts; less returns FT_ENOMEM, and so does a step whose batch needs more.  Results are
+ * anything else while the setting lasts and steps enqueued under it run; less returns FT_ENOMEM, and so does a step whose batch needs more.  Results are
  * bit-identical from run to run and with recomputation, graph and second stream.  Changing it drops a captured graph. */
 size_t ft_attention_window_bytes(const ft_model* m, int32_t window, int32_t n_sinks);
 ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, void* dev_scratch, uint64_t scratch_bytes);
@@ -394,16 +394,17 @@ ft_status ft_k_attention_bwd_noalloc(const void* dev_qkv, const void* dev_o, con
 
 /* Causal attention over a sliding window with sink keys: query i sees key j iff j <= i and (i - j < window or
  * j < n_sinks).  window >= 1, n_sinks >= 0, either may exceed S (window >= S is ft_k_attention_fwd's mask).  Buffers as
- * in ft_k_attention_fwd, 16-byte aligned; work and traffic are linear in S.  Rows past the end of a shorter sequence
- * (right padding) are computed like any other and never reach earlier rows; every visible AND every masked value of a
- * 128-query tile has to be finite, because a masked key's value row is multiplied by 0. */
+ * in ft_k_attention_fwd, 16-byte aligned (dev_lse: 4); buffers that overlap are refused.  Work and traffic are linear in S.
+ * Rows past the end of a shorter sequence (right padding) are computed like any other and never reach earlier rows; every
+ * visible AND every masked value of a 128-query tile has to be finite, because a masked key's value row is multiplied by 0. */
 ft_status ft_k_attention_window_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
                                     int32_t n_kv_heads, int32_t head_dim, int32_t window, int32_t n_sinks, void* stream);
 
 /* Its backward, with the conventions of ft_k_attention_bwd (d_q, d_k rotated back when dev_cos / dev_sin [S, d/2] are
- * given).  dev_scratch: ft_k_attention_window_scratch_bytes(...) bytes (0: the shape is refused), 256-byte aligned,
- * caller-owned; contents on entry do not matter and are unspecified afterwards; two calls that share it must not overlap
- * on the GPU.  Too small a scratch returns FT_ENOMEM and launches nothing. */
+ * given, 16-byte aligned).  dev_scratch: ft_k_attention_window_scratch_bytes(...) bytes (0: the shape is refused), 256-byte
+ * aligned, caller-owned; contents on entry do not matter and are unspecified afterwards; two calls that share it must not overlap
+ * on the GPU.  Too small a scratch returns FT_ENOMEM, a gradient or scratch that overlaps another buffer FT_EINVAL; neither
+ * launches anything. */
 size_t ft_k_attention_window_scratch_bytes(int32_t B, int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                            int32_t window, int32_t n_sinks);
 ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* dev_o, const void* dev_do, const float* dev_lse,
@@ -414,7 +415,7 @@ ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* dev_o, cons
 /* LayerNorm of `rows` rows of h elements (1 <= h <= 16384), row r at dev_x + r * ldx (elements): mean and
  * rstd = 1 / sqrt(var + eps) of each row in fp32, y = R((x - mean) rstd gain + bias).  dtype of x, gain, bias and y: 0 bf16,
  * 1 fp32.  dev_bias may be NULL.  Any stride >= h and any alignment of the element; 16-byte aligned rows are fastest.
- * dev_y may be dev_x. */
+ * dev_y may be dev_x when their strides are equal; other overlaps of rows are the caller's mistake. */
 ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const void* dev_gain, const void* dev_bias, void* dev_y,
                              int64_t ldy, float* dev_mean, float* dev_rstd, int32_t rows, int32_t h, float eps,
                              int32_t dtype, void* stream);
@@ -422,7 +423,7 @@ ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const void* dev_gai
 /* Its backward from the saved statistics: with g = dy gain and xhat = (x - mean) rstd,
  * dx = R(rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid), dgain = sum_rows dy xhat and dbias = sum_rows dy in fp32 (fixed
  * summation order).  dev_resid (the gradient arriving along the residual connection) and dev_dbias may be NULL; dev_dx
- * may be dev_dy or dev_resid when their strides are equal.  dev_scratch: ft_k_layernorm_scratch_bytes(rows, h) bytes (0:
+ * may be dev_dy, dev_x or dev_resid when their strides are equal.  dev_scratch: ft_k_layernorm_scratch_bytes(rows, h) bytes (0:
  * refused), 16-byte aligned, used as above. */
 size_t ft_k_layernorm_scratch_bytes(int32_t rows, int32_t h);
 ft_status ft_k_layernorm_bwd(const void* dev_dy, int64_t lddy, const void* dev_x, int64_t ldx, const float* dev_mean,

@@ -461,6 +461,9 @@ def k_attention_bwd_noalloc(qkv, o, d_o, lse, dqkv, B, S, n_heads, n_kv, d, cos=
 # ---- decoder-block operators -------------------------------------------------------------------------------
 # Unlike the calls above these check the tensors they are given (type, shape, layout, device) before anything is launched;
 # a refused call raises ForgeStepError with status FT_EINVAL.
+_INT32_MAX = 2 ** 31 - 1
+
+
 def _refuse(what: str):
     raise ForgeStepError(FT_EINVAL, what)
 
@@ -516,6 +519,8 @@ def _window_shape(B, S, n_heads, n_kv, d, window, n_sinks):
 def attention_window_scratch_bytes(B, S, n_heads, n_kv, d, window, n_sinks) -> int:
     """Bytes of device scratch k_attention_window_bwd needs."""
     window, n_sinks = _window_shape(B, S, n_heads, n_kv, d, window, n_sinks)
+    if max(B, S, n_heads) > _INT32_MAX:
+        _refuse(f"B {B}, S {S}, heads {n_heads}: more than 32 bits hold")
     return int(lib().ft_k_attention_window_scratch_bytes(B, S, n_heads, n_kv, d, window, n_sinks))
 
 
@@ -557,7 +562,10 @@ def k_attention_window_bwd(qkv, o, d_o, lse, dqkv, scratch, B, S, n_heads, n_kv,
 def _rows_of(x):
     if x.dim() != 2:
         _refuse(f"x: expected [rows, h], got {tuple(x.shape)}")
-    return x.shape
+    rows, h = x.shape
+    if rows > _INT32_MAX or h > _INT32_MAX:
+        _refuse(f"x: {rows} x {h}, more than 32 bits hold")  # which ctypes would cut off without a word
+    return rows, h
 
 
 def k_layernorm_fwd(x, gain, bias, y, mean, rstd, eps=1e-5):
@@ -577,6 +585,8 @@ def k_layernorm_fwd(x, gain, bias, y, mean, rstd, eps=1e-5):
 
 def layernorm_scratch_bytes(rows, h) -> int:
     """Bytes of device scratch k_layernorm_bwd needs (0: the shape is refused)."""
+    if max(rows, h) > _INT32_MAX:
+        return 0
     return int(lib().ft_k_layernorm_scratch_bytes(rows, h))
 
 
@@ -606,6 +616,8 @@ def k_dropout_add(x, resid, y, p, seed, site, step=None, scale=1.0):
     torch = _torch or _import_torch()
     dt, dev, dtype = _row_dtype(x), _current_device(x), x.dtype
     rows, h = _rows_of(x)
+    if not 0 <= site <= _INT32_MAX:
+        _refuse(f"site {site}")
     px, ldx = _check_rows("x", x, dtype, rows, h, dev)
     py, ldy = _check_rows("y", y, dtype, rows, h, dev)
     pr, ldr = _check_rows("resid", resid, dtype, rows, h, dev) if resid is not None else (None, 0)

@@ -1475,12 +1475,29 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
 // =============================================================================== entry points
 namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+// bytes of the packed q, k, v (and of their gradients), of o (and dO) and of lse
+struct Sizes {
+  size_t qkv, o, lse;
+  Sizes(int32_t B, int32_t S, int32_t nh, int32_t nkv, int32_t d) {
+    const size_t rows = (size_t)B * S;
+    qkv = rows * (nh + 2 * nkv) * d * 2;
+    o = rows * nh * d * 2;
+    lse = rows * nh * 4;
+  }
+};
 ft_status status_of(cudaError_t e) { return e == cudaSuccess ? FT_OK : e == cudaErrorInvalidValue ? FT_EINVAL : FT_ECUDA; }
 }  // namespace
 
 extern "C" ft_status ft_k_attention_window_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
                                                int32_t n_kv_heads, int32_t head_dim, int32_t window, int32_t n_sinks, void* stream) {
   if (!dev_qkv || !dev_o || !dev_lse || !aligned16(dev_qkv) || !aligned16(dev_o)) return FT_EINVAL;
+  if (fs::attention_window_scratch_bytes(B, S, n_heads, n_kv_heads, head_dim, window, n_sinks) == 0) return FT_EINVAL;
+  const Sizes n(B, S, n_heads, n_kv_heads, head_dim);
+  if (overlap(dev_o, n.o, dev_qkv, n.qkv) || overlap(dev_lse, n.lse, dev_qkv, n.qkv) || overlap(dev_lse, n.lse, dev_o, n.o)) return FT_EINVAL;
   int* status = fs::attention_status_word();
   if (!status) return FT_ECUDA;
   return status_of(fs::attention_window_fwd(reinterpret_cast<const fs::bf16*>(dev_qkv), reinterpret_cast<fs::bf16*>(dev_o), dev_lse, B,
@@ -1504,6 +1521,11 @@ extern "C" ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* 
   const size_t need = fs::attention_window_scratch_bytes(B, S, n_heads, n_kv_heads, head_dim, window, n_sinks);
   if (need == 0) return FT_EINVAL;
   if (scratch_bytes < need) return FT_ENOMEM;
+  const Sizes n(B, S, n_heads, n_kv_heads, head_dim);
+  const struct { const void* p; size_t bytes; } inputs[] = {{dev_qkv, n.qkv}, {dev_o, n.o}, {dev_do, n.o}, {dev_lse, n.lse}};
+  for (const auto& in : inputs)
+    if (overlap(dev_dqkv, n.qkv, in.p, in.bytes) || overlap(dev_scratch, need, in.p, in.bytes)) return FT_EINVAL;
+  if (overlap(dev_dqkv, n.qkv, dev_scratch, need)) return FT_EINVAL;
   int* status = fs::attention_status_word();
   if (!status) return FT_ECUDA;
   return status_of(fs::attention_window_bwd(

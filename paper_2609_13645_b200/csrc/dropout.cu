@@ -189,6 +189,7 @@ extern "C" ft_status ft_k_dropout_add(const void* dev_x, int64_t ldx, const void
                                       const int64_t* dev_step, int32_t dtype, void* stream) {
   if (!dev_x || !dev_y || rows <= 0 || h <= 0 || (dtype != 0 && dtype != 1) || site < 0) return FT_EINVAL;
   if (!(p >= 0.f && p < 1.f) || !isfinite(scale) || ldx < h || ldy < h || (dev_resid && ldr < h)) return FT_EINVAL;
+  if (rows > 1 && ((dev_y == dev_x && ldy != ldx) || (dev_y == dev_resid && ldy != ldr))) return FT_EINVAL;
   const uintptr_t mask = dtype == 0 ? 1u : 3u;
   if (((uintptr_t)dev_x | (uintptr_t)dev_resid | (uintptr_t)dev_y) & mask || (uintptr_t)dev_step & 7u) return FT_EINVAL;
   cudaError_t e = fs::dropout_add(dev_x, ldx, dev_resid, ldr, dev_y, ldy, rows, h, p, scale, seed, site,

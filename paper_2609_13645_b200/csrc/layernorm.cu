@@ -587,6 +587,8 @@ namespace {
 bool rows_ok(int32_t rows, int32_t h, int32_t dtype) {
   return rows > 0 && h > 0 && h <= fs::kLayerNormMaxWidth && (dtype == 0 || dtype == 1);
 }
+// the same rows, or rows that start elsewhere: an output over an input has to lie as it does
+bool same_rows(const void* out, int64_t ldo, const void* in, int64_t ldi, int32_t rows) { return out != in || ldo == ldi || rows == 1; }
 bool elem_aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == 0 ? 1u : 3u)) == 0; }
 }  // namespace
 
@@ -594,7 +596,7 @@ extern "C" ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const vo
                                         int64_t ldy, float* dev_mean, float* dev_rstd, int32_t rows, int32_t h, float eps,
                                         int32_t dtype, void* stream) {
   if (!dev_x || !dev_gain || !dev_y || !dev_mean || !dev_rstd || !rows_ok(rows, h, dtype)) return FT_EINVAL;
-  if (ldx < h || ldy < h || !(eps >= 0.f)) return FT_EINVAL;
+  if (ldx < h || ldy < h || !(eps >= 0.f) || !same_rows(dev_y, ldy, dev_x, ldx, rows)) return FT_EINVAL;
   if (!elem_aligned(dev_x, dtype) || !elem_aligned(dev_gain, dtype) || !elem_aligned(dev_bias, dtype) || !elem_aligned(dev_y, dtype))
     return FT_EINVAL;
   cudaError_t e = fs::layernorm_fwd(dev_x, ldx, dev_gain, dev_bias, dev_y, ldy, dev_mean, dev_rstd, rows, h, eps, dtype,
@@ -611,6 +613,8 @@ extern "C" ft_status ft_k_layernorm_bwd(const void* dev_dy, int64_t lddy, const 
   if (!dev_dy || !dev_x || !dev_mean || !dev_rstd || !dev_gain || !dev_dx || !dev_dgain || !dev_scratch || !rows_ok(rows, h, dtype))
     return FT_EINVAL;
   if (lddy < h || ldx < h || lddx < h || (dev_resid && ldr < h)) return FT_EINVAL;
+  if (!same_rows(dev_dx, lddx, dev_dy, lddy, rows) || !same_rows(dev_dx, lddx, dev_x, ldx, rows) || !same_rows(dev_dx, lddx, dev_resid, ldr, rows))
+    return FT_EINVAL;
   if (!elem_aligned(dev_dy, dtype) || !elem_aligned(dev_x, dtype) || !elem_aligned(dev_gain, dtype) ||
       !elem_aligned(dev_resid, dtype) || !elem_aligned(dev_dx, dtype) || (reinterpret_cast<uintptr_t>(dev_scratch) & 15u) != 0)
     return FT_EINVAL;

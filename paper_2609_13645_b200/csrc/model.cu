@@ -1301,7 +1301,9 @@ ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, 
   if (window < 0 || n_sinks < 0) return fail(m, FT_EINVAL, "window and n_sinks must not be negative");
   if (window > 0) {
     if (!dev_scratch || (reinterpret_cast<uintptr_t>(dev_scratch) & 255u) != 0) return fail(m, FT_EINVAL, "scratch: null or not 256-byte aligned");
-    if (scratch_bytes < ft_attention_window_bytes(m, window, n_sinks)) return fail(m, FT_ENOMEM, "scratch smaller than ft_attention_window_bytes");
+    const size_t need = ft_attention_window_bytes(m, window, n_sinks);
+    if (need == 0) return fail(m, FT_EINVAL, "no windowed attention for this model's shape");
+    if (scratch_bytes < need) return fail(m, FT_ENOMEM, "scratch smaller than ft_attention_window_bytes");
   }
   m->attn_window = window;
   m->attn_sinks = n_sinks;

@@ -239,3 +239,7 @@ def test_every_tensor_at_an_alignment_of_its_own(rows, h, dtype):
     assert torch.equal(z, y) or _rel(z, y_ref) < tol
     Bn.k_layernorm_bwd(dy, x, mean, rstd, gain, r, r, dgain, dbias, scratch)
     assert float((r.double() - dx_ref).norm()) < tol * float(dx_ref.norm()) + slack
+    w, d = _at(x, h + 3, 1), _at(x, h + 3, 1)
+    Bn.k_layernorm_bwd(dy, w, mean, rstd, gain, None, d, dgain, dbias, scratch)
+    Bn.k_layernorm_bwd(dy, w, mean, rstd, gain, None, w, dgain, dbias, scratch)
+    assert torch.equal(w, d)

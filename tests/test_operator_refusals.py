@@ -130,6 +130,46 @@ def test_the_binding_refuses_host_tensors_and_bad_shapes(L):
         _refused(lambda: B.attention_window_scratch_bytes(*_att(**bad)))
 
 
+def test_attention_window_buffers_that_overlap(L):
+    need = L.ft_k_attention_window_scratch_bytes(*_att())
+    T, row = 2 * 200, (4 + 2 * 2) * 64 * 2
+    apart = [P + i * GIB for i in range(6)]  # qkv, o, dO, lse, dqkv, scratch
+
+    def bwd(p):
+        return L.ft_k_attention_window_bwd(p[0], p[1], p[2], p[3], p[4], None, None, p[5], need, *_att(), None)
+    for out in (4, 5):
+        for other in range(6):
+            if other != out:
+                for shift in (0, 256, -256):
+                    p = list(apart)
+                    p[out] = p[other] + shift
+                    assert bwd(p) == B.FT_EINVAL, (out, other, shift)
+    q = P
+    for o, lse in ((q, q + GIB), (q + GIB, q), (q + GIB, q + GIB), (q + T * row - 16, q + GIB), (q + GIB, q + T * row - 4)):
+        assert L.ft_k_attention_window_fwd(q, o, lse, *_att(), None) == B.FT_EINVAL
+
+
+def test_outputs_over_inputs_of_another_stride(L):
+    Q = P + GIB
+    assert L.ft_k_layernorm_fwd(P, 64, Q, None, P, 72, Q, Q, 8, 64, 1e-5, 0, None) == B.FT_EINVAL
+    bwd = lambda dy, lddy, x, r, ldr, dx, lddx: L.ft_k_layernorm_bwd(dy, lddy, x, 64, Q, Q, Q, r, ldr, dx, lddx, Q, Q, Q, GIB, 8, 64, 0, None)  # noqa: E731
+    assert bwd(P, 64, Q, None, 0, P, 72) == B.FT_EINVAL
+    assert bwd(Q, 64, Q, P, 64, P, 72) == B.FT_EINVAL
+    assert bwd(Q, 64, P, None, 0, P, 72) == B.FT_EINVAL
+    drop = lambda x, ldx, r, ldr, y, ldy: L.ft_k_dropout_add(x, ldx, r, ldr, y, ldy, 8, 64, 0.1, 1.0, 3, 0, None, 0, None)  # noqa: E731
+    assert drop(P, 64, None, 0, P, 72) == B.FT_EINVAL and drop(Q, 64, P, 80, P, 72) == B.FT_EINVAL
+
+
+def test_sizes_beyond_32_bits():
+    wide = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="meta")  # noqa: E731
+    for shape in ((2 ** 31, 1), (1, 2 ** 31)):
+        _refused(lambda: B._rows_of(wide(*shape)))
+    assert B._rows_of(wide(2 ** 31 - 1, 1)) == (2 ** 31 - 1, 1)
+    for kw in (dict(B=2 ** 32 + 2), dict(S=2 ** 32 + 200), dict(nh=2 ** 32 + 4)):
+        _refused(lambda: B.attention_window_scratch_bytes(*_att(**kw)))
+    assert B.layernorm_scratch_bytes(2 ** 32 + 5, 64) == 0 and B.layernorm_scratch_bytes(5, 2 ** 32 + 64) == 0
+
+
 @pytest.mark.gpu
 def test_the_binding_refuses_tensors_of_another_layout():
     dev = "cuda"
@@ -164,5 +204,9 @@ def test_the_binding_refuses_tensors_of_another_layout():
     _refused(lambda: B.k_layernorm_bwd(x, x, m, m, g, None, bf(8, 64), f(64), None, u8(16)[:0]))
     _refused(lambda: B.k_dropout_add(x, bf(8, 63), bf(8, 64), 0.1, 1, 0))
     _refused(lambda: B.k_dropout_add(x, None, bf(8, 64), 1.0, 1, 0))
+    _refused(lambda: B.k_dropout_add(x, None, bf(8, 64), 0.1, 1, 2 ** 32))
+    _refused(lambda: B.k_dropout_add(x, None, bf(8, 64), 0.1, 1, -1))
+    _refused(lambda: B.k_attention_window_bwd(qkv, o, o, lse, qkv, u8(need), 1, S, nh, nkv, d, 50, 2))
+    _refused(lambda: call(o=qkv.view(-1)[:S * nh * d]))
     _refused(lambda: B.k_dropout_add(x, None, bf(8, 64), 0.1, 1, 0, step=torch.zeros(1, dtype=torch.int32, device=dev)))
     _refused(lambda: B.k_dropout_add(x, None, bf(8, 64), 0.1, 1, 0, step=torch.zeros(1, dtype=torch.int64)))
