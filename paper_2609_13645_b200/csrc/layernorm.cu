@@ -309,13 +309,14 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
 // ---------------------------------------------------------------- backward
 // dx = rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid with g = dy gain; dgain = sum over rows of dy xhat, dbias of dy.
 // g and xhat stay in registers between the two sums of a row and its update.  A block leaves one partial row of dgain and
-// dbias, which a second kernel adds in block order.  Bound by memory beside 8 us of start, drain and column sums: 8192 x
+// dbias, which a second kernel adds in block order; small calls are one cluster of blocks (dgain given), which add them through
+// distributed shared memory.  Bound by memory beside 8 us of start, drain and column sums: 8192 x
 // 2048 bf16 with resid 28.4 us for 134 MB; 8192 x 2047 bf16 64 us, by instructions.
 template <typename T, int VEC, int EPL, int NS, int MAXT>
 __global__ void __launch_bounds__(MAXT, 1)
 layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, const float* __restrict__ mean,
                      const float* __restrict__ rstd, const T* __restrict__ gain, const T* resid, long long ldr, T* dx, long long lddx,
-                     float* __restrict__ partial, int rows, int h, int hp, int gw) {
+                     float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int rows, int h, int hp, int gw) {
   using Ring = typename RingOf<T, VEC, EPL, 3, NS>::type;
   constexpr int PAIRS = Ring::PAIRS;
   pdl_trigger();
@@ -406,9 +407,11 @@ layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, con
   // order.
   float* out = partial + (long long)blockIdx.x * 2 * hp;
   float* col = reinterpret_cast<float*>(ring_mem);
-  if (groups > 1) {
+  const bool one_cluster = dgain != nullptr;
+  if (groups > 1 || one_cluster) {
     if constexpr (NS > 0) async_wait<0>();
     __syncthreads();
+    if (one_cluster) out = col;
   }
   float* mine = groups > 1 ? col + (long long)group * 2 * hp : out;
 #pragma unroll
@@ -425,6 +428,25 @@ layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, con
       for (int g = 1; g < groups; ++g) t += col[(long long)g * 2 * hp + c];
       out[c] = t;
     }
+  }
+  if (one_cluster) {
+    cluster_sync_all();
+    for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x); c < 2 * hp; c += (int)(gridDim.x * blockDim.x)) {
+      const int rest = c - hp;
+      if ((rest < 0 && c >= h) || rest >= h || (rest >= 0 && dbias == nullptr)) continue;
+      float v[8], t = 0.f;
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r) {
+        uint32_t at;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(col + c)), "r"(r < gridDim.x ? r : 0u));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(at) : "memory");
+      }
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r)
+        if (r < gridDim.x) t += v[r];
+      if (rest < 0) dgain[c] = t; else dbias[rest] = t;
+    }
+    cluster_sync_all();  // nobody leaves while its sums are read
   }
 }
 
@@ -516,6 +538,12 @@ cudaError_t fwd_width(const void* x, int64_t ldx, const void* gain, const void* 
 #undef LN_FWD_W
 }
 
+// Rows that each group of 8 blocks may take for the backward pass to be ONE launch of a cluster of them.  Up to one it is quicker
+// on the GPU too (8 x 8192 bf16: 7.7 us in a graph against 14.2, 64 x 1024 6.7 and 6.9), at two the launch that a call saves
+// still outweighs it (64 x 2048: 9.6 us a call against 12.1, in a graph 8.5 against 7.4); EdgeRing's rows take longer (48 x 2047 at two
+// 13.9 against 12.1).
+constexpr int one_cluster_rows(int vec) { return vec == 0 ? 1 : 2; }
+
 template <typename T, int VEC, int EPL, int NS, int MAXT>
 cudaError_t bwd_launch(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd, const void* gain,
                        const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias, float* scratch, int rows,
@@ -524,17 +552,38 @@ cudaError_t bwd_launch(const void* dy, int64_t lddy, const void* x, int64_t ldx,
   auto kern = layernorm_bwd_kernel<T, VEC, EPL, NS, MAXT>;
   const int gw = (cover_of(h, VEC) + 32 * EPL - 1) / (32 * EPL), groups = MAXT / 32 / gw, threads = groups * gw * 32;
   const int hp = (h + 3) / 4 * 4;
-  int blocks = blocks_for(rows, groups, kSms);
-  if (VEC == 0) blocks = blocks_of_period(blocks, groups, rows, lddx);
-  const size_t col = groups > 1 ? (size_t)groups * 2 * hp * sizeof(float) : 0;  // at most 2 * MAXT * EPL floats
+  const size_t col = (size_t)groups * 2 * hp * sizeof(float);  // at most 2 * MAXT * EPL floats
   constexpr size_t most = Ring::bytes(MAXT) > 8 * MAXT * EPL ? Ring::bytes(MAXT) : 8 * MAXT * EPL;
   static unsigned long long smem_set = 0;
   cudaError_t e = ensure_dynamic_smem(kern, (int)most, smem_set);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kern, dim3(blocks), dim3(threads), Ring::bytes(threads) > col ? Ring::bytes(threads) : col, st,
-                 reinterpret_cast<const T*>(dy), (long long)lddy, reinterpret_cast<const T*>(x), (long long)ldx, mean, rstd,
-                 reinterpret_cast<const T*>(gain), reinterpret_cast<const T*>(resid), (long long)ldr, reinterpret_cast<T*>(dx),
-                 (long long)lddx, scratch, rows, h, hp, gw);
+  const T *dyp = reinterpret_cast<const T*>(dy), *xp = reinterpret_cast<const T*>(x), *gp = reinterpret_cast<const T*>(gain), *rp = reinterpret_cast<const T*>(resid);
+  T* dxp = reinterpret_cast<T*>(dx);
+  float* none = nullptr;
+  if (rows <= one_cluster_rows(VEC) * 8 * groups) {
+    int blocks = 1;
+    while (blocks < 8 && blocks * groups < rows) blocks *= 2;  // (8 blocks fit any period of rows)
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = Ring::bytes(threads) > col ? Ring::bytes(threads) : col;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = g_pdl ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, dyp, (long long)lddy, xp, (long long)ldx, mean, rstd, gp, rp, (long long)ldr, dxp, (long long)lddx,
+                              none, dgain, dbias, rows, h, hp, gw);
+  }
+  int blocks = blocks_for(rows, groups, kSms);
+  if (VEC == 0) blocks = blocks_of_period(blocks, groups, rows, lddx);
+  const size_t shared = groups > 1 && col > Ring::bytes(threads) ? col : Ring::bytes(threads);
+  e = launch_pdl(kern, dim3(blocks), dim3(threads), shared, st, dyp, (long long)lddy, xp, (long long)ldx, mean, rstd, gp, rp, (long long)ldr,
+                 dxp, (long long)lddx, scratch, none, none, rows, h, hp, gw);
   if (e != cudaSuccess) return e;
   const int cols = dbias != nullptr ? 2 * hp : hp;
   return launch_pdl(layernorm_colsum_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, scratch, dgain, dbias, blocks, h, hp);

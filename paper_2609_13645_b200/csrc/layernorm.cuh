@@ -13,7 +13,7 @@ cudaError_t layernorm_fwd(const void* x, int64_t ldx, const void* gain, const vo
                           float* rstd, int rows, int h, float eps, int dtype, cudaStream_t st);
 
 // dx = R(rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid), g = dy gain; dgain = sum dy xhat, dbias = sum dy (fp32, fixed
-// summation order; dbias may be null).  scratch: layernorm_scratch_bytes() bytes, 16-byte aligned.  Two launches.
+// summation order; dbias may be null).  scratch: layernorm_scratch_bytes() bytes, 16-byte aligned.  Two launches, or one of a cluster for few rows.
 size_t layernorm_scratch_bytes(int rows, int h);
 cudaError_t layernorm_bwd(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd,
                           const void* gain, const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias,
