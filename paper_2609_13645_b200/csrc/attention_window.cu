@@ -1390,9 +1390,9 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   const bool has_sink = sinks > 0 && pl.nxb > pl.nb;
   CUtensorMap tq128, tq64, td128, tsink, tout, tdo;
   if (!make_tmap_3d(&tq128, qkv, nqkv, S, B, nqkv, 128) || !make_tmap_3d(&tq64, qkv, nqkv, S, B, nqkv, 64) ||
-      !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128) || !make_tmap_3d(&tout, dqkv, nqkv, S, B, nqkv, 32) ||
-      !make_tmap_3d(&tdo, d_o, hq, S, B, hq, DkvCfg<D, BLOCK>::BQ))
+      !make_tmap_3d(&tout, dqkv, nqkv, S, B, nqkv, 32) || !make_tmap_3d(&tdo, d_o, hq, S, B, hq, DkvCfg<D, BLOCK>::BQ))
     return cudaErrorInvalidValue;
+  if (!l.stored && !make_tmap_3d(&td128, d_o, hq, S, B, hq, 128)) return cudaErrorInvalidValue;
   if (l.stored) {
     if (!has_sink) tsink = tq64;  // not read
     else if (!make_tmap_ds(&tsink, sink, sinks, (uint64_t)pl.nxb * 4, (uint64_t)pl.groups * n_rep)) return cudaErrorInvalidValue;
