@@ -234,11 +234,12 @@ __device__ __forceinline__ bool inner_row(long long row, int rows, int h) { retu
 // ---------------------------------------------------------------- forward
 // y = (x - mean) rstd gain + bias.  The row stays in registers: first the mean, then the centred sum of squares (the
 // difference of sum(x^2) / h and mean^2 would lose the variance of rows whose mean is large).  Bound by memory: 8192 x 2048
-// bf16 15.1 us (a copy of the same bytes 11.6), fp32 22.3 (6.0 TB/s); 8192 x 2047 bf16 31 us, by instructions.
-template <typename T, int VEC, int EPL, int NS, int MAXT>
+// bf16 11.3 us (5.9 TB/s), fp32 21.3 (6.3 TB/s); 8192 x 2047 bf16 30 us, by instructions.
+template <typename T, int VEC, int EPL, int NS, int MAXT, int GW>
 __global__ void __launch_bounds__(VEC == 0 && EPL <= 16 ? 1024 : MAXT == 256 ? 768 : MAXT)  // of all blocks of an SM (fwd_launch)
 layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, const T* __restrict__ bias, T* y, long long ldy,
-                     float* __restrict__ mean, float* __restrict__ rstd, int rows, int h, int gw, float eps) {
+                     float* __restrict__ mean, float* __restrict__ rstd, int rows, int h, int any_gw, float eps) {
+  const int gw = GW > 0 ? GW : any_gw;  // warps of a group
   using Ring = typename RingOf<T, VEC, EPL, 1, NS>::type;
   constexpr int PAIRS = Ring::PAIRS;
   pdl_trigger();
@@ -251,10 +252,12 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
   const long long step = (long long)gridDim.x * groups;
   long long row = (long long)blockIdx.x * groups + group, ahead = row;
   const Ring ring(ring_mem, gw * 32, gwarp * 32 + lane, h, y + row * ldy);
+  const T* x_ahead = x + ahead * ldx;
   auto fetch = [&](int stage) {
     const bool live = ahead < rows;
-    ring.fetch(stage, 0, x + (live ? ahead : 0) * ldx, live, inner_row(ahead, rows, h));
+    ring.fetch(stage, 0, live ? x_ahead : x, live, inner_row(ahead, rows, h));
     ahead += step;
+    x_ahead += step * ldx;
     async_commit();
   };
   // sum over the group; every thread gets the same bits.  The two sums of a row use different slots: each slot's readers
@@ -265,7 +268,8 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
     if (lane == 0) s_part[which][warp] = v;
     group_sync(group, gw);
     float t = s_part[which][group * gw];
-    for (int w = 1; w < gw; ++w) t += s_part[which][group * gw + w];
+#pragma unroll
+    for (int w = 1; w < (GW > 0 ? GW : gw); ++w) t += s_part[which][group * gw + w];
     return t;
   };
 #pragma unroll
@@ -291,7 +295,7 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
       v[i] = add2(v[i], m);
       ss = fma2(v[i], v[i], ss);
     }
-    const float rs = 1.0f / sqrtf(group_sum(ss, 1) * inv_h + eps);
+    const float rs = rsqrtf(group_sum(ss, 1) * inv_h + eps);  // within 2 units of the last place
     if (gwarp == 0 && lane == 0) {
       mean[row] = mu;
       rstd[row] = rs;
@@ -310,13 +314,14 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
 // dx = rstd (g - mean_h(g) - xhat mean_h(g xhat)) + resid with g = dy gain; dgain = sum over rows of dy xhat, dbias of dy.
 // g and xhat stay in registers between the two sums of a row and its update.  A block leaves one partial row of dgain and
 // dbias, which a second kernel adds in block order; small calls are one cluster of blocks (dgain given), which add them through
-// distributed shared memory.  Bound by memory beside 8 us of start, drain and column sums: 8192 x
-// 2048 bf16 with resid 28.4 us for 134 MB; 8192 x 2047 bf16 64 us, by instructions.
-template <typename T, int VEC, int EPL, int NS, int MAXT>
+// distributed shared memory.  Bound by memory beside 7 us of start, drain and column sums: 8192 x
+// 2048 bf16 with resid 27.8 us for 134 MB; 8192 x 2047 bf16 58 us, by instructions.
+template <typename T, int VEC, int EPL, int NS, int MAXT, int GW>
 __global__ void __launch_bounds__(MAXT, 1)
 layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, const float* __restrict__ mean,
                      const float* __restrict__ rstd, const T* __restrict__ gain, const T* resid, long long ldr, T* dx, long long lddx,
-                     float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int rows, int h, int hp, int gw) {
+                     float* __restrict__ partial, float* __restrict__ dgain, float* __restrict__ dbias, int rows, int h, int hp, int any_gw) {
+  const int gw = GW > 0 ? GW : any_gw;  // warps of a group
   using Ring = typename RingOf<T, VEC, EPL, 3, NS>::type;
   constexpr int PAIRS = Ring::PAIRS;
   pdl_trigger();
@@ -386,7 +391,8 @@ layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, con
     group_sync(group, gw);
     s1 = s_part[parity][group * gw][0];
     s2 = s_part[parity][group * gw][1];
-    for (int w = 1; w < gw; ++w) {
+#pragma unroll
+    for (int w = 1; w < (GW > 0 ? GW : gw); ++w) {
       s1 += s_part[parity][group * gw + w][0];
       s2 += s_part[parity][group * gw + w][1];
     }
@@ -504,18 +510,38 @@ int cover_of(int h, int vec) { return vec == 0 ? h + 15 : h; }
 // them is an instruction: fewer a thread, more threads; 4099 x 771 fp32 backward 17.7 us with 8, 28.7 with 16).
 int elements_per_thread(int cover, bool narrow) { return cover <= 256 || (narrow && cover <= 4096) ? 8 : cover <= 8192 ? 16 : 32; }
 
+// Warps of a group, if the kernel is compiled for that number (0: any).  The sums over a group are then straight code, and the
+// kernel's integer work shrinks: in a graph, 8192 x 2048 bf16 10.8 us forward (13.8 with any number) and 21.5 backward (22.7),
+// 2048 x 8192 bf16 14.8 (22.6) and 34.3 (35.5), 20000 x 771 fp32 29.5 (42) and 47.5 (56.5), 8192 x 2047 bf16 backward 46 (51).
+// Not where it was slower: EdgeRing forward (8192 x 2047: 34.7 against 30.8) and 16 warps of fp32 backward (2048 x 8192: 46.9
+// against 40.5).
+template <typename T, int VEC, int EPL, bool FWD>
+constexpr int fixed_warps(int gw) {
+  if (VEC == 0 && EPL == 16 && !FWD) return gw <= 5 ? gw : 0;
+  if (VEC * sizeof(T) == 16 && EPL == 16) return gw <= 4 || gw == 8 || (gw == 16 && (FWD || sizeof(T) == 2)) ? gw : 0;
+  if (VEC > 0 && VEC * sizeof(T) < 16 && EPL == 8) return gw == 2 || gw == 4 || gw == 8 ? gw : 0;
+  return 0;
+}
+
+// kern becomes the instantiation for gw warps, where there is one and a block of MAXT threads can hold them.
+#define LN_PICK(KERNEL, FWD, N) \
+  if constexpr (fixed_warps<T, VEC, EPL, FWD>(N) == N && N * 32 <= MAXT) { if (gw == N) kern = KERNEL<T, VEC, EPL, NS, MAXT, N>; }
+#define LN_PICK_ALL(K, F) \
+  LN_PICK(K, F, 1) LN_PICK(K, F, 2) LN_PICK(K, F, 3) LN_PICK(K, F, 4) LN_PICK(K, F, 5) LN_PICK(K, F, 8) LN_PICK(K, F, 16)
+
 template <typename T, int VEC, int EPL, int MAXT>
 cudaError_t fwd_launch(const void* x, int64_t ldx, const void* gain, const void* bias, void* y, int64_t ldy, float* mean, float* rstd,
                        int rows, int h, float eps, cudaStream_t st) {
   constexpr int NS = 3;
   using Ring = typename RingOf<T, VEC, EPL, 1, NS>::type;
-  auto kern = layernorm_fwd_kernel<T, VEC, EPL, NS, MAXT>;
-  const int gw = (cover_of(h, VEC) + 32 * EPL - 1) / (32 * EPL);
+  const int gw = (cover_of(h, VEC) + 32 * EPL - 1) / (32 * EPL), fixed = fixed_warps<T, VEC, EPL, true>(gw);
+  auto kern = layernorm_fwd_kernel<T, VEC, EPL, NS, MAXT, 0>;
+  LN_PICK_ALL(layernorm_fwd_kernel, true)
   int groups = MAXT / 32 / gw;
   if (rows <= kSms * groups) groups = 1;  // few rows: spread them over the SMs
   const int threads = groups * gw * 32;
-  static unsigned long long smem_set = 0;
-  cudaError_t e = ensure_dynamic_smem(kern, (int)Ring::bytes(MAXT), smem_set);
+  static unsigned long long smem_set[17] = {};  // by kernel
+  cudaError_t e = ensure_dynamic_smem(kern, (int)Ring::bytes(MAXT), smem_set[fixed]);
   if (e != cudaSuccess) return e;
   // 768 threads an SM (8192 x 2048 bf16: 3 blocks of 256 15.9 us, 1 of 512 20.2, 4 of 256 18.9; as many as fit 17.0).  EdgeRing,
   // which computes more for its bytes: 1024 (8192 x 2047: 30 us, 40 with 480)
@@ -549,13 +575,15 @@ cudaError_t bwd_launch(const void* dy, int64_t lddy, const void* x, int64_t ldx,
                        const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias, float* scratch, int rows,
                        int h, cudaStream_t st) {
   using Ring = typename RingOf<T, VEC, EPL, 3, NS>::type;
-  auto kern = layernorm_bwd_kernel<T, VEC, EPL, NS, MAXT>;
   const int gw = (cover_of(h, VEC) + 32 * EPL - 1) / (32 * EPL), groups = MAXT / 32 / gw, threads = groups * gw * 32;
+  const int fixed = fixed_warps<T, VEC, EPL, false>(gw);
+  auto kern = layernorm_bwd_kernel<T, VEC, EPL, NS, MAXT, 0>;
+  LN_PICK_ALL(layernorm_bwd_kernel, false)
   const int hp = (h + 3) / 4 * 4;
   const size_t col = (size_t)groups * 2 * hp * sizeof(float);  // at most 2 * MAXT * EPL floats
   constexpr size_t most = Ring::bytes(MAXT) > 8 * MAXT * EPL ? Ring::bytes(MAXT) : 8 * MAXT * EPL;
-  static unsigned long long smem_set = 0;
-  cudaError_t e = ensure_dynamic_smem(kern, (int)most, smem_set);
+  static unsigned long long smem_set[17] = {};  // by kernel
+  cudaError_t e = ensure_dynamic_smem(kern, (int)most, smem_set[fixed]);
   if (e != cudaSuccess) return e;
   const T *dyp = reinterpret_cast<const T*>(dy), *xp = reinterpret_cast<const T*>(x), *gp = reinterpret_cast<const T*>(gain), *rp = reinterpret_cast<const T*>(resid);
   T* dxp = reinterpret_cast<T*>(dx);
