@@ -234,7 +234,7 @@ __device__ __forceinline__ bool inner_row(long long row, int rows, int h) { retu
 // ---------------------------------------------------------------- forward
 // y = (x - mean) rstd gain + bias.  The row stays in registers: first the mean, then the centred sum of squares (the
 // difference of sum(x^2) / h and mean^2 would lose the variance of rows whose mean is large).  Bound by memory: 8192 x 2048
-// bf16 11.3 us (5.9 TB/s), fp32 21.3 (6.3 TB/s); 8192 x 2047 bf16 30 us, by instructions.
+// bf16 11.4 us (5.9 TB/s), fp32 21.3 (6.3 TB/s); 8192 x 2047 bf16 30 us, by instructions.
 template <typename T, int VEC, int EPL, int NS, int MAXT, int GW>
 __global__ void __launch_bounds__(VEC == 0 && EPL <= 16 ? 1024 : MAXT == 256 ? 768 : MAXT)  // of all blocks of an SM (fwd_launch)
 layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, const T* __restrict__ bias, T* y, long long ldy,
