@@ -1374,7 +1374,7 @@ Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l,
 
 template <int D, int BLOCK>
 cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs, const float* sn,
-                  uint8_t* scratch, int B, int S, int nh, int nkv, int window, int sinks, int* err, cudaStream_t st) {
+                  uint8_t* scratch, int B, int S, int nh, int nkv, int window, int sinks, int* err, cudaStream_t st, int& launches) {
   Scratch l;
   Plan pl = make_plan(B, S, nh, nkv, window, sinks, &l, D, BLOCK);
   static unsigned long long set_kv = 0, set_q = 0, set_r = 0;
@@ -1402,6 +1402,7 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   int dev = 0, sms = kSms;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   e = attention_delta(o, d_o, delta, B, S, nh, D, st);
+  launches = 1;
   const int per_round = pl.groups;
   Join jn{partial, dqkv, cs, sn, scale, pl.parts > 1 ? pl.nxb : pl.parts_sink > 1 ? pl.n_sink : 0};
   const Join none{partial, dqkv, cs, sn, scale, 0};
@@ -1410,19 +1411,23 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
     pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
     e = launch_pdl(attn_window_dkv_kernel<D, BLOCK>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D, BLOCK>::SMEM_BYTES, st,
                    tq128, DkvCfg<D, BLOCK>::BQ == 128 ? tq128 : tq64, tdo, tout, lse, delta, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
+    ++launches;
     if (e != cudaSuccess || !l.stored) continue;
     const bool last = g0 + per_round >= pl.all_groups;
     const long long ctas = (long long)pl.nxb * pl.groups * n_rep + (last ? jn.units(pl, D) : 0);
     e = launch_pdl(attn_window_dq_kernel<D>, dim3((unsigned)(ctas < 2 * sms ? ctas : 2 * sms)), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
                    (const bf16*)band, tsink, tq64, tout, cs, sn, pl, last ? jn : none, scale, err);
+    ++launches;
   }
   if (e != cudaSuccess) return e;
   if (!l.stored) {
     e = launch_pdl(attn_window_dq_recompute_kernel<D>, dim3((unsigned)(pl.nxb * nh * B)), dim3(DQR_THREADS), DqrCfg<D>::SMEM_BYTES, st,
                    tq128, tq64, td128, lse, delta, dqkv, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess) return e;
+    ++launches;
   }
   if (l.stored || jn.cut == 0) return cudaSuccess;
+  ++launches;
   return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)jn.units(pl, D)), dim3(256), 0, st, jn, pl);
 }
 
@@ -1461,13 +1466,15 @@ size_t attention_window_scratch_bytes(int B, int S, int nh, int nkv, int d, int 
 
 cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs,
                                  const float* sn, void* scratch, int B, int S, int nh, int nkv, int d, int window, int sinks, int* err,
-                                 cudaStream_t st) {
+                                 cudaStream_t st, int* launches) {
   if (!shape_ok(B, S, nh, nkv, d, window, sinks) || !err || (cs == nullptr) != (sn == nullptr)) return cudaErrorInvalidValue;
   clamp_mask(S, window, sinks);
   uint8_t* s = reinterpret_cast<uint8_t*>(scratch);
-  if (block_of(B, S, nh, d, window) == 64) return bwd_t<64, 64>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
-  if (d == 64) return bwd_t<64, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
-  return bwd_t<128, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st);
+  int unused = 0;
+  int& n = launches != nullptr ? *launches : unused;
+  if (block_of(B, S, nh, d, window) == 64) return bwd_t<64, 64>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st, n);
+  if (d == 64) return bwd_t<64, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st, n);
+  return bwd_t<128, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st, n);
 }
 
 }  // namespace fs

@@ -679,15 +679,16 @@ ft_status layer_backward(ft_model* m, int l, LayerActs& a, int B, int S) {
   if (s) return s;
   if ((s = wait_wgrad(m, 3))) return s;  // the previous layer's qkv weight gradient still reads d_qkv
   prof_begin(m);
+  int attn_launches = 3;  // delta, dK / dV, dQ
   if (m->attn_window > 0)
     FT_CUDA(attention_window_bwd(a.qkv, a.o, m->d_o, a.lse, m->d_qkv, m->rope_cos, m->rope_sin, m->attn_window_ws, B, S, m->cfg.n_heads,
-                                 m->cfg.n_kv_heads, m->d, m->attn_window, m->attn_sinks, &m->sc->err, st));
+                                 m->cfg.n_kv_heads, m->d, m->attn_window, m->attn_sinks, &m->sc->err, st, &attn_launches));
   else
     FT_CUDA(attention_bwd_ws(a.qkv, a.o, m->d_o, a.lse, m->delta, m->d_qkv, m->rope_cos, m->rope_sin,
                              m->attn_ds_on ? m->attn_ds : nullptr, m->attn_ds_bytes, B, S, m->cfg.n_heads, m->cfg.n_kv_heads,
                              m->d, &m->sc->err, st));
-  m->launches += 3;  // delta, dK / dV, dQ
-  prof_end(m, FT_PROF_ATTN_BWD, 2.0 * attention_flops(m, B, S), 3);
+  m->launches += attn_launches;
+  prof_end(m, FT_PROF_ATTN_BWD, 2.0 * attention_flops(m, B, S), attn_launches);
   if (m->cfg.qk_norm) {
     // d_q, d_k so far are gradients of the normalised heads: through the per-head norm, in place, and the two gain gradients
     FT_LAUNCH(FT_PROF_NORM, 6.0 * T * (hq + m->hkv),

@@ -1,0 +1,73 @@
+"""The windowed train step in every way its backward pass can be planned: dS^T of all heads at once, in two rounds of heads, and
+not stored at all.  What the model says it launched is compared with the kernels in a captured call of the same operator."""
+import pytest
+import torch
+
+import synth_inputs as SI
+from tests.parity_util import lib_config, oracle_config, to_dev
+
+pytestmark = pytest.mark.gpu
+
+# heads of 64 (query, kv), tokens, window, sinks.  A head's dS^T band over 4200 tokens is 33 x 33 blocks of 32 KB, 36 MB: twelve
+# heads on each of three kv heads are kept two kv heads at a time (1 GiB), 64 heads on one kv head (2.3 GB) not at all.
+PLANS = {"at_once": (4, 2, 300, 70, 5), "two_rounds": (36, 3, 4200, 4150, 0), "not_stored": (64, 1, 4200, 4150, 3)}
+
+
+def _kernels(call):
+    """Kernels in a captured call, counted by the driver."""
+    from cuda.bindings import runtime as rt
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    raw = graph.raw_cuda_graph()
+    err, _, n = rt.cudaGraphGetNodes(raw)
+    assert err == rt.cudaError_t.cudaSuccess
+    err, nodes, n = rt.cudaGraphGetNodes(raw, n)
+    assert err == rt.cudaError_t.cudaSuccess
+    kinds = [rt.cudaGraphNodeGetType(node)[1] for node in nodes[:n]]
+    return sum(k == rt.cudaGraphNodeType.cudaGraphNodeTypeKernel for k in kinds)
+
+
+def _backward_kernels(nh, nkv, S, window, sinks):
+    from paper_2609_13645_b200 import binding as Bn
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    qkv, o, lse = bf(S, (nh + 2 * nkv) * 64), bf(S, nh * 64), torch.zeros(1, nh, S, device="cuda")
+    if window == 0:
+        delta, grad = torch.zeros_like(lse), bf(*qkv.shape)
+        return _kernels(lambda: Bn.k_attention_bwd(qkv, o, o, lse, delta, grad, 1, S, nh, nkv, 64))
+    grad, size = bf(*qkv.shape), (1, S, nh, nkv, 64, window, sinks)
+    scratch = torch.empty(Bn.attention_window_scratch_bytes(*size), dtype=torch.uint8, device="cuda")
+    return _kernels(lambda: Bn.k_attention_window_bwd(qkv, o, o, lse, grad, scratch, *size))
+
+
+def _config(nh, nkv):
+    return oracle_config(n_layers=2, d_model=256, n_heads=nh, n_kv_heads=nkv, head_dim=64, d_ffn=688, vocab=1024)
+
+
+@pytest.mark.parametrize("plan", list(PLANS))
+def test_the_launch_counts_are_those_of_the_plan(plan):
+    from paper_2609_13645_b200 import binding as B
+    nh, nkv, S, window, sinks = PLANS[plan]
+    per_layer = _backward_kernels(nh, nkv, S, window, sinks)
+    assert per_layer == {"at_once": 3, "two_rounds": 5, "not_stored": 4}[plan]  # the latter with a kernel that adds partial sums
+    ocfg = _config(nh, nkv)
+    tok, lab = (to_dev(t) for t in SI.batch(ocfg.vocab, 1, S, "zipf", seed=3))
+    m = B.Model(lib_config(B, ocfg, 1, S), seed=2)
+    m.set_graph(False)
+
+    def launched():
+        m.train_step(tok, lab)  # the first step of a setting may make one-time launches
+        before = m.launch_count
+        m.train_step(tok, lab)
+        return m.launch_count - before
+    dense = launched()
+    m.set_attention_window(window, sinks)
+    assert launched() - dense == ocfg.n_layers * (per_layer - _backward_kernels(nh, nkv, S, 0, 0))
+    m.set_profiling(True)
+    m.train_step(tok, lab)
+    prof = m.get_profile()
+    assert prof["attn_bwd"]["launches"] == ocfg.n_layers * per_layer
+    assert prof["attn_fwd"]["launches"] == ocfg.n_layers
+    m.close()
