@@ -1529,9 +1529,11 @@ extern "C" ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* 
   if (need == 0) return FT_EINVAL;
   if (scratch_bytes < need) return FT_ENOMEM;
   const Sizes n(B, S, n_heads, n_kv_heads, head_dim);
-  const struct { const void* p; size_t bytes; } inputs[] = {{dev_qkv, n.qkv}, {dev_o, n.o}, {dev_do, n.o}, {dev_lse, n.lse}};
+  const size_t table = (size_t)S * (head_dim / 2) * sizeof(float);
+  const struct { const void* p; size_t bytes; } inputs[] = {{dev_qkv, n.qkv}, {dev_o, n.o}, {dev_do, n.o}, {dev_lse, n.lse},
+                                                            {dev_cos, table}, {dev_sin, table}};
   for (const auto& in : inputs)
-    if (overlap(dev_dqkv, n.qkv, in.p, in.bytes) || overlap(dev_scratch, need, in.p, in.bytes)) return FT_EINVAL;
+    if (in.p && (overlap(dev_dqkv, n.qkv, in.p, in.bytes) || overlap(dev_scratch, need, in.p, in.bytes))) return FT_EINVAL;
   if (overlap(dev_dqkv, n.qkv, dev_scratch, need)) return FT_EINVAL;
   int* status = fs::attention_status_word();
   if (!status) return FT_ECUDA;
