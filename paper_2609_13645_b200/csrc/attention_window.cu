@@ -1482,6 +1482,7 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
 // =============================================================================== entry points
 namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
@@ -1501,7 +1502,7 @@ ft_status status_of(cudaError_t e) { return e == cudaSuccess ? FT_OK : e == cuda
 
 extern "C" ft_status ft_k_attention_window_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
                                                int32_t n_kv_heads, int32_t head_dim, int32_t window, int32_t n_sinks, void* stream) {
-  if (!dev_qkv || !dev_o || !dev_lse || !aligned16(dev_qkv) || !aligned16(dev_o)) return FT_EINVAL;
+  if (!dev_qkv || !dev_o || !dev_lse || !aligned16(dev_qkv) || !aligned16(dev_o) || !aligned4(dev_lse)) return FT_EINVAL;
   if (fs::attention_window_scratch_bytes(B, S, n_heads, n_kv_heads, head_dim, window, n_sinks) == 0) return FT_EINVAL;
   const Sizes n(B, S, n_heads, n_kv_heads, head_dim);
   if (overlap(dev_o, n.o, dev_qkv, n.qkv) || overlap(dev_lse, n.lse, dev_qkv, n.qkv) || overlap(dev_lse, n.lse, dev_o, n.o)) return FT_EINVAL;
@@ -1523,7 +1524,7 @@ extern "C" ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* 
                                                int32_t head_dim, int32_t window, int32_t n_sinks, void* stream) {
   if (!dev_qkv || !dev_o || !dev_do || !dev_lse || !dev_dqkv || !dev_scratch) return FT_EINVAL;
   if (!aligned16(dev_qkv) || !aligned16(dev_o) || !aligned16(dev_do) || !aligned16(dev_dqkv) || !aligned16(dev_cos) ||
-      !aligned16(dev_sin) || (reinterpret_cast<uintptr_t>(dev_scratch) & 255u) != 0)
+      !aligned16(dev_sin) || !aligned4(dev_lse) || (reinterpret_cast<uintptr_t>(dev_scratch) & 255u) != 0)
     return FT_EINVAL;
   const size_t need = fs::attention_window_scratch_bytes(B, S, n_heads, n_kv_heads, head_dim, window, n_sinks);
   if (need == 0) return FT_EINVAL;

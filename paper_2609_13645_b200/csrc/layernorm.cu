@@ -677,6 +677,7 @@ bool rows_ok(int32_t rows, int32_t h, int32_t dtype) {
 // the same rows, or rows that start elsewhere: an output over an input has to lie as it does
 bool same_rows(const void* out, int64_t ldo, const void* in, int64_t ldi, int32_t rows) { return out != in || ldo == ldi || rows == 1; }
 bool elem_aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == 0 ? 1u : 3u)) == 0; }
+bool f32_aligned(const float* p) { return elem_aligned(p, 1); }
 }  // namespace
 
 extern "C" ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const void* dev_gain, const void* dev_bias, void* dev_y,
@@ -684,7 +685,8 @@ extern "C" ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const vo
                                         int32_t dtype, void* stream) {
   if (!dev_x || !dev_gain || !dev_y || !dev_mean || !dev_rstd || !rows_ok(rows, h, dtype)) return FT_EINVAL;
   if (ldx < h || ldy < h || !(eps >= 0.f) || !same_rows(dev_y, ldy, dev_x, ldx, rows)) return FT_EINVAL;
-  if (!elem_aligned(dev_x, dtype) || !elem_aligned(dev_gain, dtype) || !elem_aligned(dev_bias, dtype) || !elem_aligned(dev_y, dtype))
+  if (!elem_aligned(dev_x, dtype) || !elem_aligned(dev_gain, dtype) || !elem_aligned(dev_bias, dtype) || !elem_aligned(dev_y, dtype) ||
+      !f32_aligned(dev_mean) || !f32_aligned(dev_rstd))
     return FT_EINVAL;
   cudaError_t e = fs::layernorm_fwd(dev_x, ldx, dev_gain, dev_bias, dev_y, ldy, dev_mean, dev_rstd, rows, h, eps, dtype,
                                     reinterpret_cast<cudaStream_t>(stream));
@@ -703,7 +705,8 @@ extern "C" ft_status ft_k_layernorm_bwd(const void* dev_dy, int64_t lddy, const 
   if (!same_rows(dev_dx, lddx, dev_dy, lddy, rows) || !same_rows(dev_dx, lddx, dev_x, ldx, rows) || !same_rows(dev_dx, lddx, dev_resid, ldr, rows))
     return FT_EINVAL;
   if (!elem_aligned(dev_dy, dtype) || !elem_aligned(dev_x, dtype) || !elem_aligned(dev_gain, dtype) ||
-      !elem_aligned(dev_resid, dtype) || !elem_aligned(dev_dx, dtype) || (reinterpret_cast<uintptr_t>(dev_scratch) & 15u) != 0)
+      !elem_aligned(dev_resid, dtype) || !elem_aligned(dev_dx, dtype) || !f32_aligned(dev_mean) || !f32_aligned(dev_rstd) ||
+      !f32_aligned(dev_dgain) || !f32_aligned(dev_dbias) || (reinterpret_cast<uintptr_t>(dev_scratch) & 15u) != 0)
     return FT_EINVAL;
   if (scratch_bytes < fs::layernorm_scratch_bytes(rows, h)) return FT_ENOMEM;
   cudaError_t e = fs::layernorm_bwd(dev_dy, lddy, dev_x, ldx, dev_mean, dev_rstd, dev_gain, dev_resid, ldr, dev_dx, lddx, dev_dgain,

@@ -24,3 +24,18 @@ def test_rotation_tables_must_not_overlap_a_gradient_or_the_scratch(L):
                 p = list(apart)
                 p[t] = p[out] + at
                 assert L.ft_k_attention_window_bwd(*p, need, *SHAPE, None) == B.FT_EINVAL, (t, out, at)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_fp32_buffers_start_at_an_element(L, shift):
+    q, need = P + shift, L.ft_k_attention_window_scratch_bytes(*SHAPE)
+    a = [P + i * GIB for i in range(8)]
+    assert L.ft_k_attention_window_fwd(a[0], a[1], a[2] + shift, *SHAPE, None) == B.FT_EINVAL
+    assert L.ft_k_attention_window_bwd(a[0], a[1], a[2], a[3] + shift, a[4], None, None, a[7], need, *SHAPE, None) == B.FT_EINVAL
+    fwd = lambda mean, rstd: L.ft_k_layernorm_fwd(a[0], 64, a[1], None, a[2], 64, mean, rstd, 4, 64, 1e-5, 0, None)  # noqa: E731
+    assert fwd(q, a[4]) == B.FT_EINVAL and fwd(a[3], q) == B.FT_EINVAL
+    ok = dict(mean=a[2], rstd=a[3], dgain=a[5], dbias=a[6])
+    for name in ok:
+        b = dict(ok, **{name: q})
+        assert L.ft_k_layernorm_bwd(a[0], 64, a[1], 64, b["mean"], b["rstd"], a[4], None, 0, a[7], 64, b["dgain"], b["dbias"], a[7] + GIB,
+                                    GIB, 4, 64, 0, None) == B.FT_EINVAL, name
