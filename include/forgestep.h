@@ -437,9 +437,9 @@ ft_status ft_k_layernorm_bwd(const void* dev_dy, int64_t lddy, const void* dev_x
  * (lowest first) of mix(key ^ (i / 4) C3); kept iff bits >= t, t = min(65535, round(65536 p)), p' = t / 65536.  mix is the
  * splitmix64 finaliser, C1 = 0xD1B54A32D192ED03, C2 = 0xA24BAED4963EE407, C3 = 0x8CB92BA72F3D8DD7, all modulo 2^64.
  * site >= 0 tells the branches of a model apart; dev_step (int64 on the device, NULL: 0) is read when the kernel runs, so
- * that every replay of a captured step draws a new mask.  0 <= p < 1; a dropped element contributes exactly 0, whatever
- * its value.  dtype 0 bf16, 1 fp32; strides and alignment as in LayerNorm; dev_y may be dev_x or dev_resid when their
- * strides are equal. */
+ * that every replay of a captured step draws a new mask.  0 <= p < 1; scale / (1 - p') has to be finite in fp32; a dropped
+ * element contributes exactly 0, whatever its value.  dtype 0 bf16, 1 fp32; strides and alignment as in LayerNorm; dev_y may be
+ * dev_x or dev_resid when their strides are equal. */
 ft_status ft_k_dropout_add(const void* dev_x, int64_t ldx, const void* dev_resid, int64_t ldr, void* dev_y, int64_t ldy,
                            int32_t rows, int32_t h, float p, float scale, uint64_t seed, int32_t site,
                            const int64_t* dev_step, int32_t dtype, void* stream);

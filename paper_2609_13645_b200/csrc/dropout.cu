@@ -149,6 +149,10 @@ dropout_add_rows_kernel(const T* x, long long ldx, const T* resid, long long ldr
   }
 }
 
+// Elements whose 16 bits are below it are dropped; the factor of the others.
+uint32_t threshold(float p) { return (uint32_t)fmin(65535.0, floor((double)p * 65536.0 + 0.5)); }
+float kept_factor(float p, float scale) { return (float)((double)scale * 65536.0 / (65536.0 - (double)threshold(p))); }
+
 int blocks_for(long long chunks, int per_thread) {
   const long long want = (chunks + 256 * per_thread - 1) / (256 * per_thread);
   return (int)(want < 1 ? 1 : want < 148 * 16 ? want : 148 * 16);
@@ -175,8 +179,8 @@ cudaError_t launch(const void* x, int64_t ldx, const void* resid, int64_t ldr, v
 
 cudaError_t dropout_add(const void* x, int64_t ldx, const void* resid, int64_t ldr, void* y, int64_t ldy, int rows, int h, float p,
                         float scale, uint64_t seed, int32_t site, const long long* step, int dtype, cudaStream_t st) {
-  const uint32_t t = (uint32_t)fmin(65535.0, floor((double)p * 65536.0 + 0.5));
-  const float factor = (float)((double)scale * 65536.0 / (65536.0 - (double)t));
+  const uint32_t t = threshold(p);
+  const float factor = kept_factor(p, scale);
   const unsigned long long base = splitmix64(seed ^ ((unsigned long long)(long long)(site + 1ll) * kSite));
   if (dtype == 0) return launch<bf16>(x, ldx, resid, ldr, y, ldy, rows, h, base, step, t, factor, st);
   return launch<float>(x, ldx, resid, ldr, y, ldy, rows, h, base, step, t, factor, st);
@@ -188,7 +192,7 @@ extern "C" ft_status ft_k_dropout_add(const void* dev_x, int64_t ldx, const void
                                       int32_t rows, int32_t h, float p, float scale, uint64_t seed, int32_t site,
                                       const int64_t* dev_step, int32_t dtype, void* stream) {
   if (!dev_x || !dev_y || rows <= 0 || h <= 0 || (dtype != 0 && dtype != 1) || site < 0) return FT_EINVAL;
-  if (!(p >= 0.f && p < 1.f) || !isfinite(scale) || ldx < h || ldy < h || (dev_resid && ldr < h)) return FT_EINVAL;
+  if (!(p >= 0.f && p < 1.f) || !isfinite(scale) || !isfinite(fs::kept_factor(p, scale)) || ldx < h || ldy < h || (dev_resid && ldr < h)) return FT_EINVAL;
   if (rows > 1 && ((dev_y == dev_x && ldy != ldx) || (dev_y == dev_resid && ldy != ldr))) return FT_EINVAL;
   const uintptr_t mask = dtype == 0 ? 1u : 3u;
   if (((uintptr_t)dev_x | (uintptr_t)dev_resid | (uintptr_t)dev_y) & mask || (uintptr_t)dev_step & 7u) return FT_EINVAL;

@@ -39,3 +39,9 @@ def test_fp32_buffers_start_at_an_element(L, shift):
         b = dict(ok, **{name: q})
         assert L.ft_k_layernorm_bwd(a[0], 64, a[1], 64, b["mean"], b["rstd"], a[4], None, 0, a[7], 64, b["dgain"], b["dbias"], a[7] + GIB,
                                     GIB, 4, 64, 0, None) == B.FT_EINVAL, name
+
+
+def test_dropout_whose_factor_passes_fp32(L):
+    """scale / (1 - p') is one fp32 number: beyond its range an element of 0 would become 0 * inf."""
+    drop = lambda p, scale: L.ft_k_dropout_add(P, 64, None, 0, P + GIB, 64, 4, 64, p, scale, 1, 0, None, 0, None)  # noqa: E731
+    assert drop(0.5, 3e38) == B.FT_EINVAL and drop(0.99999, -1e36) == B.FT_EINVAL
