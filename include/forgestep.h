@@ -136,8 +136,8 @@ ft_status ft_set_attention_stored_ds(ft_model* m, int32_t enable);
  * or j < n_sinks); see ft_k_attention_window_fwd.  The paper has no counterpart.  window 0 (the default): causal over the whole
  * sequence, with results that do not depend on this setting ever having been used.  dev_scratch: device memory of
  * ft_attention_window_bytes(m, window, n_sinks) bytes (0: refused), 256-byte aligned, the caller's, alive and not used by
- * anything else while the setting lasts and steps enqueued under it run; less returns FT_ENOMEM, and so does a step whose batch needs more.  Results are
- * bit-identical from run to run and with recomputation, graph and second stream.  Changing it drops a captured graph. */
+ * anything else while the setting lasts and steps enqueued under it run; less returns FT_ENOMEM.  The size is that of the batch
+ * within max_batch and max_seq that needs most.  Results are bit-identical from run to run and with recomputation, graph and second stream.  Changing it drops a captured graph. */
 size_t ft_attention_window_bytes(const ft_model* m, int32_t window, int32_t n_sinks);
 ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, void* dev_scratch, uint64_t scratch_bytes);
 

@@ -1341,7 +1341,7 @@ Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l,
   const long long sink_len = p.n_sink > 0 ? n_rep * p.nxb : 0;
   const long long window_len = p.n_sink < p.nxb ? n_rep * p.blocks_seen(p.n_sink) : 0;
   long long total = window_len * (p.nxb - p.n_sink);
-  for (int x = 0; x < p.n_sink; ++x) total += n_rep * p.blocks_seen(x);
+  total += n_rep * ((long long)p.n_sink * p.nxb - (long long)p.n_sink * (p.n_sink - 1) / 2);  // sink block x: nxb - x
   total *= p.all_groups;
   const long long slots = kSms * (block == 64 ? 2 : 1);  // CTAs that run at a time
   const long long per_slot = (total + slots - 1) / slots;
@@ -1462,6 +1462,26 @@ size_t attention_window_scratch_bytes(int B, int S, int nh, int nkv, int d, int 
   Scratch l;
   make_plan(B, S, nh, nkv, window, sinks, &l, d, block_of(B, S, nh, d, window));
   return l.total;
+}
+
+// Not monotonic in S: a window or a number of sinks that S does not exceed is cut to it.  Within a 128-token block nothing but the
+// size of what is kept per token changes with S, upwards, on either side of S = window (up to it there are no sinks); while S is
+// within the sinks, the rows kept of them grow with S too, and the heads kept at a time step down: every S counts.
+size_t attention_window_most_scratch_bytes(int max_batch, int max_seq, int nh, int nkv, int d, int window, int sinks) {
+  size_t most = 0;
+  auto count = [&](int B, int S) {
+    const size_t n = attention_window_scratch_bytes(B, S, nh, nkv, d, window, sinks);
+    if (n > most) most = n;
+  };
+  for (int B = 1; B <= max_batch; ++B)
+    for (int S0 = 1; S0 <= max_seq; S0 += 128) {
+      const int S1 = max_seq - S0 < 127 ? max_seq : S0 + 127;
+      if (S0 <= window && window < S1) count(B, window);
+      const int every = S0 > window ? S0 : window + 1;  // the sinks count from here on
+      for (int S = every; S <= sinks && S < S1; ++S) count(B, S);
+      count(B, S1);
+    }
+  return most;
 }
 
 cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs,

@@ -1286,15 +1286,7 @@ ft_status ft_set_attention_stored_ds(ft_model* m, int32_t enable) {
 size_t ft_attention_window_bytes(const ft_model* m, int32_t window, int32_t n_sinks) {
   if (!m || window < 1 || n_sinks < 0) return 0;
   const ft_config& c = m->cfg;
-  size_t most = 0;
-  // both ends of every 128-token block: what is kept grows with the blocks, how the work is split with what there is of it
-  for (int B = 1; B <= c.max_batch; ++B)
-    for (int S0 = 1; S0 <= c.max_seq; S0 += 128)
-      for (int S : {S0, S0 + 127 < c.max_seq ? S0 + 127 : c.max_seq}) {
-        const size_t n = attention_window_scratch_bytes(B, S, c.n_heads, c.n_kv_heads, m->d, window, n_sinks);
-        if (n > most) most = n;
-      }
-  return most;
+  return attention_window_most_scratch_bytes(c.max_batch, c.max_seq, c.n_heads, c.n_kv_heads, m->d, window, n_sinks);
 }
 
 ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, void* dev_scratch, uint64_t scratch_bytes) {
