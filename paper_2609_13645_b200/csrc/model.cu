@@ -976,7 +976,7 @@ __global__ void wait_probe_kernel(long long limit_cycles, int* err) {
     mbar_fence_init();
   }
   __syncthreads();
-  if (threadIdx.x == 0) mbar_wait(smem_u32(&bar), 0u, &abort_flag, err, limit_cycles, 0x61);
+  if (threadIdx.x == 0) mbar_wait(smem_u32(&bar), 0u, &abort_flag, err, limit_cycles, 0x01);
   __syncthreads();
 }
 
