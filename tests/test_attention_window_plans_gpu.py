@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import synth_inputs as SI
-from tests.parity_util import lib_config, oracle_config, to_dev
+from oracle import decoder as D
+from tests.parity_util import lib_config, load_params, oracle_config, rel_l2, to_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +72,28 @@ def test_the_launch_counts_are_those_of_the_plan(plan):
     assert prof["attn_bwd"]["launches"] == ocfg.n_layers * per_layer
     assert prof["attn_fwd"]["launches"] == ocfg.n_layers
     m.close()
+
+
+@pytest.mark.parametrize("plan", list(PLANS))
+def test_a_step_whose_window_covers_the_sequence_is_the_causal_step(plan):
+    """The same definition through the windowed kernels and through the causal ones, which the oracle pins.  Each is allowed 2e-2
+    against the oracle on every gradient and 1e-2 on the loss.  The two share every rounding but those inside the attention
+    (P, dS), so that they are at most as far from one another as each may be from the oracle."""
+    from paper_2609_13645_b200 import binding as B
+    nh, nkv, S, _, _ = PLANS[plan]
+    ocfg = _config(nh, nkv)
+    params = D.init_params(ocfg, 11)
+    tok, lab = (to_dev(t) for t in SI.batch(ocfg.vocab, 1, S, "zipf", seed=4))
+    out = []
+    for window in (0, S):
+        m = B.Model(lib_config(B, ocfg, 1, S), seed=1)
+        m.set_attention_window(window)
+        m.set_fused_update(False)  # the gradients are compared
+        load_params(m, params)
+        loss, _ = m.train_step(tok, lab)
+        out.append((loss, {n: m.get_param(n, B.KIND_GRAD) for n in params}))
+        m.close()
+    (loss0, grads0), (loss1, grads1) = out
+    assert abs(loss0 - loss1) < 1e-2
+    for name in params:
+        assert rel_l2(grads1[name], grads0[name]) < 2e-2, name
