@@ -13,7 +13,7 @@
 #include <math.h>
 
 #include "../../include/forgestep.h"
-#include "layernorm.cuh"
+#include "dropout.cuh"
 #include "rows.cuh"
 
 namespace fs {

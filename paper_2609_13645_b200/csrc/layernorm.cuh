@@ -19,8 +19,4 @@ cudaError_t layernorm_bwd(const void* dy, int64_t lddy, const void* x, int64_t l
                           const void* gain, const void* resid, int64_t ldr, void* dx, int64_t lddx, float* dgain, float* dbias,
                           float* scratch, int rows, int h, int dtype, cudaStream_t st);
 
-// y[r, c] = R(resid[r, c] + scale / (1 - p) * keep(r h + c) * x[r, c]) (resid may be null: 0).
-cudaError_t dropout_add(const void* x, int64_t ldx, const void* resid, int64_t ldr, void* y, int64_t ldy, int rows, int h, float p,
-                        float scale, uint64_t seed, int32_t site, const long long* step, int dtype, cudaStream_t st);
-
 }  // namespace fs

@@ -16,9 +16,10 @@ namespace fs {
 template <typename T, int VEC>
 struct RowVec;
 
+// 2, 4 or 8 elements (bf16 rows that share less are put together from pieces)
 template <int VEC>
 struct RowVec<bf16, VEC> {
-  typedef typename std::conditional<VEC == 8, uint4, typename std::conditional<VEC == 4, uint2, typename std::conditional<VEC == 2, uint32_t, uint16_t>::type>::type>::type Raw;
+  typedef typename std::conditional<VEC == 8, uint4, typename std::conditional<VEC == 4, uint2, uint32_t>::type>::type Raw;
   static __device__ __forceinline__ Raw zero() {
     Raw r;
     memset(&r, 0, sizeof(r));
@@ -26,26 +27,18 @@ struct RowVec<bf16, VEC> {
   }
   static __device__ __forceinline__ Raw load(const bf16* p) { return *reinterpret_cast<const Raw*>(p); }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[VEC]) {
-    if constexpr (VEC == 1) {
-      f[0] = __uint_as_float((uint32_t)r << 16);
-    } else {
-      uint32_t w[VEC / 2];
-      memcpy(w, &r, sizeof(r));
+    uint32_t w[VEC / 2];
+    memcpy(w, &r, sizeof(r));
 #pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
-    }
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
   }
   static __device__ __forceinline__ void store(bf16* p, const float (&f)[VEC]) {
-    if constexpr (VEC == 1) {
-      *p = __float2bfloat16_rn(f[0]);
-    } else {
-      uint32_t w[VEC / 2];
+    uint32_t w[VEC / 2];
 #pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
-      Raw r;
-      memcpy(&r, w, sizeof(r));
-      *reinterpret_cast<Raw*>(p) = r;
-    }
+    for (int i = 0; i < VEC / 2; ++i) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+    Raw r;
+    memcpy(&r, w, sizeof(r));
+    *reinterpret_cast<Raw*>(p) = r;
   }
 };
 
