@@ -32,3 +32,11 @@ def flops_per_token(n_layers, d_model, n_heads, n_kv_heads, head_dim, d_ffn, voc
         out["mtp"] = 3 * (proj + ffn + core + head + 2 * (2 * h) * h)
     out["total"] = sum(out.values())
     return out
+
+
+def visible_pairs(S: int, window: int = 0, sinks: int = 0) -> int:
+    """(query, key) pairs that one head's mask lets through: j <= i and (i - j < window or j < sinks); window 0: causal."""
+    w = min(window, S) if window > 0 else S
+    left = S - w  # queries whose window has left keys behind: they see 1, 2, .. up to `sinks` of these
+    k = min(sinks, left)
+    return w * (w + 1) // 2 + left * w + k * (k + 1) // 2 + (left - k) * k

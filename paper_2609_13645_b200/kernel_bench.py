@@ -3,7 +3,9 @@
     python -m paper_2609_13645_b200.kernel_bench gemm --M 8192 --N 11264 --K 2048 --layout tn --iters 20
     python -m paper_2609_13645_b200.kernel_bench attn_fwd --B 4 --S 2048 --nh 16 --nkv 8 --d 128
     python -m paper_2609_13645_b200.kernel_bench attn_bwd --B 4 --S 2048 --nh 16 --nkv 8 --d 128
+    python -m paper_2609_13645_b200.kernel_bench attn_bwd --B 1 --S 16384 --window 1024 --sinks 4
     python -m paper_2609_13645_b200.kernel_bench step --workload c3_1b --layers 1 --iters 3
+    python -m paper_2609_13645_b200.kernel_bench step --workload c5_1b_long --layers 16 --window 1024 --sinks 4
 
 `step` runs whole train steps of a workload cut down to --layers layers (a few GB on the device): the in-situ target
 for ncu captures of the kernels that have no entry point of their own (norms, SwiGLU backward, cross-entropy, the
@@ -25,6 +27,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 def main():
     import torch
     from paper_2609_13645_b200 import binding as B
+    from paper_2609_13645_b200.flops import visible_pairs
 
     ap = argparse.ArgumentParser()
     ap.add_argument("kernel", choices=["gemm", "attn_fwd", "attn_bwd", "step"])
@@ -41,6 +44,8 @@ def main():
     ap.add_argument("--nh", type=int, default=16)
     ap.add_argument("--nkv", type=int, default=8)
     ap.add_argument("--d", type=int, default=128)
+    ap.add_argument("--window", type=int, default=0, help="attention and step: sliding window (0: causal over the whole sequence)")
+    ap.add_argument("--sinks", type=int, default=0, help="sink keys beside the window")
     ap.add_argument("--iters", type=int, default=10)
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--no-flush", action="store_true")
@@ -62,6 +67,8 @@ def main():
                             Bsz, S, recompute=w.get("recompute", 0), qk_norm=int(a.qk_norm))
         model = B.Model(cfg, seed=SI.WEIGHT_SEED)
         model.set_fused_update(not a.unfused)
+        if a.window:
+            model.set_attention_window(a.window, a.sinks)
         total = 0.0
         for it in range(a.warmup + a.iters):
             tok, lab = SI.batch(w["vocab"], Bsz, S, w["dist"], step=it)
@@ -71,8 +78,8 @@ def main():
             torch.cuda.synchronize()
             if it >= a.warmup:
                 total += e0.elapsed_time(e1)
-        print(json.dumps(dict(kernel="step", workload=a.workload, layers=a.layers, fused=not a.unfused, ms=total / a.iters,
-                              iters=a.iters)))
+        print(json.dumps(dict(kernel="step", workload=a.workload, layers=a.layers, fused=not a.unfused, window=a.window, sinks=a.sinks,
+                              ms=total / a.iters, iters=a.iters)))
         model.close()
         return
     flush = None if a.no_flush else torch.empty(256 << 20, dtype=torch.uint8, device=dev)
@@ -120,7 +127,15 @@ def main():
             if a.ws:
                 ds = torch.empty(Bsz * nh, S, S, dtype=torch.bfloat16, device=dev)
                 run = lambda: B.k_attention_bwd_ws(qkv, o, do, lse, delta, dqkv, ds, Bsz, S, nh, nkv, d)
-        desc = dict(kernel=a.kernel, B=Bsz, S=S, n_heads=nh, n_kv=nkv, d=d, ws=bool(a.ws))
+        if a.window:
+            size = (Bsz, S, nh, nkv, d, a.window, a.sinks)
+            flops = 4.0 * Bsz * nh * d * visible_pairs(S, a.window, a.sinks) * (2.5 if a.kernel == "attn_bwd" else 1.0)  # 2 and 5 products
+            B.k_attention_window_fwd(qkv, o, lse, *size)
+            run = lambda: B.k_attention_window_fwd(qkv, o, lse, *size)
+            if a.kernel == "attn_bwd":
+                scratch = torch.empty(B.attention_window_scratch_bytes(*size), dtype=torch.uint8, device=dev)
+                run = lambda: B.k_attention_window_bwd(qkv, o, do, lse, dqkv, scratch, *size)
+        desc = dict(kernel=a.kernel, B=Bsz, S=S, n_heads=nh, n_kv=nkv, d=d, ws=bool(a.ws), window=a.window, sinks=a.sinks)
 
     for _ in range(a.warmup):
         run()
