@@ -137,7 +137,8 @@ ft_status ft_set_attention_stored_ds(ft_model* m, int32_t enable);
  * sequence, with results that do not depend on this setting ever having been used.  dev_scratch: device memory of
  * ft_attention_window_bytes(m, window, n_sinks) bytes (0: refused), 256-byte aligned, the caller's, alive and not used by
  * anything else while the setting lasts and steps enqueued under it run; less returns FT_ENOMEM.  The size is that of the batch
- * within max_batch and max_seq that needs most.  Results are bit-identical from run to run and with recomputation, graph and second stream.  Changing it drops a captured graph. */
+ * within max_batch and max_seq that needs most.  Results are bit-identical from run to run and with recomputation, graph and
+ * second stream.  Changing it drops a captured graph. */
 size_t ft_attention_window_bytes(const ft_model* m, int32_t window, int32_t n_sinks);
 ft_status ft_set_attention_window(ft_model* m, int32_t window, int32_t n_sinks, void* dev_scratch, uint64_t scratch_bytes);
 
@@ -395,16 +396,18 @@ ft_status ft_k_attention_bwd_noalloc(const void* dev_qkv, const void* dev_o, con
 /* Causal attention over a sliding window with sink keys: query i sees key j iff j <= i and (i - j < window or
  * j < n_sinks).  window >= 1, n_sinks >= 0, either may exceed S (window >= S is ft_k_attention_fwd's mask).  Buffers as
  * in ft_k_attention_fwd, 16-byte aligned (dev_lse: 4); buffers that overlap are refused.  Work and traffic are linear in S.
- * Rows past the end of a shorter sequence (right padding) are computed like any other and never reach earlier rows; every
- * visible AND every masked value of a 128-query tile has to be finite, because a masked key's value row is multiplied by 0. */
+ * Rows past the end of a shorter sequence (right padding) are computed like any other and, while they are finite, never reach
+ * earlier rows.  Finite they have to be: a masked key's value row is multiplied by 0, so an infinity or NaN in v reaches every
+ * query of the 128-query tiles that stream its 64-key block.  (q and k of masked pairs may hold anything.) */
 ft_status ft_k_attention_window_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
                                     int32_t n_kv_heads, int32_t head_dim, int32_t window, int32_t n_sinks, void* stream);
 
 /* Its backward, with the conventions of ft_k_attention_bwd (d_q, d_k rotated back when dev_cos / dev_sin [S, d/2] are
  * given, 16-byte aligned).  dev_scratch: ft_k_attention_window_scratch_bytes(...) bytes (0: the shape is refused), 256-byte
  * aligned, caller-owned; contents on entry do not matter and are unspecified afterwards; two calls that share it must not overlap
- * on the GPU.  Too small a scratch returns FT_ENOMEM, a gradient or scratch that overlaps another buffer FT_EINVAL; neither
- * launches anything. */
+ * on the GPU.  Every element of q, k, v, o and dO, padding included, has to be finite: the weight of a masked pair is 0, but its
+ * products are formed, and 0 times an infinity or NaN reaches the gradients of both rows' 128-row blocks.  Too small a scratch
+ * returns FT_ENOMEM, a gradient or scratch that overlaps another buffer FT_EINVAL; neither launches anything. */
 size_t ft_k_attention_window_scratch_bytes(int32_t B, int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                            int32_t window, int32_t n_sinks);
 ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* dev_o, const void* dev_do, const float* dev_lse,

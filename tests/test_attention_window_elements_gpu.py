@@ -153,3 +153,19 @@ def test_masked_scores_that_overflow_when_taken_for_visible_ones(d, loud):
     # the 3e-3 of a tensor's 2-norm
     hq = nh * d
     assert n(o[163:], o1[63:]) < 6e-3 and n(got[163:, :hq], got1[63:, :hq]) < 6e-3 and n(got[163:, hq:], got1[63:, hq:]) < 6e-3
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_masked_keys_may_hold_anything_in_the_forward_pass(d, bad):
+    """Keys (not values) that a query does not see change no bit of its row, in the warps and blocks where others see them too."""
+    S, nh, nkv, window, sinks = 400, 2, 2, 64, 3
+    qkv, _ = _inputs(1, S, nh, nkv, d, seed=12)
+    o, lse = _fwd(qkv, 1, S, nh, nkv, d, window, sinks)
+    k = qkv.view(S, 3, nh, d)[:, 1]
+    k[40:50] = bad
+    k[200:203, :, ::3] = bad
+    o1, lse1 = _fwd(qkv, 1, S, nh, nkv, d, window, sinks)
+    clear = torch.ones(S, dtype=torch.bool, device="cuda")
+    clear[40:49 + window] = clear[200:202 + window] = False  # the queries that see one of them
+    assert torch.equal(o1[clear], o[clear]) and torch.equal(lse1[..., clear], lse[..., clear])
