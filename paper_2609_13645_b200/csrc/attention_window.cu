@@ -43,9 +43,13 @@ struct KeyRuns {
 // ============================================================================ forward
 // One CTA per (128 queries, head, batch row), two an SM; K and V blocks of 64 keys are streamed, S_{j+1} = Q K_{j+1}^T is
 // issued ahead of O += P_j V_j, four softmax warps hold a query row a thread.  Bound by that chain and by power: the tensor
-// pipe is 46 % busy, the exponential unit 45, instruction issue 45.  S 16384, 16 / 8 heads of 128, window 1024, 4 sinks: 159 us
-// (870 TFLOP/s of visible pairs), 187 sustained, where the clock drops by a sixth; B 4, S 2048, window 512: 52 and 58.  128-key blocks,
-// two query tiles a CTA, 8 or 16 softmax warps and persistent CTAs were all slower (188 to 220 us).
+// pipe is 46 % busy, the exponential unit 45, instruction issue 45.  S 16384, 16 / 8 heads of 128, window 1024, 4 sinks: 158 us
+// (845 TFLOP/s of visible pairs), 185 sustained, where the clock drops by a sixth; B 4, S 2048, window 512: 58; B 8, S 1024, 12
+// heads of 64, window 256: 24.  128-key blocks, two query tiles a CTA, 8 or 16 softmax warps and persistent CTAs were all
+// slower (188 to 220 us).
+// P is rounded to bf16 on its way to the tensor cores, which multiply it with the bf16 V; sums, references and the log-sum-exp are
+// fp32.  Against fp32 weights this takes the error of o from 1.6e-3 (its own rounding) to 2.2e-3 in the 2-norm, as in the
+// dense kernel; wider operands would halve the product's rate and double P's share of TMEM.
 enum { B_QFULL = 0, B_KFULL = 1, B_KEMPTY = 4, B_VFULL = 7, B_VEMPTY = 9, B_SFULL = 11, B_PFULL = 13, B_ODONE = 15,
        B_OFINAL = 16, B_COUNT = 17 };
 constexpr int FWD_THREADS = 224;  // Q + K producer, MMA issuer, 4 softmax warps, V producer
@@ -370,6 +374,8 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
 // fills both.)
 // dS^T also goes to a scratch array, from which dQ = dS K is one banded contraction (below): five products per pair of
 // blocks in all instead of the seven of a backward pass that computes S and dP twice.
+// P and dS enter their products, and the scratch, rounded to bf16 (the other operand's type): 2.4e-3 of a gradient's 2-norm where
+// the gradient's own rounding takes 1.7e-3.
 // A block of 128 queries takes 3150 cycles at D = 128, of which 2500 are the 320 KB that its products, loads and stores move
 // through shared memory; a CTA's start takes 6000 and its end 5000.  S 16384, 16 / 8 heads, window 1024: 335 us.  B 8, S 1024, 12
 // heads of 64, window 256: 48 us.
@@ -1324,7 +1330,8 @@ int window_blocks(int S, int window) {
 
 // Queries that a streamed block of the dK/dV kernel has.  Heads of 64: half blocks and two CTAs an SM, except in launches of
 // no more than six whole blocks an SM, whose CTAs run alone and want to be quick (B 8, S 1024, 12 heads: 57 against 69 us at
-// window 128, 67 against 79 at 256, 91 against 103 at 1024; B 3, S 1531, 6 heads on one: 41 against 37).
+// window 128, 67 against 79 at 256, 91 against 103 at 1024; B 3, S 1531, 6 heads on one: 41 against 37).  Those are launches of
+// 1536 blocks and more and of 864; on which side those between are better was not measured.
 int block_of(int B, int S, int nh, int d, int window) {
   return d == 64 && (long long)B * nh * ((S + 127) / 128) * window_blocks(S, window) > 6 * kSms ? 64 : 128;
 }

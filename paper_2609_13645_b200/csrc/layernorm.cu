@@ -315,7 +315,7 @@ layernorm_fwd_kernel(const T* x, long long ldx, const T* __restrict__ gain, cons
 // g and xhat stay in registers between the two sums of a row and its update.  A block leaves one partial row of dgain and
 // dbias, which a second kernel adds in block order; small calls are one cluster of blocks (dgain given), which add them through
 // distributed shared memory.  Bound by memory beside 7 us of start, drain and column sums: 8192 x
-// 2048 bf16 with resid 27.8 us for 134 MB; 8192 x 2047 bf16 58 us, by instructions.
+// 2048 bf16 with resid 27.8 us for 134 MB; 8192 x 2047 bf16 58 us with resid, 47 without, by instructions.
 template <typename T, int VEC, int EPL, int NS, int MAXT, int GW>
 __global__ void __launch_bounds__(MAXT, 1)
 layernorm_bwd_kernel(const T* dy, long long lddy, const T* x, long long ldx, const float* __restrict__ mean,
@@ -523,8 +523,10 @@ int elements_per_thread(int cover, bool narrow) { return cover <= 256 || (narrow
 // Warps of a group, if the kernel is compiled for that number (0: any).  The sums over a group are then straight code, and the
 // kernel's integer work shrinks: in a graph, 8192 x 2048 bf16 10.8 us forward (13.8 with any number) and 21.5 backward (22.7),
 // 2048 x 8192 bf16 14.8 (22.6) and 34.3 (35.5), 20000 x 771 fp32 29.5 (42) and 47.5 (56.5), 8192 x 2047 bf16 backward 46 (51).
-// Not where it was slower: EdgeRing forward (8192 x 2047: 34.7 against 30.8) and 16 warps of fp32 backward (2048 x 8192: 46.9
-// against 40.5).
+// (backward without resid).  Not where it was slower: EdgeRing forward (8192 x 2047: 34.7 against 30.8) and 16 warps of fp32
+// backward (2048 x 8192: 46.9 against 40.5).  The numbers compiled in are those of the widths timed: powers of two and odd
+// neighbours.  Widths between take the kernel for any number and pay for it: bf16 rows of 5, 10 and 12 warps, 8192 x 2560 24 us forward
+// and 31 backward, 8192 x 5120 67 and 68, 8192 x 6144 70 and 75.  Whether they gain as much was not tried.
 template <typename T, int VEC, int EPL, bool FWD>
 constexpr int fixed_warps(int gw) {
   if (VEC == 0 && EPL == 16 && !FWD) return gw <= 5 ? gw : 0;

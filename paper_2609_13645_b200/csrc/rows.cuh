@@ -2,7 +2,7 @@
 // floats.  VEC is the widest power of two, up to 16 bytes, that divides the row length, every row stride and every
 // pointer (row_vec).  Rows that share less are read as the aligned 16-byte pieces that hold them, and moved into place in
 // registers (realign), where single elements would take much longer (8192 x 2047 bf16: LayerNorm 41 us forward and 108
-// backward by elements, 30 and 58 by pieces; dropout into rows of 2048 76 and 33).
+// backward with a residual gradient by elements, 30 and 58 by pieces; dropout into rows of 2048 76 and 33).
 #pragma once
 #include <stdint.h>
 #include <string.h>
