@@ -1475,6 +1475,8 @@ size_t attention_window_scratch_bytes(int B, int S, int nh, int nkv, int d, int 
 // size of what is kept per token changes with S, upwards, on either side of S = window (up to it there are no sinks); while S is
 // within the sinks, the rows kept of them grow with S too, and the heads kept at a time step down: every S counts.
 size_t attention_window_most_scratch_bytes(int max_batch, int max_seq, int nh, int nkv, int d, int window, int sinks) {
+  if (window > max_seq) window = max_seq;
+  if (sinks > max_seq) sinks = max_seq;
   size_t most = 0;
   auto count = [&](int B, int S) {
     const size_t n = attention_window_scratch_bytes(B, S, nh, nkv, d, window, sinks);

@@ -31,3 +31,16 @@ def test_every_batch_fits_the_scratch_of_the_setting(nh, nkv, d, max_batch, max_
         loss, gn = m.train_step(tok, lab)
         assert math.isfinite(loss) and math.isfinite(gn)
     m.close()
+
+
+def test_masks_beyond_the_sequence_need_what_those_at_its_end_need():
+    from paper_2609_13645_b200 import binding as B
+    L, top = B.lib(), 2 ** 31 - 1
+    ocfg = oracle_config(n_layers=1, d_model=256, n_heads=4, n_kv_heads=2, head_dim=64, d_ffn=688, vocab=1024)
+    m = B.Model(lib_config(B, ocfg, 2, 700), seed=1)
+    for far, near in (((top, top), (700, 700)), ((top, 0), (700, 0)), ((30, top), (30, 700)), ((top - 1, 5), (700, 5))):
+        assert L.ft_attention_window_bytes(m._h, *far) == L.ft_attention_window_bytes(m._h, *near) > 0
+    m.set_attention_window(top, top)
+    tok, lab = (to_dev(t) for t in SI.batch(ocfg.vocab, 2, 700, "zipf", seed=2))
+    assert math.isfinite(m.train_step(tok, lab)[0])
+    m.close()
