@@ -398,7 +398,9 @@ ft_status ft_k_attention_bwd_noalloc(const void* dev_qkv, const void* dev_o, con
  * in ft_k_attention_fwd, 16-byte aligned (dev_lse: 4); buffers that overlap are refused.  Work and traffic are linear in S.
  * Rows past the end of a shorter sequence (right padding) are computed like any other and, while they are finite, never reach
  * earlier rows.  Finite they have to be: a masked key's value row is multiplied by 0, so an infinity or NaN in v reaches every
- * query of the 128-query tiles that stream its 64-key block.  (q and k of masked pairs may hold anything.) */
+ * query of the 128-query tiles that stream its 64-key block.  (q and k of masked pairs may hold anything.)  Visible scores
+ * |q . k| / sqrt(d) have to stay under 2^30, beyond which the spacing of fp32 numbers takes a row's weights out of range (NaN);
+ * the calls above have the same limit. */
 ft_status ft_k_attention_window_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
                                     int32_t n_kv_heads, int32_t head_dim, int32_t window, int32_t n_sinks, void* stream);
 
