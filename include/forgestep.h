@@ -419,7 +419,8 @@ ft_status ft_k_attention_window_bwd(const void* dev_qkv, const void* dev_o, cons
 
 /* LayerNorm of `rows` rows of h elements (1 <= h <= 16384), row r at dev_x + r * ldx (elements): mean and
  * rstd = 1 / sqrt(var + eps) of each row in fp32, y = R((x - mean) rstd gain + bias).  dtype of x, gain, bias and y: 0 bf16,
- * 1 fp32.  dev_bias may be NULL.  Any stride >= h and any alignment of the element; 16-byte aligned rows are fastest.
+ * 1 fp32.  dev_bias may be NULL.  Sums are fp32: a row's sum of squares about its mean has to stay within it (elements up to
+ * about 1e17).  Any stride >= h and any alignment of the element; 16-byte aligned rows are fastest.
  * dev_y may be dev_x when their strides are equal; other overlaps of rows are the caller's mistake. */
 ft_status ft_k_layernorm_fwd(const void* dev_x, int64_t ldx, const void* dev_gain, const void* dev_bias, void* dev_y,
                              int64_t ldy, float* dev_mean, float* dev_rstd, int32_t rows, int32_t h, float eps,
