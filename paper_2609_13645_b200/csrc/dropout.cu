@@ -8,8 +8,8 @@
 //
 // mix is the splitmix64 finaliser that also keys the weight initialiser.  16 bits an element put the drop rate within
 // 2^-17 of p (within 2^-16 above 65535.5 / 65536, where t stops at 65535); the factor of the kept elements is
-// 65536 / (65536 - t), the inverse of the rate really used, so the expectation is exact.  A word costs about 25 integer instructions for 16-24 bytes of traffic: the kernel stays bound
-// by memory (16384 x 2048 bf16 with a residual: 33.4 us, 6.0 TB/s).
+// 65536 / (65536 - t), the inverse of the rate really used, so the expectation is exact.  A word costs about 25 integer
+// instructions for 16-24 bytes of traffic: the kernel stays bound by memory (16384 x 2048 bf16 with a residual: 33.4 us, 6.0 TB/s).
 #include <math.h>
 
 #include "../../include/forgestep.h"
