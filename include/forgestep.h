@@ -341,8 +341,9 @@ ft_status ft_k_gemm_ws(const void* dev_A, int32_t a_mn, int64_t lda, const void*
 
 /* The single-kernel attention calls below keep their device status word inside the library (ft_k_gemm takes the
  * caller's dev_err instead).  ft_k_status waits for `stream`, then returns FT_ETIMEOUT if a bounded device-side wait ran
- * out in any ft_k_attention_* call (ft_k_attention_window_* among them) on the current device since the last ft_k_status (and
- * clears the word), else FT_OK.
+ * out in any ft_k_attention_* call (ft_k_attention_window_* and ft_k_attention_packed_* among them) on the current device since
+ * the last ft_k_status (and clears the word), FT_EINVAL if ft_k_packed_bounds or ft_k_rotary met a value on the device that they
+ * refuse, else FT_OK.
  * (Keeping host synchronisation out of the hot loop, Section "Sources of the Speedup", is why the calls themselves do not check.) */
 ft_status ft_k_status(void* stream);
 
@@ -449,6 +450,80 @@ ft_status ft_k_layernorm_bwd(const void* dev_dy, int64_t lddy, const void* dev_x
 ft_status ft_k_dropout_add(const void* dev_x, int64_t ldx, const void* dev_resid, int64_t ldr, void* dev_y, int64_t ldy,
                            int32_t rows, int32_t h, float p, float scale, uint64_t seed, int32_t site,
                            const int64_t* dev_step, int32_t dtype, void* stream);
+
+/* ---- Operators of a train step over packed documents, of the same manner.  A packed batch is one buffer of T rows (tokens) that
+ * holds documents of any length, empty ones among them, one behind the other; rows behind the last document are nobody's. ---- */
+
+/* The bounds of every row's document, once a batch, for all calls below.  dev_offsets: int32 [n_docs + 1], the documents' first
+ * rows and the end of the last, ascending from 0 to at most T.  dev_bounds: int32 [3][T]: the document's first row, the row behind
+ * its last, and the row's position in it (the dev_positions of ft_k_rotary); a row behind the last document has T, the number of
+ * rows in front of it, and 0.  longest: rows that a document has at most.  Offsets that break these rules are reported by
+ * ft_k_status as FT_EINVAL; what the calls below then compute is unspecified, within their buffers. */
+ft_status ft_k_packed_bounds(const int32_t* dev_offsets, int32_t n_docs, int32_t T, int32_t longest, int32_t* dev_bounds, void* stream);
+
+/* Causal attention inside the documents of a packed batch: row i sees the rows from its document's first one to itself.  Buffers
+ * and alignments as in ft_k_attention_window_fwd with B = 1 and S = T: qkv bf16 [T, (n_h + 2 n_kv) * d], o bf16 [T, n_h * d], lse fp32
+ * [n_h, T].  Rows behind the last document may hold anything, and are left as they were in dev_o and dev_lse.  Elements of rows
+ * inside documents have to be finite: a masked pair's weight is 0, but its product is formed, so an infinity or NaN can reach
+ * other rows, of a neighbouring document too, that share a tile of 128 rows with it. */
+ft_status ft_k_attention_packed_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, const int32_t* dev_bounds, int32_t T, int32_t n_heads,
+                                    int32_t n_kv_heads, int32_t head_dim, void* stream);
+
+/* Its backward, with the conventions of ft_k_attention_window_bwd.  longest: as given to ft_k_packed_bounds, or more; the scratch
+ * depends on it.  dev_cos, dev_sin: fp32 [longest, d / 2] tables by which d_q and d_k are rotated back at their rows' positions, or NULL.
+ * Rows of dev_dqkv behind the last document are left as they were. */
+size_t ft_k_attention_packed_scratch_bytes(int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t longest);
+ft_status ft_k_attention_packed_bwd(const void* dev_qkv, const void* dev_o, const void* dev_do, const float* dev_lse, void* dev_dqkv,
+                                    const int32_t* dev_bounds, const float* dev_cos, const float* dev_sin, void* dev_scratch,
+                                    uint64_t scratch_bytes, int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                    int32_t longest, void* stream);
+
+/* Rotary positions: of every head (head n of row r at dev_x + r * ldx + n * head_dim) the first rot elements are pairs, element i with
+ * i + rot / 2 (interleaved = 0) or 2 i with 2 i + 1 (1), and pair (a, b) becomes R(a c - b s), R(b c + a s), c and s being entry
+ * [position, i] of the tables (fp32 [n_positions, rot / 2]); inverse = 1 takes -s, which is the transpose and with it the backward
+ * pass.  The other elements are passed on.  dev_positions: int32 [rows] (NULL: the row's number, rows <= n_positions); a row whose
+ * position is outside [0, n_positions) is not written and ft_k_status returns FT_EINVAL.  dtype 0 bf16, 1 fp32; rot even; strides
+ * and alignment as in LayerNorm; dev_y may be dev_x when their strides are equal (heads of q and k inside packed qkv rows, for one). */
+ft_status ft_k_rotary(const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy, const int32_t* dev_positions, const float* dev_cos,
+                      const float* dev_sin, int32_t n_positions, int32_t rows, int32_t n_heads, int32_t head_dim, int32_t rot,
+                      int32_t interleaved, int32_t inverse, int32_t dtype, void* stream);
+
+/* Tables for it and for the attention's backward passes: cos and sin, times mscale, of p * theta^(-2 i / rot) / dev_factors[i] for
+ * p < n_positions and i < rot / 2 (dev_factors fp32, NULL: 1).  With factors and mscale this is the form of ft_set_rope_scaling, which
+ * linear, frequency-wise and LongRoPE stretching of the context share.  Angles are formed in 64 bits. */
+ft_status ft_k_rotary_tables(float* dev_cos, float* dev_sin, const float* dev_factors, int32_t n_positions, int32_t rot, float theta,
+                             float mscale, void* stream);
+
+/* One AdamW step over a list of tensors in one launch: g' = grad_scale g, m = beta1 m + (1 - beta1) g', v = beta2 v + (1 - beta2) g'^2,
+ * p -= lr (m_hat / (sqrt(v_hat) + eps) + weight_decay p), as in ft_apply_update; then the bf16 copy, if there is one.
+ * param_dtype and grad_dtype: 0 bf16, 1 fp32 (copies for fp32 parameters only; a bf16 parameter is rounded to nearest).
+ * state_bits 32: m and v are fp32.  8: runs of 256 elements share an fp32 scale (m_scale, v_scale: one for every run begun), and m
+ * and the SQUARE ROOT of v are kept as 8-bit floats (e4m3) times it.  scale = the run's greatest magnitude / 448 (below 2^-100: 0 and
+ * the run is 0); |x| / scale is rounded to floor(|x| / (scale u) + r) u, u its spacing of e4m3 values (at least 2^-9), r in [0, 1) 16 bits of a
+ * counter-based generator, and a v that is not 0 keeps at least 2^-9 scale.  r: with mix, C2 and C3 of ft_k_dropout_add and
+ * key = mix(mix(seed) ^ step C2), elements 2 k and 2 k + 1 take the 16-bit parts (lowest first) of mix(key ^ k C3) for m, v, m, v; elements
+ * are counted through the list, each tensor rounded up to 256.  Scales and codes are those
+ * of these formulas in 64 bits, bit for bit.  A non-finite element makes its run non-finite.
+ *   ft_k_adamw_plan_bytes   bytes of a plan (0: the list is refused: a null or misaligned buffer, buffers that overlap).
+ *   ft_k_adamw_plan         writes the plan to HOST memory (8-byte aligned); the caller copies it to the device, 16-byte
+ *                           aligned, and keeps both while steps run.  It holds the tensors' addresses; numel 0 is passed over.
+ *   ft_k_adamw              the step.  dev_step: int64 on the device, the number of this step, from 1 on; dev_lr and
+ *                           dev_grad_scale: floats on the device (NULL: lr, 1); all three are read when the kernel runs.
+ * Any alignment of the elements; 32-byte aligned arrays are fastest. */
+typedef struct {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale; /* state_bits 8, else NULL */
+  void* copy;               /* bf16 or NULL */
+  int64_t numel;
+  float weight_decay;
+} ft_adamw_tensor;
+size_t ft_k_adamw_plan_bytes(const ft_adamw_tensor* tensors, int32_t n_tensors, int32_t param_dtype, int32_t grad_dtype, int32_t state_bits);
+ft_status ft_k_adamw_plan(const ft_adamw_tensor* tensors, int32_t n_tensors, int32_t param_dtype, int32_t grad_dtype, int32_t state_bits,
+                          void* host_plan, uint64_t bytes);
+ft_status ft_k_adamw(const void* host_plan, const void* dev_plan, uint64_t plan_bytes, double lr, double beta1, double beta2, double eps,
+                     const int64_t* dev_step, const float* dev_lr, const float* dev_grad_scale, uint64_t seed, void* stream);
 
 #ifdef __cplusplus
 }

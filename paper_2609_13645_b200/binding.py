@@ -33,6 +33,11 @@ class FtConfig(C.Structure):
                [("mtp", C.c_int32), ("mtp_weight", C.c_float), ("dp_world", C.c_int32), ("dp_rank", C.c_int32)]
 
 
+class FtAdamWTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + \
+               [("numel", C.c_int64), ("weight_decay", C.c_float)]
+
+
 class ForgeStepError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 7 else status}: {msg}")
@@ -128,8 +133,20 @@ def lib():
         L.ft_k_layernorm_scratch_bytes.restype = C.c_size_t
         L.ft_k_layernorm_scratch_bytes.argtypes = [i32, i32]
         L.ft_k_dropout_add.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, C.c_float, C.c_float, C.c_uint64, i32, vp, i32, vp]
+        L.ft_k_packed_bounds.argtypes = [vp, i32, i32, i32, vp, vp]
+        L.ft_k_attention_packed_fwd.argtypes = [vp] * 4 + [i32] * 4 + [vp]
+        L.ft_k_attention_packed_scratch_bytes.restype = C.c_size_t
+        L.ft_k_attention_packed_scratch_bytes.argtypes = [i32] * 5
+        L.ft_k_attention_packed_bwd.argtypes = [vp] * 9 + [C.c_uint64] + [i32] * 5 + [vp]
+        L.ft_k_rotary.argtypes = [vp, i64, vp, i64, vp, vp, vp] + [i32] * 8 + [vp]
+        L.ft_k_rotary_tables.argtypes = [vp, vp, vp, i32, i32, C.c_float, C.c_float, vp]
+        L.ft_k_adamw_plan_bytes.restype = C.c_size_t
+        L.ft_k_adamw_plan_bytes.argtypes = [vp, i32, i32, i32, i32]
+        L.ft_k_adamw_plan.argtypes = [vp, i32, i32, i32, i32, vp, C.c_uint64]
+        L.ft_k_adamw.argtypes = [vp, vp, C.c_uint64] + [C.c_double] * 4 + [vp, vp, vp, C.c_uint64, vp]
         for name in ("ft_k_attention_window_fwd", "ft_k_attention_window_bwd", "ft_k_layernorm_fwd", "ft_k_layernorm_bwd",
-                     "ft_k_dropout_add"):
+                     "ft_k_dropout_add", "ft_k_packed_bounds", "ft_k_attention_packed_fwd", "ft_k_attention_packed_bwd", "ft_k_rotary",
+                     "ft_k_rotary_tables", "ft_k_adamw_plan", "ft_k_adamw"):
             getattr(L, name).restype = C.c_int
         for name in ("ft_init_model", "ft_train_step", "ft_train_step_host", "ft_forward_loss", "ft_forward_backward",
                      "ft_apply_update", "ft_param_info", "ft_get_param", "ft_set_param", "ft_get_step", "ft_set_step",
@@ -625,3 +642,184 @@ def k_dropout_add(x, resid, y, p, seed, site, step=None, scale=1.0):
                                 _check_flat("step", step, torch.int64, 1, dev) if step is not None else None, dt, _stream_of(dev))
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_dropout_add")
+
+
+# ---- operators of a train step over packed documents ---------------------------------------------------------
+def _packed_shape(T, n_heads, n_kv, d, longest=1):
+    if min(T, n_heads, n_kv, longest) < 1 or n_heads % n_kv or d not in (64, 128) or max(T, n_heads, longest) > _INT32_MAX:
+        _refuse(f"T {T}, heads {n_heads} / {n_kv} of {d}, longest document {longest}")
+
+
+def k_packed_bounds(offsets, bounds, T, longest=None):
+    """The bounds of every row's document in a packed batch of T rows, once a batch.  offsets: int32 [documents + 1], the first rows of
+    the documents and the end of the last, ascending from 0 to at most T (on the device; what breaks this is reported by k_status);
+    bounds: int32 [3, T]: first row, row behind the last, position in the document; longest: rows of a document, at most (None: T)."""
+    torch = _torch or _import_torch()
+    longest = T if longest is None else min(longest, T)
+    if not 1 <= T <= _INT32_MAX or longest < 1:
+        _refuse(f"T {T}, longest document {longest}")
+    dev = _current_device(offsets)
+    n = offsets.numel()
+    if n < 1 or n > _INT32_MAX:
+        _refuse(f"offsets: {n} elements")
+    st = lib().ft_k_packed_bounds(_check_flat("offsets", offsets, torch.int32, n, dev), n - 1, T, longest,
+                                  _check_flat("bounds", bounds, torch.int32, 3 * T, dev), _stream_of(dev))
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_packed_bounds")
+
+
+def attention_packed_scratch_bytes(T, n_heads, n_kv, d, longest=None) -> int:
+    """Bytes of device scratch k_attention_packed_bwd needs; longest: rows of a document, at most (None: T)."""
+    longest = T if longest is None else min(longest, T)
+    _packed_shape(T, n_heads, n_kv, d, longest)
+    return int(lib().ft_k_attention_packed_scratch_bytes(T, n_heads, n_kv, d, longest))
+
+
+def k_attention_packed_fwd(qkv, o, lse, bounds, T, n_heads, n_kv, d):
+    """Causal attention inside the documents of a packed batch: a row sees the rows from its document's first one to itself.  qkv
+    [T, (n_heads + 2 n_kv) d], o [T, n_heads d] (bf16), lse [n_heads, T] (fp32), bounds: what k_packed_bounds left.  Rows behind the
+    last document are left as they were."""
+    torch = _torch or _import_torch()
+    _packed_shape(T, n_heads, n_kv, d)
+    dev = _current_device(qkv)
+    st = lib().ft_k_attention_packed_fwd(_check_flat("qkv", qkv, torch.bfloat16, T * (n_heads + 2 * n_kv) * d, dev),
+                                         _check_flat("o", o, torch.bfloat16, T * n_heads * d, dev),
+                                         _check_flat("lse", lse, torch.float32, T * n_heads, dev),
+                                         _check_flat("bounds", bounds, torch.int32, 3 * T, dev), T, n_heads, n_kv, d, _stream_of(dev))
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_attention_packed_fwd")
+
+
+def k_attention_packed_bwd(qkv, o, d_o, lse, dqkv, bounds, scratch, T, n_heads, n_kv, d, longest=None, cos=None, sin=None):
+    """Gradient of k_attention_packed_fwd; scratch: a uint8 tensor of attention_packed_scratch_bytes(...) bytes; longest: as given to
+    k_packed_bounds, or more; cos, sin: fp32 [longest or more, d / 2] tables by which d_q and d_k are rotated back at their rows'
+    positions, or None.  Rows of dqkv behind the last document are left as they were."""
+    torch = _torch or _import_torch()
+    longest = T if longest is None else min(longest, T)
+    _packed_shape(T, n_heads, n_kv, d, longest)
+    dev, bf16, f32 = _current_device(qkv), torch.bfloat16, torch.float32
+    if (cos is None) != (sin is None):
+        _refuse("cos and sin: both or neither")
+    if cos is not None and (cos.numel() < longest * d // 2 or cos.shape != sin.shape):
+        _refuse(f"cos {tuple(cos.shape)}, sin {tuple(sin.shape)}: [{longest} or more, {d // 2}] are needed")
+    st = lib().ft_k_attention_packed_bwd(
+        _check_flat("qkv", qkv, bf16, T * (n_heads + 2 * n_kv) * d, dev), _check_flat("o", o, bf16, T * n_heads * d, dev),
+        _check_flat("d_o", d_o, bf16, T * n_heads * d, dev), _check_flat("lse", lse, f32, T * n_heads, dev),
+        _check_flat("dqkv", dqkv, bf16, T * (n_heads + 2 * n_kv) * d, dev), _check_flat("bounds", bounds, torch.int32, 3 * T, dev),
+        _check_flat("cos", cos, f32, cos.numel(), dev) if cos is not None else None,
+        _check_flat("sin", sin, f32, sin.numel(), dev) if sin is not None else None,
+        _check_flat("scratch", scratch, torch.uint8, scratch.numel(), dev), scratch.numel(), T, n_heads, n_kv, d, longest, _stream_of(dev))
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_attention_packed_bwd")
+
+
+def k_status():
+    """Waits for the current stream and raises if a call since the last k_status met a wait that ran out (FT_ETIMEOUT) or a value on
+    the device that it refuses (FT_EINVAL): offsets of documents, positions."""
+    st = lib().ft_k_status(_stream_ptr())
+    if st != FT_OK:
+        raise ForgeStepError(st, "a call on the device")
+
+
+def _check_tables(cos, sin, index):
+    torch = _torch or _import_torch()
+    if cos.dim() != 2 or cos.shape != sin.shape or min(cos.shape) < 1 or max(cos.shape) > _INT32_MAX // 2:
+        _refuse(f"cos {tuple(cos.shape)}, sin {tuple(sin.shape)}: [positions, pairs] are needed")
+    return (_check_flat("cos", cos, torch.float32, cos.numel(), index), _check_flat("sin", sin, torch.float32, sin.numel(), index))
+
+
+def k_rotary(x, y, cos, sin, n_heads, d, positions=None, interleaved=False, inverse=False):
+    """Rotary positions on the heads of x [rows, n_heads d] (bf16 or fp32, any row stride) into y, which may be x.  cos, sin: fp32
+    [positions, pairs] tables; the first 2 pairs elements of each head are rotated, as (i, i + pairs) or, interleaved, as
+    (2 i, 2 i + 1), the others passed on.  positions: int32 [rows] (None: the row's number); one outside the tables is reported by
+    k_status and its row not written.  inverse: the transpose, which is the backward pass."""
+    torch = _torch or _import_torch()
+    dt, dev, dtype = _row_dtype(x), _current_device(x), x.dtype
+    rows, h = _rows_of(x)
+    if n_heads < 1 or d < 1 or n_heads * d != h:
+        _refuse(f"x: {h} columns are not {n_heads} heads of {d}")
+    px, ldx = _check_rows("x", x, dtype, rows, h, dev)
+    py, ldy = _check_rows("y", y, dtype, rows, h, dev)
+    pc, ps = _check_tables(cos, sin, dev)
+    st = lib().ft_k_rotary(px, ldx, py, ldy, _check_flat("positions", positions, torch.int32, rows, dev) if positions is not None else None,
+                           pc, ps, cos.shape[0], rows, n_heads, d, 2 * cos.shape[1], 1 if interleaved else 0, 1 if inverse else 0, dt,
+                           _stream_of(dev))
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_rotary")
+
+
+def k_rotary_tables(cos, sin, theta=1e4, factors=None, mscale=1.0):
+    """Fills cos and sin (fp32 [positions, pairs]) with mscale times those of p theta^(-i / pairs) / factors[i] (fp32 [pairs], None: 1)."""
+    torch = _torch or _import_torch()
+    dev = _current_device(cos)
+    pc, ps = _check_tables(cos, sin, dev)
+    st = lib().ft_k_rotary_tables(pc, ps, _check_flat("factors", factors, torch.float32, cos.shape[1], dev) if factors is not None else None,
+                                  cos.shape[0], 2 * cos.shape[1], theta, mscale, _stream_of(dev))
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_rotary_tables")
+
+
+class AdamWPlan:
+    """The tensors that k_adamw steps through, handed over once.  Lists of equal length: params (all bf16 or all fp32), grads (all
+    bf16 or all fp32), first and second moments (all fp32, or all torch.float8_e4m3fn: m and the square root of v over the scales
+    m_scales, v_scales, fp32, one for every 256 elements begun), weight_decay (a number or a list), copies (bf16, or None).  All
+    contiguous and on one device.  The plan keeps them alive and steps through their memory as it is now: give gradients that
+    stay where they are."""
+
+    def __init__(self, params, grads, m, v, weight_decay=0.0, m_scales=None, v_scales=None, copies=None):
+        torch = _torch or _import_torch()
+        n = len(params)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        lists = [list(t) if t is not None else None for t in (params, grads, m, v, m_scales, v_scales, copies)]
+        if n == 0 or any(len(t) != n for t in lists if t is not None) or len(decay) != n:
+            _refuse("params, grads, m, v, weight_decay, scales and copies: lists of one length")
+        params, grads, m, v, m_scales, v_scales, copies = lists
+        pt, gt, mt = params[0].dtype, grads[0].dtype, m[0].dtype
+        param_dtype, grad_dtype = _row_dtype(params[0]), _row_dtype(grads[0])
+        if mt not in (torch.float32, torch.float8_e4m3fn):
+            _refuse(f"{mt}: moments are fp32 or float8_e4m3fn")
+        bits = 32 if mt == torch.float32 else 8
+        if (bits == 8) != (m_scales is not None) or (bits == 8) != (v_scales is not None):
+            _refuse("m_scales and v_scales belong to moments in 8 bits")
+        self.device_index = params[0].get_device()
+        if self.device_index < 0:
+            _refuse(f"tensors on {params[0].device}: a CUDA device is needed")
+        table = (FtAdamWTensor * n)()
+        for i in range(n):
+            e = params[i].numel()
+            runs = (e + 255) // 256
+            for field, what, t, dtype, count in (("param", "params", params, pt, e), ("grad", "grads", grads, gt, e), ("m", "m", m, mt, e),
+                                                 ("v", "v", v, mt, e), ("m_scale", "m_scales", m_scales, torch.float32, runs),
+                                                 ("v_scale", "v_scales", v_scales, torch.float32, runs),
+                                                 ("copy", "copies", copies, torch.bfloat16, e)):
+                if t is not None and t[i] is not None:
+                    setattr(table[i], field, _check_flat(f"{what}[{i}]", t[i], dtype, count, self.device_index))
+            table[i].numel, table[i].weight_decay = e, decay[i]
+        size = int(lib().ft_k_adamw_plan_bytes(table, n, param_dtype, grad_dtype, bits))
+        if size == 0:
+            _refuse("AdamWPlan: buffers that are missing, misaligned or overlap")
+        self.host = np.zeros((size + 7) // 8, dtype=np.uint64)
+        st = lib().ft_k_adamw_plan(table, n, param_dtype, grad_dtype, bits, self.host.ctypes.data, size)
+        if st != FT_OK:
+            raise ForgeStepError(st, "ft_k_adamw_plan")
+        self.bytes = size
+        self.device = torch.from_numpy(self.host.view(np.uint8)).to(params[0].device)
+        self._host_address, self._device_address = self.host.ctypes.data, self.device.data_ptr()
+        self.tensors = lists
+
+
+def k_adamw(plan, lr, beta1, beta2, eps, step, lr_tensor=None, grad_scale=None, seed=0):
+    """One AdamW step over the tensors of an AdamWPlan.  step: int64 tensor of one element, the number of this step, from 1 on;
+    lr_tensor and grad_scale: fp32 tensors of one element (None: lr, 1); all three are read when the kernel runs.  seed: of the
+    roundings of moments in 8 bits."""
+    torch = _torch or _import_torch()
+    dev = _current_device(step)
+    if plan.device_index != dev:
+        _refuse(f"a plan of cuda:{plan.device_index}, current device cuda:{dev}")
+    st = lib().ft_k_adamw(plan._host_address, plan._device_address, plan.bytes, lr, beta1, beta2, eps,
+                          _check_flat("step", step, torch.int64, 1, dev),
+                          _check_flat("lr_tensor", lr_tensor, torch.float32, 1, dev) if lr_tensor is not None else None,
+                          _check_flat("grad_scale", grad_scale, torch.float32, 1, dev) if grad_scale is not None else None,
+                          seed & 0xFFFFFFFFFFFFFFFF, _stream_of(dev))
+    if st != FT_OK:
+        raise ForgeStepError(st, "ft_k_adamw")

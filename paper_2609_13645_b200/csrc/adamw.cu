@@ -1,0 +1,519 @@
+// One AdamW step over many tensors in one launch, with moments in 32 bits or in 8.
+//
+// A plan lists the tensors once: the host cuts them into chunks of 2048 elements and writes both lists into a blob that the
+// caller copies to the device, so that a step costs one launch whatever the number and sizes of the tensors.  A block walks over
+// chunks; a thread holds 8 consecutive elements of each array.  Every array is read and written once: bound by memory (30
+// bytes an element with fp32 moments and gradients and a bf16 copy, 16.1 with 8-bit moments and bf16 gradients).
+//
+// Moments in 8 bits: runs of 256 elements share a scale, the run's greatest magnitude / 448; an element is a signed 8-bit float
+// (4 exponent and 3 mantissa bits, at most 448) times it.  The second moment is kept as its square root, which halves the
+// range that the codes have to span.  A moment moves by a fraction 1 - beta of its distance to the gradient's in a step, far less
+// than the 6 to 12 % between two codes: rounded to nearest it would never move again.  So codes are rounded up or down at
+// random, with probabilities that keep the mean, by 16 bits of a counter-based generator (the dropout masks' one):
+//   key = mix(mix(seed) ^ step C2),   word of elements 2 k and 2 k + 1 = mix(key ^ k C3)
+// whose 16-bit parts, lowest first, serve m and sqrt(v) of the first and of the second; elements count through the tensors in the
+// plan's order, each tensor rounded up to 256.  A second moment that is not 0 never becomes 0, which would let the next update
+// divide by epsilon alone.  The codes and scales are, bit for bit, those of this definition in 64 bits: fp32 decides where it can, and what it
+// leaves open is formed again in 64 bits.
+#include <cuda_fp8.h>
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+#include <vector>
+
+#include "../../include/forgestep.h"
+#include "adamw_math.cuh"
+#include "common.cuh"
+
+namespace fs {
+namespace {
+
+constexpr int kChunk = 2048, kThreads = 256, kRun = 256;
+constexpr uint32_t kMagic = 0x41445750u;
+constexpr unsigned long long kStepKey = 0xA24BAED4963EE407ull, kGroupKey = 0x8CB92BA72F3D8DD7ull;
+
+struct PlanHeader {
+  uint32_t magic;
+  int32_t n_tensors, n_chunks, param16, grad16, bits, pad0, pad1;
+  uint64_t bytes, chunk_offset;  // of the blob; of the chunk list in it
+};
+struct PlanTensor {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *ms, *vs;
+  bf16* copy;
+  long long n;
+  long long base;  // elements of the tensors before, each rounded up to 256
+  float wd;
+  int aligned;  // whole threads' elements can be moved as vectors
+};
+struct PlanChunk {
+  int tensor, index;
+};
+
+struct StepArgs {
+  float lr, eps;
+  double beta1, omb1, beta2, omb2, log_beta1, log_beta2;  // omb = 1 - beta
+  float b1[2], o1[2], b2[2], o2[2];                       // the first four in two fp32 parts
+  const long long* step;
+  const float *dev_lr, *grad_scale;
+  unsigned long long seed;
+};
+
+// ---- 8 consecutive elements of a thread
+__device__ __forceinline__ void load32(const void* p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void load8(const float* p, int n, bool vec, float (&f)[8]) {
+  if (vec) {
+    uint32_t w[8];
+    load32(p, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const bf16* p, int n, bool vec, float (&f)[8]) {
+  if (vec) {
+    const uint4 r = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? __bfloat162float(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, bool vec, const float (&f)[8]) {
+  if (vec) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(f[i]);
+    store32(p, w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = f[i];
+  }
+}
+__device__ __forceinline__ void store8(bf16* p, int n, bool vec, const float (&f)[8]) {
+  if (vec) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = __float2bfloat16_rn(f[i]);
+  }
+}
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, int n, bool vec) {
+  if (vec) return *reinterpret_cast<const uint2*>(p);
+  uint8_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = i < n ? p[i] : 0;
+  uint2 r;
+  memcpy(&r, b, 8);
+  return r;
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int n, bool vec, uint2 w) {
+  if (vec) {
+    *reinterpret_cast<uint2*>(p) = w;
+  } else {
+    uint8_t b[8];
+    memcpy(b, &w, 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = b[i];
+  }
+}
+
+// The values of 8 codes over a scale.
+__device__ __forceinline__ void decode(uint2 w, float scale, float (&f)[8]) {
+  const uint32_t h[2] = {w.x, w.y};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(h[i >> 1] >> (16 * (i & 1))), __NV_E4M3));
+    const float2 x = __half22float2(v);
+    f[2 * i] = x.x * scale;
+    f[2 * i + 1] = x.y * scale;
+  }
+}
+__device__ __forceinline__ float code_value(uint2 w, int i) {
+  const uint32_t code = (i < 4 ? w.x >> (8 * i) : w.y >> (8 * (i - 4))) & 0xffu;
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+__device__ __forceinline__ void put_code(uint2& w, int i, uint32_t code) {
+  const uint32_t at = 8 * (i & 3), keep = ~(0xffu << at);
+  if (i < 4) w.x = (w.x & keep) | code << at;
+  else w.y = (w.y & keep) | code << at;
+}
+
+// ---- numbers of two fp32 parts, about 45 bits
+struct Two {
+  float h, l;
+};
+__device__ __forceinline__ Two product(float a, float b) {
+  const float h = __fmul_rn(a, b);
+  return {h, __fmaf_rn(a, b, -h)};
+}
+__device__ __forceinline__ Two product(Two a, Two b) {
+  const Two p = product(a.h, b.h);
+  return {p.h, __fmaf_rn(a.h, b.l, __fmaf_rn(a.l, b.h, p.l))};
+}
+__device__ __forceinline__ Two sum(Two a, Two b) {
+  const float s = __fadd_rn(a.h, b.h), t = __fsub_rn(s, a.h);
+  const float e = __fadd_rn(__fadd_rn(__fsub_rn(a.h, __fsub_rn(s, t)), __fsub_rn(b.h, t)), __fadd_rn(a.l, b.l));
+  const float h = __fadd_rn(s, e);
+  return {h, __fsub_rn(e, __fsub_rn(h, s))};
+}
+__device__ __forceinline__ Two root(Two a) {  // a.h > 0
+  float r, inv;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(a.h));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(r));
+  const float e = __fmul_rn(__fadd_rn(__fmaf_rn(-r, r, a.h), a.l), 0.5f * inv), h = __fadd_rn(r, e);
+  return {h, __fsub_rn(e, __fsub_rn(h, r))};
+}
+
+// A moment (ROOT: the second one's root) of an element from its code, scale and gradient: in two parts, and in 64 bits as the
+// definition orders the operations.
+template <bool ROOT>
+__device__ __forceinline__ Two moment_two(const StepArgs& a, float code, float scale, float g, float clip) {
+  const Two kept = product(code, scale), d = product(g, clip);
+  if (!ROOT) return sum(product(Two{a.b1[0], a.b1[1]}, kept), product(Two{a.o1[0], a.o1[1]}, d));
+  return root(sum(product(Two{a.b2[0], a.b2[1]}, product(kept, kept)), product(product(Two{a.o2[0], a.o2[1]}, d), d)));
+}
+template <bool ROOT>
+__device__ __forceinline__ double moment_64(const StepArgs& a, float code, float scale, float g, float clip) {
+  const double kept = __dmul_rn((double)code, (double)scale), d = __dmul_rn((double)g, (double)clip);
+  if (!ROOT) return __dadd_rn(__dmul_rn(a.beta1, kept), __dmul_rn(a.omb1, d));
+  return __dsqrt_rn(__dadd_rn(__dmul_rn(a.beta2, __dmul_rn(kept, kept)), __dmul_rn(__dmul_rn(a.omb2, d), d)));
+}
+
+// ---- codes without sign
+// floor(|y| / step + bits / 65536) steps.  From 2^-6 on a step is the last of 3 mantissa bits, below it is 2^-9: there 2^-6 is added
+// first, which gives the number the same step.  rest: what the floor cuts off, in 2^-20 steps; b: the number it was cut off from.
+__device__ __forceinline__ uint32_t round_random(float a, uint32_t bits, uint32_t& rest, float& b) {
+  const bool small = a < 0.015625f;
+  b = small ? a + 0.015625f : a;
+  const uint32_t u = __float_as_uint(b) + (bits << 4);
+  rest = u & 0xfffffu;
+  return min((u >> 20) - (small ? 968u : 960u), 126u);
+}
+__device__ __forceinline__ uint32_t round_random(double a, uint32_t bits) {
+  const int e = a < 0.015625 ? 0 : (__double2hiint(a) >> 20) - 1023 + 6;  // binades above 2^-6
+  const double steps = a * __hiloint2double((1023 + 9 - e) << 20, 0);     // 8 to 16 of them in a binade, up to 8 below
+  return min((uint32_t)((int)floor(steps + (double)bits * (1.0 / 65536.0)) + 8 * e), 126u);
+}
+
+// A run's greatest element: its fp32 bits, and the scale that belongs to it in 64 bits.  Infinities and NaN are the greatest bit patterns.
+// Every lane brings its own greatest element (index, gradient); the winner among them is found on their values in two parts.
+struct RunTop {
+  uint32_t own, top;  // bits of the lane's, of the run's
+  int index;          // of the lane's
+  float g;
+  float scale;  // 0: the run is 0; infinite or NaN: so is the run
+  __device__ __forceinline__ bool coded() const { return top >= 0x0d800000u && top < 0x7f800000u; }  // from 2^-100 on
+};
+// That scale in 64 bits, from the elements within a few roundings of the greatest fp32 one.
+template <bool ROOT>
+__device__ __noinline__ double run_unit(const RunTop& t, const StepArgs& a, uint2 codes, float scale, float clip) {
+  double most = t.own >= t.top - 64u ? fabs(moment_64<ROOT>(a, code_value(codes, t.index), scale, t.g, clip)) : 0.0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
+  return __dmul_rn(most, 1.0 / 448.0);
+}
+template <bool ROOT>
+__device__ __forceinline__ RunTop run_top(const float (&x)[8], const float (&g)[8], const StepArgs& a, uint2 codes, float scale, float clip) {
+  RunTop t{0u, 0u, 0, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
+    if (bits > t.own) { t.own = bits; t.index = i; t.g = g[i]; }
+  }
+  t.top = __reduce_max_sync(0xffffffffu, t.own);
+  if (t.coded()) {
+    const Two v = moment_two<ROOT>(a, code_value(codes, t.index), scale, t.g, clip);
+    const uint32_t h = t.own >= t.top - 64u ? __float_as_uint(v.h) & 0x7fffffffu : 0u, most = __reduce_max_sync(0xffffffffu, h);
+    const float l = h == most ? (v.h < 0.f ? -v.l : v.l) : -INFINITY;
+    const uint32_t k = __float_as_uint(l), order = k >> 31 ? ~k : k | 0x80000000u;  // floats as ordered integers
+    const uint32_t best = __reduce_max_sync(0xffffffffu, order);
+    const Two m{__uint_as_float(most), __uint_as_float(best >> 31 ? best & 0x7fffffffu : ~best)};
+    const Two s = product(m, Two{1.f / 448.f, (float)(1.0 / 448.0 - (double)(1.f / 448.f))});
+    t.scale = __fadd_rn(s.h, s.l);
+    // Half way between two fp32 numbers but for the last places of 64 bits (one run in a thousand: the betas are decimal fractions,
+    // whose multiples of fp32 numbers land there)
+    const float half_step = __uint_as_float(__float_as_uint(t.scale) & 0x7f800000u) * 5.9604645e-8f;
+    if (fabsf(fabsf(__fadd_rn(__fsub_rn(s.h, t.scale), s.l)) - half_step) < half_step * 1e-3f) t.scale = (float)run_unit<ROOT>(t, a, codes, scale, clip);
+  } else if (t.top >= 0x7f800000u) {
+    t.scale = __uint_as_float(t.top);
+  }
+  return t;
+}
+// Codes that fp32 leaves open (bits of `close`), formed in 64 bits.
+template <bool ROOT, typename G>
+__device__ __noinline__ uint2 settle(uint2 codes, uint32_t close, const RunTop& t, const StepArgs& a, uint2 old, float scale, float clip, const G* grad,
+                                     unsigned long long key, unsigned long long first) {
+  const double unit = run_unit<ROOT>(t, a, old, scale, clip);
+  for (; close != 0; close &= close - 1) {
+    const int i = __ffs(close) - 1;
+    const unsigned long long word = splitmix64(key ^ ((first + (unsigned long long)(i >> 1)) * kGroupKey));
+    const uint32_t bits = (uint32_t)(word >> (32 * (i & 1) + (ROOT ? 16 : 0))) & 0xffffu;
+    const double e = moment_64<ROOT>(a, code_value(old, i), scale, (float)grad[i], clip);
+    uint32_t code = round_random(__ddiv_rn(fabs(e), unit), bits);
+    if (ROOT && e > 0.0) code = max(code, 1u);
+    if (!ROOT && e < 0.0) code |= 0x80u;
+    put_code(codes, i, code);
+  }
+  return codes;
+}
+
+template <bool PARAM16, bool GRAD16>
+__device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, bool vec, const StepArgs& a, const AdamCoef& c, float clip,
+                                      float root_rbc2, unsigned long long key) {
+  typedef typename std::conditional<PARAM16, bf16, float>::type P;
+  typedef typename std::conditional<GRAD16, bf16, float>::type G;
+  P* pp = reinterpret_cast<P*>(w.p) + at;
+  const G* gp = reinterpret_cast<const G*>(w.g) + at;
+  uint8_t *mp = reinterpret_cast<uint8_t*>(w.m) + at, *vp = reinterpret_cast<uint8_t*>(w.v) + at;
+  float g[8], m[8], r[8];
+  const uint2 old_m = load_codes(mp, n, vec), old_v = load_codes(vp, n, vec);
+  const float scale_m = w.ms[at / kRun], scale_v = w.vs[at / kRun];
+  load8(gp, n, vec, g);
+  decode(old_m, scale_m, m);
+  decode(old_v, scale_v, r);
+  {
+    float p[8];
+    load8(pp, n, vec, p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float d = g[i] * clip;
+      m[i] = fmaf(c.beta1, m[i], c.omb1 * d);
+      r[i] = fmaf(c.beta2, r[i] * r[i], c.omb2 * d * d);
+      asm("sqrt.approx.f32 %0, %1;" : "=f"(r[i]) : "f"(r[i]));
+      float quot;  // within 2^-22, as the 32-bit update's
+      asm("div.approx.f32 %0, %1, %2;" : "=f"(quot) : "f"(m[i] * c.rbc1), "f"(fmaf(r[i], root_rbc2, c.eps)));
+      p[i] = fmaf(-c.lr, fmaf(w.wd, p[i], quot), p[i]);
+      if (i >= n) m[i] = r[i] = 0.f;
+    }
+    store8(pp, n, vec, p);
+    if (w.copy != nullptr) store8(w.copy + at, n, vec, p);
+  }
+  const RunTop tm = run_top<false>(m, g, a, old_m, scale_m, clip), tv = run_top<true>(r, g, a, old_v, scale_v, clip);
+  const float inv_m = tm.coded() ? __fdividef(448.f, __uint_as_float(tm.top)) : 0.f, inv_v = tv.coded() ? __fdividef(448.f, __uint_as_float(tv.top)) : 0.f;
+  const unsigned long long first = (unsigned long long)(w.base + at) / 2;
+  unsigned long long group = first * kGroupKey;
+  uint2 cm = make_uint2(0u, 0u), cv = make_uint2(0u, 0u);
+  uint32_t close_m = 0, close_v = 0;
+  // an element's fp32 error in 2^-20 steps, which are the last places of b: a dozen roundings, of what it was added up from where that cancels
+  const float grads = 16.f * c.omb1 * fabsf(clip) * inv_m;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    static_assert(kRun == 256, "a word serves two elements");
+    const unsigned long long word = splitmix64(key ^ (group + (unsigned long long)(i >> 1) * kGroupKey));
+    const uint32_t bits = (uint32_t)(word >> (32 * (i & 1)));
+    uint32_t rest;
+    float b;
+    uint32_t code = round_random(fabsf(m[i]) * inv_m, bits & 0xffffu, rest, b) | ((__float_as_uint(m[i]) >> 24) & 0x80u);
+    const uint32_t off = 40u + (uint32_t)fminf(fabsf(g[i]) * grads * __uint_as_float(0x7f000000u - (__float_as_uint(b) & 0x7f800000u)), 262144.f);
+    if (((rest + off) & 0xfffffu) <= 2 * off) close_m |= 1u << i;
+    if (i < 4) cm.x |= code << (8 * i);
+    else cm.y |= code << (8 * (i - 4));
+    code = max(round_random(r[i] * inv_v, bits >> 16, rest, b), r[i] > 0.f ? 1u : 0u);
+    if (((rest + 32u) & 0xfffffu) <= 64u) close_v |= 1u << i;
+    if (i < 4) cv.x |= code << (8 * i);
+    else cv.y |= code << (8 * (i - 4));
+  }
+  if (!tm.coded()) cm = tm.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);  // all 1: what the scale is
+  else if (__any_sync(0xffffffffu, close_m != 0)) cm = settle<false, G>(cm, n == 8 ? close_m : close_m & ((1u << n) - 1u), tm, a, old_m, scale_m, clip, gp, key, first);
+  if (!tv.coded()) cv = tv.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);
+  else if (__any_sync(0xffffffffu, close_v != 0)) cv = settle<true, G>(cv, n == 8 ? close_v : close_v & ((1u << n) - 1u), tv, a, old_v, scale_v, clip, gp, key, first);
+  store_codes(mp, n, vec, cm);
+  store_codes(vp, n, vec, cv);
+  __syncwarp();  // every lane has read the scales
+  if ((threadIdx.x & 31) == 0) {
+    w.ms[at / kRun] = tm.scale;
+    w.vs[at / kRun] = tv.scale;
+  }
+}
+
+template <bool PARAM16, bool GRAD16, int BITS>
+__global__ void __launch_bounds__(kThreads, BITS == 8 ? 4 : 4)
+adamw_kernel(const uint8_t* __restrict__ plan, int n_chunks, unsigned long long chunk_offset, const __grid_constant__ StepArgs a) {
+  typedef typename std::conditional<PARAM16, bf16, float>::type P;
+  typedef typename std::conditional<GRAD16, bf16, float>::type G;
+  __shared__ float s_bc[2];
+  pdl_trigger();
+  pdl_wait();
+  const long long t = max(__ldg(a.step), 1ll);
+  if (threadIdx.x < 2) s_bc[threadIdx.x] = (float)-expm1((double)t * (threadIdx.x == 0 ? a.log_beta1 : a.log_beta2));
+  __syncthreads();
+  AdamCoef c = make_adam_coef(a.dev_lr != nullptr ? __ldg(a.dev_lr) : a.lr, (float)a.beta1, (float)a.beta2, a.eps, s_bc[0], s_bc[1]);
+  c.omb1 = (float)a.omb1;
+  c.omb2 = (float)a.omb2;
+  const float clip = a.grad_scale != nullptr ? __ldg(a.grad_scale) : 1.f;
+  const unsigned long long key = BITS == 8 ? splitmix64(splitmix64(a.seed) ^ ((unsigned long long)t * kStepKey)) : 0;
+  const float root_rbc2 = sqrtf(c.rbc2);
+  const PlanTensor* tensors = reinterpret_cast<const PlanTensor*>(plan + sizeof(PlanHeader));
+  const PlanChunk* chunks = reinterpret_cast<const PlanChunk*>(plan + chunk_offset);
+  for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
+    const PlanChunk ch = chunks[k];
+    const PlanTensor& w = tensors[ch.tensor];
+    const long long at = (long long)ch.index * kChunk + threadIdx.x * 8;
+    const long long left = w.n - at;
+    const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+    if (BITS == 32 ? n == 0 : at / kRun * kRun >= w.n) continue;  // with 8 bits a run's 32 threads stay together
+    const bool vec = n == 8 && w.aligned != 0;
+    if constexpr (BITS == 8) {
+      step8<PARAM16, GRAD16>(w, at, n, vec, a, c, clip, root_rbc2, key);
+    } else {
+      float p[8], g[8], m[8], v[8];
+      load8(reinterpret_cast<const P*>(w.p) + at, n, vec, p);
+      load8(reinterpret_cast<const G*>(w.g) + at, n, vec, g);
+      load8(reinterpret_cast<const float*>(w.m) + at, n, vec, m);
+      load8(reinterpret_cast<const float*>(w.v) + at, n, vec, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) adamw_elem(__fmul_rn(g[i], clip), w.wd, c, p[i], m[i], v[i]);
+      store8(reinterpret_cast<P*>(w.p) + at, n, vec, p);
+      if (w.copy != nullptr) store8(w.copy + at, n, vec, p);
+      store8(reinterpret_cast<float*>(w.m) + at, n, vec, m);
+      store8(reinterpret_cast<float*>(w.v) + at, n, vec, v);
+    }
+  }
+}
+
+template <bool PARAM16, bool GRAD16>
+cudaError_t launch(const PlanHeader& h, const uint8_t* plan, const StepArgs& a, cudaStream_t st) {
+  const unsigned blocks = (unsigned)std::min(h.n_chunks, 148 * 8);
+  if (h.bits == 8) return launch_pdl(adamw_kernel<PARAM16, GRAD16, 8>, dim3(blocks), dim3(kThreads), 0, st, plan, h.n_chunks, (unsigned long long)h.chunk_offset, a);
+  return launch_pdl(adamw_kernel<PARAM16, GRAD16, 32>, dim3(blocks), dim3(kThreads), 0, st, plan, h.n_chunks, (unsigned long long)h.chunk_offset, a);
+}
+
+// Bytes of an array's n elements, by what it is.
+struct Kinds {
+  int param, grad, moment;
+};
+
+// FT_OK, and the number of chunks, for a list that the kernels can take.
+ft_status check(const ft_adamw_tensor* list, int32_t n, int32_t param_dtype, int32_t grad_dtype, int32_t bits, long long* chunks) {
+  if (!list || n <= 0 || (param_dtype & ~1) || (grad_dtype & ~1) || (bits != 8 && bits != 32)) return FT_EINVAL;
+  const Kinds k{param_dtype == 0 ? 2 : 4, grad_dtype == 0 ? 2 : 4, bits / 8};
+  long long total = 0;
+  std::vector<std::pair<uintptr_t, uintptr_t>> written, read;
+  for (int i = 0; i < n; ++i) {
+    const ft_adamw_tensor& t = list[i];
+    if (t.numel < 0 || t.numel > (1ll << 40) || !isfinite(t.weight_decay)) return FT_EINVAL;
+    if (t.numel == 0) continue;
+    if (!t.param || !t.grad || !t.m || !t.v || (bits == 8) != (t.m_scale != nullptr) || (bits == 8) != (t.v_scale != nullptr)) return FT_EINVAL;
+    if (t.copy && param_dtype == 0) return FT_EINVAL;  // a bf16 parameter is its own copy
+    const uintptr_t odd = ((uintptr_t)t.param % k.param) | ((uintptr_t)t.grad % k.grad) | ((uintptr_t)t.m % k.moment) | ((uintptr_t)t.v % k.moment) |
+                          ((uintptr_t)t.copy % 2) | ((uintptr_t)t.m_scale % 4) | ((uintptr_t)t.v_scale % 4);
+    if (odd) return FT_EINVAL;
+    const size_t e = (size_t)t.numel, runs = (e + kRun - 1) / kRun;
+    auto add = [](std::vector<std::pair<uintptr_t, uintptr_t>>& to, const void* p, size_t bytes) {
+      if (p) to.emplace_back((uintptr_t)p, (uintptr_t)p + bytes);
+    };
+    add(written, t.param, e * k.param);
+    add(written, t.m, e * k.moment);
+    add(written, t.v, e * k.moment);
+    add(written, t.copy, e * 2);
+    add(written, t.m_scale, runs * 4);
+    add(written, t.v_scale, runs * 4);
+    add(read, t.grad, e * k.grad);
+    total += (t.numel + kChunk - 1) / kChunk;
+    if (total > INT32_MAX / 2) return FT_EINVAL;
+  }
+  // what the step writes is written by one thread, and not read as a gradient
+  std::sort(written.begin(), written.end());
+  for (size_t i = 1; i < written.size(); ++i)
+    if (written[i].first < written[i - 1].second) return FT_EINVAL;
+  for (const auto& r : read) {
+    auto next = std::lower_bound(written.begin(), written.end(), std::make_pair(r.second, (uintptr_t)0));
+    if (next != written.begin() && std::prev(next)->second > r.first) return FT_EINVAL;
+  }
+  *chunks = total;
+  return FT_OK;
+}
+
+size_t chunk_list_at(int32_t n) { return (sizeof(PlanHeader) + (size_t)n * sizeof(PlanTensor) + 15) / 16 * 16; }
+
+}  // namespace
+}  // namespace fs
+
+extern "C" size_t ft_k_adamw_plan_bytes(const ft_adamw_tensor* tensors, int32_t n_tensors, int32_t param_dtype, int32_t grad_dtype,
+                                        int32_t state_bits) {
+  try {
+    long long chunks = 0;
+    if (fs::check(tensors, n_tensors, param_dtype, grad_dtype, state_bits, &chunks) != FT_OK) return 0;
+    return fs::chunk_list_at(n_tensors) + (size_t)chunks * sizeof(fs::PlanChunk);
+  } catch (...) {
+    return 0;
+  }
+}
+
+extern "C" ft_status ft_k_adamw_plan(const ft_adamw_tensor* tensors, int32_t n_tensors, int32_t param_dtype, int32_t grad_dtype,
+                                     int32_t state_bits, void* host_plan, uint64_t bytes) {
+  try {
+    long long chunks = 0;
+    const ft_status s = fs::check(tensors, n_tensors, param_dtype, grad_dtype, state_bits, &chunks);
+    if (s != FT_OK) return s;
+    if (!host_plan || (reinterpret_cast<uintptr_t>(host_plan) & 7u) != 0) return FT_EINVAL;
+    const size_t need = fs::chunk_list_at(n_tensors) + (size_t)chunks * sizeof(fs::PlanChunk);
+    if (bytes < need) return FT_ENOMEM;
+    memset(host_plan, 0, need);
+    uint8_t* blob = reinterpret_cast<uint8_t*>(host_plan);
+    fs::PlanHeader* h = reinterpret_cast<fs::PlanHeader*>(blob);
+    fs::PlanTensor* list = reinterpret_cast<fs::PlanTensor*>(blob + sizeof(fs::PlanHeader));
+    fs::PlanChunk* ch = reinterpret_cast<fs::PlanChunk*>(blob + fs::chunk_list_at(n_tensors));
+    h->magic = fs::kMagic;
+    h->n_tensors = n_tensors;
+    h->n_chunks = (int32_t)chunks;
+    h->param16 = param_dtype == 0;
+    h->grad16 = grad_dtype == 0;
+    h->bits = state_bits;
+    h->bytes = need;
+    h->chunk_offset = fs::chunk_list_at(n_tensors);
+    long long base = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+      const ft_adamw_tensor& t = tensors[i];
+      // a thread moves 8 elements of an array at once: 32 bytes of fp32, 16 of bf16, 8 of codes
+      const uintptr_t odd = ((uintptr_t)t.param & (h->param16 ? 15u : 31u)) | ((uintptr_t)t.grad & (h->grad16 ? 15u : 31u)) |
+                            (((uintptr_t)t.m | (uintptr_t)t.v) & (state_bits == 8 ? 7u : 31u)) | ((uintptr_t)t.copy & 15u);
+      list[i] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, reinterpret_cast<fs::bf16*>(t.copy), t.numel, base, t.weight_decay, odd == 0};
+      for (long long k = 0; k < (t.numel + fs::kChunk - 1) / fs::kChunk; ++k) *ch++ = {i, (int)k};
+      base += (t.numel + fs::kRun - 1) / fs::kRun * fs::kRun;
+    }
+    return FT_OK;
+  } catch (...) {
+    return FT_ENOMEM;
+  }
+}
+
+extern "C" ft_status ft_k_adamw(const void* host_plan, const void* dev_plan, uint64_t plan_bytes, double lr, double beta1, double beta2, double eps,
+                                const int64_t* dev_step, const float* dev_lr, const float* dev_grad_scale, uint64_t seed, void* stream) {
+  if (!host_plan || !dev_plan || !dev_step || (reinterpret_cast<uintptr_t>(host_plan) & 7u) || (reinterpret_cast<uintptr_t>(dev_plan) & 15u)) return FT_EINVAL;
+  if (((uintptr_t)dev_step & 7u) || ((uintptr_t)dev_lr & 3u) || ((uintptr_t)dev_grad_scale & 3u)) return FT_EINVAL;
+  if (!isfinite((float)lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !isfinite((float)eps)) return FT_EINVAL;
+  const fs::PlanHeader& h = *reinterpret_cast<const fs::PlanHeader*>(host_plan);
+  if (plan_bytes < sizeof(h) || h.magic != fs::kMagic || h.bytes != plan_bytes) return FT_EINVAL;
+  if (h.n_chunks == 0) return FT_OK;
+  auto low = [](double v) { return (float)(v - (double)(float)v); };
+  const double omb1 = 1.0 - beta1, omb2 = 1.0 - beta2;
+  const fs::StepArgs a{(float)lr, (float)eps, beta1, omb1, beta2, omb2, log(beta1), log(beta2),
+                       {(float)beta1, low(beta1)}, {(float)omb1, low(omb1)}, {(float)beta2, low(beta2)}, {(float)omb2, low(omb2)}, reinterpret_cast<const long long*>(dev_step), dev_lr, dev_grad_scale, seed};
+  const uint8_t* plan = reinterpret_cast<const uint8_t*>(dev_plan);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (h.param16) e = h.grad16 ? fs::launch<true, true>(h, plan, a, st) : fs::launch<true, false>(h, plan, a, st);
+  else e = h.grad16 ? fs::launch<false, true>(h, plan, a, st) : fs::launch<false, false>(h, plan, a, st);
+  return e == cudaSuccess ? FT_OK : FT_ECUDA;
+}

@@ -92,18 +92,20 @@ __device__ __forceinline__ void stage_rows(uint32_t out, int lane, uint32_t tmem
     stage_cols<32>(out, lane, c, v);
   }
 }
-// The same for rows that are rotated back by the tables cs, sn (fp32 [S, D / 2]; row0: position of the warp's first row).
+// The same for rows that are rotated back by the tables cs, sn (fp32 [positions, D / 2]).  table_row: the table rows of the warp's
+// rows lane / 4, lane / 4 + 8, + 16 and + 24.
 // 16 columns of the warp's 32 table rows at a time are read in whole 64-byte runs into `table` (4 KB of the warp's own: a row
 // of 64 bytes each, its 16-byte pieces xor-ed with bits of the row against bank conflicts) and from there by row.
 template <int D>
 __device__ __forceinline__ void stage_rows_unrotated(uint32_t out, uint32_t table, int lane, uint32_t tmem_row, float scale,
-                                                     const float* __restrict__ cs, const float* __restrict__ sn, int row0, int S) {
+                                                     const float* __restrict__ cs, const float* __restrict__ sn, int4 table_row) {
   constexpr int H = D / 2;
+  const int rows[4] = {table_row.x, table_row.y, table_row.z, table_row.w};
   float4 c4[4], s4[4];
   auto fetch = [&](int i0) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const long long at = (long long)min(row0 + k * 8 + (lane >> 2), S - 1) * H + i0 + (lane & 3) * 4;
+      const long long at = (long long)rows[k] * H + i0 + (lane & 3) * 4;
       c4[k] = *reinterpret_cast<const float4*>(cs + at);
       s4[k] = *reinterpret_cast<const float4*>(sn + at);
     }

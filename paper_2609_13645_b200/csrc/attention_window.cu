@@ -13,6 +13,15 @@
 //     equal length that run as CTAs of their own and leave fp32 partial sums, which are added in part order (no atomics:
 //     results are bit-identical from run to run).  Key blocks are also cut when a batch has fewer of them than
 //     the GPU has SMs (few kv heads, short sequences).
+//
+// The same kernels, as instances of their own (DOCS), attend inside the documents of a packed batch: one sequence of rows, row i
+// sees the rows from its document's first one to itself.  Tiles are cut from the packed rows and not from the documents, so short
+// documents share tiles instead of leaving them half empty, the grid is known on the host, and only the runs' ends (from the
+// per-row bounds that ft_k_packed_bounds leaves) and the element tests differ:
+//
+//   * a query tile streams the blocks from its first row's document on, a key block those up to its last row's document's end;
+//   * rows behind the last document may hold anything, NaN included, and are left alone: operands that a product sums over have
+//     those rows set to zero in shared memory, and outputs are clipped at the last document's end.
 #include "attention_window.cuh"
 
 #include <limits.h>
@@ -31,6 +40,12 @@ constexpr int kSms = 148;
 // The 64-key blocks that the 128 queries from q0 see: [0, n_sink) and then [first, first + count - n_sink).
 struct KeyRuns {
   int n_sink, first, count;
+  KeyRuns() = default;
+  __device__ __forceinline__ KeyRuns(int q0, int rows_end, int doc_start) {  // documents: one run
+    first = doc_start >> 6;
+    n_sink = 0;
+    count = ((min(rows_end, q0 + 128) + 63) >> 6) - first;
+  }
   __device__ __forceinline__ KeyRuns(int q0, int S, int window, int sinks) {
     const int end = (min(S, q0 + 128) + 63) >> 6;
     first = max(0, q0 - window + 1) >> 6;
@@ -39,6 +54,44 @@ struct KeyRuns {
   }
   __device__ __forceinline__ int block(int j) const { return j < n_sink ? j : first + j - n_sink; }
 };
+
+// ---- packed documents
+// Rows of the batch that belong to documents: [0, total).  A row behind them has end = total and start = the number of rows.
+__device__ __forceinline__ int docs_total(const Docs& docs, int S) {
+  const int e = __ldg(docs.end + S - 1);
+  return e < 0 ? 0 : e < S ? e : S;
+}
+__device__ __forceinline__ int docs_start(const Docs& docs, int row) {  // of a row's document, within [0, row]
+  const int a = __ldg(docs.start + row);
+  return a < 0 ? 0 : a < row ? a : row;
+}
+// Sets rows [from, ROWS) of a swizzled tile of D columns in shared memory to zero; all threads of a warp.
+template <int D, int ROWS>
+__device__ __forceinline__ void zero_rows(uint32_t tile, int from, int lane) {
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+  for (int i = lane; i < (ROWS - from) * (D / 8); i += 32) {
+    const int c = i / ((ROWS - from) * 8), r = i % ((ROWS - from) * 8);  // 64-column box, 16-byte piece of its rows
+    st_shared_v4(tile + (uint32_t)(c * (ROWS * 128) + from * 128 + r * 16), zero);
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+// send_rows() of rows that may end inside the warp's 32.
+template <int D>
+__device__ __forceinline__ void send_rows_clipped(const void* tmap, bf16* dst, long long ld, uint32_t out, int lane, int x, int y, int total) {
+  if (y + 32 <= total) {
+    send_rows<D>(tmap, out, lane, x, y, 0, total);
+  } else {
+    __syncwarp();
+    if (y + lane < total) {
+      bf16* row = dst + (long long)(y + lane) * ld + x;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c)
+        *reinterpret_cast<uint4*>(row + c * 8) = ld_shared_v4(out + (uint32_t)((c >> 3) * 4096 + lane * 128 + (((c & 7) ^ (lane & 7)) * 16)));
+    }
+  }
+}
 
 // ============================================================================ forward
 // One CTA per (128 queries, head, batch row), two an SM; K and V blocks of 64 keys are streamed, S_{j+1} = Q K_{j+1}^T is
@@ -51,7 +104,7 @@ struct KeyRuns {
 // fp32.  Against fp32 weights this takes the error of o from 1.6e-3 (its own rounding) to 2.2e-3 in the 2-norm, as in the
 // dense kernel; wider operands would halve the product's rate and double P's share of TMEM.
 enum { B_QFULL = 0, B_KFULL = 1, B_KEMPTY = 4, B_VFULL = 7, B_VEMPTY = 9, B_SFULL = 11, B_PFULL = 13, B_ODONE = 15,
-       B_OFINAL = 16, B_COUNT = 17 };
+       B_OFINAL = 16, B_TAIL = 17, B_COUNT = 18 };
 constexpr int FWD_THREADS = 224;  // Q + K producer, MMA issuer, 4 softmax warps, V producer
 
 template <int D>
@@ -63,7 +116,7 @@ struct FwdCfg {
   static constexpr int OFF_K = Q_BYTES;
   static constexpr int OFF_V = OFF_K + NK * KV_BYTES;
   static constexpr int OFF_BAR = OFF_V + NV * KV_BYTES;
-  static constexpr int SMEM_BYTES = OFF_BAR + 160;
+  static constexpr int SMEM_BYTES = OFF_BAR + 168;
   static constexpr int TMEM_COLS = 256;  // S0 [0,64) S1 [64,128) (bf16 P over the first 32 columns of each), O from 128
   static constexpr int O_COL = 128;
 };
@@ -85,11 +138,11 @@ __device__ __forceinline__ void softmax_chunk(const uint32_t (&r)[32], float sca
   }
 }
 
-template <int D>
+template <int D, bool DOCS>
 __global__ void __launch_bounds__(FWD_THREADS, 2)
 attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKV,
-                       const __grid_constant__ CUtensorMap tmO, float* __restrict__ lse, int S, int n_heads, int n_kv, int n_batch, int n_qblocks, int window, int sinks,
-                       float scale_log2, int* err) {
+                       const __grid_constant__ CUtensorMap tmO, bf16* __restrict__ o, float* __restrict__ lse, int S, int n_heads, int n_kv, int n_batch, int n_qblocks, int window, int sinks,
+                       const __grid_constant__ Docs docs, float scale_log2, int* err) {
   using C = FwdCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
@@ -112,7 +165,16 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   const int kvh = n / (n_heads / n_kv);
   const int hq = n_heads * D, hkv = n_kv * D;
   const int q0 = qb * C::BQ;
-  const KeyRuns runs(q0, S, window, sinks);
+  int rows_end = S;  // rows behind it are nobody's
+  KeyRuns runs;
+  if constexpr (DOCS) {
+    pdl_wait();
+    rows_end = docs_total(docs, S);
+    if (q0 >= rows_end) return;
+    runs = KeyRuns(q0, rows_end, docs_start(docs, q0));
+  } else {
+    runs = KeyRuns(q0, S, window, sinks);
+  }
   const int nb = runs.count;
 
   auto load_k = [&](int j) {
@@ -139,6 +201,7 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     }
     mbar_init(bar(B_ODONE), 1);
     mbar_init(bar(B_OFINAL), 1);
+    if constexpr (DOCS) mbar_init(bar(B_TAIL), 1);
     *abort_flag = 0;
     mbar_fence_init();
     // the first loads do not wait for the rest of the set-up
@@ -168,15 +231,32 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
       }
     }
   } else if (warp == 6) {
+    auto load_v = [&](int j, uint32_t full) {
+      mbar_expect_tx(full, C::KV_BYTES);
+#pragma unroll
+      for (int kc = 0; kc < C::KC; ++kc)
+        tma_load_3d(sbase + C::OFF_V + j % C::NV * C::KV_BYTES + kc * (C::BK * 128), &tmKV, full, hq + hkv + kvh * D + kc * 64,
+                    runs.block(j) * C::BK, b);
+    };
+    // a last block that reaches behind the last document: its V arrives on a barrier of its own and loses those rows first
+    const bool tail = DOCS && (runs.block(nb - 1) + 1) * C::BK > rows_end;
+    bool ok = true;
     if (lane == 0) {
       for (int j = 0; j < nb; ++j) {
         const int st = j % C::NV;
-        if (!mbar_wait(bar(B_VEMPTY + st), ((uint32_t)(j / C::NV) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x62)) break;
-        mbar_expect_tx(bar(B_VFULL + st), C::KV_BYTES);
-#pragma unroll
-        for (int kc = 0; kc < C::KC; ++kc)
-          tma_load_3d(sbase + C::OFF_V + st * C::KV_BYTES + kc * (C::BK * 128), &tmKV, bar(B_VFULL + st),
-                      hq + hkv + kvh * D + kc * 64, runs.block(j) * C::BK, b);
+        ok = mbar_wait(bar(B_VEMPTY + st), ((uint32_t)(j / C::NV) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x62);
+        if (!ok) break;
+        load_v(j, bar(tail && j == nb - 1 ? B_TAIL : B_VFULL + st));
+      }
+    }
+    if constexpr (DOCS) {
+      if (tail && __shfl_sync(0xffffffffu, (int)ok, 0) != 0) {
+        const int st = (nb - 1) % C::NV;
+        ok = mbar_wait(bar(B_TAIL), 0, abort_flag, err, kWaitLimitCycles, 0x6a);
+        if (__all_sync(0xffffffffu, ok)) {
+          zero_rows<D, C::BK>(sbase + C::OFF_V + st * C::KV_BYTES, rows_end - runs.block(nb - 1) * C::BK, lane);
+          if (lane == 0) mbar_arrive(bar(B_VFULL + st));
+        }
       }
     }
   } else if (warp == 1) {
@@ -230,6 +310,12 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
     const int row = q0 + q * 32 + lane;
     const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
     const int wmin = q0 + q * 32, wmax = wmin + 31;  // rows of this warp
+    int own = 0, own_min = 0, own_max = 0;  // first row of this row's document, and the least and greatest in the warp
+    if constexpr (DOCS) {
+      own = row < rows_end ? docs_start(docs, row) : S;
+      own_min = __shfl_sync(0xffffffffu, own, 0);
+      own_max = __shfl_sync(0xffffffffu, own, 31);
+    }
     // The row reference is an integer in the log2 domain: any such reference gives the same softmax, and bf16 rounding commutes
     // with powers of two.  So it need not be the maximum, only near it: the exponentials of a block are taken against the
     // reference that the blocks before left, in one pass, and taken again against a new one only if their maximum turns out
@@ -248,8 +334,8 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
       const int first = runs.block(j) * C::BK, last = first + C::BK - 1;
       // 64 keys of which no row of the warp sees any are not read, and only those on an edge of the mask are tested one by one
       // (both warp-uniform)
-      const bool none = first > wmax || (last < wmin - window + 1 && first >= sinks);
-      const bool all = last <= wmin && (first > wmax - window || last < sinks);
+      const bool none = first > wmax || (DOCS ? last < own_min : last < wmin - window + 1 && first >= sinks);
+      const bool all = last <= wmin && (DOCS ? first >= own_max : first > wmax - window || last < sinks);
       uint32_t pw[32];  // bf16 pairs: keys 2c, 2c+1 in word c
       float2 psum = both(0.f);
       if (none) {
@@ -263,8 +349,9 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
           tmem_ld_wait();
           if (!all) {
             const int hi = row - first;
-            const uint32_t seen0 = visible(hi, hi - window + 1, sinks - first);
-            const uint32_t seen1 = visible(hi - 32, hi - 32 - window + 1, sinks - first - 32);
+            const int lo = DOCS ? own - first : hi - window + 1, sk = DOCS ? 0 : sinks - first;
+            const uint32_t seen0 = visible(hi, lo, sk);
+            const uint32_t seen1 = visible(hi - 32, lo - 32, sk - 32);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               r0[e] = seen0 & (1u << e) ? r0[e] : 0xff800000u;  // -inf
@@ -321,8 +408,9 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
       tc_fence_after();
       const uint32_t out = sbase + (uint32_t)(q * 32 * D * 2);  // Q has been read
       stage_rows<D>(out, lane, tlane + (uint32_t)C::O_COL, 1.0f / nsum);
-      send_rows<D>(&tmO, out, lane, n * D, q0 + q * 32, b, S);
-      if (row < S) lse[((long long)b * n_heads + n) * S + row] = (mref + log2f(lsum)) * kLn2;
+      if constexpr (DOCS) send_rows_clipped<D>(&tmO, o, hq, out, lane, n * D, q0 + q * 32, rows_end);
+      else send_rows<D>(&tmO, out, lane, n * D, q0 + q * 32, b, S);
+      if (row < rows_end) lse[((long long)b * n_heads + n) * S + row] = (mref + log2f(lsum)) * kLn2;
       if (lane == 0) bulk_wait_group0();
     }
   }
@@ -342,12 +430,12 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   }
 }
 
-template <int D>
-cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, int nkv, int window, int sinks, int* err,
+template <int D, bool DOCS>
+cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, int nkv, int window, int sinks, const Docs& docs, int* err,
                   cudaStream_t st) {
   using C = FwdCfg<D>;
   static unsigned long long smem_set = 0;
-  cudaError_t e = ensure_dynamic_smem(attn_window_fwd_kernel<D>, C::SMEM_BYTES, smem_set);
+  cudaError_t e = ensure_dynamic_smem(attn_window_fwd_kernel<D, DOCS>, C::SMEM_BYTES, smem_set);
   if (e != cudaSuccess) return e;
   const int nqkv = (nh + 2 * nkv) * D;
   CUtensorMap tmQ, tmKV, tmO;
@@ -356,8 +444,8 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
     return cudaErrorInvalidValue;
   const float scale_log2 = (float)((1.0 / sqrt((double)D)) * 1.4426950408889634);
   const int nqb = (S + C::BQ - 1) / C::BQ;
-  return launch_pdl(attn_window_fwd_kernel<D>, dim3((unsigned)(nqb * nh * B)), dim3(FWD_THREADS), C::SMEM_BYTES, st, tmQ, tmKV, tmO, lse,
-                    S, nh, nkv, B, nqb, window, sinks, scale_log2, err);
+  return launch_pdl(attn_window_fwd_kernel<D, DOCS>, dim3((unsigned)(nqb * nh * B)), dim3(FWD_THREADS), C::SMEM_BYTES, st, tmQ, tmKV, tmO, o, lse,
+                    S, nh, nkv, B, nqb, window, sinks, docs, scale_log2, err);
 }
 
 // ============================================================================ backward
@@ -380,7 +468,7 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, int B, int S, int nh, in
 // through shared memory; a CTA's start takes 6000 and its end 5000.  S 16384, 16 / 8 heads, window 1024: 335 us.  B 8, S 1024, 12
 // heads of 64, window 256: 48 us.
 enum { K_XFULL = 0, K_QFULL = 1, K_QEMPTY = 4, K_OFULL = 7, K_OEMPTY = 10, K_STFULL = 13, K_STEMPTY = 15, K_SFULL = 17, K_DPFULL = 18,
-       K_PFULL = 19, K_DSFULL = 20, K_ACCDONE = 21, K_COUNT = 22 };
+       K_PFULL = 19, K_DSFULL = 20, K_ACCDONE = 21, K_TAIL = 22, K_COUNT = 23 };
 constexpr int DKV_THREADS = 320;  // producer, MMA issuer, 8 compute warps
 
 template <int D, int BLOCK>
@@ -411,13 +499,27 @@ struct Plan {
   int parts_sink, parts;  // parts of a sink block and of any other, at most
   int group0, groups;     // groups of this launch: [group0, group0 + groups)
   int all_groups;
+  Docs docs;              // packed documents; window is then the longest one's length, and the counts above are upper limits
   // blocks [x, queries_end(x)) of the queries see a key of block x
   __host__ __device__ int blocks_seen(int x) const {
     if (x < n_sink) return nxb - x;
     return nxb - x < nb ? nxb - x : nb;
   }
-  __host__ __device__ int parts_of(int x) const {
-    return (int)(((long long)blocks_seen(x) * (n_heads / n_kv) + chunk - 1) / chunk);
+  __host__ __device__ int parts_of(int x) const { return parts_for(blocks_seen(x)); }
+  __host__ __device__ int parts_for(int seen) const { return (int)(((long long)seen * (n_heads / n_kv) + chunk - 1) / chunk); }
+  // Where the tiles of dS^T of key block x begin in what is kept of a head, and how many there are.  Packed batches, whose longest
+  // document may be most of the batch, keep no room for blocks behind the last one.
+  template <bool DOCS>
+  __host__ __device__ long long band_at(int x) const {
+    const long long over = DOCS && x > nxb - nb ? x - (nxb - nb) : 0;
+    return (long long)x * nb - over * (over - 1) / 2;
+  }
+  // The same of a packed batch: to the block in which the document of the block's last row ends; 0 behind the last document.
+  __device__ int docs_blocks_seen(int x, int total) const {
+    const int last = min(S, x * 128 + 128) - 1;
+    if (x * 128 >= total) return 0;
+    if (last >= total) return 1;
+    return min(max((min(__ldg(docs.end + last), total) + 127) / 128 - x, 1), blocks_seen(x));
   }
   // first slot of a key block's partial sums
   __host__ __device__ int rank_of(int x) const {
@@ -425,6 +527,18 @@ struct Plan {
   }
   __host__ __device__ int ranks() const { return n_sink * parts_sink + (nxb - n_sink) * parts; }
 };
+
+// Rows of the rotation tables that a lane reads of the 32 rows from row0 on: those of rows row0 + 8 k + lane / 4.
+template <bool DOCS>
+__device__ __forceinline__ int4 table_rows(const Plan& pl, int row0, int lane) {
+  const int r = row0 + (lane >> 2), last = pl.S - 1;
+  int4 t = make_int4(min(r, last), min(r + 8, last), min(r + 16, last), min(r + 24, last));
+  if constexpr (DOCS) {  // positions in the documents, of which the tables have `window`
+    auto position = [&](int row) { return min(max(__ldg(pl.docs.pos + row), 0), pl.window - 1); };
+    t = make_int4(position(t.x), position(t.y), position(t.z), position(t.w));
+  }
+  return t;
+}
 
 // A thread's row of 32 or 64 scores out of TMEM, and their bf16 pairs back into it.
 template <int W>
@@ -439,11 +553,11 @@ __device__ __forceinline__ void load_scores(uint32_t t, float (&v)[W]) {
 __device__ __forceinline__ void store_pairs(uint32_t t, const uint32_t (&w)[32]) { tmem_st32(t, w); }
 __device__ __forceinline__ void store_pairs(uint32_t t, const uint32_t (&w)[16]) { tmem_st16(t, w); }
 
-template <int D, int BLOCK>
+template <int D, int BLOCK, bool DOCS>
 __global__ void __launch_bounds__(DKV_THREADS, DkvCfg<D, BLOCK>::CTAS)
 attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
                        const __grid_constant__ CUtensorMap tm_out, const float* __restrict__ lse, const float* __restrict__ delta,
-                       float* __restrict__ partial, bf16* __restrict__ ds_band, bf16* __restrict__ ds_sink,
+                       bf16* __restrict__ dqkv, float* __restrict__ partial, bf16* __restrict__ ds_band, bf16* __restrict__ ds_sink,
                        const float* __restrict__ rope_cos, const float* __restrict__ rope_sin, const __grid_constant__ Plan pl,
                        float scale, float scale_log2, int* err) {
   using C = DkvCfg<D, BLOCK>;
@@ -470,7 +584,15 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   const int x = rank < n_sink_ranks ? rank / pl.parts_sink : pl.n_sink + (rank - n_sink_ranks) / pl.parts;
   const int part = rank < n_sink_ranks ? rank % pl.parts_sink : (rank - n_sink_ranks) % pl.parts;
   const int x0 = x * 128;
-  const int per_head = pl.blocks_seen(x), total = per_head * n_rep, np = pl.parts_of(x);
+  int rows_end = S, per_head;  // rows behind the first are nobody's; query blocks of a head that this key block meets
+  if constexpr (DOCS) {
+    pdl_wait();
+    rows_end = docs_total(pl.docs, S);
+    per_head = pl.docs_blocks_seen(x, rows_end);
+  } else {
+    per_head = pl.blocks_seen(x);
+  }
+  const int total = per_head * n_rep, np = pl.parts_for(per_head);
   if (part >= np) return;
   const int first128 = (int)((long long)total * part / np);
   const int iters = ((int)((long long)total * (part + 1) / np) - first128) * C::SUB;
@@ -480,19 +602,21 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   auto rel_of = [&](int it) { return (first128 + it / C::SUB) % per_head; };
   auto head_of = [&](int it) { return kvh * n_rep + rep_of(it); };
   auto query_of = [&](int it) { return (x + rel_of(it)) * 128 + it % C::SUB * C::BQ; };
-  auto load_q = [&](int it) {
+  // a block that reaches behind the last document arrives on a barrier of its own and loses those rows first
+  auto tail_of = [&](int it) { return DOCS && query_of(it) + C::BQ > rows_end; };
+  auto load_q = [&](int it, uint32_t full) {
     const int st = it % C::NQ;
-    mbar_expect_tx(bar(K_QFULL + st), C::Y_TILE);
+    mbar_expect_tx(full, C::Y_TILE);
 #pragma unroll
     for (int kc = 0; kc < C::KC; ++kc)
-      tma_load_3d(sbase + C::OFF_Q + st * C::Y_TILE + kc * (C::BQ * 128), &tm_q, bar(K_QFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
+      tma_load_3d(sbase + C::OFF_Q + st * C::Y_TILE + kc * (C::BQ * 128), &tm_q, full, head_of(it) * D + kc * 64, query_of(it), b);
   };
-  auto load_do = [&](int it) {
+  auto load_do = [&](int it, uint32_t full) {
     const int st = it % C::NO;
-    mbar_expect_tx(bar(K_OFULL + st), C::Y_TILE);
+    mbar_expect_tx(full, C::Y_TILE);
 #pragma unroll
     for (int kc = 0; kc < C::KC; ++kc)
-      tma_load_3d(sbase + C::OFF_O + st * C::Y_TILE + kc * (C::BQ * 128), &tm_do, bar(K_OFULL + st), head_of(it) * D + kc * 64, query_of(it), b);
+      tma_load_3d(sbase + C::OFF_O + st * C::Y_TILE + kc * (C::BQ * 128), &tm_do, full, head_of(it) * D + kc * 64, query_of(it), b);
   };
   if (threadIdx.x == 0) {
     mbar_init(bar(K_XFULL), 1);
@@ -513,6 +637,7 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     mbar_init(bar(K_PFULL), 8);
     mbar_init(bar(K_DSFULL), 8);
     mbar_init(bar(K_ACCDONE), 1);
+    if constexpr (DOCS) mbar_init(bar(K_TAIL), 1);
     *abort_flag = 0;
     mbar_fence_init();
     // the first loads do not wait for the rest of the set-up
@@ -521,11 +646,11 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
 #pragma unroll
     for (int kc = 0; kc < C::KC; ++kc)
       tma_load_3d(sbase + C::OFF_K + kc * 16384, &tm_qkv, bar(K_XFULL), hq + kvh * D + kc * 64, x0, b);
-    load_q(0);
+    if (!tail_of(0)) load_q(0, bar(K_QFULL));
 #pragma unroll
     for (int kc = 0; kc < C::KC; ++kc)
       tma_load_3d(sbase + C::OFF_V + kc * 16384, &tm_qkv, bar(K_XFULL), hq + hkv + kvh * D + kc * 64, x0, b);
-    load_do(0);
+    if (!tail_of(0)) load_do(0, bar(K_OFULL));
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
@@ -540,16 +665,29 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
+    uint32_t tail_parity = 0;
+    // waits for the tile that was sent to the barrier of the tails, clears its rows behind the last document and hands it on
+    auto clear_tail = [&](int it, uint32_t tile, uint32_t full) {
+      const bool ok = mbar_wait(bar(K_TAIL), tail_parity, abort_flag, err, kWaitLimitCycles, 0x7f);
+      tail_parity ^= 1u;
+      if (!__all_sync(0xffffffffu, ok)) return false;
+      zero_rows<D, C::BQ>(tile, max(rows_end - query_of(it), 0), lane);
+      if (lane == 0) mbar_arrive(full);
+      return true;
+    };
     for (int it = 0; it < iters; ++it) {
       const int n = head_of(it), q0 = query_of(it), ss = it & 1;
       bool ok = true;
-      if (it > 0) {  // block 0 is on its way
+      const bool tail = tail_of(it);
+      if (it > 0 || tail) {  // block 0 is on its way
         ok = mbar_wait(bar(K_QEMPTY + it % C::NQ), ((uint32_t)(it / C::NQ) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x71);
         if (!__all_sync(0xffffffffu, ok)) break;
-        if (lane == 0) load_q(it);
+        if (lane == 0) load_q(it, bar(tail ? K_TAIL : K_QFULL + it % C::NQ));
+        if (DOCS && tail && !clear_tail(it, sbase + C::OFF_Q + it % C::NQ * C::Y_TILE, bar(K_QFULL + it % C::NQ))) break;
         ok = mbar_wait(bar(K_OEMPTY + it % C::NO), ((uint32_t)(it / C::NO) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x72);
         if (!__all_sync(0xffffffffu, ok)) break;
-        if (lane == 0) load_do(it);
+        if (lane == 0) load_do(it, bar(tail ? K_TAIL : K_OFULL + it % C::NO));
+        if (DOCS && tail && !clear_tail(it, sbase + C::OFF_O + it % C::NO * C::Y_TILE, bar(K_OFULL + it % C::NO))) break;
       }
       ok = mbar_wait(bar(K_STEMPTY + ss), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x73);
       if (!__all_sync(0xffffffffu, ok)) break;
@@ -557,8 +695,8 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
 #pragma unroll
       for (int e = 0; e < C::BQ / 32; ++e) {
         const int qq = q0 + lane + 32 * e;
-        s_stat[ss * 2 * C::BQ + lane + 32 * e] = qq < S ? lse[stat + qq] * kLog2e : 0.f;
-        s_stat[ss * 2 * C::BQ + C::BQ + lane + 32 * e] = qq < S ? delta[stat + qq] : 0.f;
+        s_stat[ss * 2 * C::BQ + lane + 32 * e] = qq < rows_end ? lse[stat + qq] * kLog2e : 0.f;
+        s_stat[ss * 2 * C::BQ + C::BQ + lane + 32 * e] = qq < rows_end ? delta[stat + qq] : 0.f;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(K_STFULL + ss));
@@ -638,7 +776,13 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
     const uint32_t t_s = tlane + (uint32_t)(C::COL_S + ch * C::W), t_dp = tlane + (uint32_t)(C::COL_DP + ch * C::W);
     const uint32_t stage = sbase + (uint32_t)(C::OFF_DS + (warp - 2) * 4096);
     // the queries that see key `row` are [row, row_end)
-    const int row_end = row < pl.sinks || S - row < pl.window ? S : row + pl.window;
+    int row_end, least_end = 0;  // of all rows of the warp (documents)
+    if constexpr (DOCS) {
+      row_end = row < rows_end ? min(__ldg(pl.docs.end + row), rows_end) : 0;
+      least_end = __reduce_min_sync(0xffffffffu, row_end);
+    } else {
+      row_end = row < pl.sinks || S - row < pl.window ? S : row + pl.window;
+    }
     bool ok = true;
     for (int it = 0; it < iters; ++it) {
       const int ss = it & 1;
@@ -662,9 +806,10 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
         p[i + 3] = fast_exp2(fmaf(p[i + 3], scale_log2, -l4.w));
       }
       // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
-      const bool full = cmin >= rmax && cmin + C::W <= S && (rmax < pl.sinks || cmin + C::W - 1 - rmin < pl.window);
+      const bool full = cmin >= rmax && (DOCS ? cmin + C::W <= least_end
+                                              : cmin + C::W <= S && (rmax < pl.sinks || cmin + C::W - 1 - rmin < pl.window));
+      const int lo = row - cmin, hi = row_end - cmin;
       if (!full) {
-        const int lo = row - cmin, hi = row_end - cmin;
 #pragma unroll
         for (int i = 0; i < C::W; ++i)
           if (i < lo || i >= hi) p[i] = 0.f;
@@ -692,6 +837,11 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
           p[i + 1] *= d[i + 1] - e4.y;
           p[i + 2] *= d[i + 2] - e4.z;
           p[i + 3] *= d[i + 3] - e4.w;
+        }
+        if (DOCS && !full) {  // rows behind the last document: 0 times what they hold may be anything
+#pragma unroll
+          for (int i = 0; i < C::W; ++i)
+            if (i < lo || i >= hi) p[i] = 0.f;
         }
       }
 #pragma unroll
@@ -723,7 +873,7 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
           __syncwarp();
           if (lane == 0) {
             uint8_t* dst = reinterpret_cast<uint8_t*>(ds_band) +
-                           (((z * pl.nxb + x) * pl.nb + rel) * 8 + (q >> 1) * 4 + chunk) * 4096 + (q & 1) * 2048;
+                           ((z * pl.band_at<DOCS>(pl.nxb) + pl.band_at<DOCS>(x) + rel) * 8 + (q >> 1) * 4 + chunk) * 4096 + (q & 1) * 2048;
 #pragma unroll
             for (int c = 0; c < C::W / 32; ++c) bulk_store(dst + c * 4096, stage + c * 2048, 2048);
             bulk_commit_group();
@@ -752,12 +902,13 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
         // this CTA holds the whole sum: one warp of a lane quarter takes dK (scaled, rotated back), the other dV
         const uint32_t out = sbase + (uint32_t)((warp - 2) * 32 * D * 2);  // K and V have been read
         if (ch == 0) {
-          if (rope_cos != nullptr) stage_rows_unrotated<D>(out, stage, lane, t_dk, scale, rope_cos, rope_sin, rmin, S);
+          if (rope_cos != nullptr) stage_rows_unrotated<D>(out, stage, lane, t_dk, scale, rope_cos, rope_sin, table_rows<DOCS>(pl, rmin, lane));
           else stage_rows<D>(out, lane, t_dk, scale);
         } else {
           stage_rows<D>(out, lane, t_dv, 1.0f);
         }
-        send_rows<D>(&tm_out, out, lane, hq + ch * hkv + kvh * D, rmin, b, S);
+        if constexpr (DOCS) send_rows_clipped<D>(&tm_out, dqkv, hq + 2 * hkv, out, lane, hq + ch * hkv + kvh * D, rmin, rows_end);
+        else send_rows<D>(&tm_out, out, lane, hq + ch * hkv + kvh * D, rmin, b, S);
         if (lane == 0) bulk_wait_group0();
       } else {
         // partial sums [part][dK columns, dV columns][128 keys]: a warp writes 32 consecutive keys of a column
@@ -807,13 +958,19 @@ struct Join {
 constexpr int JOIN_SMEM = 32 * 132 * 4;
 
 // all THREADS of a CTA; s_sum: [column][key]
-template <int D, int THREADS>
+template <int D, int THREADS, bool DOCS>
 __device__ __forceinline__ void join_unit(const Join& jn, const Plan& pl, int unit, float (*s_sum)[132]) {
   constexpr int H = D / 2, K_UNITS = H / 16, WARPS = THREADS / 32, OWN = (32 + WARPS - 1) / WARPS;
   const int groups = pl.all_groups, S = pl.S, n_heads = pl.n_heads, n_kv = pl.n_kv;
   const int piece = unit % (D / 16), x = unit / (D / 16) / groups, grp = unit / (D / 16) % groups;
-  const int np = pl.parts_of(x);
-  if (np == 1) return;
+  int rows_end = S, np;
+  if constexpr (DOCS) {
+    rows_end = docs_total(pl.docs, S);
+    np = pl.parts_for(pl.docs_blocks_seen(x, rows_end));
+  } else {
+    np = pl.parts_of(x);
+  }
+  if (np <= 1) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool is_k = piece < K_UNITS;
   const int c0 = is_k ? piece * 16 : (piece - K_UNITS) * 32;
@@ -842,7 +999,7 @@ __device__ __forceinline__ void join_unit(const Join& jn, const Plan& pl, int un
   const int kvh = grp % n_kv, b = grp / n_kv;
   for (int v = threadIdx.x; v < 256; v += THREADS) {
     const int r = v & 127, part = v >> 7, row = x * 128 + r;
-    if (row >= S) continue;
+    if (row >= rows_end) continue;
     bf16* dst = jn.dqkv + ((long long)b * S + row) * (long long)((n_heads + 2 * n_kv) * D) + (n_heads + (is_k ? 0 : n_kv) + kvh) * D + c0;
     if (is_k) {
       float lo[8], hi[8];
@@ -852,7 +1009,10 @@ __device__ __forceinline__ void join_unit(const Join& jn, const Plan& pl, int un
         lo[i] = s_sum[i0 + i][r] * jn.scale;
         hi[i] = s_sum[16 + i0 + i][r] * jn.scale;
       }
-      if (jn.rope_cos != nullptr) unrotate<8>(lo, hi, jn.rope_cos + (long long)row * H + c0 + i0, jn.rope_sin + (long long)row * H + c0 + i0);
+      if (jn.rope_cos != nullptr) {
+        const long long at = (long long)(DOCS ? min(max(__ldg(pl.docs.pos + row), 0), pl.window - 1) : row) * H + c0 + i0;
+        unrotate<8>(lo, hi, jn.rope_cos + at, jn.rope_sin + at);
+      }
       store_bf16_row<8>(dst + i0, lo);
       store_bf16_row<8>(dst + H + i0, hi);
     } else {
@@ -866,13 +1026,13 @@ __device__ __forceinline__ void join_unit(const Join& jn, const Plan& pl, int un
 }
 
 // The same behind the dQ kernel that recomputes the scores.
-template <int D>
+template <int D, bool DOCS>
 __global__ void __launch_bounds__(256)
 attn_window_join_kernel(const __grid_constant__ Join jn, const __grid_constant__ Plan pl) {
   pdl_trigger();
   pdl_wait();
   __shared__ float s_sum[32][132];
-  join_unit<D, 256>(jn, pl, (int)blockIdx.x, s_sum);
+  join_unit<D, 256, DOCS>(jn, pl, (int)blockIdx.x, s_sum);
 }
 
 // ---------------------------------------------------------------- dQ from the stored dS^T
@@ -895,10 +1055,10 @@ struct DqCfg {
   static constexpr int TMEM_COLS = 2 * D;
 };
 
-template <int D>
+template <int D, bool DOCS>
 __global__ void __launch_bounds__(DQ_THREADS, 2)
 attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ CUtensorMap tm_sink,
-                      const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_out, const float* __restrict__ rope_cos,
+                      const __grid_constant__ CUtensorMap tm_qkv, const __grid_constant__ CUtensorMap tm_out, bf16* __restrict__ dqkv, const float* __restrict__ rope_cos,
                       const float* __restrict__ rope_sin, const __grid_constant__ Plan pl, const __grid_constant__ Join jn, float scale,
                       int* err) {
   using C = DqCfg<D>;
@@ -910,7 +1070,8 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
   auto empty_bar = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
   auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * C::STAGES + a); };
   auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * C::STAGES + 2 + a); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4);
+  const uint32_t tail_bar = bar0 + 8u * (2 * C::STAGES + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 5);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if ((sbase & 1023u) != 0u) {
@@ -918,6 +1079,7 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
     return;
   }
   if (threadIdx.x == 0) {
+    if constexpr (DOCS) mbar_init(tail_bar, 1);
     for (int s = 0; s < C::STAGES; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
@@ -944,34 +1106,61 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
 
   const int S = pl.S, n_rep = pl.n_heads / pl.n_kv;
   const int hq = pl.n_heads * D;
-  const int nz = pl.groups * n_rep, ntiles = pl.nxb * nz;
+  const int nz = pl.groups * n_rep;
+  const int rows_end = DOCS ? docs_total(pl.docs, S) : S;
+  const int nqb = DOCS ? (rows_end + 127) / 128 : pl.nxb;  // query blocks with rows
+  const int ntiles = nqb * nz;
   // tile t: query block qt of head z of this launch; 64-key steps: sink keys behind the band, then the band
   struct Tile {
     int qt, z, kvh, n, b, x_first, n_sink64, steps;
   };
   auto tile_of = [&](int t) {
     Tile r;
-    r.qt = pl.nxb - 1 - t / nz;
+    r.qt = nqb - 1 - t / nz;
     r.z = t % nz;
     const int grp = pl.group0 + r.z / n_rep;
     r.kvh = grp % pl.n_kv;
     r.b = grp / pl.n_kv;
     r.n = r.kvh * n_rep + r.z % n_rep;
     r.x_first = max(0, r.qt - pl.nb + 1);
-    r.n_sink64 = (min(pl.sinks, r.x_first * 128) + 63) / 64;
+    if constexpr (DOCS) r.x_first = max(r.x_first, docs_start(pl.docs, r.qt * 128) / 128);
+    r.n_sink64 = DOCS ? 0 : (min(pl.sinks, r.x_first * 128) + 63) / 64;
     r.steps = r.n_sink64 + (r.qt - r.x_first + 1) * 2;
     return r;
   };
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (DOCS || lane == 0) {  // documents: the whole warp, which clears the K rows behind the last one
       int stage = 0;
-      uint32_t phase = 0;
+      uint32_t phase = 0, tail_parity = 0;
       bool ok = true;
       for (int t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
         const Tile r = tile_of(t);
         for (int i = 0; i < r.steps; ++i) {
-          if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, err, kWaitLimitCycles, 0x81)) { ok = false; break; }
+          ok = mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, err, kWaitLimitCycles, 0x81);
+          if constexpr (DOCS) ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if constexpr (DOCS) {
+            const int x = r.x_first + (i >> 1), key0 = x * 128 + (i & 1) * 64;
+            const bool tail = key0 + 64 > rows_end;
+            const uint32_t fb = tail ? tail_bar : full_bar(stage), a_dst = sbase + stage * C::STAGE_BYTES, b_dst = a_dst + C::A_BYTES;
+            if (lane == 0) {
+              mbar_expect_tx(fb, C::STAGE_BYTES);
+              bulk_load(a_dst, ds_band + ((r.z * pl.band_at<DOCS>(pl.nxb) + pl.band_at<DOCS>(x) + r.qt - x) * 2 + (i & 1)) * 8192, C::A_BYTES, fb);
+#pragma unroll
+              for (int c = 0; c < D / 64; ++c) tma_load_3d(b_dst + c * 8192, &tm_qkv, fb, hq + r.kvh * D + 64 * c, key0, r.b);
+            }
+            if (tail) {
+              ok = mbar_wait(tail_bar, tail_parity, abort_flag, err, kWaitLimitCycles, 0x85);
+              tail_parity ^= 1u;
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              zero_rows<D, 64>(b_dst, max(rows_end - key0, 0), lane);
+              if (lane == 0) mbar_arrive(full_bar(stage));
+            }
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            continue;
+          }
           const uint32_t fb = full_bar(stage);
           mbar_expect_tx(fb, C::STAGE_BYTES);
           const uint32_t a_dst = sbase + stage * C::STAGE_BYTES, b_dst = a_dst + C::A_BYTES;
@@ -1033,12 +1222,13 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * D);
       if (lane == 0) bulk_wait_group_read0();  // the last tile's rows have left the staging buffer
       __syncwarp();
-      if (rope_cos != nullptr) stage_rows_unrotated<D>(out, table, lane, taddr, scale, rope_cos, rope_sin, row0, S);
+      if (rope_cos != nullptr) stage_rows_unrotated<D>(out, table, lane, taddr, scale, rope_cos, rope_sin, table_rows<DOCS>(pl, row0, lane));
       else stage_rows<D>(out, lane, taddr, scale);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
-      send_rows<D>(&tm_out, out, lane, r.n * D, row0, r.b, S);
+      if constexpr (DOCS) send_rows_clipped<D>(&tm_out, dqkv, hq + 2 * pl.n_kv * D, out, lane, r.n * D, row0, rows_end);
+      else send_rows<D>(&tm_out, out, lane, r.n * D, row0, r.b, S);
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
     }
@@ -1061,7 +1251,7 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
   static_assert(JOIN_SMEM <= C::OFF_OUT, "the stages hold a unit's columns");
   const int units = jn.units(pl, D);
   for (int u = (int)(gridDim.x - 1 - blockIdx.x); u < units; u += (int)gridDim.x)
-    join_unit<D, DQ_THREADS>(jn, pl, u, reinterpret_cast<float (*)[132]>(smem));
+    join_unit<D, DQ_THREADS, DOCS>(jn, pl, u, reinterpret_cast<float (*)[132]>(smem));
 }
 
 // ---------------------------------------------------------------- dQ without stored dS^T
@@ -1069,7 +1259,7 @@ attn_window_dq_kernel(const bf16* __restrict__ ds_band, const __grid_constant__ 
 // blocks (K, V) streamed, S and dP computed again into one of two TMEM buffers, dQ += dS K.
 // (S 8400, window 2000, 64 heads of 128: on one kv head, which takes this way, the backward pass is 2.58 ms with 29 MB of
 // scratch; on two, whose dS^T is stored, 2.26 ms with 1.2 GB.)
-enum { BB_XFULL = 0, BB_YFULL = 1, BB_YEMPTY = 5, BB_SDPFULL = 9, BB_TFULL = 11, BB_ACCDONE = 13, BB_COUNT = 14 };
+enum { BB_XFULL = 0, BB_YFULL = 1, BB_YEMPTY = 5, BB_SDPFULL = 9, BB_TFULL = 11, BB_ACCDONE = 13, BB_TAIL = 14, BB_COUNT = 15 };
 constexpr int DQR_THREADS = 352;  // producer, 2 MMA issuers, 8 compute warps
 
 template <int D>
@@ -1085,7 +1275,7 @@ struct DqrCfg {
   static constexpr int ACC0 = 256;
 };
 
-template <int D>
+template <int D, bool DOCS>
 __global__ void __launch_bounds__(DQR_THREADS, 1)
 attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, const __grid_constant__ CUtensorMap tm_qkv64,
                                 const __grid_constant__ CUtensorMap tm_do128, const float* __restrict__ lse,
@@ -1113,7 +1303,16 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
   const int rank = (int)blockIdx.x / all, grp = (int)blockIdx.x % all;
   const int x0 = (pl.nxb - 1 - rank) * 128;  // the first query blocks, with fewer keys, end the launch
   const int n_q = grp % n_heads, b = grp / n_heads, kvh = n_q / (n_heads / n_kv);
-  const KeyRuns runs(x0, S, pl.window, pl.sinks);
+  int rows_end = S;
+  KeyRuns runs;
+  if constexpr (DOCS) {
+    pdl_wait();
+    rows_end = docs_total(pl.docs, S);
+    if (x0 >= rows_end) return;
+    runs = KeyRuns(x0, rows_end, docs_start(pl.docs, x0));
+  } else {
+    runs = KeyRuns(x0, S, pl.window, pl.sinks);
+  }
   const int iters = runs.count;
 
   if (threadIdx.x == 0) {
@@ -1127,6 +1326,7 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
       mbar_init(bar(BB_TFULL + i), 8);
     }
     mbar_init(bar(BB_ACCDONE), 2);
+    if constexpr (DOCS) mbar_init(bar(BB_TAIL), 1);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tm_qkv128);
@@ -1157,11 +1357,23 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
         const int st = it % C::NST, y0 = runs.block(it) * 64;
         if (!mbar_wait(bar(BB_YEMPTY + st), (((uint32_t)(it / C::NST)) & 1u) ^ 1u, abort_flag, err, kWaitLimitCycles, 0x91)) break;
         const uint32_t ydst = sbase + C::OFF_Y + st * 2 * C::Y_BYTES;
-        mbar_expect_tx(bar(BB_YFULL + st), 2 * C::Y_BYTES);
+        const uint32_t full = bar(DOCS && y0 + 64 > rows_end ? BB_TAIL : BB_YFULL + st);  // only the last block can reach behind the end
+        mbar_expect_tx(full, 2 * C::Y_BYTES);
 #pragma unroll
         for (int kc = 0; kc < C::KC; ++kc) {
-          tma_load_3d(ydst + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), hq + kvh * D + kc * 64, y0, b);
-          tma_load_3d(ydst + C::Y_BYTES + kc * 8192, &tm_qkv64, bar(BB_YFULL + st), hq + hkv + kvh * D + kc * 64, y0, b);
+          tma_load_3d(ydst + kc * 8192, &tm_qkv64, full, hq + kvh * D + kc * 64, y0, b);
+          tma_load_3d(ydst + C::Y_BYTES + kc * 8192, &tm_qkv64, full, hq + hkv + kvh * D + kc * 64, y0, b);
+        }
+      }
+    }
+    if constexpr (DOCS) {  // its K loses the rows behind the last document (what V holds there only reaches masked scores)
+      __syncwarp();
+      const int y0 = runs.block(iters - 1) * 64, st = (iters - 1) % C::NST;
+      if (y0 + 64 > rows_end) {
+        const bool ok = mbar_wait(bar(BB_TAIL), 0, abort_flag, err, kWaitLimitCycles, 0x97);
+        if (__all_sync(0xffffffffu, ok)) {
+          zero_rows<D, 64>(sbase + C::OFF_Y + st * 2 * C::Y_BYTES, rows_end - y0, lane);
+          if (lane == 0) mbar_arrive(bar(BB_YFULL + st));
         }
       }
     }
@@ -1231,7 +1443,12 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
     const uint32_t tlane = tmem_base + ((uint32_t)(q * 32) << 16);
     const int rmin = x0 + q * 32, rmax = rmin + 31;
     float lse2_row = 0.f, delta_row = 0.f;
-    if (row < S) {
+    int own = 0, own_max = 0;  // first row of this row's document, and the greatest in the warp
+    if constexpr (DOCS) {
+      own = row < rows_end ? docs_start(pl.docs, row) : S;
+      own_max = __shfl_sync(0xffffffffu, own, 31);
+    }
+    if (row < rows_end) {
       const long long stat = ((long long)b * n_heads + n_q) * S;
       lse2_row = lse[stat + row] * kLog2e;
       delta_row = delta[stat + row];
@@ -1250,13 +1467,15 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
 
       // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
       const int cmin = runs.block(it) * 64 + ch * 32;
-      const bool full = cmin + 31 <= rmin && (rmax - cmin < pl.window || cmin + 32 <= pl.sinks);
-      const int hi = row - cmin, lo = row - pl.window + 1 - cmin, sk = pl.sinks - cmin;
+      const bool full = cmin + 31 <= rmin && (DOCS ? cmin >= own_max : rmax - cmin < pl.window || cmin + 32 <= pl.sinks);
+      const int hi = row - cmin, lo = DOCS ? own - cmin : row - pl.window + 1 - cmin, sk = DOCS ? 0 : pl.sinks - cmin;
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         float p = fast_exp2(fmaf(__uint_as_float(rs[i]), scale_log2, -lse2_row));
-        if (!full && (i > hi || (i < lo && i >= sk))) p = 0.f;
-        rp[i] = __float_as_uint(p * (__uint_as_float(rp[i]) - delta_row));
+        const bool masked = !full && (i > hi || (i < lo && i >= sk));
+        if (masked) p = 0.f;
+        const float ds = p * (__uint_as_float(rp[i]) - delta_row);
+        rp[i] = __float_as_uint(DOCS && masked ? 0.f : ds);
       }
       // bf16 pairs back into TMEM, over this warp's own (already loaded) fp32 columns
       uint32_t wd[16];
@@ -1283,10 +1502,10 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
 #pragma unroll
       for (int i = 0; i < W; ++i) { lo[i] *= scale; hi[i] *= scale; }
       if (rope_cos != nullptr) {
-        const int pos = min(row, S - 1);
+        const int pos = DOCS ? min(max(__ldg(pl.docs.pos + min(row, S - 1)), 0), pl.window - 1) : min(row, S - 1);
         unrotate<W>(lo, hi, rope_cos + (long long)pos * H + i0, rope_sin + (long long)pos * H + i0);
       }
-      if (row < S) {
+      if (row < rows_end) {
         bf16* dst = dqkv + ((long long)b * S + row) * ld + n_q * D;
         store_bf16_row<W>(dst + i0, lo);
         store_bf16_row<W>(dst + H + i0, hi);
@@ -1312,8 +1531,10 @@ attn_window_dq_recompute_kernel(const __grid_constant__ CUtensorMap tm_qkv128, c
 // Parts: where the launch has several times more streamed blocks than SMs, a part is as long as a window block's whole list
 // (or an eighth of a slot's share, if that is longer), so that only sink blocks are cut.  Smaller launches are cut into one
 // part per slot (of a CTA on an SM), of at least 4 blocks: the set-up and the partial sums of a part cost about as much as 2.
-// Groups: dS^T is kept for as many (batch row, kv head) groups at a time as kDsBytes holds.
-constexpr size_t kDsBytes = (size_t)1 << 30;
+// Groups: dS^T is kept for as many (batch row, kv head) groups at a time as kDsBytes holds; of packed documents, whose lists
+// differ far more in length, as kDocsDsBytes holds: every round of groups ends with SMs that wait for its longest list (T 16384,
+// 4 documents of up to 5622 rows, 16 / 8 heads of 128: in 8 rounds 2213 us).
+constexpr size_t kDsBytes = (size_t)1 << 30, kDocsDsBytes = (size_t)4 << 30;
 
 struct Scratch {
   size_t delta, partial, band, sink, total;  // byte offsets and size
@@ -1336,7 +1557,7 @@ int block_of(int B, int S, int nh, int d, int window) {
   return d == 64 && (long long)B * nh * ((S + 127) / 128) * window_blocks(S, window) > 6 * kSms ? 64 : 128;
 }
 
-Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l, int d, int block) {
+Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l, int d, int block, bool docs) {
   Plan p;
   p.S = S; p.n_heads = nh; p.n_kv = nkv; p.window = window; p.sinks = sinks;
   p.nxb = (S + 127) / 128;
@@ -1364,12 +1585,13 @@ Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l,
   l->delta = 0;
   l->partial = round256((size_t)B * nh * S * sizeof(float));
   l->band = l->partial + part_slots * p.all_groups * (2 * d * 128) * sizeof(float);
-  const size_t band = (size_t)n_rep * p.nxb * p.nb * 32768;  // of one group
+  const size_t tiles = docs ? p.band_at<true>(p.nxb) : p.band_at<false>(p.nxb), keep = docs ? kDocsDsBytes : kDsBytes;
+  const size_t band = (size_t)n_rep * tiles * 32768;  // of one group
   const size_t sink = p.nxb > p.nb ? (size_t)n_rep * p.nxb * 4 * sinks * 64 : 0;
-  l->stored = band + sink <= 2 * kDsBytes;
+  l->stored = band + sink <= (docs ? keep : 2 * keep);
   l->sink = l->total = l->band;
   if (l->stored) {
-    size_t fit = kDsBytes / (band + sink);
+    size_t fit = keep / (band + sink);
     if (fit < 1) fit = 1;
     const int rounds = (int)((p.all_groups + fit - 1) / fit);
     p.groups = (p.all_groups + rounds - 1) / rounds;
@@ -1379,15 +1601,17 @@ Plan make_plan(int B, int S, int nh, int nkv, int window, int sinks, Scratch* l,
   return p;
 }
 
-template <int D, int BLOCK>
+template <int D, int BLOCK, bool DOCS>
 cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs, const float* sn,
-                  uint8_t* scratch, int B, int S, int nh, int nkv, int window, int sinks, int* err, cudaStream_t st, int& launches) {
+                  uint8_t* scratch, int B, int S, int nh, int nkv, int window, int sinks, const Docs& docs, int* err, cudaStream_t st,
+                  int& launches) {
   Scratch l;
-  Plan pl = make_plan(B, S, nh, nkv, window, sinks, &l, D, BLOCK);
+  Plan pl = make_plan(B, S, nh, nkv, window, sinks, &l, D, BLOCK, DOCS);
+  pl.docs = docs;
   static unsigned long long set_kv = 0, set_q = 0, set_r = 0;
-  cudaError_t e = ensure_dynamic_smem(attn_window_dkv_kernel<D, BLOCK>, DkvCfg<D, BLOCK>::SMEM_BYTES, set_kv);
-  if (e == cudaSuccess && l.stored) e = ensure_dynamic_smem(attn_window_dq_kernel<D>, DqCfg<D>::SMEM_BYTES, set_q);
-  if (e == cudaSuccess && !l.stored) e = ensure_dynamic_smem(attn_window_dq_recompute_kernel<D>, DqrCfg<D>::SMEM_BYTES, set_r);
+  cudaError_t e = ensure_dynamic_smem(attn_window_dkv_kernel<D, BLOCK, DOCS>, DkvCfg<D, BLOCK>::SMEM_BYTES, set_kv);
+  if (e == cudaSuccess && l.stored) e = ensure_dynamic_smem(attn_window_dq_kernel<D, DOCS>, DqCfg<D>::SMEM_BYTES, set_q);
+  if (e == cudaSuccess && !l.stored) e = ensure_dynamic_smem(attn_window_dq_recompute_kernel<D, DOCS>, DqrCfg<D>::SMEM_BYTES, set_r);
   if (e != cudaSuccess) return e;
   float* delta = reinterpret_cast<float*>(scratch + l.delta);
   float* partial = reinterpret_cast<float*>(scratch + l.partial);
@@ -1416,26 +1640,26 @@ cudaError_t bwd_t(const bf16* qkv, const bf16* o, const bf16* d_o, const float* 
   for (int g0 = 0; g0 < pl.all_groups && e == cudaSuccess; g0 += per_round) {
     pl.group0 = g0;
     pl.groups = pl.all_groups - g0 < per_round ? pl.all_groups - g0 : per_round;
-    e = launch_pdl(attn_window_dkv_kernel<D, BLOCK>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D, BLOCK>::SMEM_BYTES, st,
-                   tq128, DkvCfg<D, BLOCK>::BQ == 128 ? tq128 : tq64, tdo, tout, lse, delta, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
+    e = launch_pdl(attn_window_dkv_kernel<D, BLOCK, DOCS>, dim3((unsigned)pl.ranks() * pl.groups), dim3(DKV_THREADS), DkvCfg<D, BLOCK>::SMEM_BYTES, st,
+                   tq128, DkvCfg<D, BLOCK>::BQ == 128 ? tq128 : tq64, tdo, tout, lse, delta, dqkv, partial, band, sink, cs, sn, pl, scale, scale_log2, err);
     ++launches;
     if (e != cudaSuccess || !l.stored) continue;
     const bool last = g0 + per_round >= pl.all_groups;
     const long long ctas = (long long)pl.nxb * pl.groups * n_rep + (last ? jn.units(pl, D) : 0);
-    e = launch_pdl(attn_window_dq_kernel<D>, dim3((unsigned)(ctas < 2 * sms ? ctas : 2 * sms)), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
-                   (const bf16*)band, tsink, tq64, tout, cs, sn, pl, last ? jn : none, scale, err);
+    e = launch_pdl(attn_window_dq_kernel<D, DOCS>, dim3((unsigned)(ctas < 2 * sms ? ctas : 2 * sms)), dim3(DQ_THREADS), DqCfg<D>::SMEM_BYTES, st,
+                   (const bf16*)band, tsink, tq64, tout, dqkv, cs, sn, pl, last ? jn : none, scale, err);
     ++launches;
   }
   if (e != cudaSuccess) return e;
   if (!l.stored) {
-    e = launch_pdl(attn_window_dq_recompute_kernel<D>, dim3((unsigned)(pl.nxb * nh * B)), dim3(DQR_THREADS), DqrCfg<D>::SMEM_BYTES, st,
+    e = launch_pdl(attn_window_dq_recompute_kernel<D, DOCS>, dim3((unsigned)(pl.nxb * nh * B)), dim3(DQR_THREADS), DqrCfg<D>::SMEM_BYTES, st,
                    tq128, tq64, td128, lse, delta, dqkv, cs, sn, pl, scale, scale_log2, err);
     if (e != cudaSuccess) return e;
     ++launches;
   }
   if (l.stored || jn.cut == 0) return cudaSuccess;
   ++launches;
-  return launch_pdl(attn_window_join_kernel<D>, dim3((unsigned)jn.units(pl, D)), dim3(256), 0, st, jn, pl);
+  return launch_pdl(attn_window_join_kernel<D, DOCS>, dim3((unsigned)jn.units(pl, D)), dim3(256), 0, st, jn, pl);
 }
 
 // Shapes the kernels take: 32-bit grids and tensor-map extents, element counts of one row within 31 bits.
@@ -1459,15 +1683,15 @@ cudaError_t attention_window_fwd(const bf16* qkv, bf16* o, float* lse, int B, in
                                  int* err, cudaStream_t st) {
   if (!shape_ok(B, S, nh, nkv, d, window, sinks) || !err) return cudaErrorInvalidValue;
   clamp_mask(S, window, sinks);
-  if (d == 64) return fwd_t<64>(qkv, o, lse, B, S, nh, nkv, window, sinks, err, st);
-  return fwd_t<128>(qkv, o, lse, B, S, nh, nkv, window, sinks, err, st);
+  if (d == 64) return fwd_t<64, false>(qkv, o, lse, B, S, nh, nkv, window, sinks, Docs{}, err, st);
+  return fwd_t<128, false>(qkv, o, lse, B, S, nh, nkv, window, sinks, Docs{}, err, st);
 }
 
 size_t attention_window_scratch_bytes(int B, int S, int nh, int nkv, int d, int window, int sinks) {
   if (!shape_ok(B, S, nh, nkv, d, window, sinks)) return 0;
   clamp_mask(S, window, sinks);
   Scratch l;
-  make_plan(B, S, nh, nkv, window, sinks, &l, d, block_of(B, S, nh, d, window));
+  make_plan(B, S, nh, nkv, window, sinks, &l, d, block_of(B, S, nh, d, window), false);
   return l.total;
 }
 
@@ -1501,9 +1725,38 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
   uint8_t* s = reinterpret_cast<uint8_t*>(scratch);
   int unused = 0;
   int& n = launches != nullptr ? *launches : unused;
-  if (block_of(B, S, nh, d, window) == 64) return bwd_t<64, 64>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st, n);
-  if (d == 64) return bwd_t<64, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st, n);
-  return bwd_t<128, 128>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, err, st, n);
+  if (block_of(B, S, nh, d, window) == 64) return bwd_t<64, 64, false>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, Docs{}, err, st, n);
+  if (d == 64) return bwd_t<64, 128, false>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, Docs{}, err, st, n);
+  return bwd_t<128, 128, false>(qkv, o, d_o, lse, dqkv, cs, sn, s, B, S, nh, nkv, window, sinks, Docs{}, err, st, n);
+}
+
+// ---------------------------------------------------------------- packed documents: one sequence of T rows
+// The plan is that of a window as long as the longest document, which no key block can meet more query blocks than; what the
+// documents really need is read on the device.
+cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int nh, int nkv, int d, int* err, cudaStream_t st) {
+  if (!shape_ok(1, T, nh, nkv, d, 1, 0) || !err) return cudaErrorInvalidValue;
+  if (d == 64) return fwd_t<64, true>(qkv, o, lse, 1, T, nh, nkv, T, 0, docs, err, st);
+  return fwd_t<128, true>(qkv, o, lse, 1, T, nh, nkv, T, 0, docs, err, st);
+}
+
+size_t attention_packed_scratch_bytes(int T, int nh, int nkv, int d, int longest) {
+  if (!shape_ok(1, T, nh, nkv, d, longest, 0)) return 0;
+  if (longest > T) longest = T;
+  Scratch l;
+  make_plan(1, T, nh, nkv, longest, 0, &l, d, block_of(1, T, nh, d, longest), true);
+  return l.total;
+}
+
+cudaError_t attention_packed_bwd(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cs,
+                                 const float* sn, const Docs& docs, void* scratch, int T, int nh, int nkv, int d, int longest, int* err,
+                                 cudaStream_t st) {
+  if (!shape_ok(1, T, nh, nkv, d, longest, 0) || !err || (cs == nullptr) != (sn == nullptr)) return cudaErrorInvalidValue;
+  if (longest > T) longest = T;
+  uint8_t* s = reinterpret_cast<uint8_t*>(scratch);
+  int n = 0;
+  if (block_of(1, T, nh, d, longest) == 64) return bwd_t<64, 64, true>(qkv, o, d_o, lse, dqkv, cs, sn, s, 1, T, nh, nkv, longest, 0, docs, err, st, n);
+  if (d == 64) return bwd_t<64, 128, true>(qkv, o, d_o, lse, dqkv, cs, sn, s, 1, T, nh, nkv, longest, 0, docs, err, st, n);
+  return bwd_t<128, 128, true>(qkv, o, d_o, lse, dqkv, cs, sn, s, 1, T, nh, nkv, longest, 0, docs, err, st, n);
 }
 
 }  // namespace fs

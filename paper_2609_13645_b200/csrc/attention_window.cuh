@@ -21,4 +21,18 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
                                  const float* sin, void* scratch, int B, int S, int n_heads, int n_kv, int d, int window, int sinks,
                                  int* err, cudaStream_t st, int* launches = nullptr);
 
+// Attention inside the documents of a packed batch of T rows: row i sees the rows from its document's first one to itself.
+// start, end: first row of a row's document and the one behind its last (rows behind the last document: T and the number of rows
+// in front of them); pos: row - start, the row of the rotation tables.
+struct Docs {
+  const int *start, *end, *pos;
+};
+cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int n_heads, int n_kv, int d, int* err,
+                                 cudaStream_t st);
+// longest: rows of the longest document, at most; cos, sin: fp32 [longest, d / 2] or null.
+size_t attention_packed_scratch_bytes(int T, int n_heads, int n_kv, int d, int longest);
+cudaError_t attention_packed_bwd(const bf16* qkv, const bf16* o, const bf16* d_o, const float* lse, bf16* dqkv, const float* cos,
+                                 const float* sin, const Docs& docs, void* scratch, int T, int n_heads, int n_kv, int d, int longest,
+                                 int* err, cudaStream_t st);
+
 }  // namespace fs

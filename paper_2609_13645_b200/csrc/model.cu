@@ -1790,7 +1790,7 @@ ft_status ft_k_status(void* stream) {
   if (v == 0) return FT_OK;
   if (cudaMemsetAsync(status, 0, sizeof(int), st) != cudaSuccess) return FT_ECUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return FT_ECUDA;
-  return FT_ETIMEOUT;
+  return (v & 0xff) == ERR_BAD_INDEX ? FT_EINVAL : FT_ETIMEOUT;
 }
 
 ft_status ft_k_attention_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, int32_t B, int32_t S, int32_t n_heads,
