@@ -184,14 +184,7 @@ __device__ __forceinline__ Two root(Two a) {  // a.h > 0
   return {h, __fsub_rn(e, __fsub_rn(h, r))};
 }
 
-// A moment (ROOT: the second one's root) of an element from its code, scale and gradient: in two parts, and in 64 bits as the
-// definition orders the operations.
-template <bool ROOT>
-__device__ __forceinline__ Two moment_two(const StepArgs& a, float code, float scale, float g, float clip) {
-  const Two kept = product(code, scale), d = product(g, clip);
-  if (!ROOT) return sum(product(Two{a.b1[0], a.b1[1]}, kept), product(Two{a.o1[0], a.o1[1]}, d));
-  return root(sum(product(Two{a.b2[0], a.b2[1]}, product(kept, kept)), product(product(Two{a.o2[0], a.o2[1]}, d), d)));
-}
+// A moment (ROOT: the second one's root) of an element from its code, scale and gradient, as the definition orders the operations.
 template <bool ROOT>
 __device__ __forceinline__ double moment_64(const StepArgs& a, float code, float scale, float g, float clip) {
   const double kept = __dmul_rn((double)code, (double)scale), d = __dmul_rn((double)g, (double)clip);
@@ -199,73 +192,79 @@ __device__ __forceinline__ double moment_64(const StepArgs& a, float code, float
   return __dsqrt_rn(__dadd_rn(__dmul_rn(a.beta2, __dmul_rn(kept, kept)), __dmul_rn(__dmul_rn(a.omb2, d), d)));
 }
 
-// ---- codes without sign
-// floor(|y| / step + bits / 65536) steps.  From 2^-6 on a step is the last of 3 mantissa bits, below it is 2^-9: there 2^-6 is added
-// first, which gives the number the same step.  rest: what the floor cuts off, in 2^-20 steps; b: the number it was cut off from.
-__device__ __forceinline__ uint32_t round_random(float a, uint32_t bits, uint32_t& rest, float& b) {
-  const bool small = a < 0.015625f;
-  b = small ? a + 0.015625f : a;
-  const uint32_t u = __float_as_uint(b) + (bits << 4);
-  rest = u & 0xfffffu;
-  return min((u >> 20) - (small ? 968u : 960u), 126u);
-}
+// ---- rounding: floor(|y| / step + bits / 65536) steps; from 2^-6 on a step is the last of 3 mantissa bits, below it is 2^-9
+// y 2^-120 has its code in bits 20 to 26 (below 2^-6 it is a denormal number, whose bits count the same steps), and what is cut off behind
+// them.  Here all that lies 4 places further up, so that the code ends at the top byte without y's sign, and `random` (16 bits, 8
+// places up) is added.
+__device__ __forceinline__ uint32_t with_random(float small, uint32_t random) { return __float_as_uint(small) * 16u + random; }
+// Whether what lies behind the code is within off / 2^20 steps of a border; off in the low 23 bits of its argument.
+__device__ __forceinline__ bool at_border(uint32_t sum, uint32_t off) { return sum * 256u + off * 4096u <= off * 8192u; }
 __device__ __forceinline__ uint32_t round_random(double a, uint32_t bits) {
   const int e = a < 0.015625 ? 0 : (__double2hiint(a) >> 20) - 1023 + 6;  // binades above 2^-6
   const double steps = a * __hiloint2double((1023 + 9 - e) << 20, 0);     // 8 to 16 of them in a binade, up to 8 below
   return min((uint32_t)((int)floor(steps + (double)bits * (1.0 / 65536.0)) + 8 * e), 126u);
 }
 
-// A run's greatest element: its fp32 bits, and the scale that belongs to it in 64 bits.  Infinities and NaN are the greatest bit patterns.
-// Every lane brings its own greatest element (index, gradient); the winner among them is found on their values in two parts.
+// A run's greatest element: fp32 bits (infinities and NaN are the greatest), and its scale.
 struct RunTop {
-  uint32_t own, top;  // bits of the lane's, of the run's
-  int index;          // of the lane's
-  float g;
-  float scale;  // 0: the run is 0; infinite or NaN: so is the run
+  uint32_t own, top;  // of the lane, with the element's number in place of the last 3 bits; of the run, without them
+  float g, code;      // the lane's element's gradient and old code
+  float scale;        // 0: the run is 0; infinite or NaN: so is the run
   __device__ __forceinline__ bool coded() const { return top >= 0x0d800000u && top < 0x7f800000u; }  // from 2^-100 on
+  __device__ __forceinline__ bool may_win() const { return own >= top - 64u; }                         // a few roundings below
 };
-// That scale in 64 bits, from the elements within a few roundings of the greatest fp32 one.
+__device__ __forceinline__ RunTop greatest(const float (&x)[8], const float (&g)[8], uint2 old) {
+  RunTop t;
+  uint32_t key[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) key[i] = (__float_as_uint(x[i]) & 0x7ffffff8u) | (uint32_t)i;
+  t.own = max(max(max(key[0], key[1]), max(key[2], key[3])), max(max(key[4], key[5]), max(key[6], key[7])));
+  t.top = __reduce_max_sync(0xffffffffu, t.own) & ~7u;
+  const bool b0 = t.own & 1u, b1 = t.own & 2u, b2 = t.own & 4u;
+  const float g01 = b0 ? g[1] : g[0], g23 = b0 ? g[3] : g[2], g45 = b0 ? g[5] : g[4], g67 = b0 ? g[7] : g[6];
+  t.g = b2 ? (b1 ? g67 : g45) : (b1 ? g23 : g01);
+  t.code = code_value(old, t.own & 7);
+  t.scale = t.top >= 0x7f800000u ? __uint_as_float(t.top) : 0.f;
+  return t;
+}
+// The scale in 64 bits.
 template <bool ROOT>
-__device__ __noinline__ double run_unit(const RunTop& t, const StepArgs& a, uint2 codes, float scale, float clip) {
-  double most = t.own >= t.top - 64u ? fabs(moment_64<ROOT>(a, code_value(codes, t.index), scale, t.g, clip)) : 0.0;
+__device__ __noinline__ double run_unit(const RunTop& t, const StepArgs& a, float scale, float clip) {
+  double most = t.may_win() ? fabs(moment_64<ROOT>(a, t.code, scale, t.g, clip)) : 0.0;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
   return __dmul_rn(most, 1.0 / 448.0);
 }
-template <bool ROOT>
-__device__ __forceinline__ RunTop run_top(const float (&x)[8], const float (&g)[8], const StepArgs& a, uint2 codes, float scale, float clip) {
-  RunTop t{0u, 0u, 0, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
-    if (bits > t.own) { t.own = bits; t.index = i; t.g = g[i]; }
-  }
-  t.top = __reduce_max_sync(0xffffffffu, t.own);
-  if (t.coded()) {
-    const Two v = moment_two<ROOT>(a, code_value(codes, t.index), scale, t.g, clip);
-    const uint32_t h = t.own >= t.top - 64u ? __float_as_uint(v.h) & 0x7fffffffu : 0u, most = __reduce_max_sync(0xffffffffu, h);
-    const float l = h == most ? (v.h < 0.f ? -v.l : v.l) : -INFINITY;
-    const uint32_t k = __float_as_uint(l), order = k >> 31 ? ~k : k | 0x80000000u;  // floats as ordered integers
-    const uint32_t best = __reduce_max_sync(0xffffffffu, order);
-    const Two m{__uint_as_float(most), __uint_as_float(best >> 31 ? best & 0x7fffffffu : ~best)};
-    const Two s = product(m, Two{1.f / 448.f, (float)(1.0 / 448.0 - (double)(1.f / 448.f))});
-    t.scale = __fadd_rn(s.h, s.l);
-    // Half way between two fp32 numbers but for the last places of 64 bits (one run in a thousand: the betas are decimal fractions,
-    // whose multiples of fp32 numbers land there)
-    const float half_step = __uint_as_float(__float_as_uint(t.scale) & 0x7f800000u) * 5.9604645e-8f;
-    if (fabsf(fabsf(__fadd_rn(__fsub_rn(s.h, t.scale), s.l)) - half_step) < half_step * 1e-3f) t.scale = (float)run_unit<ROOT>(t, a, codes, scale, clip);
-  } else if (t.top >= 0x7f800000u) {
-    t.scale = __uint_as_float(t.top);
-  }
-  return t;
+// The scales of both moments: the winners' values in two parts, m's on the lower lanes and the root of v's on the upper ones.  Where more
+// than one lane may hold the winner, or the scale lies half way between two fp32 numbers but for the last places of 64 bits (one
+// run in a thousand: the betas are decimal fractions, whose multiples of fp32 numbers land there), in 64 bits.
+__device__ __forceinline__ void run_scales(RunTop& m, RunTop& v, const StepArgs& a, float scale_m, float scale_v, float clip) {
+  const uint32_t who_m = __ballot_sync(0xffffffffu, m.may_win()), who_v = __ballot_sync(0xffffffffu, v.may_win());
+  const int lane_m = __ffs(who_m) - 1, lane_v = __ffs(who_v) - 1;
+  const float gm = __shfl_sync(0xffffffffu, m.g, lane_m), cm = __shfl_sync(0xffffffffu, m.code, lane_m);
+  const float gv = __shfl_sync(0xffffffffu, v.g, lane_v), cv = __shfl_sync(0xffffffffu, v.code, lane_v);
+  const bool second = (threadIdx.x & 16u) != 0;
+  Two kept = product(second ? cv : cm, second ? scale_v : scale_m);
+  const Two d = product(second ? gv : gm, clip);
+  Two grown = product(second ? Two{a.o2[0], a.o2[1]} : Two{a.o1[0], a.o1[1]}, d);
+  const Two square = product(kept, kept), twice = product(grown, d);
+  if (second) { kept = square; grown = twice; }
+  Two x = sum(product(second ? Two{a.b2[0], a.b2[1]} : Two{a.b1[0], a.b1[1]}, kept), grown);
+  const Two r = root(x);
+  if (second) x = r;
+  x = product(x, Two{1.f / 448.f, (float)(1.0 / 448.0 - (double)(1.f / 448.f))});
+  const float scale = __fadd_rn(x.h, x.l), half_step = __uint_as_float(__float_as_uint(scale) & 0x7f800000u) * 5.9604645e-8f;
+  const uint32_t tie = __ballot_sync(0xffffffffu, fabsf(fabsf(__fadd_rn(__fsub_rn(x.h, scale), x.l)) - half_step) < half_step * 1e-3f);
+  const float sm = fabsf(__shfl_sync(0xffffffffu, scale, 0)), sv = __shfl_sync(0xffffffffu, scale, 16);
+  if (m.coded()) m.scale = (who_m & (who_m - 1)) != 0 || (tie & 1u) != 0 ? (float)run_unit<false>(m, a, scale_m, clip) : sm;
+  if (v.coded()) v.scale = (who_v & (who_v - 1)) != 0 || (tie & 0x10000u) != 0 ? (float)run_unit<true>(v, a, scale_v, clip) : sv;
 }
-// Codes that fp32 leaves open (bits of `close`), formed in 64 bits.
+// The codes of lanes in which fp32 leaves one open, formed in 64 bits.
 template <bool ROOT, typename G>
-__device__ __noinline__ uint2 settle(uint2 codes, uint32_t close, const RunTop& t, const StepArgs& a, uint2 old, float scale, float clip, const G* grad,
+__device__ __noinline__ uint2 settle(uint2 codes, bool open, int n, const RunTop& t, const StepArgs& a, uint2 old, float scale, float clip, const G* grad,
                                      unsigned long long key, unsigned long long first) {
-  const double unit = run_unit<ROOT>(t, a, old, scale, clip);
-  for (; close != 0; close &= close - 1) {
-    const int i = __ffs(close) - 1;
+  const double unit = run_unit<ROOT>(t, a, scale, clip);
+  for (int i = 0; i < (open ? n : 0); ++i) {
     const unsigned long long word = splitmix64(key ^ ((first + (unsigned long long)(i >> 1)) * kGroupKey));
     const uint32_t bits = (uint32_t)(word >> (32 * (i & 1) + (ROOT ? 16 : 0))) & 0xffffu;
     const double e = moment_64<ROOT>(a, code_value(old, i), scale, (float)grad[i], clip);
@@ -277,6 +276,21 @@ __device__ __noinline__ uint2 settle(uint2 codes, uint32_t close, const RunTop& 
   return codes;
 }
 
+__device__ __forceinline__ float approx_root(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float approx_inverse(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// 8 elements a thread, a run a warp.  Bound by instructions: 835 a run (104 an element), of which those of the integer unit (58 % busy,
+// with 67 % of all issue slots) matter most: codes are shifted and added by multiplications, and pairs of fp32 numbers share an
+// instruction.  Of 124M parameters' 557 us, the random bits take about 110, the scales in two parts 60, codes settled in 64
+// bits 30; the bytes would take 334.
 template <bool PARAM16, bool GRAD16>
 __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, bool vec, const StepArgs& a, const AdamCoef& c, float clip,
                                       float root_rbc2, unsigned long long key) {
@@ -294,49 +308,70 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   {
     float p[8];
     load8(pp, n, vec, p);
+    const float wd = w.wd;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float d = g[i] * clip;
-      m[i] = fmaf(c.beta1, m[i], c.omb1 * d);
-      r[i] = fmaf(c.beta2, r[i] * r[i], c.omb2 * d * d);
-      asm("sqrt.approx.f32 %0, %1;" : "=f"(r[i]) : "f"(r[i]));
-      float quot;  // within 2^-22, as the 32-bit update's
-      asm("div.approx.f32 %0, %1, %2;" : "=f"(quot) : "f"(m[i] * c.rbc1), "f"(fmaf(r[i], root_rbc2, c.eps)));
-      p[i] = fmaf(-c.lr, fmaf(w.wd, p[i], quot), p[i]);
-      if (i >= n) m[i] = r[i] = 0.f;
+    for (int i = 0; i < 8; i += 2) {
+      const float2 d = mul2(make_float2(g[i], g[i + 1]), both(clip)), r0 = make_float2(r[i], r[i + 1]), p0 = make_float2(p[i], p[i + 1]);
+      const float2 m1 = fma2(both(c.beta1), make_float2(m[i], m[i + 1]), mul2(both(c.omb1), d));
+      const float2 v1 = fma2(both(c.beta2), mul2(r0, r0), mul2(mul2(both(c.omb2), d), d));
+      const float2 r1 = make_float2(approx_root(v1.x), approx_root(v1.y));
+      const float2 den = fma2(r1, both(root_rbc2), both(c.eps));
+      const float2 quot = mul2(mul2(m1, both(c.rbc1)), make_float2(approx_inverse(den.x), approx_inverse(den.y)));  // within 2^-21
+      const float2 p1 = fma2(both(-c.lr), fma2(both(wd), p0, quot), p0);
+      m[i] = m1.x; m[i + 1] = m1.y;
+      r[i] = r1.x; r[i + 1] = r1.y;
+      p[i] = p1.x; p[i + 1] = p1.y;
     }
     store8(pp, n, vec, p);
     if (w.copy != nullptr) store8(w.copy + at, n, vec, p);
   }
-  const RunTop tm = run_top<false>(m, g, a, old_m, scale_m, clip), tv = run_top<true>(r, g, a, old_v, scale_v, clip);
-  const float inv_m = tm.coded() ? __fdividef(448.f, __uint_as_float(tm.top)) : 0.f, inv_v = tv.coded() ? __fdividef(448.f, __uint_as_float(tv.top)) : 0.f;
-  const unsigned long long first = (unsigned long long)(w.base + at) / 2;
-  unsigned long long group = first * kGroupKey;
-  uint2 cm = make_uint2(0u, 0u), cv = make_uint2(0u, 0u);
-  uint32_t close_m = 0, close_v = 0;
-  // an element's fp32 error in 2^-20 steps, which are the last places of b: a dozen roundings, of what it was added up from where that cancels
-  const float grads = 16.f * c.omb1 * fabsf(clip) * inv_m;
+  if (n < 8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    static_assert(kRun == 256, "a word serves two elements");
-    const unsigned long long word = splitmix64(key ^ (group + (unsigned long long)(i >> 1) * kGroupKey));
-    const uint32_t bits = (uint32_t)(word >> (32 * (i & 1)));
-    uint32_t rest;
-    float b;
-    uint32_t code = round_random(fabsf(m[i]) * inv_m, bits & 0xffffu, rest, b) | ((__float_as_uint(m[i]) >> 24) & 0x80u);
-    const uint32_t off = 40u + (uint32_t)fminf(fabsf(g[i]) * grads * __uint_as_float(0x7f000000u - (__float_as_uint(b) & 0x7f800000u)), 262144.f);
-    if (((rest + off) & 0xfffffu) <= 2 * off) close_m |= 1u << i;
-    if (i < 4) cm.x |= code << (8 * i);
-    else cm.y |= code << (8 * (i - 4));
-    code = max(round_random(r[i] * inv_v, bits >> 16, rest, b), r[i] > 0.f ? 1u : 0u);
-    if (((rest + 32u) & 0xfffffu) <= 64u) close_v |= 1u << i;
-    if (i < 4) cv.x |= code << (8 * i);
-    else cv.y |= code << (8 * (i - 4));
+    for (int i = 0; i < 8; ++i)
+      if (i >= n) m[i] = r[i] = 0.f;
   }
+  RunTop tm = greatest(m, g, old_m), tv = greatest(r, g, old_v);
+  run_scales(tm, tv, a, scale_m, scale_v, clip);
+  const float less = 1.f - 4.76837158e-7f;
+  const float inv_m = tm.coded() ? approx_inverse(tm.scale) * less : 0.f, inv_v = tv.coded() ? approx_inverse(tv.scale) * less : 0.f;
+  const unsigned long long first = (unsigned long long)(w.base + at) / 2;
+  uint2 cm, cv;
+  bool open_m = false, open_v = false;
+  // An element's fp32 error in 2^-20 steps, which are the last places of what the floor is taken of: under 8 for its own roundings (6 at
+  // most in the element, 2 in the inverse), 4 more that the inverse is made smaller by (the greatest element stays under 448), and 1.5 of
+  // the terms' that it was added up from, |beta1 m| <= |sum| + |gradient's|.
+  const float grads = 4.f * c.omb1 * fabsf(clip) * inv_m;
+  const uint32_t off_v = 14u;
+  uint32_t sm[8], sv[8];
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const unsigned long long word = splitmix64(key ^ ((first + (unsigned long long)(i >> 1)) * kGroupKey));
+    const float2 ym = mul2(make_float2(m[i], m[i + 1]), both(inv_m)), yv = mul2(make_float2(r[i], r[i + 1]), both(inv_v));
+    const float2 fm = mul2(ym, both(7.52316385e-37f)), fv = mul2(yv, both(7.52316385e-37f));
+    const float2 t = mul2(make_float2(fabsf(g[i]), fabsf(g[i + 1])), both(grads));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t bits = (uint32_t)(word >> (32 * k));
+      const float y = k == 0 ? ym.x : ym.y;
+      // 2^-e of the binade that the number, or 2^-6 where that is more, lies in; the sum's low bits are the number of places
+      const float binade = __uint_as_float(0x7f000000u - (__float_as_uint(fmaxf(fabsf(y), 0.015625f)) & 0x7f800000u));
+      const float places = fmaf(fminf((k == 0 ? t.x : t.y) * binade, 262144.f), 1.f, 8388608.f + 14.f);
+      sm[i + k] = with_random(k == 0 ? fm.x : fm.y, __byte_perm(bits, 0u, 0x4104));
+      open_m |= at_border(sm[i + k], __float_as_uint(places));
+      sm[i + k] = (sm[i + k] & 0x7fffffffu) | (__float_as_uint(m[i + k]) & 0x80000000u);
+      sv[i + k] = with_random(k == 0 ? fv.x : fv.y, __byte_perm(bits, 0u, 0x4324));
+      open_v |= at_border(sv[i + k], off_v);
+      if (r[i + k] > 0.f) sv[i + k] = max(sv[i + k], 0x01000000u);
+      else sv[i + k] = 0u;
+    }
+  }
+  auto top_bytes = [](const uint32_t* x) { return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410); };
+  cm = make_uint2(top_bytes(sm), top_bytes(sm + 4));
+  cv = make_uint2(top_bytes(sv), top_bytes(sv + 4));
   if (!tm.coded()) cm = tm.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);  // all 1: what the scale is
-  else if (__any_sync(0xffffffffu, close_m != 0)) cm = settle<false, G>(cm, n == 8 ? close_m : close_m & ((1u << n) - 1u), tm, a, old_m, scale_m, clip, gp, key, first);
+  else if (__any_sync(0xffffffffu, open_m)) cm = settle<false, G>(cm, open_m, n, tm, a, old_m, scale_m, clip, gp, key, first);
   if (!tv.coded()) cv = tv.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);
-  else if (__any_sync(0xffffffffu, close_v != 0)) cv = settle<true, G>(cv, n == 8 ? close_v : close_v & ((1u << n) - 1u), tv, a, old_v, scale_v, clip, gp, key, first);
+  else if (__any_sync(0xffffffffu, open_v)) cv = settle<true, G>(cv, open_v, n, tv, a, old_v, scale_v, clip, gp, key, first);
   store_codes(mp, n, vec, cm);
   store_codes(vp, n, vec, cv);
   __syncwarp();  // every lane has read the scales
@@ -346,8 +381,24 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   }
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+// Asks for a whole chunk's arrays, by one thread, so that a block that gets to them finds them in L2.  It pays with 8-bit moments, whose
+// kernel has registers for 3 blocks an SM (599 us without, 573 with it), and not with fp32 ones (647 and 670).
 template <bool PARAM16, bool GRAD16, int BITS>
-__global__ void __launch_bounds__(kThreads, BITS == 8 ? 4 : 4)
+__device__ __forceinline__ void prefetch_chunk(const PlanTensor& w, int index) {
+  const long long at = (long long)index * kChunk;
+  if (w.aligned == 0 || at + kChunk > w.n) return;
+  constexpr int P = PARAM16 ? 2 : 4, G = GRAD16 ? 2 : 4, M = BITS / 8;
+  prefetch_l2(reinterpret_cast<const uint8_t*>(w.p) + at * P, kChunk * P);
+  prefetch_l2(reinterpret_cast<const uint8_t*>(w.g) + at * G, kChunk * G);
+  prefetch_l2(reinterpret_cast<const uint8_t*>(w.m) + at * M, kChunk * M);
+  prefetch_l2(reinterpret_cast<const uint8_t*>(w.v) + at * M, kChunk * M);
+}
+
+template <bool PARAM16, bool GRAD16, int BITS>
+__global__ void __launch_bounds__(kThreads, BITS == 8 ? 3 : 4)
 adamw_kernel(const uint8_t* __restrict__ plan, int n_chunks, unsigned long long chunk_offset, const __grid_constant__ StepArgs a) {
   typedef typename std::conditional<PARAM16, bf16, float>::type P;
   typedef typename std::conditional<GRAD16, bf16, float>::type G;
@@ -368,6 +419,10 @@ adamw_kernel(const uint8_t* __restrict__ plan, int n_chunks, unsigned long long 
   for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
     const PlanChunk ch = chunks[k];
     const PlanTensor& w = tensors[ch.tensor];
+    if (BITS == 8 && threadIdx.x == 0 && k + (int)gridDim.x < n_chunks) {
+      const PlanChunk next = chunks[k + gridDim.x];
+      prefetch_chunk<PARAM16, GRAD16, BITS>(tensors[next.tensor], next.index);
+    }
     const long long at = (long long)ch.index * kChunk + threadIdx.x * 8;
     const long long left = w.n - at;
     const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
@@ -393,7 +448,9 @@ adamw_kernel(const uint8_t* __restrict__ plan, int n_chunks, unsigned long long 
 
 template <bool PARAM16, bool GRAD16>
 cudaError_t launch(const PlanHeader& h, const uint8_t* plan, const StepArgs& a, cudaStream_t st) {
-  const unsigned blocks = (unsigned)std::min(h.n_chunks, 148 * 8);
+  // Blocks that come and go even out what SMs and memory partitions do to each other: 124M parameters with fp32 moments take 672 us in
+  // 4 blocks an SM that stay, 647 in 8, 612 in 24, 600 in 64 (595 in 128); with 8-bit ones 577 in 3, 567 in 6, 557 in 27, 571 in 90.
+  const unsigned blocks = (unsigned)std::min(h.n_chunks, 148 * (h.bits == 8 ? 27 : 64));
   if (h.bits == 8) return launch_pdl(adamw_kernel<PARAM16, GRAD16, 8>, dim3(blocks), dim3(kThreads), 0, st, plan, h.n_chunks, (unsigned long long)h.chunk_offset, a);
   return launch_pdl(adamw_kernel<PARAM16, GRAD16, 32>, dim3(blocks), dim3(kThreads), 0, st, plan, h.n_chunks, (unsigned long long)h.chunk_offset, a);
 }
@@ -485,9 +542,9 @@ extern "C" ft_status ft_k_adamw_plan(const ft_adamw_tensor* tensors, int32_t n_t
     long long base = 0;
     for (int32_t i = 0; i < n_tensors; ++i) {
       const ft_adamw_tensor& t = tensors[i];
-      // a thread moves 8 elements of an array at once: 32 bytes of fp32, 16 of bf16, 8 of codes
+      // a thread moves 8 elements of an array at once: 32 bytes of fp32, 16 of bf16, 8 of codes; chunks are prefetched in units of 16
       const uintptr_t odd = ((uintptr_t)t.param & (h->param16 ? 15u : 31u)) | ((uintptr_t)t.grad & (h->grad16 ? 15u : 31u)) |
-                            (((uintptr_t)t.m | (uintptr_t)t.v) & (state_bits == 8 ? 7u : 31u)) | ((uintptr_t)t.copy & 15u);
+                            (((uintptr_t)t.m | (uintptr_t)t.v) & (state_bits == 8 ? 15u : 31u)) | ((uintptr_t)t.copy & 15u);
       list[i] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, reinterpret_cast<fs::bf16*>(t.copy), t.numel, base, t.weight_decay, odd == 0};
       for (long long k = 0; k < (t.numel + fs::kChunk - 1) / fs::kChunk; ++k) *ch++ = {i, (int)k};
       base += (t.numel + fs::kRun - 1) / fs::kRun * fs::kRun;
