@@ -154,6 +154,34 @@ __device__ __forceinline__ void send_rows(const void* tmap, uint32_t out, int la
   }
 }
 
+// Sets rows [from, ROWS) of a swizzled tile of D columns in shared memory to zero; all threads of a warp.
+template <int D, int ROWS>
+__device__ __forceinline__ void zero_rows(uint32_t tile, int from, int lane) {
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+  for (int i = lane; i < (ROWS - from) * (D / 8); i += 32) {
+    const int c = i / ((ROWS - from) * 8), r = i % ((ROWS - from) * 8);  // 64-column box, 16-byte piece of its rows
+    st_shared_v4(tile + (uint32_t)(c * (ROWS * 128) + from * 128 + r * 16), zero);
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+// send_rows() of rows that may end inside the warp's 32.
+template <int D>
+__device__ __forceinline__ void send_rows_clipped(const void* tmap, bf16* dst, long long ld, uint32_t out, int lane, int x, int y, int total) {
+  if (y + 32 <= total) {
+    send_rows<D>(tmap, out, lane, x, y, 0, total);
+  } else {
+    __syncwarp();
+    if (y + lane < total) {
+      bf16* row = dst + (long long)(y + lane) * ld + x;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c)
+        *reinterpret_cast<uint4*>(row + c * 8) = ld_shared_v4(out + (uint32_t)((c >> 3) * 4096 + lane * 128 + (((c & 7) ^ (lane & 7)) * 16)));
+    }
+  }
+}
+
 // Untiled bulk copies (both addresses and the size multiples of 16 bytes).
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"

@@ -65,33 +65,6 @@ __device__ __forceinline__ int docs_start(const Docs& docs, int row) {  // of a 
   const int a = __ldg(docs.start + row);
   return a < 0 ? 0 : a < row ? a : row;
 }
-// Sets rows [from, ROWS) of a swizzled tile of D columns in shared memory to zero; all threads of a warp.
-template <int D, int ROWS>
-__device__ __forceinline__ void zero_rows(uint32_t tile, int from, int lane) {
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll 1
-  for (int i = lane; i < (ROWS - from) * (D / 8); i += 32) {
-    const int c = i / ((ROWS - from) * 8), r = i % ((ROWS - from) * 8);  // 64-column box, 16-byte piece of its rows
-    st_shared_v4(tile + (uint32_t)(c * (ROWS * 128) + from * 128 + r * 16), zero);
-  }
-  fence_proxy_async_smem();
-  __syncwarp();
-}
-// send_rows() of rows that may end inside the warp's 32.
-template <int D>
-__device__ __forceinline__ void send_rows_clipped(const void* tmap, bf16* dst, long long ld, uint32_t out, int lane, int x, int y, int total) {
-  if (y + 32 <= total) {
-    send_rows<D>(tmap, out, lane, x, y, 0, total);
-  } else {
-    __syncwarp();
-    if (y + lane < total) {
-      bf16* row = dst + (long long)(y + lane) * ld + x;
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c)
-        *reinterpret_cast<uint4*>(row + c * 8) = ld_shared_v4(out + (uint32_t)((c >> 3) * 4096 + lane * 128 + (((c & 7) ^ (lane & 7)) * 16)));
-    }
-  }
-}
 
 // ============================================================================ forward
 // One CTA per (128 queries, head, batch row), two an SM; K and V blocks of 64 keys are streamed, S_{j+1} = Q K_{j+1}^T is
@@ -1733,7 +1706,7 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
 // ---------------------------------------------------------------- packed documents: one sequence of T rows
 // The plan is that of a window as long as the longest document, which no key block can meet more query blocks than; what the
 // documents really need is read on the device.
-cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int nh, int nkv, int d, int* err, cudaStream_t st) {
+cudaError_t attention_packed_fwd_tile(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int nh, int nkv, int d, int* err, cudaStream_t st) {
   if (!shape_ok(1, T, nh, nkv, d, 1, 0) || !err) return cudaErrorInvalidValue;
   if (d == 64) return fwd_t<64, true>(qkv, o, lse, 1, T, nh, nkv, T, 0, docs, err, st);
   return fwd_t<128, true>(qkv, o, lse, 1, T, nh, nkv, T, 0, docs, err, st);

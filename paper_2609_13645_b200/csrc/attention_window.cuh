@@ -27,6 +27,9 @@ cudaError_t attention_window_bwd(const bf16* qkv, const bf16* o, const bf16* d_o
 struct Docs {
   const int *start, *end, *pos;
 };
+// attention_packed_fwd_tile: its kernel of one tile a CTA, for small calls (attention_packed_fwd chooses).
+cudaError_t attention_packed_fwd_tile(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int n_heads, int n_kv, int d, int* err,
+                                      cudaStream_t st);
 cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int n_heads, int n_kv, int d, int* err,
                                  cudaStream_t st);
 // longest: rows of the longest document, at most; cos, sin: fp32 [longest, d / 2] or null.

@@ -234,3 +234,38 @@ def test_offsets_that_are_refused_on_the_device(cu):
     Bn.k_status()
     b = bounds.cpu()
     assert (b[:2] >= 0).all() and (b[:2] <= T).all() and (b[2] >= 0).all() and (b[2] < T).all()
+
+
+@pytest.mark.parametrize("nh,nkv,d,T", [(30, 15, 64, 6500), (24, 24, 64, 7900), (33, 11, 64, 5900), (30, 15, 128, 6500), (24, 24, 128, 7900), (25, 5, 128, 7700)])
+def test_two_tiles_a_block(nh, nkv, d, T):
+    """Calls of ten and more tiles an SM, whose blocks work on two tiles: heads that share K and V or have their own, odd numbers of
+    them, an odd number of query blocks, documents from one row to most of the batch, rows behind them; bit-identical twice."""
+    g = np.random.RandomState(T + nh)
+    lens = [1, 0, 127, 129, 1, 2500] + [int(m) for m in g.randint(0, 400, 11)]
+    tail = T - sum(lens)
+    assert tail > 0 and (T + 127) // 128 * nh >= 1480
+    n = sum(lens)
+    qkv, _ = inputs(lens, tail, nh, nkv, d, 31)
+    o, lse, _ = run_fwd(qkv, lens, T, nh, nkv, d)
+    for a in range(0, nh, nh // nkv):  # the reference by kv heads: its scores are many
+        r = nh // nkv
+        cols = [h * d + c for h in list(range(a, a + r)) + [nh + a // r, nh + nkv + a // r] for c in range(d)]
+        want, want_lse = reference_fwd(qkv[:, cols], lens, r, 1, d)
+        assert rel(o[:n, a * d:(a + r) * d], want) < 3e-3 and float((lse[a:a + r, :n].double() - want_lse).abs().max()) < 2e-5
+    assert (o[n:] == 7).all() and (lse[:, n:] == 7).all()
+    o2, lse2, _ = run_fwd(qkv, lens, T, nh, nkv, d)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_large_scores_in_two_tiles_a_block():
+    """References that move by hundreds, up and down, between a row's blocks."""
+    nh, nkv, d, lens, T = 30, 15, 64, [3000, 700, 2600], 6500
+    n = sum(lens)
+    qkv, _ = inputs(lens, T - n, nh, nkv, d, 12)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    qkv[:n, nh * d:(nh + nkv) * d] *= torch.exp2(torch.randint(-6, 7, (n, 1), generator=g, device="cuda").float()).bfloat16()  # keys of any size
+    o, lse, _ = run_fwd(qkv, lens, T, nh, nkv, d)
+    cols = [h * d + c for h in (0, 1, nh, nh + nkv) for c in range(d)]
+    want, want_lse = reference_fwd(qkv[:, cols], lens, 2, 1, d)
+    # scores of up to 64 * 30: an fp32 score is off by up to 2^-24 * 64 of 2000 = 0.008, which moves near ties' weights by 1 %
+    assert rel(o[:n, :2 * d], want) < 1e-2 and float((lse[:2, :n].double() - want_lse).abs().max()) < 0.01
