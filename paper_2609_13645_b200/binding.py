@@ -723,9 +723,11 @@ def k_status():
 
 def _check_tables(cos, sin, index):
     torch = _torch or _import_torch()
-    if cos.dim() != 2 or cos.shape != sin.shape or min(cos.shape) < 1 or max(cos.shape) > _INT32_MAX // 2:
-        _refuse(f"cos {tuple(cos.shape)}, sin {tuple(sin.shape)}: [positions, pairs] are needed")
-    return (_check_flat("cos", cos, torch.float32, cos.numel(), index), _check_flat("sin", sin, torch.float32, sin.numel(), index))
+    shape = cos.shape
+    if len(shape) != 2 or sin.shape != shape or not 0 < shape[0] <= _INT32_MAX or not 0 < shape[1] <= 1 << 20:
+        _refuse(f"cos {tuple(shape)}, sin {tuple(sin.shape)}: [positions, pairs] are needed")
+    n = shape[0] * shape[1]
+    return _check_flat("cos", cos, torch.float32, n, index), _check_flat("sin", sin, torch.float32, n, index)
 
 
 def k_rotary(x, y, cos, sin, n_heads, d, positions=None, interleaved=False, inverse=False):

@@ -3,7 +3,9 @@
 // elements of a head; the others are passed on.  With -s it is the transpose, which is the backward pass.
 //
 // Bound by memory: each element is read and written once.  A thread keeps its pairs' table entries in registers and walks over
-// heads of its row, up to 4 in flight, so that the tables cost one read a row and not one a head.
+// heads of its row, two in flight, so that the tables cost one read for four heads; blocks stay, four an SM, and look at the next
+// row's position early.  (Four heads in flight take 117 registers: 21.4 us for 4096 rows of 40 heads of 128 bf16 in place, of which
+// two take 18.0; a block for every three rows 19.5 with two, 18.0 with four heads in flight behind the tables.)
 #include <math.h>
 
 #include "../../include/forgestep.h"
@@ -43,100 +45,97 @@ struct RotaryShape {
   int rows, heads, d, rot, n_pos;
   int units;   // of a head: pieces of pairs, then (unless in place) pieces that are passed on
   int turned;  // the former
-  int lanes;   // threads that share the heads of a unit
+  int lanes;   // threads that share the heads of a unit; units * lanes is at most 256, or lanes is 1
 };
 
 // P pairs a unit: two pieces of P elements, or one of 2 P (interleaved, P > 1); what is passed on goes in pieces of W.
 template <typename T, int P, bool PAIRS>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 4)
 rotary_kernel(const T* x, T* y, const int* __restrict__ positions, const float* __restrict__ cos, const float* __restrict__ sin,
               float sign, const __grid_constant__ RotaryShape s, int* err) {
   constexpr bool WHOLE = PAIRS && P > 1;
-  constexpr int W = WHOLE ? 2 * P : P, U = 4;
+  constexpr int W = WHOLE ? 2 * P : P, U = 2, N = WHOLE ? 1 : 2;  // N: pieces a unit
   pdl_trigger();
-  pdl_wait();
   const int per_row = s.units * s.lanes, half = s.rot / 2;
-  // a block takes whole rows where they are small, else a row is walked over
-  const int rows_a_block = per_row < 256 ? 256 / per_row : 1;
-  const int mine = per_row < 256 ? (int)threadIdx.x / per_row : 0;
+  const int rows_a_block = per_row <= 256 ? 256 / per_row : 1;  // whole rows; a longer one is walked over
+  const int mine = per_row <= 256 ? (int)threadIdx.x / per_row : 0;
   if (mine >= rows_a_block) return;
-  for (long long row = (long long)blockIdx.x * rows_a_block + mine; row < s.rows; row += (long long)gridDim.x * rows_a_block) {
-    const int pos = positions != nullptr ? __ldg(positions + row) : (int)row;
-    if (pos < 0 || pos >= s.n_pos) {
-      atomicCAS(err, (int)ERR_NONE, (int)ERR_BAD_INDEX);
-      continue;
-    }
-    for (int i = (int)threadIdx.x - mine * per_row; i < per_row; i += 256) {
-      const int u = i % s.units, lane = i / s.units;
-      const T* in = x + row * s.ldx;
-      T* out = y + row * s.ldy;
-      if (u >= s.turned) {
-        const int at = s.rot + (u - s.turned) * W;
-        for (int h = lane; h < s.heads; h += s.lanes) {
-          Piece<T, W> v;
-          v.load(in + (long long)h * s.d + at);
-          v.store(out + (long long)h * s.d + at);
-        }
-        continue;
-      }
+  const int lane = per_row <= 256 ? ((int)threadIdx.x - mine * per_row) / s.units : 0;
+  const int u0 = (int)threadIdx.x - mine * per_row - lane * s.units;
+  pdl_wait();
+  const long long stride = (long long)gridDim.x * rows_a_block;
+  auto position = [&](long long row) { return row >= s.rows ? 0 : positions != nullptr ? __ldg(positions + row) : (int)row; };
+  int next = position((long long)blockIdx.x * rows_a_block + mine);
+  for (long long row = (long long)blockIdx.x * rows_a_block + mine; row < s.rows; row += stride) {
+    const int pos = next;
+    next = position(row + stride);
+    const T* in = x + row * s.ldx;
+    T* out = y + row * s.ldy;
+    for (int u = u0; u < s.units; u += 256) {
+      const bool turn = u < s.turned;
+      const int first = !turn ? s.rot + (u - s.turned) * W : PAIRS ? u * 2 * P : u * P, partner = PAIRS ? 1 : half;
       float c[P], n[P];
-      const float *cr = cos + (long long)pos * half + u * P, *sr = sin + (long long)pos * half + u * P;
-#pragma unroll
-      for (int e = 0; e < P; e += (P < 4 ? P : 4)) {
-        Piece<float, (P < 4 ? P : 4)> a, b;
-        a.load(cr + e);
-        b.load(sr + e);
-        float fa[P < 4 ? P : 4], fb[P < 4 ? P : 4];
-        a.unpack(fa);
-        b.unpack(fb);
-#pragma unroll
-        for (int k = 0; k < (P < 4 ? P : 4); ++k) { c[e + k] = fa[k]; n[e + k] = sign * fb[k]; }
-      }
-      const int first = PAIRS ? u * 2 * P : u * P, partner = PAIRS ? 1 : half;
       for (int h0 = lane; h0 < s.heads; h0 += U * s.lanes) {
-        if constexpr (WHOLE) {
-          Piece<T, 2 * P> v[U];
+        // the elements are on their way before the position is looked at, on which the tables' rows hang
+        Piece<T, W> v[U][N];
 #pragma unroll
-          for (int k = 0; k < U; ++k)
-            if (h0 + k * s.lanes < s.heads) v[k].load(in + (long long)(h0 + k * s.lanes) * s.d + first);
+        for (int k = 0; k < U; ++k) {
+          if (h0 + k * s.lanes >= s.heads) break;
+          const T* from = in + (long long)(h0 + k * s.lanes) * s.d + first;
+          v[k][0].load(from);
+          if (N == 2 && turn) v[k][N - 1].load(from + partner);
+        }
+        if (pos < 0 || pos >= s.n_pos) {
+          atomicCAS(err, (int)ERR_NONE, (int)ERR_BAD_INDEX);
+          break;
+        }
+        if (turn && h0 == lane) {
+          constexpr int F = P < 4 ? P : 4;
+          const float *cr = cos + (long long)pos * half + u * P, *sr = sin + (long long)pos * half + u * P;
+          Piece<float, F> a[P / F], b[P / F];
 #pragma unroll
-          for (int k = 0; k < U; ++k) {
-            if (h0 + k * s.lanes >= s.heads) break;
-            float f[2 * P], r[2 * P];
-            v[k].unpack(f);
+          for (int e = 0; e < P / F; ++e) {
+            a[e].load(cr + e * F);
+            b[e].load(sr + e * F);
+          }
+#pragma unroll
+          for (int e = 0; e < P / F; ++e) {
+            float fa[F], fb[F];
+            a[e].unpack(fa);
+            b[e].unpack(fb);
+#pragma unroll
+            for (int k = 0; k < F; ++k) { c[e * F + k] = fa[k]; n[e * F + k] = sign * fb[k]; }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          if (h0 + k * s.lanes >= s.heads) break;
+          T* to = out + (long long)(h0 + k * s.lanes) * s.d + first;
+          if (!turn) {
+            v[k][0].store(to);
+          } else if constexpr (WHOLE) {
+            float f[W], r[W];
+            v[k][0].unpack(f);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
               r[2 * e] = f[2 * e] * c[e] - f[2 * e + 1] * n[e];
               r[2 * e + 1] = f[2 * e + 1] * c[e] + f[2 * e] * n[e];
             }
-            v[k].pack(r);
-            v[k].store(out + (long long)(h0 + k * s.lanes) * s.d + first);
-          }
-        } else {
-          Piece<T, P> va[U], vb[U];
-#pragma unroll
-          for (int k = 0; k < U; ++k)
-            if (h0 + k * s.lanes < s.heads) {
-              const T* p = in + (long long)(h0 + k * s.lanes) * s.d + first;
-              va[k].load(p);
-              vb[k].load(p + partner);
-            }
-#pragma unroll
-          for (int k = 0; k < U; ++k) {
-            if (h0 + k * s.lanes >= s.heads) break;
+            v[k][0].pack(r);
+            v[k][0].store(to);
+          } else {
             float a[P], b[P], ra[P], rb[P];
-            va[k].unpack(a);
-            vb[k].unpack(b);
+            v[k][0].unpack(a);
+            v[k][N - 1].unpack(b);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
               ra[e] = a[e] * c[e] - b[e] * n[e];
               rb[e] = b[e] * c[e] + a[e] * n[e];
             }
-            va[k].pack(ra);
-            vb[k].pack(rb);
-            T* p = out + (long long)(h0 + k * s.lanes) * s.d + first;
-            va[k].store(p);
-            vb[k].store(p + partner);
+            v[k][0].pack(ra);
+            v[k][N - 1].pack(rb);
+            v[k][0].store(to);
+            v[k][N - 1].store(to + partner);
           }
         }
       }
@@ -144,27 +143,36 @@ rotary_kernel(const T* x, T* y, const int* __restrict__ positions, const float* 
   }
 }
 
-// Tables of position p and frequency i: angle = p theta^(-2 i / rot) / factor_i, cos and sin times mscale.  The angle is formed in
-// turns in 64 bits and reduced to half a turn there; what is left goes through the fp32 functions of pi x, so that far
-// positions lose nothing.
+// Tables of position p and frequency i: angle = p theta^(-2 i / rot) / factor_i, cos and sin times mscale.  A position's step is kept as
+// a 64-bit fraction of a turn, of which p times is taken modulo one turn by integer products: far positions lose nothing (2^-64 turns a
+// position), and what is left goes through the fp32 functions of pi x.  A thread keeps its frequency and walks over positions.
 __global__ void __launch_bounds__(256)
 rotary_tables_kernel(float* __restrict__ cos, float* __restrict__ sin, const float* __restrict__ factors, int n_pos, int half,
                      double log2_step, float mscale) {
   pdl_trigger();
   pdl_wait();
-  extern __shared__ double turns[];  // a position's step in each frequency
-  for (int i = threadIdx.x; i < half; i += 256)
-    turns[i] = exp2(i * log2_step) * 0.15915494309189533577 / (factors != nullptr ? (double)__ldg(factors + i) : 1.0);
+  extern __shared__ unsigned long long steps[];  // formed once a block: 64-bit floating point is what this kernel has least of
+  for (int i = threadIdx.x; i < half; i += 256) {
+    const double turns = exp2(i * log2_step) * 0.15915494309189533577 / (factors != nullptr ? (double)__ldg(factors + i) : 1.0);
+    const double part = turns - floor(turns);
+    steps[i] = part < 1.0 ? (unsigned long long)(part * 18446744073709551616.0) : 0ull;
+  }
   __syncthreads();
-  const long long n = (long long)n_pos * half, stride = (long long)gridDim.x * 256;
-  for (long long k = (long long)blockIdx.x * 256 + threadIdx.x; k < n; k += stride) {
-    const int p = n <= 0xffffffffll ? (int)((unsigned)k / (unsigned)half) : (int)(k / half);
-    const double t = p * turns[k - (long long)p * half];
-    const float x = 2.0f * (float)(t - rint(t));
-    float s, c;
-    sincospif(x, &s, &c);
-    cos[k] = c * mscale;
-    sin[k] = s * mscale;
+  const int rows = half < 256 ? 256 / half : 1;  // positions a block takes at a time
+  const int mine = half < 256 ? (int)threadIdx.x / half : 0;
+  if (mine >= rows) return;
+  for (int i = (int)threadIdx.x - mine * half; i < half; i += 256) {
+    const unsigned long long step = steps[i];
+    const int by = (int)gridDim.x * rows;
+#pragma unroll 4
+    for (int p = (int)blockIdx.x * rows + mine; p < n_pos; p += by) {
+      const int frac = (int)((step * (unsigned long long)p + 0x80000000ull) >> 32);  // of a turn, in [-1/2, 1/2)
+      float s, c;
+      sincospif((float)frac * 4.656612873077393e-10f, &s, &c);
+      cos[(long long)p * half + i] = c * mscale;
+      sin[(long long)p * half + i] = s * mscale;
+      if (p > n_pos - by) break;  // p + by may not fit
+    }
   }
 }
 
@@ -178,9 +186,10 @@ cudaError_t launch(const void* x, void* y, const int* positions, const float* co
   const long long work = (long long)s.rows * s.units * s.heads;
   const int each = work >= 148ll * 2048 * 4 ? 4 : work >= 148ll * 2048 ? 2 : 1;
   s.lanes = (s.heads + each - 1) / each;
-  const int per_row = s.units * s.lanes, rows_a_block = per_row < 256 ? 256 / per_row : 1;
+  if (s.units * s.lanes > 256) s.lanes = s.units < 256 ? 256 / s.units : 1;
+  const int per_row = s.units * s.lanes, rows_a_block = per_row <= 256 ? 256 / per_row : 1;
   const long long want = ((long long)s.rows + rows_a_block - 1) / rows_a_block;
-  return launch_pdl(rotary_kernel<T, P, PAIRS>, dim3((unsigned)(want < 148 * 64 ? want : 148 * 64)), dim3(256), 0, st,
+  return launch_pdl(rotary_kernel<T, P, PAIRS>, dim3((unsigned)(want < 148 * 4 ? want : 148 * 4)), dim3(256), 0, st,
                     reinterpret_cast<const T*>(x), reinterpret_cast<T*>(y), positions, cos, sin, sign, s, err);
 }
 
@@ -246,9 +255,10 @@ extern "C" ft_status ft_k_rotary_tables(float* dev_cos, float* dev_sin, const fl
   const size_t n = (size_t)n_positions * (rot / 2), bytes = n * sizeof(float);
   const uintptr_t c = (uintptr_t)dev_cos, s = (uintptr_t)dev_sin, f = (uintptr_t)dev_factors, fb = (size_t)rot / 2 * sizeof(float);
   if ((c < s + bytes && s < c + bytes) || (f && ((f < c + bytes && c < f + fb) || (f < s + bytes && s < f + fb)))) return FT_EINVAL;
-  const size_t blocks = (n + 1023) / 1024;
+  const int at_a_time = rot / 2 < 256 ? 256 / (rot / 2) : 1;
+  const size_t blocks = ((size_t)n_positions + 4 * at_a_time - 1) / (4 * at_a_time);  // 4 positions a thread and more
   const cudaError_t e = fs::launch_pdl(fs::rotary_tables_kernel, dim3((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8)), dim3(256),
-                                       (size_t)rot / 2 * sizeof(double), reinterpret_cast<cudaStream_t>(stream), dev_cos, dev_sin, dev_factors,
+                                       (size_t)rot / 2 * sizeof(unsigned long long), reinterpret_cast<cudaStream_t>(stream), dev_cos, dev_sin, dev_factors,
                                        n_positions, rot / 2, -2.0 / rot * log2((double)theta), mscale);
   return e == cudaSuccess ? FT_OK : FT_ECUDA;
 }
