@@ -483,7 +483,8 @@ ft_status ft_k_attention_packed_bwd(const void* dev_qkv, const void* dev_o, cons
  * [position, i] of the tables (fp32 [n_positions, rot / 2]); inverse = 1 takes -s, which is the transpose and with it the backward
  * pass.  The other elements are passed on.  dev_positions: int32 [rows] (NULL: the row's number, rows <= n_positions); a row whose
  * position is outside [0, n_positions) is not written and ft_k_status returns FT_EINVAL.  dtype 0 bf16, 1 fp32; rot even; strides
- * and alignment as in LayerNorm; dev_y may be dev_x when their strides are equal (heads of q and k inside packed qkv rows, for one). */
+ * and alignment as in LayerNorm; dev_y may be dev_x when their strides are equal (heads of q and k inside packed qkv rows, for one), or
+ * other columns of the same rows; otherwise it shares nothing with what is read. */
 ft_status ft_k_rotary(const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy, const int32_t* dev_positions, const float* dev_cos,
                       const float* dev_sin, int32_t n_positions, int32_t rows, int32_t n_heads, int32_t head_dim, int32_t rot,
                       int32_t interleaved, int32_t inverse, int32_t dtype, void* stream);

@@ -216,6 +216,15 @@ int pairs_a_unit(const void* x, const void* y, const void* cos, const void* sin,
   return 1;
 }
 
+bool overlap(uintptr_t a, size_t na, uintptr_t b, size_t nb) { return a < b + nb && b < a + na; }
+// Whether rows of `width` bytes at x and at y share any: with equal strides they may lie beside each other in the same rows.
+bool rows_share(uintptr_t x, size_t ldx, uintptr_t y, size_t ldy, size_t rows, size_t width) {
+  if (!overlap(x, (rows - 1) * ldx + width, y, (rows - 1) * ldy + width)) return false;
+  if (ldx != ldy) return true;
+  const size_t apart = (x < y ? y - x : x - y) % ldx;
+  return apart < width || apart > ldx - width;
+}
+
 }  // namespace
 }  // namespace fs
 
@@ -229,6 +238,12 @@ extern "C" ft_status ft_k_rotary(const void* dev_x, int64_t ldx, void* dev_y, in
   if (rows > 1 && dev_y == dev_x && ldy != ldx) return FT_EINVAL;
   const int elem = dtype == 0 ? 2 : 4;
   if (((uintptr_t)dev_x | (uintptr_t)dev_y) % elem || ((uintptr_t)dev_cos | (uintptr_t)dev_sin | (uintptr_t)dev_positions) & 3u) return FT_EINVAL;
+  const size_t w = (size_t)width * elem, lx = (rows > 1 ? (size_t)ldx : (size_t)width) * elem, ly = (rows > 1 ? (size_t)ldy : (size_t)width) * elem;
+  const uintptr_t x = (uintptr_t)dev_x, y = (uintptr_t)dev_y;
+  const size_t span = (size_t)(rows - 1) * ly + w, table = (size_t)n_positions * (rot / 2) * sizeof(float);
+  if ((x != y && fs::rows_share(x, lx, y, ly, (size_t)rows, w)) || fs::overlap((uintptr_t)dev_cos, table, y, span) ||
+      fs::overlap((uintptr_t)dev_sin, table, y, span) || (dev_positions && fs::overlap((uintptr_t)dev_positions, (size_t)rows * 4, y, span)))
+    return FT_EINVAL;
   int* status = fs::attention_status_word();
   if (!status) return FT_ECUDA;
   fs::RotaryShape s{};

@@ -84,8 +84,7 @@ def clone(t):
     return {k: [x.clone() for x in v] if v is not None else None for k, v in t.items()}
 
 
-def check(old, new, bits, decay, step, clip, seed, lr=LR):
-    base = 0
+def check(old, new, bits, decay, step, clip, seed, lr=LR, base=0):
     for k, n in enumerate(old["p"]):
         n = n.numel()
         p, g = old["p"][k].double(), old["g"][k].double() * clip
@@ -239,3 +238,43 @@ def test_replays_read_step_rate_and_scale():
             old = clone(t)
             graph.replay()
             check(old, t, bits, [0.1, 0.1], s, c, 8, lr=float(lr[0]))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_elements_past_32_bits(bits):
+    """The last elements of a tensor of more than 2^31, and a tensor behind it."""
+    from paper_2609_13645_b200 import binding as Bn
+    far, last = 1 << 31, 1000
+    t = make([last, 300], torch.bfloat16, torch.bfloat16, bits, False, 21)
+    big = {}
+    for name, v in t.items():
+        if v is not None and len(v):
+            skipped = far // 256 if name in ("ms", "vs") else far
+            big[name] = torch.zeros(skipped + v[0].numel(), dtype=v[0].dtype, device="cuda")
+            big[name][skipped:] = v[0]
+    whole = {name: [big[name], v[1]] if v else v for name, v in t.items()}
+    Bn.k_adamw(plan_of(whole, 0.1, bits), LR, B1, B2, EPS, torch.tensor([4], device="cuda"), seed=3)
+    new = {name: [v[0][-t[name][0].numel():], v[1]] if v else v for name, v in whole.items()}
+    first = {name: v[:1] if v else v for name, v in new.items()}
+    check({name: v[:1] if v else v for name, v in t.items()}, first, bits, [0.1], 4, 1.0, 3, base=far)
+    assert not big["p"][:far].any() and not big["m"][:far].view(torch.uint8).any()
+
+
+def test_two_plans_on_two_streams():
+    """Steps that run at the same time, and in other orders, give the bits of steps one after the other."""
+    from paper_2609_13645_b200 import binding as Bn
+    step, streams = torch.tensor([2], device="cuda"), [torch.cuda.Stream() for _ in range(2)]
+    for bits in (32, 8):
+        a = [make(SIZES + [1 << 20], torch.float32, torch.float32, bits, True, s) for s in (1, 2)]
+        b = [clone(t) for t in a]
+        plans = [plan_of(t, 0.1, bits) for t in b]
+        for t in a:
+            Bn.k_adamw(plan_of(t, 0.1, bits), LR, B1, B2, EPS, step, seed=5)
+        torch.cuda.synchronize()
+        for plan, stream in zip(plans, streams):
+            with torch.cuda.stream(stream):
+                Bn.k_adamw(plan, LR, B1, B2, EPS, step, seed=5)
+        torch.cuda.synchronize()
+        for x, y in zip(a, b):
+            for name in ("p", "m", "v", "ms", "vs", "copy"):
+                assert all(torch.equal(u.view(torch.uint8), w.view(torch.uint8)) for u, w in zip(x[name], y[name]))

@@ -269,3 +269,55 @@ def test_large_scores_in_two_tiles_a_block():
     want, want_lse = reference_fwd(qkv[:, cols], lens, 2, 1, d)
     # scores of up to 64 * 30: an fp32 score is off by up to 2^-24 * 64 of 2000 = 0.008, which moves near ties' weights by 1 %
     assert rel(o[:n, :2 * d], want) < 1e-2 and float((lse[:2, :n].double() - want_lse).abs().max()) < 0.01
+
+
+def test_elements_past_32_bits():
+    """A batch whose qkv has more than 2^31 elements: the last documents, which rows behind them follow."""
+    from paper_2609_13645_b200 import binding as Bn
+    nh, nkv, d, tail = 16, 8, 128, 77
+    last = [300, 1, 700]
+    lens = [1000] * 540 + last
+    T, n = sum(lens) + tail, sum(lens)
+    m = sum(last)
+    assert (n - m) * (nh + 2 * nkv) * d > 2 ** 31
+    qkv = torch.zeros(T, (nh + 2 * nkv) * d, dtype=torch.bfloat16, device="cuda")
+    do = torch.zeros(T, nh * d, dtype=torch.bfloat16, device="cuda")
+    qkv[n - m:], do[n - m:] = inputs(last, tail, nh, nkv, d, 5)
+    o, lse, bounds = run_fwd(qkv, lens, T, nh, nkv, d)
+    want, want_lse = reference_fwd(qkv[n - m:n], last, nh, nkv, d)
+    assert rel(o[n - m:n], want) < 3e-3 and float((lse[:, n - m:n].double() - want_lse).abs().max()) < 2e-5
+    assert not o[:n - m].any() and (o[n:] == 7).all() and (lse[:, n:] == 7).all()
+    cos, sin = tables(1000, d)
+    dqkv = run_bwd(qkv, o, do, lse, bounds, T, nh, nkv, d, 1000, cos, sin)
+    want = reference_bwd(qkv[n - m:n], o[n - m:n], do[n - m:n], last, nh, nkv, d, cos, sin)
+    got = dqkv[n - m:n].view(m, -1, d)
+    for a, b in ((0, nh), (nh, nh + nkv), (nh + nkv, nh + 2 * nkv)):
+        assert rel(got[:, a:b], want.view(m, -1, d)[:, a:b]) < 3e-3
+    assert not dqkv[:n - m].any() and (dqkv[n:] == 9).all()
+
+
+def test_two_calls_on_two_streams():
+    """Batches that are worked on at the same time, each with its own scratch, give the bits of batches one after the other."""
+    from paper_2609_13645_b200 import binding as Bn
+    shapes = [([700, 3, 900], 5, 4, 2, 128), ([128] * 9, 0, 6, 1, 64)]
+    runs, streams = [], [torch.cuda.Stream() for _ in shapes]
+    for k, (lens, tail, nh, nkv, d) in enumerate(shapes):
+        T = sum(lens) + tail
+        qkv, do = inputs(lens, tail, nh, nkv, d, k)
+        o, lse, bounds = run_fwd(qkv, lens, T, nh, nkv, d)
+        runs.append((qkv, do, o, lse, bounds, run_bwd(qkv, o, do, lse, bounds, T, nh, nkv, d, max(lens)), T, nh, nkv, d, max(lens)))
+    torch.cuda.synchronize()
+    again = []
+    for qkv, do, o, lse, bounds, dqkv, *shape in runs:
+        scratch = torch.empty(Bn.attention_packed_scratch_bytes(*shape), dtype=torch.uint8, device="cuda")
+        again.append((torch.full_like(o, 7.0), torch.full_like(lse, 7.0), torch.full_like(dqkv, 9.0), scratch))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (qkv, do, o, lse, bounds, dqkv, *shape), (o2, lse2, dqkv2, scratch), stream in zip(runs, again, streams):
+            with torch.cuda.stream(stream):
+                Bn.k_attention_packed_fwd(qkv, o2, lse2, bounds, *shape[:4])
+                Bn.k_attention_packed_bwd(qkv, o2, do, lse2, dqkv2, bounds, scratch, *shape)
+    torch.cuda.synchronize()
+    Bn.k_status()
+    for (qkv, do, o, lse, bounds, dqkv, *shape), (o2, lse2, dqkv2, scratch) in zip(runs, again):
+        assert torch.equal(o, o2) and torch.equal(lse, lse2) and torch.equal(dqkv, dqkv2)

@@ -61,6 +61,14 @@ def test_rotary():
     same = [v for v in ok]
     same[2], same[3] = G, 520  # in place with another stride
     assert L.ft_k_rotary(*same, None) == Bn.FT_EINVAL
+    # y over part of x, its tables or its positions (in bf16: rows of 1024 bytes)
+    for i, v in ((2, G + 2), (2, G + 1024 * 9 + 1022), (0, 2 * G + 1022), (2, 4 * G - 2), (2, 5 * G + 64 * 256 - 2), (2, 3 * G + 38)):
+        assert L.ft_k_rotary(*[v if j == i else x for j, x in enumerate(ok)], None) == Bn.FT_EINVAL, (i, v)
+    wide = [v for v in ok]
+    wide[1] = wide[3] = 1500  # rows of 3000 bytes of which x has the first 1024
+    for v in (G + 1022, G + 3000 * 2 + 2, G + 3000 - 1022):
+        assert L.ft_k_rotary(*[v if j == 2 else x for j, x in enumerate(wide)], None) == Bn.FT_EINVAL, v
+    assert L.ft_k_rotary(*[{2: G + 1024, 3: 1540}.get(j, x) for j, x in enumerate(wide)], None) == Bn.FT_EINVAL  # another stride
     fp32 = [v for v in ok]
     fp32[14], fp32[0] = 1, G + 2
     assert L.ft_k_rotary(*fp32, None) == Bn.FT_EINVAL

@@ -123,3 +123,37 @@ def test_replays_read_the_positions():
     graph.replay()
     ref, mag = reference(x, cos, sin, pos, heads, d, False, False)
     check(y, ref, mag, torch.bfloat16)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_columns_beside_each_other(interleaved):
+    """From some columns of a row into others; columns that share any are refused."""
+    from paper_2609_13645_b200 import binding as Bn
+    rows, heads, d = 70, 3, 32
+    w = heads * d
+    both = torch.randn(rows, 2 * w + 8, device="cuda").bfloat16()
+    old = both.clone()
+    cos, sin = torch.randn(rows, d // 2, device="cuda"), torch.randn(rows, d // 2, device="cuda")
+    Bn.k_rotary(both[:, :w], both[:, w + 8:], cos, sin, heads, d, interleaved=interleaved)
+    ref, mag = reference(old[:, :w], cos, sin, torch.arange(rows, device="cuda"), heads, d, interleaved, False)
+    check(both[:, w + 8:], ref, mag, torch.bfloat16)
+    assert torch.equal(both[:, :w + 8], old[:, :w + 8])
+    for y in (both[:, w - 8:2 * w - 8], both[:, 8:w + 8]):
+        with pytest.raises(Bn.ForgeStepError) as e:
+            Bn.k_rotary(both[:, :w], y, cos, sin, heads, d, interleaved=interleaved)
+        assert e.value.status == Bn.FT_EINVAL
+
+
+def test_rows_past_32_bits():
+    from paper_2609_13645_b200 import binding as Bn
+    heads, d, ld = 2, 64, (1 << 30) + 64
+    buf = torch.empty(2 * ld + heads * d, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (3, heads * d), (ld, 1))
+    x.copy_(torch.randn(3, heads * d, device="cuda"))
+    cos, sin = torch.randn(3, 32, device="cuda"), torch.randn(3, 32, device="cuda")
+    ref, mag = reference(x, cos, sin, torch.arange(3, device="cuda"), heads, d, False, False)
+    y = torch.empty(3, heads * d, dtype=torch.bfloat16, device="cuda")
+    Bn.k_rotary(x, y, cos, sin, heads, d)
+    Bn.k_rotary(x, x, cos, sin, heads, d)
+    check(y, ref, mag, torch.bfloat16)
+    assert torch.equal(x, y)
