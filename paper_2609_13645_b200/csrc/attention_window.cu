@@ -46,6 +46,13 @@ struct KeyRuns {
     n_sink = 0;
     count = ((min(rows_end, q0 + 128) + 63) >> 6) - first;
   }
+  __device__ static __forceinline__ KeyRuns of_count(int q0, int rows_end, int count) {  // the same of a known number of blocks
+    KeyRuns r;
+    r.first = ((min(rows_end, q0 + 128) + 63) >> 6) - count;
+    r.n_sink = 0;
+    r.count = count;
+    return r;
+  }
   __device__ __forceinline__ KeyRuns(int q0, int S, int window, int sinks) {
     const int end = (min(S, q0 + 128) + 63) >> 6;
     first = max(0, q0 - window + 1) >> 6;
@@ -65,6 +72,65 @@ __device__ __forceinline__ int docs_start(const Docs& docs, int row) {  // of a 
   const int a = __ldg(docs.start + row);
   return a < 0 ? 0 : a < row ? a : row;
 }
+
+// CTAs of packed documents differ in length by what their tile meets of its documents, and a long one that starts late leaves the
+// rest of the GPU waiting: launches of more CTAs than run at a time start the longest first.  A warp finds the tile at a place of that
+// order: it reads a bound of every tile (before it needs anything else from memory), turns them into lengths, halves the range
+// of the lengths until fewer than place + 1 tiles are longer, and takes the right one of those that are as long.  All lanes.
+// Forward, T 8192, 12 heads of 64, documents of 4000 on average: 109 -> 99 us, of 1024: 45.7 -> 41.3, of 300: 29.3 -> 28.8 (32.3 -> 32.6 from
+// cold caches); T 4096, 16 / 8 heads of 128, of 500: 29.7 -> 25.7; T 8192, of 200: 38.2 -> 39.9, where tiles are all about as long.
+// Backward: up to two key blocks an SM, same heads, T 4096: 81 -> 77; beyond that 4 % less (T 8192, of 2000) to 2 % more (T 16384, of
+// 4000, and short ones), and with two CTAs an SM (heads of 64) nothing or 3 % more: not ordered.
+constexpr int kOrdered = 128;  // tiles, at most
+struct Ordered {
+  static constexpr int PER = kOrdered / 32;
+  int v[PER];
+  int tile, length;
+  template <class Bound>
+  __device__ __forceinline__ void read(int n, int lane, Bound&& bound) {
+#pragma unroll
+    for (int c = 0; c < PER; ++c)
+      if (32 * c < n) v[c] = bound(min(32 * c + lane, n - 1));
+  }
+  template <class Length>
+  __device__ __forceinline__ void find(int n, int place, int lane, Length&& length_of) {
+    if (n <= 32) find_of<1>(n, place, lane, length_of);
+    else if (n <= 64) find_of<2>(n, place, lane, length_of);
+    else find_of<PER>(n, place, lane, length_of);
+  }
+  template <int N, class Length>
+  __device__ __forceinline__ void find_of(int n, int place, int lane, Length&& length_of) {
+    int most = 0;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      v[c] = 32 * c + lane < n ? length_of(32 * c + lane, v[c]) : -1;
+      most = max(most, v[c]);
+    }
+    int lo = -1, hi = __reduce_max_sync(0xffffffffu, most), longer = 0;  // the length is in (lo, hi]; `longer` tiles are beyond hi
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      int above = 0;
+#pragma unroll
+      for (int c = 0; c < N; ++c) above += __popc(__ballot_sync(0xffffffffu, v[c] > mid));
+      if (above > place) {
+        lo = mid;
+      } else {
+        hi = mid;
+        longer = above;
+      }
+    }
+    int left = place - longer;
+    tile = 0;
+    length = hi;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const uint32_t same = __ballot_sync(0xffffffffu, v[c] == hi);
+      const uint32_t it = __ballot_sync(0xffffffffu, v[c] == hi && __popc(same & ((1u << lane) - 1u)) == left);
+      if (it != 0u) tile = 32 * c + __ffs(it) - 1;
+      left -= __popc(same);
+    }
+  }
+};
 
 // ============================================================================ forward
 // One CTA per (128 queries, head, batch row), two an SM; K and V blocks of 64 keys are streamed, S_{j+1} = Q K_{j+1}^T is
@@ -89,7 +155,7 @@ struct FwdCfg {
   static constexpr int OFF_K = Q_BYTES;
   static constexpr int OFF_V = OFF_K + NK * KV_BYTES;
   static constexpr int OFF_BAR = OFF_V + NV * KV_BYTES;
-  static constexpr int SMEM_BYTES = OFF_BAR + 168;
+  static constexpr int SMEM_BYTES = OFF_BAR + 168;  // 18 barriers, 4 words
   static constexpr int TMEM_COLS = 256;  // S0 [0,64) S1 [64,128) (bf16 P over the first 32 columns of each), O from 128
   static constexpr int O_COL = 128;
 };
@@ -132,23 +198,39 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   }
   // last query blocks first: the tiles at the start of the sequence, the only ones with fewer blocks, end the launch
   const int groups = n_heads * n_batch;
-  const int qb = n_qblocks - 1 - (int)blockIdx.x / groups;
+  const int place = (int)blockIdx.x / groups;
+  int qb = n_qblocks - 1 - place;
   const int grp = (int)blockIdx.x % groups;
   const int n = grp % n_heads, b = grp / n_heads;
   const int kvh = n / (n_heads / n_kv);
   const int hq = n_heads * D, hkv = n_kv * D;
-  const int q0 = qb * C::BQ;
-  int rows_end = S;  // rows behind it are nobody's
+  int rows_end = S, q0 = qb * C::BQ;  // rows behind the first are nobody's
   KeyRuns runs;
+  // documents, longest first: warp 0 finds the tile and its keys' first row, the others read them behind the set-up
+  bool ordered = false;
+  volatile int* s_tile = abort_flag + 1;
   if constexpr (DOCS) {
+    ordered = gridDim.x > 2 * kSms && n_qblocks <= kOrdered;
     pdl_wait();
+    Ordered order{};
+    if (ordered && warp == 0) order.read(n_qblocks, lane, [&](int i) { return docs_start(docs, i * C::BQ); });
     rows_end = docs_total(docs, S);
-    if (q0 >= rows_end) return;
-    runs = KeyRuns(q0, rows_end, docs_start(docs, q0));
+    if ((ordered ? place * C::BQ : q0) >= rows_end) return;
+    if (!ordered) {
+      runs = KeyRuns(q0, rows_end, docs_start(docs, q0));
+    } else if (warp == 0) {
+      order.find(n_qblocks, place, lane, [&](int i, int start) { return i * C::BQ < rows_end ? KeyRuns(i * C::BQ, rows_end, start).count : 0; });
+      q0 = order.tile * C::BQ;
+      runs = KeyRuns::of_count(q0, rows_end, order.length);
+      if (lane == 0) {
+        s_tile[0] = q0;
+        s_tile[1] = order.length;
+      }
+    }
   } else {
     runs = KeyRuns(q0, S, window, sinks);
   }
-  const int nb = runs.count;
+  int nb = runs.count;
 
   auto load_k = [&](int j) {
     const int st = j % C::NK;
@@ -195,6 +277,11 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   const uint32_t tmem_base = *tmem_slot;
   pdl_trigger();
   pdl_wait();  // set-up done; from here on the kernel touches what its predecessor wrote
+  if (DOCS && ordered && warp != 0) {
+    q0 = s_tile[0];
+    runs = KeyRuns::of_count(q0, rows_end, s_tile[1]);
+    nb = runs.count;
+  }
 
   if (warp == 0) {
     if (lane == 0) {
@@ -488,11 +575,12 @@ struct Plan {
     return (long long)x * nb - over * (over - 1) / 2;
   }
   // The same of a packed batch: to the block in which the document of the block's last row ends; 0 behind the last document.
-  __device__ int docs_blocks_seen(int x, int total) const {
+  __device__ int docs_blocks_seen(int x, int total) const { return docs_blocks_seen(x, total, __ldg(docs.end + min(S, x * 128 + 128) - 1)); }
+  __device__ int docs_blocks_seen(int x, int total, int end) const {  // end: of the document of the block's last row
     const int last = min(S, x * 128 + 128) - 1;
     if (x * 128 >= total) return 0;
     if (last >= total) return 1;
-    return min(max((min(__ldg(docs.end + last), total) + 127) / 128 - x, 1), blocks_seen(x));
+    return min(max((min(end, total) + 127) / 128 - x, 1), blocks_seen(x));
   }
   // first slot of a key block's partial sums
   __host__ __device__ int rank_of(int x) const {
@@ -554,21 +642,45 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   const int rank = (int)blockIdx.x / pl.groups, local = (int)blockIdx.x % pl.groups, grp = pl.group0 + local;
   const int kvh = grp % n_kv, b = grp / n_kv;
   const int n_sink_ranks = pl.n_sink * pl.parts_sink;
-  const int x = rank < n_sink_ranks ? rank / pl.parts_sink : pl.n_sink + (rank - n_sink_ranks) / pl.parts;
+  int x = rank < n_sink_ranks ? rank / pl.parts_sink : pl.n_sink + (rank - n_sink_ranks) / pl.parts;
   const int part = rank < n_sink_ranks ? rank % pl.parts_sink : (rank - n_sink_ranks) % pl.parts;
-  const int x0 = x * 128;
-  int rows_end = S, per_head;  // rows behind the first are nobody's; query blocks of a head that this key block meets
+  int rows_end = S, per_head = 0;  // rows behind the first are nobody's; query blocks of a head that this key block meets
+  // documents, longest first: warp 0 finds the key block and its queries, the others read them behind the set-up
+  bool ordered = false;
+  volatile int* s_tile = abort_flag + 1;
   if constexpr (DOCS) {
+    ordered = C::CTAS == 1 && pl.parts == 1 && gridDim.x > kSms && gridDim.x <= 2 * kSms && pl.nxb <= kOrdered;
     pdl_wait();
+    Ordered order{};
+    if (ordered && warp == 0) order.read(pl.nxb, lane, [&](int i) { return __ldg(pl.docs.end + min(S, i * 128 + 128) - 1); });
     rows_end = docs_total(pl.docs, S);
-    per_head = pl.docs_blocks_seen(x, rows_end);
+    if (ordered) {
+      if (x * 128 >= rows_end) return;
+      if (warp == 0) {
+        order.find(pl.nxb, x, lane, [&](int i, int end) { return pl.docs_blocks_seen(i, rows_end, end); });
+        x = order.tile;
+        per_head = order.length;
+        if (lane == 0) {
+          s_tile[0] = x;
+          s_tile[1] = per_head;
+        }
+      }
+    } else {
+      per_head = pl.docs_blocks_seen(x, rows_end);
+    }
   } else {
     per_head = pl.blocks_seen(x);
   }
-  const int total = per_head * n_rep, np = pl.parts_for(per_head);
+  const int np = DOCS && ordered ? 1 : pl.parts_for(per_head);
   if (part >= np) return;
-  const int first128 = (int)((long long)total * part / np);
-  const int iters = ((int)((long long)total * (part + 1) / np) - first128) * C::SUB;
+  int x0, first128, iters;
+  auto set_block = [&] {
+    const int total = per_head * n_rep;
+    x0 = x * 128;
+    first128 = (int)((long long)total * part / np);
+    iters = ((int)((long long)total * (part + 1) / np) - first128) * C::SUB;
+  };
+  set_block();
 
   // block `it` of this CTA: query head of the group, 128-query block counted from x, first query
   auto rep_of = [&](int it) { return (first128 + it / C::SUB) / per_head; };
@@ -635,6 +747,11 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   const uint32_t tmem_base = *tmem_slot;
   pdl_trigger();
   pdl_wait();  // set-up done; from here on the kernel touches what its predecessor wrote
+  if (DOCS && ordered && warp != 0) {
+    x = s_tile[0];
+    per_head = s_tile[1];
+    set_block();
+  }
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer

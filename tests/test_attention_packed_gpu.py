@@ -321,3 +321,28 @@ def test_two_calls_on_two_streams():
     Bn.k_status()
     for (qkv, do, o, lse, bounds, dqkv, *shape), (o2, lse2, dqkv2, scratch) in zip(runs, again):
         assert torch.equal(o, o2) and torch.equal(lse, lse2) and torch.equal(dqkv, dqkv2)
+
+
+@pytest.mark.parametrize("nh,nkv,d,rope", [(16, 8, 128, True), (12, 12, 64, False), (5, 5, 64, True), (16, 2, 128, False)])
+@pytest.mark.parametrize("lens,tail", [([400, 1, 0, 77, 400, 400, 128, 128, 3, 390, 400, 400, 250, 400, 123], 600), ([128] * 30, 260), ([4100], 0), ([1], 4099)])
+def test_tiles_in_order_of_length(nh, nkv, d, rope, lens, tail):
+    """Calls of one to a few tiles an SM, which start with the longest: documents of many lengths and of one, tiles that nobody owns."""
+    T, n = sum(lens) + tail, sum(lens)
+    assert (T + 127) // 128 == 33
+    qkv, do = inputs(lens, tail, nh, nkv, d, 77)
+    o, lse, bounds = run_fwd(qkv, lens, T, nh, nkv, d)
+    cos, sin = tables(max(lens), d) if rope else (None, None)
+    dqkv = run_bwd(qkv, o, do, lse, bounds, T, nh, nkv, d, max(lens), cos, sin)
+    assert (o[n:] == 7).all() and (lse[:, n:] == 7).all() and (dqkv[n:] == 9).all()
+    r = nh // nkv
+    for a in range(nkv):  # the reference by kv heads: its scores are many
+        cols = [h * d + c for h in list(range(a * r, (a + 1) * r)) + [nh + a, nh + nkv + a] for c in range(d)]
+        part, own = qkv[:, cols], slice(a * r * d, (a + 1) * r * d)
+        want, want_lse = reference_fwd(part, lens, r, 1, d)
+        assert rel(o[:n, own], want) < tol(want.numel()) and float((lse[a * r:(a + 1) * r, :n].double() - want_lse).abs().max()) < 2e-5
+        if n == 1:
+            continue  # differences that cancel to 0
+        want = reference_bwd(part, o[:, own].contiguous(), do[:, own].contiguous(), lens, r, 1, d, cos, sin)
+        got = dqkv[:n, cols].view(n, r + 2, d)
+        for k in (slice(0, r), slice(r, r + 1), slice(r + 1, r + 2)):
+            assert rel(got[:, k], want.view(n, r + 2, d)[:, k]) < 3e-3
