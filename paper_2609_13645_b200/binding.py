@@ -646,7 +646,7 @@ def k_dropout_add(x, resid, y, p, seed, site, step=None, scale=1.0):
 
 # ---- operators of a train step over packed documents ---------------------------------------------------------
 def _packed_shape(T, n_heads, n_kv, d, longest=1):
-    if min(T, n_heads, n_kv, longest) < 1 or n_heads % n_kv or d not in (64, 128) or max(T, n_heads, longest) > _INT32_MAX:
+    if not (1 <= T <= _INT32_MAX and 1 <= n_kv <= n_heads <= _INT32_MAX and 1 <= longest <= _INT32_MAX) or n_heads % n_kv or (d != 64 and d != 128):
         _refuse(f"T {T}, heads {n_heads} / {n_kv} of {d}, longest document {longest}")
 
 
@@ -741,7 +741,7 @@ def k_rotary(x, y, cos, sin, n_heads, d, positions=None, interleaved=False, inve
     if n_heads < 1 or d < 1 or n_heads * d != h:
         _refuse(f"x: {h} columns are not {n_heads} heads of {d}")
     px, ldx = _check_rows("x", x, dtype, rows, h, dev)
-    py, ldy = _check_rows("y", y, dtype, rows, h, dev)
+    py, ldy = (px, ldx) if y is x else _check_rows("y", y, dtype, rows, h, dev)
     pc, ps = _check_tables(cos, sin, dev)
     st = lib().ft_k_rotary(px, ldx, py, ldy, _check_flat("positions", positions, torch.int32, rows, dev) if positions is not None else None,
                            pc, ps, cos.shape[0], rows, n_heads, d, 2 * cos.shape[1], 1 if interleaved else 0, 1 if inverse else 0, dt,
