@@ -14,7 +14,8 @@ namespace {
 // ============================================================================ backward pre-pass
 // delta[b, n, i] = sum_k dO[b,i,n,k] O[b,i,n,k].  D/8 lanes share one (token, head) row with one 16-byte load per
 // tensor each; every warp keeps two groups of rows in flight and walks the rows grid-strided.  The D products of a
-// row are added in a fixed order (8 per lane, then a butterfly over the row's lanes).
+// row are added in a fixed order (8 per lane, then a butterfly over the row's lanes).  Rows are counted in 32 bits, for the divisions'
+// sake (backward pass of T 8192, 16 / 8 heads of 128, documents of 500: 164.9 -> 163.4 us); 2^31 of them would fill more than a GPU.
 template <int D>
 __global__ void __launch_bounds__(256)
 attn_delta_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o, float* __restrict__ delta, int B, int S,
@@ -24,17 +25,16 @@ attn_delta_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o, floa
   constexpr int LPR = D / 8;    // lanes per row
   constexpr int RPW = 32 / LPR;  // rows per warp and load
   const int lane = threadIdx.x & 31, sub = lane / LPR, l = lane % LPR;
-  const long long total = (long long)B * S * n_heads;
-  const long long nwarps = ((long long)gridDim.x * blockDim.x) >> 5;
-  for (long long base = (((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5) * (2 * RPW); base < total;
-       base += nwarps * (2 * RPW)) {
+  const uint32_t total = (uint32_t)B * S * n_heads;
+  const uint32_t nwarps = ((uint32_t)gridDim.x * blockDim.x) >> 5;
+  for (uint32_t base = (((uint32_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5) * (2 * RPW); base < total; base += nwarps * (2 * RPW)) {
     uint4 a[2], d[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const long long w = base + u * RPW + sub;
+      const uint32_t w = base + u * RPW + sub;
       const bool ok = w < total;
-      a[u] = ok ? *reinterpret_cast<const uint4*>(o + w * D + l * 8) : make_uint4(0, 0, 0, 0);
-      d[u] = ok ? *reinterpret_cast<const uint4*>(d_o + w * D + l * 8) : make_uint4(0, 0, 0, 0);
+      a[u] = ok ? *reinterpret_cast<const uint4*>(o + (long long)w * D + l * 8) : make_uint4(0, 0, 0, 0);
+      d[u] = ok ? *reinterpret_cast<const uint4*>(d_o + (long long)w * D + l * 8) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -44,11 +44,10 @@ attn_delta_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o, floa
       acc += bf16_lo(a[u].w) * bf16_lo(d[u].w) + bf16_hi(a[u].w) * bf16_hi(d[u].w);
 #pragma unroll
       for (int off = LPR / 2; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
-      const long long w = base + u * RPW + sub;
+      const uint32_t w = base + u * RPW + sub;
       if (l == 0 && w < total) {
-        const int n = (int)(w % n_heads);
-        const long long tok = w / n_heads;
-        const int b = (int)(tok / S), i = (int)(tok % S);
+        const uint32_t tok = w / (uint32_t)n_heads;
+        const int n = (int)(w - tok * n_heads), b = B == 1 ? 0 : (int)(tok / (uint32_t)S), i = (int)(tok - (uint32_t)b * S);
         delta[((long long)b * n_heads + n) * S + i] = acc;
       }
     }
@@ -61,6 +60,7 @@ cudaError_t attention_delta(const bf16* o, const bf16* d_o, float* delta, int B,
   const long long rows = (long long)B * S * nh;
   const long long want = (rows * (d / 8) + 2 * 256 - 1) / (2 * 256);  // blocks if every thread took one load pair
   const int blocks = (int)(want < 148 * 8 ? (want > 0 ? want : 1) : 148 * 8);
+  if (rows > (1ll << 31)) return cudaErrorInvalidValue;
   if (d == 64) return launch_pdl(attn_delta_kernel<64>, blocks, 256, 0, st, o, d_o, delta, B, S, nh);
   if (d == 128) return launch_pdl(attn_delta_kernel<128>, blocks, 256, 0, st, o, d_o, delta, B, S, nh);
   return cudaErrorInvalidValue;
