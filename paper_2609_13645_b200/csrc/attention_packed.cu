@@ -18,7 +18,7 @@
 // The grid has a CTA a work item, the last queries first; a CTA that has issued all loads of its item takes over the next one that has
 // not started (clusterlaunchcontrol), so that the next item's loads go on while the last one ends, and items of any length even out.
 //
-// T 16384, 4 documents of up to 5622 rows, 16 / 8 heads of 128: 296 us, 1060 TFLOP/s of visible pairs; the tensor pipe and the exponential
+// T 16384, 4 documents of up to 5622 rows, 16 / 8 heads of 128: 278 us, 1130 TFLOP/s of visible pairs; the tensor pipe and the exponential
 // unit are 60 % busy.  What bounds it is each tile's chain of about 3600 cycles a block: scores to registers 200, maxima 200,
 // exponentials 1100, P to TMEM 150, then P V and the next S on the tensor cores, behind the other tile's (1100 and 650 of latencies); TMEM is
 // full, so the next S cannot be formed before P V has read P.  Measured beside it: two warps a row with 64 keys each 338 us (twice
@@ -494,11 +494,12 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T,
 
 cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int nh, int nkv, int d, int* err, cudaStream_t st) {
   if (attention_packed_scratch_bytes(T, nh, nkv, d, 1) == 0 || !err) return cudaErrorInvalidValue;
-  // Two tiles a CTA from ten tiles an SM on.  16 / 8 heads of 128, documents of about 4000: T 16384 276 us (one tile a CTA: 298), one of
-  // 16384: 532 (563); 12 heads of 64, T 16384, one document: 318 (343).  Below, a CTA's start and end count, and two small
-  // ones an SM hide each other's: T 8192, 16 / 8 heads of 128, documents of 2000: 92.6 (88.8), of 200: 39.4 (38.0); 12 heads of 64,
-  // of 300: 30.6 (29.1); T 256, 4 heads of 64: 9.7 (5.6).
-  if ((long long)((T + 127) / 128) * nh < 10 * 148) return attention_packed_fwd_tile(qkv, o, lse, docs, T, nh, nkv, d, err, st);
+  // Two tiles a CTA from ten tiles of heads of 128, or eleven of 64, an SM on; below, a CTA's start and end count, and two small ones an
+  // SM hide each other's.  us, in brackets with one tile a CTA, for documents of 200 / 1000 / 4000 on average:
+  //   16 / 8 heads of 128   T 8192: 39.3 64.1 147 (39.8 61.3 142);  T 12288: 52.9 84.8 211 (57.2 87.9 216);  T 16384: 66.4 107 272 (71.7 111 285)
+  //   heads of 64, 12   T 12288: 39.5 67.2 152 (36.5 60.3 145), T 16384: 50.0 84.9 191 (49.3 80.1 193);  16 / 8   T 16384: 58.3 97.7 241 (61.0 102 251)
+  // and T 256, 4 heads of 64: 9.7 (5.6).
+  if ((long long)((T + 127) / 128) * nh < (d == 64 ? 11 : 10) * 148) return attention_packed_fwd_tile(qkv, o, lse, docs, T, nh, nkv, d, err, st);
   if (d == 64) return fwd_t<64>(qkv, o, lse, docs, T, nh, nkv, err, st);
   return fwd_t<128>(qkv, o, lse, docs, T, nh, nkv, err, st);
 }

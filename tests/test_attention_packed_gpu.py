@@ -236,9 +236,9 @@ def test_offsets_that_are_refused_on_the_device(cu):
     assert (b[:2] >= 0).all() and (b[:2] <= T).all() and (b[2] >= 0).all() and (b[2] < T).all()
 
 
-@pytest.mark.parametrize("nh,nkv,d,T", [(30, 15, 64, 6500), (24, 24, 64, 7900), (33, 11, 64, 5900), (30, 15, 128, 6500), (24, 24, 128, 7900), (25, 5, 128, 7700)])
+@pytest.mark.parametrize("nh,nkv,d,T", [(30, 15, 64, 6500), (24, 24, 64, 7900), (33, 11, 64, 5900), (34, 17, 64, 6500), (28, 28, 64, 7900), (39, 13, 64, 5900), (30, 15, 128, 6500), (24, 24, 128, 7900), (25, 5, 128, 7700)])
 def test_two_tiles_a_block(nh, nkv, d, T):
-    """Calls of ten and more tiles an SM, whose blocks work on two tiles: heads that share K and V or have their own, odd numbers of
+    """Calls of ten or eleven tiles an SM, and of more, whose blocks work on two tiles: heads that share K and V or have their own, odd numbers of
     them, an odd number of query blocks, documents from one row to most of the batch, rows behind them; bit-identical twice."""
     g = np.random.RandomState(T + nh)
     lens = [1, 0, 127, 129, 1, 2500] + [int(m) for m in g.randint(0, 400, 11)]
@@ -346,3 +346,17 @@ def test_tiles_in_order_of_length(nh, nkv, d, rope, lens, tail):
         got = dqkv[:n, cols].view(n, r + 2, d)
         for k in (slice(0, r), slice(r, r + 1), slice(r + 1, r + 2)):
             assert rel(got[:, k], want.view(n, r + 2, d)[:, k]) < 3e-3
+
+
+def test_large_scores_in_two_tiles_of_64():
+    """References that move by hundreds, up and down, between a row's blocks."""
+    nh, nkv, d, lens, T = 34, 17, 64, [3000, 700, 2600], 6500
+    n = sum(lens)
+    qkv, _ = inputs(lens, T - n, nh, nkv, d, 12)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    qkv[:n, nh * d:(nh + nkv) * d] *= torch.exp2(torch.randint(-6, 7, (n, 1), generator=g, device="cuda").float()).bfloat16()  # keys of any size
+    o, lse, _ = run_fwd(qkv, lens, T, nh, nkv, d)
+    cols = [h * d + c for h in (0, 1, nh, nh + nkv) for c in range(d)]
+    want, want_lse = reference_fwd(qkv[:, cols], lens, 2, 1, d)
+    # as in test_large_scores_in_two_tiles_a_block
+    assert rel(o[:n, :2 * d], want) < 1e-2 and float((lse[:2, :n].double() - want_lse).abs().max()) < 0.01
