@@ -15,10 +15,10 @@
 // Two tiles a CTA halve what K and V cost in shared memory, whose bandwidth bounds a CTA of one tile: a pair of blocks of
 // 128 x 128 at D = 128 takes 1024 cycles of tensor pipe, of exponential unit and (with shared K and V) of shared memory each.
 //
-// The grid has a CTA a work item, the last queries first; a CTA that has issued all loads of its item takes over the next one that has
+// The grid has a CTA a work item, the longest first; a CTA that has issued all loads of its item takes over the next one that has
 // not started (clusterlaunchcontrol), so that the next item's loads go on while the last one ends, and items of any length even out.
 //
-// T 16384, 4 documents of up to 5622 rows, 16 / 8 heads of 128: 278 us, 1130 TFLOP/s of visible pairs; the tensor pipe and the exponential
+// T 16384, 4 documents of up to 5622 rows, 16 / 8 heads of 128: 284 us, 1106 TFLOP/s of visible pairs; the tensor pipe and the exponential
 // unit are 60 % busy.  What bounds it is each tile's chain of about 3600 cycles a block: scores to registers 200, maxima 200,
 // exponentials 1100, P to TMEM 150, then P V and the next S on the tensor cores, behind the other tile's (1100 and 650 of latencies); TMEM is
 // full, so the next S cannot be formed before P V has read P.  Measured beside it: two warps a row with 64 keys each 338 us (twice
@@ -36,6 +36,7 @@ namespace fs {
 namespace {
 
 constexpr int THREADS = 320;
+constexpr int kOrdered = 256;  // blocks of queries of a head (or pairs of them), at most, that are taken in the order of their lengths
 
 template <int D>
 struct Cfg {
@@ -143,6 +144,11 @@ attn_packed_fwd_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   pdl_wait();  // set-up done; from here on the kernel touches what its predecessor wrote
+  // items: the same queries of two heads, or two blocks of queries of one; a place of the order of lengths is a block (or two)
+  const int per = by_head ? n_heads / 2 : n_heads, places = by_head ? n_qblocks : (n_qblocks + 1) / 2, rows = by_head ? 128 : 256;
+  const bool ordered = places <= kOrdered;
+  Ordered<kOrdered> order{};
+  if (ordered && warp == 0) order.read(places, lane, [&](int i) { return __ldg(docs.start + i * rows); });
   const int e_last = __ldg(docs.end + T - 1), rows_end = e_last < 0 ? 0 : e_last < T ? e_last : T;  // rows behind it are nobody's
 
   // The item that consumers work on next: waits for it, takes it over and gives its place back.
@@ -166,14 +172,24 @@ attn_packed_fwd_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       const bool got = mbar_wait(bar(i), parity, abort_flag, err, kWaitLimitCycles, site);
       return __all_sync(0xffffffffu, got) != 0;
     };
+    if (ordered)
+      order.measure(places, lane, [&](int i, int start) {
+        const int row = i * rows;
+        return row < rows_end ? (min(row + rows, rows_end) + 127) / 128 - (min(max(start, 0), row) >> 7) : 0;
+      });
     for (int k = 0; ok; ++k) {
       Item it;
       it.valid = index >= 0;
-      const int per = by_head ? n_heads / 2 : n_heads, rank = index / per, which = index % per;
+      const int rank = index / per, which = index % per;
+      int place = places - 1 - rank;
+      if (ordered && it.valid) {
+        order.find(places, rank, lane);
+        place = order.tile;
+      }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         it.head[t] = by_head ? 2 * which + t : which;
-        it.q0[t] = by_head ? (n_qblocks - 1 - rank) * 128 : ((n_qblocks + 1) / 2 - 1 - rank) * 256 + t * 128;
+        it.q0[t] = place * rows + t * (rows - 128);
         it.first[t] = it.end[t] = 0;
         if (it.valid && it.q0[t] < rows_end) {
           const int a = __ldg(docs.start + it.q0[t]);
@@ -494,12 +510,13 @@ cudaError_t fwd_t(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T,
 
 cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Docs& docs, int T, int nh, int nkv, int d, int* err, cudaStream_t st) {
   if (attention_packed_scratch_bytes(T, nh, nkv, d, 1) == 0 || !err) return cudaErrorInvalidValue;
-  // Two tiles a CTA from ten tiles of heads of 128, or eleven of 64, an SM on; below, a CTA's start and end count, and two small ones an
-  // SM hide each other's.  us, in brackets with one tile a CTA, for documents of 200 / 1000 / 4000 on average:
-  //   16 / 8 heads of 128   T 8192: 39.3 64.1 147 (39.8 61.3 142);  T 12288: 52.9 84.8 211 (57.2 87.9 216);  T 16384: 66.4 107 272 (71.7 111 285)
-  //   heads of 64, 12   T 12288: 39.5 67.2 152 (36.5 60.3 145), T 16384: 50.0 84.9 191 (49.3 80.1 193);  16 / 8   T 16384: 58.3 97.7 241 (61.0 102 251)
-  // and T 256, 4 heads of 64: 9.7 (5.6).
-  if ((long long)((T + 127) / 128) * nh < (d == 64 ? 11 : 10) * 148) return attention_packed_fwd_tile(qkv, o, lse, docs, T, nh, nkv, d, err, st);
+  // Two tiles a CTA from six tiles an SM on; below, a CTA's start and end count, and two small ones an SM hide each other's.  us for
+  // documents of 300 / 1000 / 4000 on average, in brackets with one tile a CTA:
+  //   16 / 8 heads of 128   T 2048: 16.8 36.1 37.3 (15.2 26.9 29.5);  T 6144: 33.7 45.8 83.3 (32.9 47.4 85.2);  T 16384: 70 104 269 (78 113 291)
+  //   12 heads of 64        T 2048: 15.8 33.8 33.7 (11.9 25.2 26.9);  T 8192: 29.7 42.6 98.6 (28.9 43.3 98.8);  T 16384: 52 76 178 (54 81 193)
+  // With pairs of neighbouring blocks of queries (7 heads of 64 on one, T 20000) short documents lose, 41.5 (36.3) at 200, and longer ones
+  // gain, 61 (68) and 135 (157).
+  if ((long long)((T + 127) / 128) * nh < 6 * 148) return attention_packed_fwd_tile(qkv, o, lse, docs, T, nh, nkv, d, err, st);
   if (d == 64) return fwd_t<64>(qkv, o, lse, docs, T, nh, nkv, err, st);
   return fwd_t<128>(qkv, o, lse, docs, T, nh, nkv, err, st);
 }

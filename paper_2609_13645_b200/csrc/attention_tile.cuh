@@ -142,6 +142,64 @@ __device__ __forceinline__ void stage_rows_unrotated(uint32_t out, uint32_t tabl
     stage_cols<16>(out, lane, H + i0, hi);
   }
 }
+
+// Tiles in the order of their lengths, longest first, as a warp finds it: it reads a bound of every tile (before it needs anything
+// else from memory) and turns the bounds into lengths; the tile at a place of the order is found by halving the range of the
+// lengths until no more than `place` tiles are longer, and is then the right one of those that are as long.  All lanes.
+template <int MOST>  // tiles
+struct Ordered {
+  static constexpr int PER = MOST / 32;
+  int v[PER], longest;
+  int tile, length;  // what find() found
+  template <class Bound>
+  __device__ __forceinline__ void read(int n, int lane, Bound&& bound) {
+#pragma unroll
+    for (int c = 0; c < PER; ++c)
+      if (32 * c < n) v[c] = bound(min(32 * c + lane, n - 1));
+  }
+  template <class Length>
+  __device__ __forceinline__ void measure(int n, int lane, Length&& length_of) {
+    longest = 0;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+      v[c] = 32 * c + lane < n ? length_of(32 * c + lane, v[c]) : -1;
+      longest = max(longest, v[c]);
+    }
+    longest = __reduce_max_sync(0xffffffffu, longest);
+  }
+  __device__ __forceinline__ void find(int n, int place, int lane) {
+    if (n <= 64) find_of<2>(place, lane);
+    else if (n <= 128) find_of<PER < 4 ? PER : 4>(place, lane);
+    else find_of<PER>(place, lane);
+  }
+  template <int N>
+  __device__ __forceinline__ void find_of(int place, int lane) {
+    int lo = -1, hi = longest, longer = 0;  // the length is in (lo, hi]; `longer` tiles are beyond hi
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      int above = 0;
+#pragma unroll
+      for (int c = 0; c < N; ++c) above += __popc(__ballot_sync(0xffffffffu, v[c] > mid));
+      if (above > place) {
+        lo = mid;
+      } else {
+        hi = mid;
+        longer = above;
+      }
+    }
+    int left = place - longer;
+    tile = 0;
+    length = hi;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const uint32_t same = __ballot_sync(0xffffffffu, v[c] == hi);
+      const uint32_t it = __ballot_sync(0xffffffffu, v[c] == hi && __popc(same & ((1u << lane) - 1u)) == left);
+      if (it != 0u) tile = 32 * c + __ffs(it) - 1;
+      left -= __popc(same);
+    }
+  }
+};
+
 // Sends the staged rows off: D columns from x on, 32 rows from y on of batch row z.
 template <int D>
 __device__ __forceinline__ void send_rows(const void* tmap, uint32_t out, int lane, int x, int y, int z, int S) {

@@ -74,63 +74,12 @@ __device__ __forceinline__ int docs_start(const Docs& docs, int row) {  // of a 
 }
 
 // CTAs of packed documents differ in length by what their tile meets of its documents, and a long one that starts late leaves the
-// rest of the GPU waiting: launches of more CTAs than run at a time start the longest first.  A warp finds the tile at a place of that
-// order: it reads a bound of every tile (before it needs anything else from memory), turns them into lengths, halves the range
-// of the lengths until fewer than place + 1 tiles are longer, and takes the right one of those that are as long.  All lanes.
+// rest of the GPU waiting: launches of more CTAs than run at a time start the longest first (Ordered), if the tiles are at most
+constexpr int kOrdered = 128;
 // Forward, T 8192, 12 heads of 64, documents of 4000 on average: 109 -> 99 us, of 1024: 45.7 -> 41.3, of 300: 29.3 -> 28.8 (32.3 -> 32.6 from
-// cold caches); T 4096, 16 / 8 heads of 128, of 500: 29.7 -> 25.7; T 8192, of 200: 38.2 -> 39.9, where tiles are all about as long.
+// cold caches); T 4096, 16 / 8 heads of 128, of 500: 29.7 -> 25.7.
 // Backward: up to two key blocks an SM, same heads, T 4096: 81 -> 77; beyond that 4 % less (T 8192, of 2000) to 2 % more (T 16384, of
 // 4000, and short ones), and with two CTAs an SM (heads of 64) nothing or 3 % more: not ordered.
-constexpr int kOrdered = 128;  // tiles, at most
-struct Ordered {
-  static constexpr int PER = kOrdered / 32;
-  int v[PER];
-  int tile, length;
-  template <class Bound>
-  __device__ __forceinline__ void read(int n, int lane, Bound&& bound) {
-#pragma unroll
-    for (int c = 0; c < PER; ++c)
-      if (32 * c < n) v[c] = bound(min(32 * c + lane, n - 1));
-  }
-  template <class Length>
-  __device__ __forceinline__ void find(int n, int place, int lane, Length&& length_of) {
-    if (n <= 32) find_of<1>(n, place, lane, length_of);
-    else if (n <= 64) find_of<2>(n, place, lane, length_of);
-    else find_of<PER>(n, place, lane, length_of);
-  }
-  template <int N, class Length>
-  __device__ __forceinline__ void find_of(int n, int place, int lane, Length&& length_of) {
-    int most = 0;
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      v[c] = 32 * c + lane < n ? length_of(32 * c + lane, v[c]) : -1;
-      most = max(most, v[c]);
-    }
-    int lo = -1, hi = __reduce_max_sync(0xffffffffu, most), longer = 0;  // the length is in (lo, hi]; `longer` tiles are beyond hi
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      int above = 0;
-#pragma unroll
-      for (int c = 0; c < N; ++c) above += __popc(__ballot_sync(0xffffffffu, v[c] > mid));
-      if (above > place) {
-        lo = mid;
-      } else {
-        hi = mid;
-        longer = above;
-      }
-    }
-    int left = place - longer;
-    tile = 0;
-    length = hi;
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const uint32_t same = __ballot_sync(0xffffffffu, v[c] == hi);
-      const uint32_t it = __ballot_sync(0xffffffffu, v[c] == hi && __popc(same & ((1u << lane) - 1u)) == left);
-      if (it != 0u) tile = 32 * c + __ffs(it) - 1;
-      left -= __popc(same);
-    }
-  }
-};
 
 // ============================================================================ forward
 // One CTA per (128 queries, head, batch row), two an SM; K and V blocks of 64 keys are streamed, S_{j+1} = Q K_{j+1}^T is
@@ -212,14 +161,15 @@ attn_window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_con
   if constexpr (DOCS) {
     ordered = gridDim.x > 2 * kSms && n_qblocks <= kOrdered;
     pdl_wait();
-    Ordered order{};
+    Ordered<kOrdered> order{};
     if (ordered && warp == 0) order.read(n_qblocks, lane, [&](int i) { return docs_start(docs, i * C::BQ); });
     rows_end = docs_total(docs, S);
     if ((ordered ? place * C::BQ : q0) >= rows_end) return;
     if (!ordered) {
       runs = KeyRuns(q0, rows_end, docs_start(docs, q0));
     } else if (warp == 0) {
-      order.find(n_qblocks, place, lane, [&](int i, int start) { return i * C::BQ < rows_end ? KeyRuns(i * C::BQ, rows_end, start).count : 0; });
+      order.measure(n_qblocks, lane, [&](int i, int start) { return i * C::BQ < rows_end ? KeyRuns(i * C::BQ, rows_end, start).count : 0; });
+      order.find(n_qblocks, place, lane);
       q0 = order.tile * C::BQ;
       runs = KeyRuns::of_count(q0, rows_end, order.length);
       if (lane == 0) {
@@ -651,13 +601,14 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   if constexpr (DOCS) {
     ordered = C::CTAS == 1 && pl.parts == 1 && gridDim.x > kSms && gridDim.x <= 2 * kSms && pl.nxb <= kOrdered;
     pdl_wait();
-    Ordered order{};
+    Ordered<kOrdered> order{};
     if (ordered && warp == 0) order.read(pl.nxb, lane, [&](int i) { return __ldg(pl.docs.end + min(S, i * 128 + 128) - 1); });
     rows_end = docs_total(pl.docs, S);
     if (ordered) {
       if (x * 128 >= rows_end) return;
       if (warp == 0) {
-        order.find(pl.nxb, x, lane, [&](int i, int end) { return pl.docs_blocks_seen(i, rows_end, end); });
+        order.measure(pl.nxb, lane, [&](int i, int end) { return pl.docs_blocks_seen(i, rows_end, end); });
+        order.find(pl.nxb, x, lane);
         x = order.tile;
         per_head = order.length;
         if (lane == 0) {

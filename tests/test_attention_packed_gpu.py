@@ -238,7 +238,7 @@ def test_offsets_that_are_refused_on_the_device(cu):
 
 @pytest.mark.parametrize("nh,nkv,d,T", [(30, 15, 64, 6500), (24, 24, 64, 7900), (33, 11, 64, 5900), (34, 17, 64, 6500), (28, 28, 64, 7900), (39, 13, 64, 5900), (30, 15, 128, 6500), (24, 24, 128, 7900), (25, 5, 128, 7700)])
 def test_two_tiles_a_block(nh, nkv, d, T):
-    """Calls of ten or eleven tiles an SM, and of more, whose blocks work on two tiles: heads that share K and V or have their own, odd numbers of
+    """Calls of many tiles an SM, whose blocks work on two tiles: heads that share K and V or have their own, odd numbers of
     them, an odd number of query blocks, documents from one row to most of the batch, rows behind them; bit-identical twice."""
     g = np.random.RandomState(T + nh)
     lens = [1, 0, 127, 129, 1, 2500] + [int(m) for m in g.randint(0, 400, 11)]
