@@ -289,7 +289,7 @@ __device__ __forceinline__ float approx_inverse(float x) {
 
 // 8 elements a thread, a run a warp.  Bound by instructions: 835 a run (104 an element), of which those of the integer unit (58 % busy,
 // with 67 % of all issue slots) matter most: codes are shifted and added by multiplications, and pairs of fp32 numbers share an
-// instruction.  Of 124M parameters' 557 us, the random bits take about 110, the scales in two parts 60, codes settled in 64
+// instruction.  Of 134M parameters' 557 us, the random bits take about 110, the scales in two parts 60, codes settled in 64
 // bits 30; the bytes would take 334.
 template <bool PARAM16, bool GRAD16>
 __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, bool vec, const StepArgs& a, const AdamCoef& c, float clip,
@@ -448,7 +448,7 @@ adamw_kernel(const uint8_t* __restrict__ plan, int n_chunks, unsigned long long 
 
 template <bool PARAM16, bool GRAD16>
 cudaError_t launch(const PlanHeader& h, const uint8_t* plan, const StepArgs& a, cudaStream_t st) {
-  // Blocks that come and go even out what SMs and memory partitions do to each other: 124M parameters with fp32 moments take 672 us in
+  // Blocks that come and go even out what SMs and memory partitions do to each other: 134M parameters with fp32 moments take 672 us in
   // 4 blocks an SM that stay, 647 in 8, 612 in 24, 600 in 64 (595 in 128); with 8-bit ones 577 in 3, 567 in 6, 557 in 27, 571 in 90.
   const unsigned blocks = (unsigned)std::min(h.n_chunks, 148 * (h.bits == 8 ? 27 : 64));
   if (h.bits == 8) return launch_pdl(adamw_kernel<PARAM16, GRAD16, 8>, dim3(blocks), dim3(kThreads), 0, st, plan, h.n_chunks, (unsigned long long)h.chunk_offset, a);
