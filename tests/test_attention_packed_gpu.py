@@ -360,3 +360,23 @@ def test_large_scores_in_two_tiles_of_64():
     want, want_lse = reference_fwd(qkv[:, cols], lens, 2, 1, d)
     # as in test_large_scores_in_two_tiles_a_block
     assert rel(o[:n, :2 * d], want) < 1e-2 and float((lse[:2, :n].double() - want_lse).abs().max()) < 0.01
+
+
+@pytest.mark.parametrize("T,nh,nkv,d", [(10000, 5, 5, 64), (20001, 6, 3, 64), (24100, 5, 1, 64), (30100, 4, 2, 128), (16300, 7, 1, 128)])
+def test_orders_of_many_tiles(T, nh, nkv, d):
+    """Hundreds of tiles of a head, by themselves, two heads at a time and two neighbours at a time, in the order of their lengths."""
+    g = np.random.RandomState(T)
+    lens = [0, 1, 1500, 128, 128]
+    while sum(lens) < T - 700:
+        lens.append(int(g.randint(0, 600)))
+    n = sum(lens)
+    qkv, _ = inputs(lens, T - n, nh, nkv, d, 3)
+    o, lse, _ = run_fwd(qkv, lens, T, nh, nkv, d)
+    r = nh // nkv
+    for a in range(nkv):  # the reference by kv heads: its scores are many
+        cols = [h * d + c for h in list(range(a * r, (a + 1) * r)) + [nh + a, nh + nkv + a] for c in range(d)]
+        want, want_lse = reference_fwd(qkv[:, cols], lens, r, 1, d)
+        err = (o[:n, a * r * d:(a + 1) * r * d].double() - want).view(n, r, d).norm(dim=2)
+        assert float(err.max()) < 2.0 ** -6 * float(want.view(n, r, d).norm(dim=2).max())  # no row is another's: two roundings of 2^-8 each
+        assert rel(o[:n, a * r * d:(a + 1) * r * d], want) < 3e-3 and float((lse[a * r:(a + 1) * r, :n].double() - want_lse).abs().max()) < 2e-5
+    assert (o[n:] == 7).all() and (lse[:, n:] == 7).all()
