@@ -624,14 +624,10 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   }
   const int np = DOCS && ordered ? 1 : pl.parts_for(per_head);
   if (part >= np) return;
-  int x0, first128, iters;
-  auto set_block = [&] {
-    const int total = per_head * n_rep;
-    x0 = x * 128;
-    first128 = (int)((long long)total * part / np);
-    iters = ((int)((long long)total * (part + 1) / np) - first128) * C::SUB;
-  };
-  set_block();
+  const int total = per_head * n_rep;
+  int x0 = x * 128;
+  const int first128 = (int)((long long)total * part / np);
+  int iters = ((int)((long long)total * (part + 1) / np) - first128) * C::SUB;
 
   // block `it` of this CTA: query head of the group, 128-query block counted from x, first query
   auto rep_of = [&](int it) { return (first128 + it / C::SUB) / per_head; };
@@ -701,7 +697,8 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
   if (DOCS && ordered && warp != 0) {
     x = s_tile[0];
     per_head = s_tile[1];
-    set_block();
+    x0 = x * 128;
+    iters = per_head * n_rep * C::SUB;  // one part
   }
 
   if (warp == 0) {
@@ -849,8 +846,8 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       // single elements are only tested where the warp's tile touches an edge of the mask (warp-uniform)
       const bool full = cmin >= rmax && (DOCS ? cmin + C::W <= least_end
                                               : cmin + C::W <= S && (rmax < pl.sinks || cmin + C::W - 1 - rmin < pl.window));
-      const int lo = row - cmin, hi = row_end - cmin;
       if (!full) {
+        const int lo = row - cmin, hi = row_end - cmin;
         if constexpr (DOCS) {  // most blocks of short documents are on an edge: bits, which take a third of the comparisons
 #pragma unroll
           for (int c = 0; c < C::W; c += 32) {
@@ -922,8 +919,8 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            uint8_t* dst = reinterpret_cast<uint8_t*>(ds_band) +
-                           ((z * pl.band_at<DOCS>(pl.nxb) + pl.band_at<DOCS>(x) + rel) * 8 + (q >> 1) * 4 + chunk) * 4096 + (q & 1) * 2048;
+            const long long tile = DOCS ? z * pl.band_at<DOCS>(pl.nxb) + pl.band_at<DOCS>(x) + rel : (z * pl.nxb + x) * pl.nb + rel;
+            uint8_t* dst = reinterpret_cast<uint8_t*>(ds_band) + (tile * 8 + (q >> 1) * 4 + chunk) * 4096 + (q & 1) * 2048;
 #pragma unroll
             for (int c = 0; c < C::W / 32; ++c) bulk_store(dst + c * 4096, stage + c * 2048, 2048);
             bulk_commit_group();
