@@ -15,7 +15,9 @@ namespace {
 // delta[b, n, i] = sum_k dO[b,i,n,k] O[b,i,n,k].  D/8 lanes share one (token, head) row with one 16-byte load per
 // tensor each; every warp keeps two groups of rows in flight and walks the rows grid-strided.  The D products of a
 // row are added in a fixed order (8 per lane, then a butterfly over the row's lanes).  Rows are counted in 32 bits, for the divisions'
-// sake (backward pass of T 8192, 16 / 8 heads of 128, documents of 500: 164.9 -> 163.4 us); 2^31 of them would fill more than a GPU.
+// sake; 2^31 of them would fill more than a GPU.  Two blocks come and go for every one that is resident, which evens out the SMs: with
+// eight an SM that stay, the backward pass of packed T 8192, 16 / 8 heads of 128, takes 163.8 us instead of 161.9 (64-bit counts 164.9),
+// that of B 8, S 1024, 12 heads of 64, window 256, 75.3 instead of 72.8 (73.5).
 template <int D>
 __global__ void __launch_bounds__(256)
 attn_delta_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o, float* __restrict__ delta, int B, int S,
@@ -59,7 +61,7 @@ attn_delta_kernel(const bf16* __restrict__ o, const bf16* __restrict__ d_o, floa
 cudaError_t attention_delta(const bf16* o, const bf16* d_o, float* delta, int B, int S, int nh, int d, cudaStream_t st) {
   const long long rows = (long long)B * S * nh;
   const long long want = (rows * (d / 8) + 2 * 256 - 1) / (2 * 256);  // blocks if every thread took one load pair
-  const int blocks = (int)(want < 148 * 8 ? (want > 0 ? want : 1) : 148 * 8);
+  const int blocks = (int)(want < 148 * 16 ? (want > 0 ? want : 1) : 148 * 16);
   if (rows > (1ll << 31)) return cudaErrorInvalidValue;
   if (d == 64) return launch_pdl(attn_delta_kernel<64>, blocks, 256, 0, st, o, d_o, delta, B, S, nh);
   if (d == 128) return launch_pdl(attn_delta_kernel<128>, blocks, 256, 0, st, o, d_o, delta, B, S, nh);
