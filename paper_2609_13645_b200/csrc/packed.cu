@@ -16,7 +16,7 @@ packed_bounds_kernel(const int* __restrict__ cu, int n, int T, int longest, int*
   pdl_trigger();
   pdl_wait();
   const int t = (int)(blockIdx.x * 256 + threadIdx.x);
-  const int total = min(max(__ldg(cu + n), 0), T);
+  const int total = n > 0 ? min(max(__ldg(cu + n), 0), T) : 0;  // no documents: nobody's rows, whatever the one offset holds
   if (t < T) {
     int start = T, end = total, pos = 0;
     if (t < total) {
