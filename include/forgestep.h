@@ -342,8 +342,8 @@ ft_status ft_k_gemm_ws(const void* dev_A, int32_t a_mn, int64_t lda, const void*
 /* The single-kernel attention calls below keep their device status word inside the library (ft_k_gemm takes the
  * caller's dev_err instead).  ft_k_status waits for `stream`, then returns FT_ETIMEOUT if a bounded device-side wait ran
  * out in any ft_k_attention_* call (ft_k_attention_window_* and ft_k_attention_packed_* among them) on the current device since
- * the last ft_k_status (and clears the word), FT_EINVAL if ft_k_packed_bounds or ft_k_rotary met a value on the device that they
- * refuse, else FT_OK.
+ * the last ft_k_status (and clears the word), FT_EINVAL if ft_k_packed_bounds, ft_k_attention_packed_bwd or ft_k_rotary met a value on the device
+ * that they refuse, else FT_OK.
  * (Keeping host synchronisation out of the hot loop, Section "Sources of the Speedup", is why the calls themselves do not check.) */
 ft_status ft_k_status(void* stream);
 
@@ -470,7 +470,8 @@ ft_status ft_k_attention_packed_fwd(const void* dev_qkv, void* dev_o, float* dev
                                     int32_t n_kv_heads, int32_t head_dim, void* stream);
 
 /* Its backward, with the conventions of ft_k_attention_window_bwd.  longest: as given to ft_k_packed_bounds, or more; the scratch
- * depends on it.  dev_cos, dev_sin: fp32 [longest, d / 2] tables by which d_q and d_k are rotated back at their rows' positions, or NULL.
+ * depends on it, and a document of the bounds that has more rows is reported by ft_k_status as FT_EINVAL (the gradients are then
+ * unspecified, within their buffers).  dev_cos, dev_sin: fp32 [longest, d / 2] tables by which d_q and d_k are rotated back at their rows' positions, or NULL.
  * Rows of dev_dqkv behind the last document are left as they were. */
 size_t ft_k_attention_packed_scratch_bytes(int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t longest);
 ft_status ft_k_attention_packed_bwd(const void* dev_qkv, const void* dev_o, const void* dev_do, const float* dev_lse, void* dev_dqkv,

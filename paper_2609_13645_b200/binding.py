@@ -692,7 +692,7 @@ def k_attention_packed_fwd(qkv, o, lse, bounds, T, n_heads, n_kv, d):
 
 def k_attention_packed_bwd(qkv, o, d_o, lse, dqkv, bounds, scratch, T, n_heads, n_kv, d, longest=None, cos=None, sin=None):
     """Gradient of k_attention_packed_fwd; scratch: a uint8 tensor of attention_packed_scratch_bytes(...) bytes; longest: as given to
-    k_packed_bounds, or more; cos, sin: fp32 [longest or more, d / 2] tables by which d_q and d_k are rotated back at their rows'
+    k_packed_bounds, or more (a longer document in the bounds is reported by k_status); cos, sin: fp32 [longest or more, d / 2] tables by which d_q and d_k are rotated back at their rows'
     positions, or None.  Rows of dqkv behind the last document are left as they were."""
     torch = _torch or _import_torch()
     longest = T if longest is None else min(longest, T)
@@ -715,7 +715,7 @@ def k_attention_packed_bwd(qkv, o, d_o, lse, dqkv, bounds, scratch, T, n_heads, 
 
 def k_status():
     """Waits for the current stream and raises if a call since the last k_status met a wait that ran out (FT_ETIMEOUT) or a value on
-    the device that it refuses (FT_EINVAL): offsets of documents, positions."""
+    the device that it refuses (FT_EINVAL): offsets of documents, documents over the limit of a backward pass, positions."""
     st = lib().ft_k_status(_stream_ptr())
     if st != FT_OK:
         raise ForgeStepError(st, "a call on the device")

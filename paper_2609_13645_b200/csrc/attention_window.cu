@@ -739,6 +739,11 @@ attn_window_dkv_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(K_STFULL + ss));
     }
+    if (DOCS && local == 0 && part == 0) {
+      // a document of more rows than the plan has room for has lost pairs and rotations; looked for where nobody waits
+      for (int r = x0 + lane; r < min(x0 + 128, rows_end); r += 32)
+        if (__ldg(pl.docs.pos + r) >= pl.window) atomicCAS(err, (int)ERR_NONE, (int)ERR_BAD_INDEX);
+    }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
     // One queue in the order dV_j, S_{j+1}, dK_j, dP_{j+1}.  A score buffer is overwritten by the product issued behind its
