@@ -208,41 +208,41 @@ __device__ __forceinline__ uint32_t round_random(double a, uint32_t bits) {
 // A run's greatest element: fp32 bits (infinities and NaN are the greatest), and its scale.
 struct RunTop {
   uint32_t own, top;  // of the lane, with the element's number in place of the last 3 bits; of the run, without them
-  float g, code;      // the lane's element's gradient and old code
+  int lane;           // that holds it
+  bool rivals;        // there are others only a few roundings below, which may be it
   float scale;        // 0: the run is 0; infinite or NaN: so is the run
   __device__ __forceinline__ bool coded() const { return top >= 0x0d800000u && top < 0x7f800000u; }  // from 2^-100 on
-  __device__ __forceinline__ bool may_win() const { return own >= top - 64u; }                         // a few roundings below
 };
-__device__ __forceinline__ RunTop greatest(const float (&x)[8], const float (&g)[8], uint2 old) {
+__device__ __forceinline__ RunTop greatest(const float (&x)[8]) {
   RunTop t;
   uint32_t key[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) key[i] = (__float_as_uint(x[i]) & 0x7ffffff8u) | (uint32_t)i;
   t.own = max(max(max(key[0], key[1]), max(key[2], key[3])), max(max(key[4], key[5]), max(key[6], key[7])));
   t.top = __reduce_max_sync(0xffffffffu, t.own) & ~7u;
-  const bool b0 = t.own & 1u, b1 = t.own & 2u, b2 = t.own & 4u;
-  const float g01 = b0 ? g[1] : g[0], g23 = b0 ? g[3] : g[2], g45 = b0 ? g[5] : g[4], g67 = b0 ? g[7] : g[6];
-  t.g = b2 ? (b1 ? g67 : g45) : (b1 ? g23 : g01);
-  t.code = code_value(old, t.own & 7);
+  const bool may_win = t.own >= t.top - 64u;
+  const uint32_t who = __ballot_sync(0xffffffffu, may_win);
+  uint32_t second = 0;  // 2^32 less its distance to the lane's greatest
+#pragma unroll
+  for (int i = 0; i < 8; ++i) second = __viaddmax_u32(key[i], 0u - t.own, second);
+  t.lane = __ffs(who) - 1;
+  t.rivals = (who & (who - 1)) != 0 || __any_sync(0xffffffffu, may_win && second >= 0u - 72u);  // the 64, and the numbers in the last bits
   t.scale = t.top >= 0x7f800000u ? __uint_as_float(t.top) : 0.f;
   return t;
 }
-// The scale in 64 bits.
-template <bool ROOT>
-__device__ __noinline__ double run_unit(const RunTop& t, const StepArgs& a, float scale, float clip) {
-  double most = t.may_win() ? fabs(moment_64<ROOT>(a, t.code, scale, t.g, clip)) : 0.0;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
-  return __dmul_rn(most, 1.0 / 448.0);
+// The number of the lane's greatest, of 8.
+__device__ __forceinline__ float pick(const float (&g)[8], uint32_t number) {
+  const bool b0 = number & 1u, b1 = number & 2u, b2 = number & 4u;
+  const float g01 = b0 ? g[1] : g[0], g23 = b0 ? g[3] : g[2], g45 = b0 ? g[5] : g[4], g67 = b0 ? g[7] : g[6];
+  return b2 ? (b1 ? g67 : g45) : (b1 ? g23 : g01);
 }
-// The scales of both moments: the winners' values in two parts, m's on the lower lanes and the root of v's on the upper ones.  Where more
-// than one lane may hold the winner, or the scale lies half way between two fp32 numbers but for the last places of 64 bits (one
-// run in a thousand: the betas are decimal fractions, whose multiples of fp32 numbers land there), in 64 bits.
-__device__ __forceinline__ void run_scales(RunTop& m, RunTop& v, const StepArgs& a, float scale_m, float scale_v, float clip) {
-  const uint32_t who_m = __ballot_sync(0xffffffffu, m.may_win()), who_v = __ballot_sync(0xffffffffu, v.may_win());
-  const int lane_m = __ffs(who_m) - 1, lane_v = __ffs(who_v) - 1;
-  const float gm = __shfl_sync(0xffffffffu, m.g, lane_m), cm = __shfl_sync(0xffffffffu, m.code, lane_m);
-  const float gv = __shfl_sync(0xffffffffu, v.g, lane_v), cv = __shfl_sync(0xffffffffu, v.code, lane_v);
+// The scales of both moments: the winners' values in two parts, m's on the lower lanes and the root of v's on the upper ones.  Returns in
+// bits 0 and 16 whether they lie half way between two fp32 numbers but for the last places of 64 bits (one run in a thousand: the betas are
+// decimal fractions, whose multiples of fp32 numbers land there).
+__device__ __forceinline__ uint32_t run_scales(RunTop& m, RunTop& v, const StepArgs& a, uint2 old_m, uint2 old_v, float scale_m, float scale_v,
+                                               float clip, const float (&g)[8]) {
+  const float gm = __shfl_sync(0xffffffffu, pick(g, m.own), m.lane), cm = __shfl_sync(0xffffffffu, code_value(old_m, m.own & 7), m.lane);
+  const float gv = __shfl_sync(0xffffffffu, pick(g, v.own), v.lane), cv = __shfl_sync(0xffffffffu, code_value(old_v, v.own & 7), v.lane);
   const bool second = (threadIdx.x & 16u) != 0;
   Two kept = product(second ? cv : cm, second ? scale_v : scale_m);
   const Two d = product(second ? gv : gm, clip);
@@ -256,14 +256,20 @@ __device__ __forceinline__ void run_scales(RunTop& m, RunTop& v, const StepArgs&
   const float scale = __fadd_rn(x.h, x.l), half_step = __uint_as_float(__float_as_uint(scale) & 0x7f800000u) * 5.9604645e-8f;
   const uint32_t tie = __ballot_sync(0xffffffffu, fabsf(fabsf(__fadd_rn(__fsub_rn(x.h, scale), x.l)) - half_step) < half_step * 1e-3f);
   const float sm = fabsf(__shfl_sync(0xffffffffu, scale, 0)), sv = __shfl_sync(0xffffffffu, scale, 16);
-  if (m.coded()) m.scale = (who_m & (who_m - 1)) != 0 || (tie & 1u) != 0 ? (float)run_unit<false>(m, a, scale_m, clip) : sm;
-  if (v.coded()) v.scale = (who_v & (who_v - 1)) != 0 || (tie & 0x10000u) != 0 ? (float)run_unit<true>(v, a, scale_v, clip) : sv;
+  if (m.coded()) m.scale = sm;
+  if (v.coded()) v.scale = sv;
+  return tie;
 }
-// The codes of lanes in which fp32 leaves one open, formed in 64 bits.
+// The scale of a run and the codes of its open lanes in 64 bits; the greatest is looked for among the elements [from, to) of every lane.
+// x, y: the codes, z: the scale.
 template <bool ROOT, typename G>
-__device__ __noinline__ uint2 settle(uint2 codes, bool open, int n, const RunTop& t, const StepArgs& a, uint2 old, float scale, float clip, const G* grad,
+__device__ __noinline__ uint3 settle(uint2 codes, bool open, int n, int from, int to, const StepArgs& a, uint2 old, float scale, float clip, const G* grad,
                                      unsigned long long key, unsigned long long first) {
-  const double unit = run_unit<ROOT>(t, a, scale, clip);
+  double most = 0.0;
+  for (int i = from; i < to; ++i) most = fmax(most, fabs(moment_64<ROOT>(a, code_value(old, i), scale, (float)grad[i], clip)));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
+  const double unit = __dmul_rn(most, 1.0 / 448.0);
   for (int i = 0; i < (open ? n : 0); ++i) {
     const unsigned long long word = splitmix64(key ^ ((first + (unsigned long long)(i >> 1)) * kGroupKey));
     const uint32_t bits = (uint32_t)(word >> (32 * (i & 1) + (ROOT ? 16 : 0))) & 0xffffu;
@@ -273,7 +279,7 @@ __device__ __noinline__ uint2 settle(uint2 codes, bool open, int n, const RunTop
     if (!ROOT && e < 0.0) code |= 0x80u;
     put_code(codes, i, code);
   }
-  return codes;
+  return make_uint3(codes.x, codes.y, __float_as_uint((float)unit));
 }
 
 __device__ __forceinline__ float approx_root(float x) {
@@ -330,8 +336,8 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
     for (int i = 0; i < 8; ++i)
       if (i >= n) m[i] = r[i] = 0.f;
   }
-  RunTop tm = greatest(m, g, old_m), tv = greatest(r, g, old_v);
-  run_scales(tm, tv, a, scale_m, scale_v, clip);
+  RunTop tm = greatest(m), tv = greatest(r);
+  const uint32_t ties = run_scales(tm, tv, a, old_m, old_v, scale_m, scale_v, clip, g);
   const float less = 1.f - 4.76837158e-7f;
   const float inv_m = tm.coded() ? approx_inverse(tm.scale) * less : 0.f, inv_v = tv.coded() ? approx_inverse(tv.scale) * less : 0.f;
   const unsigned long long first = (unsigned long long)(w.base + at) / 2;
@@ -368,10 +374,20 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   auto top_bytes = [](const uint32_t* x) { return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410); };
   cm = make_uint2(top_bytes(sm), top_bytes(sm + 4));
   cv = make_uint2(top_bytes(sv), top_bytes(sv + 4));
+  // With rivals the scale is not known to a few roundings: the whole run in 64 bits.
+  auto settled = [&](auto root, RunTop& t, uint2 codes, bool tie, bool open, uint2 old, float scale) {
+    if (tie || t.rivals || __any_sync(0xffffffffu, open)) {
+      const int winner = t.own & 7, end = (int)(threadIdx.x & 31) == t.lane ? winner + 1 : 0;
+      const uint3 s = settle<decltype(root)::value, G>(codes, open || t.rivals, n, t.rivals ? 0 : winner, t.rivals ? n : end, a, old, scale, clip, gp, key, first);
+      codes = make_uint2(s.x, s.y);
+      t.scale = __uint_as_float(s.z);
+    }
+    return codes;
+  };
   if (!tm.coded()) cm = tm.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);  // all 1: what the scale is
-  else if (__any_sync(0xffffffffu, open_m)) cm = settle<false, G>(cm, open_m, n, tm, a, old_m, scale_m, clip, gp, key, first);
+  else cm = settled(std::false_type{}, tm, cm, (ties & 1u) != 0, open_m, old_m, scale_m);
   if (!tv.coded()) cv = tv.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);
-  else if (__any_sync(0xffffffffu, open_v)) cv = settle<true, G>(cv, open_v, n, tv, a, old_v, scale_v, clip, gp, key, first);
+  else cv = settled(std::true_type{}, tv, cv, (ties & 0x10000u) != 0, open_v, old_v, scale_v);
   store_codes(mp, n, vec, cm);
   store_codes(vp, n, vec, cv);
   __syncwarp();  // every lane has read the scales
