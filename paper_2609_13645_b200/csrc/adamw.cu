@@ -16,6 +16,7 @@
 // divide by epsilon alone.  The codes and scales are, bit for bit, those of this definition in 64 bits: fp32 decides where it can, and what it
 // leaves open is formed again in 64 bits.
 #include <cuda_fp8.h>
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -197,7 +198,7 @@ __device__ __forceinline__ double moment_64(const StepArgs& a, float code, float
 // them.  Here all that lies 4 places further up, so that the code ends at the top byte without y's sign, and `random` (16 bits, 8
 // places up) is added.
 __device__ __forceinline__ uint32_t with_random(float small, uint32_t random) { return __float_as_uint(small) * 16u + random; }
-// Whether what lies behind the code is within off / 2^20 steps of a border; off in the low 23 bits of its argument.
+// Whether what lies behind the code is within off / 2^20 steps of a border; off, under 2^19, in the low 23 bits of its argument.
 __device__ __forceinline__ bool at_border(uint32_t sum, uint32_t off) { return sum * 256u + off * 4096u <= off * 8192u; }
 __device__ __forceinline__ uint32_t round_random(double a, uint32_t bits) {
   const int e = a < 0.015625 ? 0 : (__double2hiint(a) >> 20) - 1023 + 6;  // binades above 2^-6
@@ -209,11 +210,12 @@ __device__ __forceinline__ uint32_t round_random(double a, uint32_t bits) {
 struct RunTop {
   uint32_t own, top;  // of the lane, with the element's number in place of the last 3 bits; of the run, without them
   int lane;           // that holds it
-  bool rivals;        // there are others only a few roundings below, which may be it
-  float scale;        // 0: the run is 0; infinite or NaN: so is the run
-  __device__ __forceinline__ bool coded() const { return top >= 0x0d800000u && top < 0x7f800000u; }  // from 2^-100 on
+  bool whole;         // the run is formed in 64 bits: others are only a few roundings below and may be it, or `terms` are far greater than it
+  float scale;        // 0: the run is 0
+  __device__ __forceinline__ bool coded() const { return top >= 0x0d800000u; }  // from 2^-100 on
 };
-__device__ __forceinline__ RunTop greatest(const float (&x)[8]) {
+// terms: the greatest magnitude of the lane's terms that the elements are sums of, if they may cancel.
+__device__ __forceinline__ RunTop greatest(const float (&x)[8], float terms) {
   RunTop t;
   uint32_t key[8];
 #pragma unroll
@@ -226,9 +228,18 @@ __device__ __forceinline__ RunTop greatest(const float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) second = __viaddmax_u32(key[i], 0u - t.own, second);
   t.lane = __ffs(who) - 1;
-  t.rivals = (who & (who - 1)) != 0 || __any_sync(0xffffffffu, may_win && second >= 0u - 72u);  // the 64, and the numbers in the last bits
-  t.scale = t.top >= 0x7f800000u ? __uint_as_float(t.top) : 0.f;
+  const bool near = may_win && second >= 0u - 72u;  // the 64, and the numbers in the last bits
+  t.whole = (who & (who - 1)) != 0 || __any_sync(0xffffffffu, near || terms > 4.f * __uint_as_float(t.top));
+  t.scale = 0.f;
   return t;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float magnitude(const float (&g)[8]) {
+  return max3(max3(fabsf(g[0]), fabsf(g[1]), fabsf(g[2])), max3(fabsf(g[3]), fabsf(g[4]), fabsf(g[5])), fmaxf(fabsf(g[6]), fabsf(g[7])));
 }
 // The number of the lane's greatest, of 8.
 __device__ __forceinline__ float pick(const float (&g)[8], uint32_t number) {
@@ -261,14 +272,22 @@ __device__ __forceinline__ uint32_t run_scales(RunTop& m, RunTop& v, const StepA
   return tie;
 }
 // The scale of a run and the codes of its open lanes in 64 bits; the greatest is looked for among the elements [from, to) of every lane.
-// x, y: the codes, z: the scale.
+// x, y: the codes, z: the scale.  A run that is not finite in fp32 has codes of 1, which are what the scale is.
 template <bool ROOT, typename G>
 __device__ __noinline__ uint3 settle(uint2 codes, bool open, int n, int from, int to, const StepArgs& a, uint2 old, float scale, float clip, const G* grad,
                                      unsigned long long key, unsigned long long first) {
   double most = 0.0;
-  for (int i = from; i < to; ++i) most = fmax(most, fabs(moment_64<ROOT>(a, code_value(old, i), scale, (float)grad[i], clip)));
+  bool nan = false;
+  for (int i = from; i < to; ++i) {
+    const double e = fabs(moment_64<ROOT>(a, code_value(old, i), scale, (float)grad[i], clip));
+    most = fmax(most, e);
+    nan |= !(e >= 0.0);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
+  nan = __any_sync(0xffffffffu, nan);
+  if (nan || most > FLT_MAX) return make_uint3(0x38383838u, 0x38383838u, nan ? 0x7fffffffu : 0x7f800000u);
+  if (most < 0x1p-100) return make_uint3(0u, 0u, 0u);
   const double unit = __dmul_rn(most, 1.0 / 448.0);
   for (int i = 0; i < (open ? n : 0); ++i) {
     const unsigned long long word = splitmix64(key ^ ((first + (unsigned long long)(i >> 1)) * kGroupKey));
@@ -309,6 +328,7 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   const uint2 old_m = load_codes(mp, n, vec), old_v = load_codes(vp, n, vec);
   const float scale_m = w.ms[at / kRun], scale_v = w.vs[at / kRun];
   load8(gp, n, vec, g);
+  const float grad_top = magnitude(g);
   decode(old_m, scale_m, m);
   decode(old_v, scale_v, r);
   {
@@ -336,16 +356,20 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
     for (int i = 0; i < 8; ++i)
       if (i >= n) m[i] = r[i] = 0.f;
   }
-  RunTop tm = greatest(m), tv = greatest(r);
+  // m's terms may cancel.  Up to gradients' terms of 4 times the greatest element, an element's fp32 error, of up to 3 roundings of its own and 5
+  // of the gradient's term, stays under 23 of the greatest's, and two elements that may be the greatest are within 64 last places.
+  RunTop tm = greatest(m, c.omb1 * fabsf(clip) * grad_top), tv = greatest(r, 0.f);
+  tm.whole = tm.whole || tm.top - 0x0d000000u < 0x01000000u || tm.top >= 0x7f000000u;  // next to 2^-100, and at fp32's end
+  tv.whole = tv.whole || tv.top >= 0x7f800000u;
   const uint32_t ties = run_scales(tm, tv, a, old_m, old_v, scale_m, scale_v, clip, g);
-  const float less = 1.f - 4.76837158e-7f;
-  const float inv_m = tm.coded() ? approx_inverse(tm.scale) * less : 0.f, inv_v = tv.coded() ? approx_inverse(tv.scale) * less : 0.f;
+  const float inv_m = tm.coded() ? approx_inverse(tm.scale) : 0.f, inv_v = tv.coded() ? approx_inverse(tv.scale) : 0.f;
   const unsigned long long first = (unsigned long long)(w.base + at) / 2;
   uint2 cm, cv;
   bool open_m = false, open_v = false;
-  // An element's fp32 error in 2^-20 steps, which are the last places of what the floor is taken of: under 8 for its own roundings (6 at
-  // most in the element, 2 in the inverse), 4 more that the inverse is made smaller by (the greatest element stays under 448), and 1.5 of
-  // the terms' that it was added up from, |beta1 m| <= |sum| + |gradient's|.
+  // An element's fp32 error in 2^-20 steps, which are the last places of what the floor is taken of (a rounding is up to one of them, in the
+  // upper half of a binade): under 14 for the roundings of the element (5 at most), the scale (1), its inverse (4) and the product (1), and 2.5
+  // of the terms' that it was added up from, |beta1 m| <= |sum| + |gradient's|.  The latter are at most 4 * 448 / 2^-6 in codes that are kept,
+  // which is under half a step, what at_border() holds.
   const float grads = 4.f * c.omb1 * fabsf(clip) * inv_m;
   const uint32_t off_v = 14u;
   uint32_t sm[8], sv[8];
@@ -361,7 +385,7 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
       const float y = k == 0 ? ym.x : ym.y;
       // 2^-e of the binade that the number, or 2^-6 where that is more, lies in; the sum's low bits are the number of places
       const float binade = __uint_as_float(0x7f000000u - (__float_as_uint(fmaxf(fabsf(y), 0.015625f)) & 0x7f800000u));
-      const float places = fmaf(fminf((k == 0 ? t.x : t.y) * binade, 262144.f), 1.f, 8388608.f + 14.f);
+      const float places = fmaf(k == 0 ? t.x : t.y, binade, 8388608.f + 14.f);
       sm[i + k] = with_random(k == 0 ? fm.x : fm.y, __byte_perm(bits, 0u, 0x4104));
       open_m |= at_border(sm[i + k], __float_as_uint(places));
       sm[i + k] = (sm[i + k] & 0x7fffffffu) | (__float_as_uint(m[i + k]) & 0x80000000u);
@@ -374,19 +398,18 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   auto top_bytes = [](const uint32_t* x) { return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410); };
   cm = make_uint2(top_bytes(sm), top_bytes(sm + 4));
   cv = make_uint2(top_bytes(sv), top_bytes(sv + 4));
-  // With rivals the scale is not known to a few roundings: the whole run in 64 bits.
   auto settled = [&](auto root, RunTop& t, uint2 codes, bool tie, bool open, uint2 old, float scale) {
-    if (tie || t.rivals || __any_sync(0xffffffffu, open)) {
+    if (tie || t.whole || __any_sync(0xffffffffu, open)) {
       const int winner = t.own & 7, end = (int)(threadIdx.x & 31) == t.lane ? winner + 1 : 0;
-      const uint3 s = settle<decltype(root)::value, G>(codes, open || t.rivals, n, t.rivals ? 0 : winner, t.rivals ? n : end, a, old, scale, clip, gp, key, first);
+      const uint3 s = settle<decltype(root)::value, G>(codes, open || t.whole, n, t.whole ? 0 : winner, t.whole ? n : end, a, old, scale, clip, gp, key, first);
       codes = make_uint2(s.x, s.y);
       t.scale = __uint_as_float(s.z);
     }
     return codes;
   };
-  if (!tm.coded()) cm = tm.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);  // all 1: what the scale is
+  if (!tm.coded() && !tm.whole) cm = make_uint2(0u, 0u);
   else cm = settled(std::false_type{}, tm, cm, (ties & 1u) != 0, open_m, old_m, scale_m);
-  if (!tv.coded()) cv = tv.scale == 0.f ? make_uint2(0u, 0u) : make_uint2(0x38383838u, 0x38383838u);
+  if (!tv.coded() && !tv.whole) cv = make_uint2(0u, 0u);
   else cv = settled(std::true_type{}, tv, cv, (ties & 0x10000u) != 0, open_v, old_v, scale_v);
   store_codes(mp, n, vec, cm);
   store_codes(vp, n, vec, cv);

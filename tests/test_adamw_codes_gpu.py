@@ -1,5 +1,5 @@
 """AdamW with moments in 8 bits where the definition's codes and scales are hard to reach in fp32: runs with several elements that may be
-the greatest.
+the greatest, moments whose terms cancel.
 
 Codes and scales are those of the definition in 64 bits, bit for bit.  The parameter: an fp32 first moment is off by up to 8 roundings
 (2^-24 each) of the magnitudes of its terms T = beta1 |m| + (1 - beta1) |g|; the update by 17 of its own: 3 in m times its correction, 8 in the
@@ -98,3 +98,50 @@ def test_elements_that_may_each_be_the_greatest(beta1, beta2, apart, grad):
     for count in (4, 5):
         old, new = step(t, beta1, beta2, 1e-8, count, 3)
         check(old, new, beta1, beta2, 1e-8, count, 3)
+
+
+def cancelling(n, beta1, places, seed, alone, m_scale=0.37 / 448):
+    """Codes of m and gradients a few last places (`places`, at most) from those that cancel them.  alone: every run has one such element
+    and nothing else."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    m = torch.randint(0, 127, (n,), generator=g, device="cuda") + 128 * torch.randint(0, 2, (n,), generator=g, device="cuda")
+    v = torch.randint(0, 127, (n,), generator=g, device="cuda")
+    if alone:
+        keep = torch.arange(n, device="cuda") % 256 == (torch.arange(n, device="cuda") // 256 * 37) % 256
+        m, v = torch.where(keep, m, 0), torch.where(keep, v, 0)
+    ms = torch.rand(-(-n // 256), generator=g, device="cuda") * m_scale + m_scale / 4
+    m = m.to(torch.uint8).view(torch.float8_e4m3fn)
+    grad = (-(beta1 / (1 - beta1)) * unpack(m, ms)).float()
+    off = torch.randint(-places, places + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+    grad = torch.where(grad != 0, (grad.view(torch.int32) + off).view(torch.float32), grad)
+    return m, ms, v.to(torch.uint8).view(torch.float8_e4m3fn), ms.clone(), grad
+
+
+@pytest.mark.parametrize("beta1,beta2", BETAS)
+@pytest.mark.parametrize("places", [0, 3, 40, 600, 100000])
+@pytest.mark.parametrize("alone", [False, True])
+def test_moments_whose_terms_cancel(beta1, beta2, places, alone):
+    """First moments next to 0 by cancellation, the greatest of their runs among them: no NaN codes, and the definition's."""
+    n = 256 * 400
+    t = tensors(*cancelling(n, beta1, places, places + 1, alone))
+    old, new = step(t, beta1, beta2, 1e-8, 7, 11)
+    assert ((new["m"][0].view(torch.uint8) & 127) < 127).all()
+    check(old, new, beta1, beta2, 1e-8, 7, 11)
+    for count in (8, 9):  # and what they leave behind, under other gradients
+        t["g"][0].mul_(-1e-3)
+        old, new = step(t, beta1, beta2, 1e-8, count, 11)
+        check(old, new, beta1, beta2, 1e-8, count, 11)
+
+
+def test_single_elements_whose_terms_cancel():
+    """Tensors of one element: the greatest of its run is the one that cancels."""
+    m, ms, v, vs, g = cancelling(256 * 300, 0.9, 600, 5, True)
+    keep = (torch.arange(256 * 300, device="cuda") % 256 == (torch.arange(256 * 300, device="cuda") // 256 * 37) % 256).nonzero().view(-1)
+    part = lambda x: [x[i:i + 1].clone() for i in keep.tolist()]  # noqa: E731
+    t = dict(p=[torch.ones(1, device="cuda") for _ in keep], g=part(g), m=part(m.view(torch.uint8)), v=part(v.view(torch.uint8)),
+             ms=[x.clone() for x in ms.split(1)], vs=[x.clone() for x in vs.split(1)])
+    t["m"], t["v"] = ([x.view(torch.float8_e4m3fn) for x in t[name]] for name in "mv")
+    for count in (3, 4):
+        old, new = step(t, 0.9, 0.95, 1e-8, count, 2)
+        assert all(torch.isfinite(x).all() for x in new["p"])
+        check(old, new, 0.9, 0.95, 1e-8, count, 2)
