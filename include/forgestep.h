@@ -505,7 +505,9 @@ ft_status ft_k_rotary_tables(float* dev_cos, float* dev_sin, const float* dev_fa
  * counter-based generator, and a v that is not 0 keeps at least 2^-9 scale.  r: with mix, C2 and C3 of ft_k_dropout_add and
  * key = mix(mix(seed) ^ step C2), elements 2 k and 2 k + 1 take the 16-bit parts (lowest first) of mix(key ^ k C3) for m, v, m, v; elements
  * are counted through the list, each tensor rounded up to 256.  Scales and codes are those
- * of these formulas in 64 bits, bit for bit.  A non-finite element makes its run non-finite.
+ * of these formulas in 64 bits, bit for bit, but that a root of v below 2^-79 (1.7e-24) may count as 0.  An element that is not finite in fp32
+ * makes its run non-finite.  With 8 bits eps is at least 2^-64 (5.4e-20), *dev_grad_scale is 0 or 2^-64 to 2^16 in magnitude, and where a scaled
+ * gradient or a root of v passes 2^47 (1.4e14) the parameter is unspecified.
  *   ft_k_adamw_plan_bytes   bytes of a plan (0: the list is refused: a null or misaligned buffer, buffers that overlap).
  *   ft_k_adamw_plan         writes the plan to HOST memory (8-byte aligned); the caller copies it to the device, 16-byte
  *                           aligned, and keeps both while steps run.  It holds the tensors' addresses; numel 0 is passed over.

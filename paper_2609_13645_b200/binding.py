@@ -813,7 +813,7 @@ class AdamWPlan:
 def k_adamw(plan, lr, beta1, beta2, eps, step, lr_tensor=None, grad_scale=None, seed=0):
     """One AdamW step over the tensors of an AdamWPlan.  step: int64 tensor of one element, the number of this step, from 1 on;
     lr_tensor and grad_scale: fp32 tensors of one element (None: lr, 1); all three are read when the kernel runs.  seed: of the
-    roundings of moments in 8 bits."""
+    roundings of moments in 8 bits, with which eps is at least 2^-64."""
     torch = _torch or _import_torch()
     dev = _current_device(step)
     if plan.device_index != dev:

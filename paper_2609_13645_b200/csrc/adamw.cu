@@ -33,6 +33,9 @@ namespace fs {
 namespace {
 
 constexpr int kChunk = 2048, kThreads = 256, kRun = 256;
+// Second moments in 8 bits are worked on in roots times 2^16: fp32 holds the squares of roots from 2^-79 to 2^48.  (Roots outside formed in 64 bits
+// too: 4 % more instructions, 579 -> 614 us.)
+constexpr float kUp = 65536.f, kDown = 1.f / 65536.f;
 constexpr uint32_t kMagic = 0x41445750u;
 constexpr unsigned long long kStepKey = 0xA24BAED4963EE407ull, kGroupKey = 0x8CB92BA72F3D8DD7ull;
 
@@ -251,12 +254,12 @@ __device__ __forceinline__ float pick(const float (&g)[8], uint32_t number) {
 // bits 0 and 16 whether they lie half way between two fp32 numbers but for the last places of 64 bits (one run in a thousand: the betas are
 // decimal fractions, whose multiples of fp32 numbers land there).
 __device__ __forceinline__ uint32_t run_scales(RunTop& m, RunTop& v, const StepArgs& a, uint2 old_m, uint2 old_v, float scale_m, float scale_v,
-                                               float clip, const float (&g)[8]) {
+                                               float clip_up, const float (&g)[8]) {
   const float gm = __shfl_sync(0xffffffffu, pick(g, m.own), m.lane), cm = __shfl_sync(0xffffffffu, code_value(old_m, m.own & 7), m.lane);
   const float gv = __shfl_sync(0xffffffffu, pick(g, v.own), v.lane), cv = __shfl_sync(0xffffffffu, code_value(old_v, v.own & 7), v.lane);
   const bool second = (threadIdx.x & 16u) != 0;
   Two kept = product(second ? cv : cm, second ? scale_v : scale_m);
-  const Two d = product(second ? gv : gm, clip);
+  const Two d = product(second ? gv : gm, second ? clip_up : clip_up * kDown);
   Two grown = product(second ? Two{a.o2[0], a.o2[1]} : Two{a.o1[0], a.o1[1]}, d);
   const Two square = product(kept, kept), twice = product(grown, d);
   if (second) { kept = square; grown = twice; }
@@ -316,9 +319,10 @@ __device__ __forceinline__ float approx_inverse(float x) {
 // with 67 % of all issue slots) matter most: codes are shifted and added by multiplications, and pairs of fp32 numbers share an
 // instruction.  Of 134M parameters' 557 us, the random bits take about 110, the scales in two parts 60, codes settled in 64
 // bits 30; the bytes would take 334.
+// c.omb1 / 2^16; clip_up, root_down: the scale of the gradients times 2^16 and the root of v's correction over it.
 template <bool PARAM16, bool GRAD16>
-__device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, bool vec, const StepArgs& a, const AdamCoef& c, float clip,
-                                      float root_rbc2, unsigned long long key) {
+__device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, bool vec, const StepArgs& a, const AdamCoef& c, float clip_up,
+                                      float root_down, unsigned long long key) {
   typedef typename std::conditional<PARAM16, bf16, float>::type P;
   typedef typename std::conditional<GRAD16, bf16, float>::type G;
   P* pp = reinterpret_cast<P*>(w.p) + at;
@@ -330,18 +334,18 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   load8(gp, n, vec, g);
   const float grad_top = magnitude(g);
   decode(old_m, scale_m, m);
-  decode(old_v, scale_v, r);
+  decode(old_v, scale_v * kUp, r);
   {
     float p[8];
     load8(pp, n, vec, p);
     const float wd = w.wd;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float2 d = mul2(make_float2(g[i], g[i + 1]), both(clip)), r0 = make_float2(r[i], r[i + 1]), p0 = make_float2(p[i], p[i + 1]);
+      const float2 d = mul2(make_float2(g[i], g[i + 1]), both(clip_up)), r0 = make_float2(r[i], r[i + 1]), p0 = make_float2(p[i], p[i + 1]);
       const float2 m1 = fma2(both(c.beta1), make_float2(m[i], m[i + 1]), mul2(both(c.omb1), d));
       const float2 v1 = fma2(both(c.beta2), mul2(r0, r0), mul2(mul2(both(c.omb2), d), d));
       const float2 r1 = make_float2(approx_root(v1.x), approx_root(v1.y));
-      const float2 den = fma2(r1, both(root_rbc2), both(c.eps));
+      const float2 den = fma2(r1, both(root_down), both(c.eps));
       const float2 quot = mul2(mul2(m1, both(c.rbc1)), make_float2(approx_inverse(den.x), approx_inverse(den.y)));  // within 2^-21
       const float2 p1 = fma2(both(-c.lr), fma2(both(wd), p0, quot), p0);
       m[i] = m1.x; m[i + 1] = m1.y;
@@ -358,10 +362,12 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   }
   // m's terms may cancel.  Up to gradients' terms of 4 times the greatest element, an element's fp32 error, of up to 3 roundings of its own and 5
   // of the gradient's term, stays under 23 of the greatest's, and two elements that may be the greatest are within 64 last places.
-  RunTop tm = greatest(m, c.omb1 * fabsf(clip) * grad_top), tv = greatest(r, 0.f);
+  RunTop tm = greatest(m, c.omb1 * fabsf(clip_up) * grad_top), tv = greatest(r, 0.f);
   tm.whole = tm.whole || tm.top - 0x0d000000u < 0x01000000u || tm.top >= 0x7f000000u;  // next to 2^-100, and at fp32's end
-  tv.whole = tv.whole || tv.top >= 0x7f800000u;
-  const uint32_t ties = run_scales(tm, tv, a, old_m, old_v, scale_m, scale_v, clip, g);
+  // v: but for roots from 2^-61 to 2^46, the low parts of whose squares are normal numbers
+  if (tv.top - 0x29000000u >= 0x5e800000u - 0x29000000u)
+    tv.whole = tv.top != 0u || __any_sync(0xffffffffu, grad_top != 0.f || (scale_v != 0.f && ((old_v.x | old_v.y) & 0x7f7f7f7fu) != 0u));
+  const uint32_t ties = run_scales(tm, tv, a, old_m, old_v, scale_m, scale_v * kUp, clip_up, g);
   const float inv_m = tm.coded() ? approx_inverse(tm.scale) : 0.f, inv_v = tv.coded() ? approx_inverse(tv.scale) : 0.f;
   const unsigned long long first = (unsigned long long)(w.base + at) / 2;
   uint2 cm, cv;
@@ -370,7 +376,7 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   // upper half of a binade): under 14 for the roundings of the element (5 at most), the scale (1), its inverse (4) and the product (1), and 2.5
   // of the terms' that it was added up from, |beta1 m| <= |sum| + |gradient's|.  The latter are at most 4 * 448 / 2^-6 in codes that are kept,
   // which is under half a step, what at_border() holds.
-  const float grads = 4.f * c.omb1 * fabsf(clip) * inv_m;
+  const float grads = 4.f * c.omb1 * fabsf(clip_up) * inv_m;
   const uint32_t off_v = 14u;
   uint32_t sm[8], sv[8];
 #pragma unroll
@@ -398,25 +404,26 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   auto top_bytes = [](const uint32_t* x) { return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410); };
   cm = make_uint2(top_bytes(sm), top_bytes(sm + 4));
   cv = make_uint2(top_bytes(sv), top_bytes(sv + 4));
-  auto settled = [&](auto root, RunTop& t, uint2 codes, bool tie, bool open, uint2 old, float scale) {
+  auto settled = [&](auto root, const RunTop& t, float& stored, uint2 codes, bool tie, bool open, uint2 old, float scale) {
     if (tie || t.whole || __any_sync(0xffffffffu, open)) {
       const int winner = t.own & 7, end = (int)(threadIdx.x & 31) == t.lane ? winner + 1 : 0;
-      const uint3 s = settle<decltype(root)::value, G>(codes, open || t.whole, n, t.whole ? 0 : winner, t.whole ? n : end, a, old, scale, clip, gp, key, first);
+      const uint3 s = settle<decltype(root)::value, G>(codes, open || t.whole, n, t.whole ? 0 : winner, t.whole ? n : end, a, old, scale, clip_up * kDown, gp, key, first);
       codes = make_uint2(s.x, s.y);
-      t.scale = __uint_as_float(s.z);
+      stored = __uint_as_float(s.z);
     }
     return codes;
   };
+  float new_m = tm.scale, new_v = tv.scale * kDown;
   if (!tm.coded() && !tm.whole) cm = make_uint2(0u, 0u);
-  else cm = settled(std::false_type{}, tm, cm, (ties & 1u) != 0, open_m, old_m, scale_m);
-  if (!tv.coded() && !tv.whole) cv = make_uint2(0u, 0u);
-  else cv = settled(std::true_type{}, tv, cv, (ties & 0x10000u) != 0, open_v, old_v, scale_v);
+  else cm = settled(std::false_type{}, tm, new_m, cm, (ties & 1u) != 0, open_m, old_m, scale_m);
+  if (tv.top == 0u && !tv.whole) cv = make_uint2(0u, 0u);
+  else cv = settled(std::true_type{}, tv, new_v, cv, (ties & 0x10000u) != 0, open_v, old_v, scale_v);
   store_codes(mp, n, vec, cm);
   store_codes(vp, n, vec, cv);
   __syncwarp();  // every lane has read the scales
   if ((threadIdx.x & 31) == 0) {
-    w.ms[at / kRun] = tm.scale;
-    w.vs[at / kRun] = tv.scale;
+    w.ms[at / kRun] = new_m;
+    w.vs[at / kRun] = new_v;
   }
 }
 
@@ -450,9 +457,14 @@ adamw_kernel(const uint8_t* __restrict__ plan, int n_chunks, unsigned long long 
   AdamCoef c = make_adam_coef(a.dev_lr != nullptr ? __ldg(a.dev_lr) : a.lr, (float)a.beta1, (float)a.beta2, a.eps, s_bc[0], s_bc[1]);
   c.omb1 = (float)a.omb1;
   c.omb2 = (float)a.omb2;
-  const float clip = a.grad_scale != nullptr ? __ldg(a.grad_scale) : 1.f;
+  float clip = a.grad_scale != nullptr ? __ldg(a.grad_scale) : 1.f;
   const unsigned long long key = BITS == 8 ? splitmix64(splitmix64(a.seed) ^ ((unsigned long long)t * kStepKey)) : 0;
-  const float root_rbc2 = sqrtf(c.rbc2);
+  float root_rbc2 = sqrtf(c.rbc2);
+  if (BITS == 8) {
+    c.omb1 *= kDown;
+    clip *= kUp;
+    root_rbc2 *= kDown;
+  }
   const PlanTensor* tensors = reinterpret_cast<const PlanTensor*>(plan + sizeof(PlanHeader));
   const PlanChunk* chunks = reinterpret_cast<const PlanChunk*>(plan + chunk_offset);
   for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
@@ -601,6 +613,7 @@ extern "C" ft_status ft_k_adamw(const void* host_plan, const void* dev_plan, uin
   if (!isfinite((float)lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !isfinite((float)eps)) return FT_EINVAL;
   const fs::PlanHeader& h = *reinterpret_cast<const fs::PlanHeader*>(host_plan);
   if (plan_bytes < sizeof(h) || h.magic != fs::kMagic || h.bytes != plan_bytes) return FT_EINVAL;
+  if (h.bits == 8 && eps < 0x1p-64) return FT_EINVAL;  // next to which roots that fp32 does not hold are nothing
   if (h.n_chunks == 0) return FT_OK;
   auto low = [](double v) { return (float)(v - (double)(float)v); };
   const double omb1 = 1.0 - beta1, omb2 = 1.0 - beta2;
