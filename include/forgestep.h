@@ -492,7 +492,8 @@ ft_status ft_k_rotary(const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy, 
 
 /* Tables for it and for the attention's backward passes: cos and sin, times mscale, of p * theta^(-2 i / rot) / dev_factors[i] for
  * p < n_positions and i < rot / 2 (dev_factors fp32, NULL: 1).  With factors and mscale this is the form of ft_set_rope_scaling, which
- * linear, frequency-wise and LongRoPE stretching of the context share.  Angles are formed in 64 bits. */
+ * linear, frequency-wise and LongRoPE stretching of the context share.  Angles are as exact as products in 64-bit floating point; entries
+ * are within two last places of fp32 (the model's own tables: within one rounding), and NaN where a factor is 0 or NaN. */
 ft_status ft_k_rotary_tables(float* dev_cos, float* dev_sin, const float* dev_factors, int32_t n_positions, int32_t rot, float theta,
                              float mscale, void* stream);
 

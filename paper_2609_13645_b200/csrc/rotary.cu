@@ -144,8 +144,9 @@ rotary_kernel(const T* x, T* y, const int* __restrict__ positions, const float* 
 }
 
 // Tables of position p and frequency i: angle = p theta^(-2 i / rot) / factor_i, cos and sin times mscale.  A position's step is kept as
-// a 64-bit fraction of a turn, of which p times is taken modulo one turn by integer products: far positions lose nothing (2^-64 turns a
-// position), and what is left goes through the fp32 functions of pi x.  A thread keeps its frequency and walks over positions.
+// a 64-bit fraction of a turn, of which p times is taken modulo one turn by integer products: far positions lose no more than the step's own
+// rounding to 53 bits.  The fp32 functions of pi x take the fraction's first 24 bits, and what is left, under 2^-24 of a turn, turns their
+// result by its angle.  A thread keeps its frequency and walks over positions.
 __global__ void __launch_bounds__(256)
 rotary_tables_kernel(float* __restrict__ cos, float* __restrict__ sin, const float* __restrict__ factors, int n_pos, int half,
                      double log2_step, float mscale) {
@@ -163,14 +164,18 @@ rotary_tables_kernel(float* __restrict__ cos, float* __restrict__ sin, const flo
   if (mine >= rows) return;
   for (int i = (int)threadIdx.x - mine * half; i < half; i += 256) {
     const unsigned long long step = steps[i];
+    const float factor = factors != nullptr ? __ldg(factors + i) : 1.f;
+    const float scale = factor == factor && factor != 0.f ? mscale : NAN;  // no angle
     const int by = (int)gridDim.x * rows;
 #pragma unroll 4
     for (int p = (int)blockIdx.x * rows + mine; p < n_pos; p += by) {
-      const int frac = (int)((step * (unsigned long long)p + 0x80000000ull) >> 32);  // of a turn, in [-1/2, 1/2)
+      const unsigned long long turn = step * (unsigned long long)p;
+      const int lead = (int)(turn >> 32) >> 8;  // 2^-24 turns, in [-1/2, 1/2) of one
       float s, c;
-      sincospif((float)frac * 4.656612873077393e-10f, &s, &c);
-      cos[(long long)p * half + i] = c * mscale;
-      sin[(long long)p * half + i] = s * mscale;
+      sincospif((float)lead * 1.1920928955078125e-7f, &s, &c);
+      const float angle = (float)(uint32_t)(turn >> 8) * 8.719671245021579e-17f;  // 2 pi / 2^56
+      cos[(long long)p * half + i] = fmaf(-s, angle, c) * scale;
+      sin[(long long)p * half + i] = fmaf(c, angle, s) * scale;
       if (p > n_pos - by) break;  // p + by may not fit
     }
   }
