@@ -364,7 +364,7 @@ attn_packed_fwd_kernel(const __grid_constant__ CUtensorMap tm_qkv, const __grid_
       const int row = q0 + q * 32 + lane, wmin = q0 + q * 32;
       int own = T;  // first row of this row's document
       if (row < rows_end) own = min(max(__ldg(docs.start + row), 0), row);
-      const int own_min = __shfl_sync(0xffffffffu, own, 0), own_max = __shfl_sync(0xffffffffu, own, 31);
+      const int own_max = __shfl_sync(0xffffffffu, own, 31);
       // The row reference is an integer in the log2 domain: any such reference gives the same softmax, and bf16 rounding commutes with
       // powers of two.  It moves only if a block's maximum turns out more than 2^kRefSlack above it (or, for a row that has seen nothing, far
       // below it).
