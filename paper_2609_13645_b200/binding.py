@@ -807,6 +807,7 @@ class AdamWPlan:
         self.bytes = size
         self.device = torch.from_numpy(self.host.view(np.uint8)).to(params[0].device)
         self._host_address, self._device_address = self.host.ctypes.data, self.device.data_ptr()
+        self._streams = {_stream_of(self.device_index)}  # those that torch's allocator knows to use the device's copy
         self.tensors = lists
 
 
@@ -818,10 +819,14 @@ def k_adamw(plan, lr, beta1, beta2, eps, step, lr_tensor=None, grad_scale=None, 
     dev = _current_device(step)
     if plan.device_index != dev:
         _refuse(f"a plan of cuda:{plan.device_index}, current device cuda:{dev}")
+    stream = _stream_of(dev)
+    if stream not in plan._streams:  # a plan that is dropped while a step runs there keeps its memory until the step is through
+        plan.device.record_stream(torch.cuda.current_stream(dev))
+        plan._streams.add(stream)
     st = lib().ft_k_adamw(plan._host_address, plan._device_address, plan.bytes, lr, beta1, beta2, eps,
                           _check_flat("step", step, torch.int64, 1, dev),
                           _check_flat("lr_tensor", lr_tensor, torch.float32, 1, dev) if lr_tensor is not None else None,
                           _check_flat("grad_scale", grad_scale, torch.float32, 1, dev) if grad_scale is not None else None,
-                          seed & 0xFFFFFFFFFFFFFFFF, _stream_of(dev))
+                          seed & 0xFFFFFFFFFFFFFFFF, stream)
     if st != FT_OK:
         raise ForgeStepError(st, "ft_k_adamw")
