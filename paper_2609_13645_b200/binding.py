@@ -776,6 +776,8 @@ class AdamWPlan:
         if n == 0 or any(len(t) != n for t in lists if t is not None) or len(decay) != n:
             _refuse("params, grads, m, v, weight_decay, scales and copies: lists of one length")
         params, grads, m, v, m_scales, v_scales, copies = lists
+        if any(t is None for of in (params, grads, m, v) for t in of):
+            _refuse("params, grads, m and v: a tensor is missing")
         pt, gt, mt = params[0].dtype, grads[0].dtype, m[0].dtype
         param_dtype, grad_dtype = _row_dtype(params[0]), _row_dtype(grads[0])
         if mt not in (torch.float32, torch.float8_e4m3fn):
