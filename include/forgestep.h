@@ -465,7 +465,9 @@ ft_status ft_k_packed_bounds(const int32_t* dev_offsets, int32_t n_docs, int32_t
  * and alignments as in ft_k_attention_window_fwd with B = 1 and S = T: qkv bf16 [T, (n_h + 2 n_kv) * d], o bf16 [T, n_h * d], lse fp32
  * [n_h, T].  Rows behind the last document may hold anything, and are left as they were in dev_o and dev_lse.  Elements of rows
  * inside documents have to be finite: a masked pair's weight is 0, but its product is formed, so an infinity or NaN can reach
- * other rows, of a neighbouring document too, that share a tile of 128 rows with it. */
+ * other rows, of a neighbouring document too, that share a tile of 128 rows with it.  Weights are rounded to bf16 before they multiply v, and
+ * so is dS before it multiplies q and k, as in the calls above: o and the gradients are within about 2.4e-3 of their definition in the
+ * 2-norm, of which 1.7e-3 are their own rounding.  Scores are limited as there. */
 ft_status ft_k_attention_packed_fwd(const void* dev_qkv, void* dev_o, float* dev_lse, const int32_t* dev_bounds, int32_t T, int32_t n_heads,
                                     int32_t n_kv_heads, int32_t head_dim, void* stream);
 

@@ -766,7 +766,7 @@ class AdamWPlan:
     bf16 or all fp32), first and second moments (all fp32, or all torch.float8_e4m3fn: m and the square root of v over the scales
     m_scales, v_scales, fp32, one for every 256 elements begun), weight_decay (a number or a list), copies (bf16, or None).  All
     contiguous and on one device.  The plan keeps them alive and steps through their memory as it is now: give gradients that
-    stay where they are."""
+    stay where they are (zeroed, not set to None), for a plan takes 4 us a tensor to make and waits for the GPU's copy."""
 
     def __init__(self, params, grads, m, v, weight_decay=0.0, m_scales=None, v_scales=None, copies=None):
         torch = _torch or _import_torch()

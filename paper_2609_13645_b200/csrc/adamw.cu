@@ -315,9 +315,9 @@ __device__ __forceinline__ float approx_inverse(float x) {
   return r;
 }
 
-// 8 elements a thread, a run a warp.  Bound by instructions: 835 a run (104 an element), of which those of the integer unit (58 % busy,
-// with 67 % of all issue slots) matter most: codes are shifted and added by multiplications, and pairs of fp32 numbers share an
-// instruction.  Of 134M parameters' 557 us, the random bits take about 110, the scales in two parts 60, codes settled in 64
+// 8 elements a thread, a run a warp.  Bound by instructions: 830 a run (104 an element), of which those of the integer unit (396; 68 % of all
+// issue slots are taken) matter most: codes are shifted and added by multiplications, and pairs of fp32 numbers share an
+// instruction.  Of 134M parameters' 571 us, the random bits take about 110, the scales in two parts 60, codes settled in 64
 // bits 30; the bytes would take 334.
 // c.omb1 / 2^16; clip_up, root_down: the scale of the gradients times 2^16 and the root of v's correction over it.
 template <bool PARAM16, bool GRAD16>

@@ -18,10 +18,10 @@
 // The grid has a CTA a work item, the longest first; a CTA that has issued all loads of its item takes over the next one that has
 // not started (clusterlaunchcontrol), so that the next item's loads go on while the last one ends, and items of any length even out.
 //
-// T 16384, 4 documents of up to 5622 rows, 16 / 8 heads of 128: 284 us, 1106 TFLOP/s of visible pairs; the tensor pipe and the exponential
-// unit are 60 % busy.  What bounds it is each tile's chain of about 3600 cycles a block: scores to registers 200, maxima 200,
+// T 16384, 4 documents of up to 5622 rows, 16 / 8 heads of 128: 282 us in a short run, 1114 TFLOP/s of visible pairs, and 329 in a long one, whose
+// clock the power cap lowers; the tensor pipe is 57 % and the exponential unit 58 % busy.  What bounds it is each tile's chain of about 3600 cycles a block: scores to registers 200, maxima 200,
 // exponentials 1100, P to TMEM 150, then P V and the next S on the tensor cores, behind the other tile's (1100 and 650 of latencies); TMEM is
-// full, so the next S cannot be formed before P V has read P.  Measured beside it: two warps a row with 64 keys each 338 us (twice
+// full, so the next S cannot be formed before P V has read P.  Measured beside it, in short runs when this took 277: two warps a row with 64 keys each 338 us (twice
 // the instructions around the exponentials), blocks of 64 keys with two score buffers a tile 359, the exponentials taken
 // speculatively in one pass of 64 keys 337; with 12 heads of 64 the same.
 #include <limits.h>
@@ -515,7 +515,7 @@ cudaError_t attention_packed_fwd(const bf16* qkv, bf16* o, float* lse, const Doc
   //   16 / 8 heads of 128   T 2048: 16.8 36.1 37.3 (15.2 26.9 29.5);  T 6144: 33.7 45.8 83.3 (32.9 47.4 85.2);  T 16384: 70 104 269 (78 113 291)
   //   12 heads of 64        T 2048: 15.8 33.8 33.7 (11.9 25.2 26.9);  T 8192: 29.7 42.6 98.6 (28.9 43.3 98.8);  T 16384: 52 76 178 (54 81 193)
   // With pairs of neighbouring blocks of queries (7 heads of 64 on one, T 20000) short documents lose, 41.5 (36.3) at 200, and longer ones
-  // gain, 61 (68) and 135 (157).
+  // gain, 61 (68) and 135 (157); the host, which chooses, does not know the lengths.
   if ((long long)((T + 127) / 128) * nh < 6 * 148) return attention_packed_fwd_tile(qkv, o, lse, docs, T, nh, nkv, d, err, st);
   if (d == 64) return fwd_t<64>(qkv, o, lse, docs, T, nh, nkv, err, st);
   return fwd_t<128>(qkv, o, lse, docs, T, nh, nkv, err, st);

@@ -74,7 +74,8 @@ __device__ __forceinline__ int docs_start(const Docs& docs, int row) {  // of a 
 }
 
 // CTAs of packed documents differ in length by what their tile meets of its documents, and a long one that starts late leaves the
-// rest of the GPU waiting: launches of more CTAs than run at a time start the longest first (Ordered), if the tiles are at most
+// rest of the GPU waiting: launches of more CTAs than run at a time start the longest first (Ordered), if the tiles are at most kOrdered:
+// four lengths a lane, for which the first warp has registers, and T 16384.  Longer batches come here with few heads only, in the order of their rows.
 constexpr int kOrdered = 128;
 // Forward, T 8192, 12 heads of 64, documents of 4000 on average: 109 -> 99 us, of 1024: 45.7 -> 41.3, of 300: 29.3 -> 28.8 (32.3 -> 32.6 from
 // cold caches); T 4096, 16 / 8 heads of 128, of 500: 29.7 -> 25.7.
