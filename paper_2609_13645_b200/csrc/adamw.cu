@@ -217,8 +217,8 @@ struct RunTop {
   float scale;        // 0: the run is 0
   __device__ __forceinline__ bool coded() const { return top >= 0x0d800000u; }  // from 2^-100 on
 };
-// terms: the greatest magnitude of the lane's terms that the elements are sums of, if they may cancel.
-__device__ __forceinline__ RunTop greatest(const float (&x)[8], float terms) {
+// grad_top: the lane's greatest gradient; terms: its term in the elements, if they are sums that may cancel.
+__device__ __forceinline__ RunTop greatest(const float (&x)[8], float grad_top, float terms) {
   RunTop t;
   uint32_t key[8];
 #pragma unroll
@@ -232,7 +232,8 @@ __device__ __forceinline__ RunTop greatest(const float (&x)[8], float terms) {
   for (int i = 0; i < 8; ++i) second = __viaddmax_u32(key[i], 0u - t.own, second);
   t.lane = __ffs(who) - 1;
   const bool near = may_win && second >= 0u - 72u;  // the 64, and the numbers in the last bits
-  t.whole = (who & (who - 1)) != 0 || __any_sync(0xffffffffu, near || terms > 4.f * __uint_as_float(t.top));
+  // without gradients in the run, elements that are near each other have one code and are equal
+  t.whole = ((who & (who - 1)) != 0 || __any_sync(0xffffffffu, near || terms > 4.f * __uint_as_float(t.top))) && __any_sync(0xffffffffu, grad_top != 0.f);
   t.scale = 0.f;
   return t;
 }
@@ -362,7 +363,7 @@ __device__ __forceinline__ void step8(const PlanTensor& w, long long at, int n, 
   }
   // m's terms may cancel.  Up to gradients' terms of 4 times the greatest element, an element's fp32 error, of up to 3 roundings of its own and 5
   // of the gradient's term, stays under 23 of the greatest's, and two elements that may be the greatest are within 64 last places.
-  RunTop tm = greatest(m, c.omb1 * fabsf(clip_up) * grad_top), tv = greatest(r, 0.f);
+  RunTop tm = greatest(m, grad_top, c.omb1 * fabsf(clip_up) * grad_top), tv = greatest(r, grad_top, 0.f);
   tm.whole = tm.whole || tm.top - 0x0d000000u < 0x01000000u || tm.top >= 0x7f000000u;  // next to 2^-100, and at fp32's end
   // v: but for roots from 2^-61 to 2^46, the low parts of whose squares are normal numbers
   if (tv.top - 0x29000000u >= 0x5e800000u - 0x29000000u)
